@@ -460,6 +460,69 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
                           const float* shared, int T, int d, int k, float* y, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * The norms before and after a block, with its gate and residual scale (a block = this layer, or whatever else
+ * stands between two residual additions).
+ *
+ *   n(x) = (x - m) / sqrt(mean((x - m)^2) + eps) over a row of d values;   m = 0 (MOE_NORM_RMS) or mean(x) (MOE_NORM_LAYER)
+ *
+ *   moe_norm       before   u = n(x) * w + b
+ *   moe_block_end  after    p = n_post(v) * post_w + post_b     (MOE_NORM_NONE: p = v)
+ *                           y = alpha * h + gate * p            (no gate: y = alpha * h + p)
+ *                           u = n_next(y) * next_w + next_b     (the next block's norm; MOE_NORM_NONE: no u)
+ *   moe_block_end_rows      the same, with v given as the experts' rows: v[t] = what moe_unpermute_combine makes of y_perm,
+ *                           inv_perm, gate_w [T,k] (NULL = all ones) and shared (NULL = none); v is never stored
+ *
+ * The sums are fp32, the outputs are rounded once, and u is made of the y that has not been rounded yet.
+ *
+ *   x, h, y [T,d]: x_dt, h_dt (y has h's type)      v [T,d] v_dt      u [T,d] u_dt      each MOE_F32 or MOE_BF16
+ *   w, b, post_w, post_b, next_w, next_b [d] fp32, each may be NULL (ones, zeros; NULL with MOE_NORM_NONE)
+ *   gate [gate_rows,d] fp32: gate_rows 1 (the same for all tokens) or T (a row for every token); NULL with gate_rows 0
+ *   stats: what the backward call reads, [T,2] fp32 of moe_norm, [T,4] of moe_block_end (which takes no rows form); may be NULL
+ *   y may be h itself, u may be x itself (of one type); no other output may overlap an input
+ * Requires d <= MOE_NORM_MAX_D.  Up to MOE_NORM_ANY_D any d and any alignment will do (widths that are no multiples of 8, or
+ * pointers not aligned to 16 bytes, go value by value); beyond, both are needed.  T = 0 is a no-op.
+ */
+typedef enum { MOE_NORM_NONE = 0, MOE_NORM_RMS = 1, MOE_NORM_LAYER = 2 } moe_norm_kind;
+#define MOE_NORM_MAX_D 8192
+#define MOE_NORM_ANY_D 4096
+
+MOE_API int moe_norm(const void* x, moe_dtype x_dt, const float* w, const float* b, int T, int d, moe_norm_kind kind, float eps,
+                     void* u, moe_dtype u_dt, float* stats, void* stream);
+MOE_API int moe_block_end(const void* v, moe_dtype v_dt, const void* h, moe_dtype h_dt, int T, int d,
+                          moe_norm_kind post_kind, float post_eps, const float* post_w, const float* post_b,
+                          const float* gate, int gate_rows, float alpha,
+                          moe_norm_kind next_kind, float next_eps, const float* next_w, const float* next_b,
+                          void* y, void* u, moe_dtype u_dt, float* stats, void* stream);
+MOE_API int moe_block_end_rows(const float* y_perm, const int32_t* inv_perm, const float* gate_w, const float* shared, int k,
+                               const void* h, moe_dtype h_dt, int T, int d,
+                               moe_norm_kind post_kind, float post_eps, const float* post_w, const float* post_b,
+                               const float* gate, int gate_rows, float alpha,
+                               moe_norm_kind next_kind, float next_eps, const float* next_w, const float* next_b,
+                               void* y, void* u, moe_dtype u_dt, void* stream);
+
+/* Their gradients.  The forward call's inputs, its stats and the gradients of its outputs come in; y is formed again from v and h.
+ *
+ *   moe_norm_backward       du [T,d] u_dt; dx_add [T,d] x_dt or NULL: added to dx (the residual stream's own gradient)
+ *                           -> dx [T,d] x_dt, dw, db [d] fp32 (each NULL if not wanted)
+ *   moe_block_end_backward  dy [T,d] h_dt (NULL = zero), du [T,d] u_dt (NULL = zero, or no next norm; one of the two is there)
+ *                           -> dv [T,d] v_dt, dh [T,d] h_dt, dpost_w, dpost_b, dnext_w, dnext_b [d] fp32, dgate [gate_rows,d] fp32
+ *                           (each NULL if not wanted)
+ *   ws: moe_workspace_bytes(MOE_OP_NORM_BACKWARD or MOE_OP_BLOCK_END_BACKWARD, T, d, 0, 0, 0, ...) bytes at most (for all gradients
+ *       of parameters; it takes a part of that for each, and none and NULL where none is wanted, as for a gate of T rows)
+ *   dx may be du or dx_add, dh may be dy, dv may be v (of one type); no other output may overlap an input.
+ * The gradients of parameters are summed over the tokens in a fixed order: the same call gives the same bits.  T = 0 sets them to zero.
+ */
+MOE_API int moe_norm_backward(const void* du, moe_dtype u_dt, const void* x, moe_dtype x_dt, const float* w, const float* stats,
+                              int T, int d, moe_norm_kind kind, const void* dx_add, void* dx, float* dw, float* db,
+                              void* ws, size_t ws_bytes, void* stream);
+MOE_API int moe_block_end_backward(const void* dy, const void* du, moe_dtype u_dt, const void* v, moe_dtype v_dt,
+                                   const void* h, moe_dtype h_dt, int T, int d,
+                                   moe_norm_kind post_kind, const float* post_w, const float* post_b,
+                                   const float* gate, int gate_rows, float alpha, moe_norm_kind next_kind, const float* next_w,
+                                   const float* stats, void* dv, void* dh, float* dpost_w, float* dpost_b, float* dgate,
+                                   float* dnext_w, float* dnext_b, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Asynchronous expert fetching (section 4.3): experts whose weights live in pinned host
  * memory are copied into device slots on a stream of the engine's own while the caller's
  * stream computes; a slot whose expert has finished is overwritten by the next expert
@@ -515,7 +578,7 @@ MOE_API int moe_set_expert_pointers(const void** w_in, const void** w_out, int E
 MOE_API int moe_token_threshold(double phi, int d_type, double beta);
 
 /* Scratch sizes.  op selects the call. */
-enum { MOE_OP_PERMUTE = 1 };
+enum { MOE_OP_PERMUTE = 1, MOE_OP_NORM_BACKWARD = 2, MOE_OP_BLOCK_END_BACKWARD = 3 };
 MOE_API size_t moe_workspace_bytes(int op, int T, int d, int F, int E, int k, moe_dtype dt);
 
 /* Diagnostic: a plain device-to-device copy of `bytes` bytes (a multiple of 16; src and dst

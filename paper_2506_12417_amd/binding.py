@@ -26,19 +26,22 @@ MOE_PLAN_BALANCED, MOE_PLAN_HARMOENY, MOE_PLAN_STATIC, MOE_PLAN_EVEN_SPLIT, MOE_
 MOE_MAX_EXPERTS, MOE_MAX_TOPK, MOE_MAX_BINS = 256, 8, 16
 MOE_PLAN_HDR_CTR = 4 + 2 * (MOE_MAX_BINS + 1)
 MOE_PLAN_HDR_INTS = MOE_PLAN_HDR_CTR + MOE_MAX_BINS + 1
-MOE_OP_PERMUTE = 1
+MOE_OP_PERMUTE, MOE_OP_NORM_BACKWARD, MOE_OP_BLOCK_END_BACKWARD = 1, 2, 3
+MOE_NORM_NONE, MOE_NORM_RMS, MOE_NORM_LAYER = 0, 1, 2
+MOE_NORM_MAX_D, MOE_NORM_ANY_D = 8192, 4096
 MOE_PERMUTE_STATIC_BYTES = 1 << 20
 MOE_PERMUTE_PLAN_MAX = 32768
 MOE_TILE_WHOLE_PLAN = 0x10000
 
 EXPORTS = [
     "moe_route_topk", "moe_pack_router", "moe_route_topk_packed", "moe_permute", "moe_permute_static", "moe_plan_capacity", "moe_plan_tiles", "moe_permute_plan", "moe_plan_tiles_subset", "moe_rebalance", "moe_pack_weights", "moe_pack_w_out",
-    "moe_ffn_tile_m", "moe_ffn_pick_tile_m", "moe_ffn_kernel_mode", "moe_ffn_pairs", "moe_grouped_ffn", "moe_grouped_ffn_phase", "moe_grouped_ffn_top1", "moe_grouped_ffn_top1_phase", "moe_grouped_ffn_fused", "moe_grouped_ffn_fused_phase", "moe_grouped_ffn_shared", "moe_grouped_ffn_shared_phase", "moe_grouped_ffn_gather", "moe_grouped_ffn_gather_phase", "moe_unpermute_combine", "moe_prefetch_create",
+    "moe_ffn_tile_m", "moe_ffn_pick_tile_m", "moe_ffn_kernel_mode", "moe_ffn_pairs", "moe_grouped_ffn", "moe_grouped_ffn_phase", "moe_grouped_ffn_top1", "moe_grouped_ffn_top1_phase", "moe_grouped_ffn_fused", "moe_grouped_ffn_fused_phase", "moe_grouped_ffn_shared", "moe_grouped_ffn_shared_phase", "moe_grouped_ffn_gather", "moe_grouped_ffn_gather_phase", "moe_unpermute_combine",
+    "moe_norm", "moe_norm_backward", "moe_block_end", "moe_block_end_rows", "moe_block_end_backward", "moe_prefetch_create",
     "moe_prefetch_experts", "moe_set_expert_pointers", "moe_prefetch_wait", "moe_prefetch_release", "moe_prefetch_reset", "moe_prefetch_destroy",
     "moe_token_threshold", "moe_workspace_bytes", "moe_copy_bytes", "moe_last_error", "moe_version",
 ]
 
-_vp, _i, _sz = C.c_void_p, C.c_int, C.c_size_t
+_vp, _i, _sz, _f = C.c_void_p, C.c_int, C.c_size_t, C.c_float
 lib.moe_route_topk.argtypes = [_vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]
 lib.moe_pack_router.argtypes = [_vp, _i, _i, _i, _vp, _vp, _vp]
 lib.moe_route_topk_packed.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp]
@@ -66,6 +69,12 @@ lib.moe_grouped_ffn_shared.argtypes = [_vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp
 lib.moe_grouped_ffn_gather_phase.argtypes = [_i] + lib.moe_grouped_ffn_gather.argtypes
 lib.moe_grouped_ffn_shared_phase.argtypes = [_i] + lib.moe_grouped_ffn_shared.argtypes
 lib.moe_unpermute_combine.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]
+lib.moe_norm.argtypes = [_vp, _i, _vp, _vp, _i, _i, _i, _f, _vp, _i, _vp, _vp]
+lib.moe_norm_backward.argtypes = [_vp, _i, _vp, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+_norms = [_i, _f, _vp, _vp, _vp, _i, _f, _i, _f, _vp, _vp]
+lib.moe_block_end.argtypes = [_vp, _i, _vp, _i, _i, _i] + _norms + [_vp, _vp, _i, _vp, _vp]
+lib.moe_block_end_rows.argtypes = [_vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i] + _norms + [_vp, _vp, _i, _vp]
+lib.moe_block_end_backward.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _i, _f, _i] + [_vp] * 10 + [_sz, _vp]
 lib.moe_prefetch_create.argtypes = [C.POINTER(_vp), _i, _sz, _vp]
 lib.moe_prefetch_experts.argtypes = [_vp, C.POINTER(C.c_int32), _i, C.POINTER(_vp), _sz, C.POINTER(_vp)]
 lib.moe_set_expert_pointers.argtypes = [_vp, _vp, _i, C.POINTER(C.c_int32), _i, C.POINTER(_vp), _sz, _vp]
@@ -98,6 +107,16 @@ def _p(t) -> Optional[int]:
         return None
     if isinstance(t, int):
         return t
+    return t.data_ptr()
+
+
+def _d(t) -> Optional[int]:
+    """_p, for a call that a strided tensor could reach unnoticed (a slice of a residual stream, a transposed view): such
+    a tensor is refused, the library reads rows one behind the other."""
+    if t is None or isinstance(t, int):
+        return t
+    if not t.is_contiguous():
+        raise MoeError(MOE_ERR_UNSUPPORTED, "tensor of strides %s: rows have to be contiguous" % (tuple(t.stride()),))
     return t.data_ptr()
 
 
@@ -286,6 +305,35 @@ def moe_grouped_ffn_phase(phase, x_perm, A, d, F, E, act, dt, w_in, w_out, tiles
 def moe_unpermute_combine(y_perm, inv_perm, gate_w, shared, T, d, k, y, stream=None):
     _check(lib.moe_unpermute_combine(_p(y_perm), _p(inv_perm), _p(gate_w), _p(shared), T, d, k, _p(y),
                                      _stream(stream)))
+
+
+def moe_norm(x, x_dt, w, b, T, d, kind, eps, u, u_dt, stats=None, stream=None):
+    _check(lib.moe_norm(_d(x), x_dt, _d(w), _d(b), T, d, kind, eps, _d(u), u_dt, _d(stats), _stream(stream)))
+
+
+def moe_norm_backward(du, u_dt, x, x_dt, w, stats, T, d, kind, dx_add, dx, dw, db, ws, ws_bytes, stream=None):
+    _check(lib.moe_norm_backward(_d(du), u_dt, _d(x), x_dt, _d(w), _d(stats), T, d, kind, _d(dx_add), _d(dx), _d(dw), _d(db),
+                                 _d(ws), ws_bytes, _stream(stream)))
+
+
+def moe_block_end(v, v_dt, h, h_dt, T, d, post_kind, post_eps, post_w, post_b, gate, gate_rows, alpha, next_kind, next_eps, next_w,
+                  next_b, y, u, u_dt, stats=None, stream=None):
+    _check(lib.moe_block_end(_d(v), v_dt, _d(h), h_dt, T, d, post_kind, post_eps, _d(post_w), _d(post_b), _d(gate), gate_rows, alpha,
+                             next_kind, next_eps, _d(next_w), _d(next_b), _d(y), _d(u), u_dt, _d(stats), _stream(stream)))
+
+
+def moe_block_end_rows(y_perm, inv_perm, gate_w, shared, k, h, h_dt, T, d, post_kind, post_eps, post_w, post_b, gate, gate_rows, alpha,
+                       next_kind, next_eps, next_w, next_b, y, u, u_dt, stream=None):
+    _check(lib.moe_block_end_rows(_d(y_perm), _d(inv_perm), _d(gate_w), _d(shared), k, _d(h), h_dt, T, d, post_kind, post_eps, _d(post_w),
+                                  _d(post_b), _d(gate), gate_rows, alpha, next_kind, next_eps, _d(next_w), _d(next_b), _d(y), _d(u), u_dt,
+                                  _stream(stream)))
+
+
+def moe_block_end_backward(dy, du, u_dt, v, v_dt, h, h_dt, T, d, post_kind, post_w, post_b, gate, gate_rows, alpha, next_kind, next_w,
+                           stats, dv, dh, dpost_w, dpost_b, dgate, dnext_w, dnext_b, ws, ws_bytes, stream=None):
+    _check(lib.moe_block_end_backward(_d(dy), _d(du), u_dt, _d(v), v_dt, _d(h), h_dt, T, d, post_kind, _d(post_w), _d(post_b), _d(gate),
+                                      gate_rows, alpha, next_kind, _d(next_w), _d(stats), _d(dv), _d(dh), _d(dpost_w), _d(dpost_b),
+                                      _d(dgate), _d(dnext_w), _d(dnext_b), _d(ws), ws_bytes, _stream(stream)))
 
 
 def moe_copy_bytes(src, dst, nbytes: int, stream=None):

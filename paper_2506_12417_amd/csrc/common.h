@@ -29,6 +29,9 @@ int moe_fail(int code, const char* fmt, ...);
 static inline size_t moe_elem_size(moe_dtype dt) { return dt == MOE_BF16 ? 2 : 4; }
 static inline bool moe_dtype_ok(int dt) { return dt == MOE_F32 || dt == MOE_BF16; }
 
+// norm.hip: workspace of moe_norm_backward or moe_block_end_backward for the gradients of `grads` parameters of d values
+size_t moe_norm_back_bytes(int T, int d, bool block_end, int grads);
+
 #define MOE_WAVE 64
 
 // bfloat16 <-> float (bit level; round to nearest, ties to even; NaN kept quiet)
