@@ -460,6 +460,31 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
                           const float* shared, int T, int d, int k, float* y, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * The whole layer for a few tokens (a decode step), in two launches: routing, expert FFNs, the shared expert and the
+ * weighted sum, all that moe_route_topk ... moe_unpermute_combine compute, without a sort, a plan or rows in between.
+ *
+ *   y[t] = sum_j gate_w[t,j] * FFN_{expert_idx[t,j]}(x[t])  (+ shared expert's FFN(x[t]), always SwiGLU)
+ *
+ *   x [T,d] dt      w_gate, w_norm2: MOE_BF16: w_gate_t [E,d] and w_norm2 [E] of moe_pack_router; MOE_F32: w_gate [d,E] as given,
+ *           w_norm2 NULL      bias [E] fp32 or NULL
+ *   w_in, w_out, s_w_in, s_w_out: as moe_grouped_ffn and moe_grouped_ffn_shared take them (s_w_* may be NULL with shared_F 0)
+ *   expert_idx [T,k], gate_w [T,k] out: the choice of moe_route_topk (decided as if in float64; a token whose logits are NaN gets ids
+ *           outside [0,E), NaN weights and a row of NaN)
+ *   ws: scratch of moe_layer_few_workspace() bytes: the hidden activations, which are rounded once, to IEEE half, and saturate, in MOE_BF16
+ *           (as in moe_grouped_ffn); everything else is summed in fp32
+ *   y [T,d] y_dt (MOE_F32 or MOE_BF16: rounded once) out
+ * Requires T <= MOE_FEW_MAX_T, d, F and shared_F multiples of 64, x, w_gate, ws and the matrices aligned to 16 bytes.  T = 0 is a no-op.
+ * It adds in an order of its own: the last bits differ from those of the separate calls.  (MOE_F32 routes in a launch of its own.)
+ */
+#define MOE_FEW_MAX_T 64
+MOE_API size_t moe_layer_few_workspace(int T, int F, int k, int shared_F, moe_dtype dt);
+MOE_API int moe_layer_few(const void* x, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt, int renorm,
+                          const void* w_gate, const float* w_norm2, const float* bias,
+                          const void* const* w_in, const void* const* w_out,
+                          int shared_F, const void* const* s_w_in, const void* const* s_w_out,
+                          int32_t* expert_idx, float* gate_w, void* ws, size_t ws_bytes, void* y, moe_dtype y_dt, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * The norms before and after a block, with its gate and residual scale (a block = this layer, or whatever else
  * stands between two residual additions).
  *

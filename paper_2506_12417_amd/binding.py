@@ -27,6 +27,7 @@ MOE_MAX_EXPERTS, MOE_MAX_TOPK, MOE_MAX_BINS = 256, 8, 16
 MOE_PLAN_HDR_CTR = 4 + 2 * (MOE_MAX_BINS + 1)
 MOE_PLAN_HDR_INTS = MOE_PLAN_HDR_CTR + MOE_MAX_BINS + 1
 MOE_OP_PERMUTE, MOE_OP_NORM_BACKWARD, MOE_OP_BLOCK_END_BACKWARD = 1, 2, 3
+MOE_FEW_MAX_T = 64
 MOE_NORM_NONE, MOE_NORM_RMS, MOE_NORM_LAYER = 0, 1, 2
 MOE_NORM_MAX_D, MOE_NORM_ANY_D = 8192, 4096
 MOE_PERMUTE_STATIC_BYTES = 1 << 20
@@ -36,7 +37,7 @@ MOE_TILE_WHOLE_PLAN = 0x10000
 EXPORTS = [
     "moe_route_topk", "moe_pack_router", "moe_route_topk_packed", "moe_permute", "moe_permute_static", "moe_plan_capacity", "moe_plan_tiles", "moe_permute_plan", "moe_plan_tiles_subset", "moe_rebalance", "moe_pack_weights", "moe_pack_w_out",
     "moe_ffn_tile_m", "moe_ffn_pick_tile_m", "moe_ffn_kernel_mode", "moe_ffn_pairs", "moe_grouped_ffn", "moe_grouped_ffn_phase", "moe_grouped_ffn_top1", "moe_grouped_ffn_top1_phase", "moe_grouped_ffn_fused", "moe_grouped_ffn_fused_phase", "moe_grouped_ffn_shared", "moe_grouped_ffn_shared_phase", "moe_grouped_ffn_gather", "moe_grouped_ffn_gather_phase", "moe_unpermute_combine",
-    "moe_norm", "moe_norm_backward", "moe_block_end", "moe_block_end_rows", "moe_block_end_backward", "moe_prefetch_create",
+    "moe_layer_few", "moe_layer_few_workspace", "moe_norm", "moe_norm_backward", "moe_block_end", "moe_block_end_rows", "moe_block_end_backward", "moe_prefetch_create",
     "moe_prefetch_experts", "moe_set_expert_pointers", "moe_prefetch_wait", "moe_prefetch_release", "moe_prefetch_reset", "moe_prefetch_destroy",
     "moe_token_threshold", "moe_workspace_bytes", "moe_copy_bytes", "moe_last_error", "moe_version",
 ]
@@ -69,6 +70,9 @@ lib.moe_grouped_ffn_shared.argtypes = [_vp, _i, _i, _i, _i, _i, _i, _i, _vp, _vp
 lib.moe_grouped_ffn_gather_phase.argtypes = [_i] + lib.moe_grouped_ffn_gather.argtypes
 lib.moe_grouped_ffn_shared_phase.argtypes = [_i] + lib.moe_grouped_ffn_shared.argtypes
 lib.moe_unpermute_combine.argtypes = [_vp, _vp, _vp, _vp, _i, _i, _i, _vp, _vp]
+lib.moe_layer_few.argtypes = [_vp] + [_i] * 8 + [_vp] * 5 + [_i] + [_vp] * 5 + [_sz, _vp, _i, _vp]
+lib.moe_layer_few_workspace.argtypes = [_i] * 5
+lib.moe_layer_few_workspace.restype = _sz
 lib.moe_norm.argtypes = [_vp, _i, _vp, _vp, _i, _i, _i, _f, _vp, _i, _vp, _vp]
 lib.moe_norm_backward.argtypes = [_vp, _i, _vp, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _norms = [_i, _f, _vp, _vp, _vp, _i, _f, _i, _f, _vp, _vp]
@@ -305,6 +309,16 @@ def moe_grouped_ffn_phase(phase, x_perm, A, d, F, E, act, dt, w_in, w_out, tiles
 def moe_unpermute_combine(y_perm, inv_perm, gate_w, shared, T, d, k, y, stream=None):
     _check(lib.moe_unpermute_combine(_p(y_perm), _p(inv_perm), _p(gate_w), _p(shared), T, d, k, _p(y),
                                      _stream(stream)))
+
+
+def moe_layer_few_workspace(T: int, F: int, k: int, shared_F: int, dt: int) -> int:
+    return int(lib.moe_layer_few_workspace(T, F, k, shared_F, dt))
+
+
+def moe_layer_few(x, T, d, F, E, k, act, dt, renorm, w_gate, w_norm2, bias, w_in, w_out, shared_F, s_w_in, s_w_out, expert_idx, gate_w, ws,
+                  ws_bytes, y, y_dt, stream=None):
+    _check(lib.moe_layer_few(_d(x), T, d, F, E, k, act, dt, renorm, _d(w_gate), _d(w_norm2), _d(bias), _d(w_in), _d(w_out), shared_F, _d(s_w_in),
+                             _d(s_w_out), _d(expert_idx), _d(gate_w), _d(ws), ws_bytes, _d(y), y_dt, _stream(stream)))
 
 
 def moe_norm(x, x_dt, w, b, T, d, kind, eps, u, u_dt, stats=None, stream=None):
