@@ -18,7 +18,7 @@ def test_sizes():
     for bad in (dict(T=-1), dict(d=0), dict(F=0), dict(E=0), dict(k=0), dict(k=9, E=8), dict(shared_F=-64)):
         assert call(**bad) == B.MOE_ERR_ARG, bad
     for bad in (dict(T=B.MOE_FEW_MAX_T + 1), dict(E=B.MOE_MAX_EXPERTS + 1), dict(E=32, k=B.MOE_MAX_TOPK + 1), dict(d=96), dict(F=32), dict(shared_F=8),
-                dict(act=5), dict(dt=7), dict(y_dt=7), dict(F=1 << 26), dict(d=1 << 27), dict(shared_F=1 << 26, s_w_in=FAKE, s_w_out=FAKE)):
+                dict(act=5), dict(dt=7), dict(y_dt=7), dict(F=1 << 27), dict(d=1 << 27), dict(shared_F=1 << 27, s_w_in=FAKE, s_w_out=FAKE)):
         assert call(**bad) == B.MOE_ERR_UNSUPPORTED, bad
 
 
