@@ -8,14 +8,14 @@
 // balance rows, of which there are none to balance here.  So the sort is a table of bits in LDS (one bit per expert and token),
 // made by every work-group for itself, and there is no plan: an active expert is a list of items.
 //
-// Launch 1, one work-group of sixteen wavefronts per CU.  Every work-group routes all tokens for itself (what it reads for
+// Launch 1, one work-group of eight wavefronts per CU.  Every work-group routes all tokens for itself (what it reads for
 // that, W_g and x, comes from the L2s; waiting for another work-group's answer, or another launch, costs more): logits on the matrix
 // cores in fp32 over 32 terms at a time, added up in fp64, with a rigorous error bound; logits closer than the bound are
 // computed again in fp64, so that the choice is that of exact arithmetic.  Then its wavefronts take items of 16 weight rows, each
 // alone over the whole contraction: no barrier, no partial sums.
 // Launch 2: a work-group owns 8 or 16 output columns for all tokens and all experts.  The (expert, 128-byte line) pairs of its
-// contraction are dealt out to its sixteen wavefronts in equal runs; a wavefront adds each expert's products, times the gates, to
-// sums per token of its own in LDS, and the sixteen are added in a fixed order.  So the combine costs no pass over memory, no atomics and no
+// contraction are dealt out to its wavefronts in runs of equal cost; a wavefront adds each expert's products, times the gates, to
+// sums per token of its own in LDS, and these are added in a fixed order.  So the combine costs no pass over memory, no atomics and no
 // second launch, and all CUs read equal shares of the weights whatever the routing.
 //
 // Weights and rows come in whole 128-byte lines, eight rows a load, several lines in flight per wavefront, and
@@ -33,9 +33,9 @@ typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 typedef const __attribute__((address_space(1))) unsigned char* gptr;
 typedef const __attribute__((address_space(1))) u32x4* gpiece;
 
-constexpr int NW = 16, NTH = NW * 64;            // wavefronts and threads of a work-group
+constexpr int NW = 8, NTH = NW * 64;            // wavefronts and threads of a work-group
 constexpr int MAXT = MOE_FEW_MAX_T, MAXE = MOE_MAX_EXPERTS, MAXA = MAXT * MOE_MAX_TOPK;
-static_assert(MAXT == 64, "a token is a bit of two words");
+static_assert(MAXT == 64 && MAXA <= NTH && 2 * MAXE <= NTH, "a token is a bit of two words; a thread per assignment and per word");
 
 enum { BF = 0, HF = 1, FP = 2 };                 // what the operands are: bf16, half, fp32
 
@@ -58,104 +58,280 @@ struct Lists {
     unsigned bits[MAXE][2];              // the tokens of an expert
     int first[MAXE + 1];                 // its first row
     int active[MAXE];                    // the experts with tokens, rising
+    int cost[MAXE + 1];                  // what a line of each of the active ones before costs, in all
     int n_active;
-    unsigned short a[MAXA];              // a row's assignment t k + j
-    int id[MAXA];
-    float gate[MAXA];                    // by assignment
+    const void* w[MAXE];                 // the experts' matrices
+    int id[MAXA];                        // the choice, by assignment
+    float gate[MAXA];                    // by row
+    unsigned char t[MAXA];               // a row's token
 };
-constexpr int TURN_PIECES = 2 * 16 * 8;  // 16 weight rows and 16 rows of 128 bytes, in 16-byte pieces
 
-// ids (in l.id) -> lists.  An id outside [0,E) has no row.  All threads; a barrier before and behind.
-__device__ __forceinline__ void make_lists(Lists& l, int T, int E, int k) {
-    const int tid = threadIdx.x, A = T * k;
-    for (int i = tid; i < 2 * MAXE; i += NTH) (&l.bits[0][0])[i] = 0u;
-    __syncthreads();
-    int e = -1, t = 0;
-    if (tid < A) {
-        e = l.id[tid];
-        t = tid / k;
-        if ((unsigned)e < (unsigned)E) atomicOr(&l.bits[e][t >> 5], 1u << (t & 31));
-    }
+__device__ __forceinline__ int line_cost(int m);
+
+// Every thread's assignment (expert e of token t with weight gate; e outside [0,E): none) -> lists.  The bits are clear.  A barrier before
+// and behind.
+__device__ __forceinline__ void make_lists(Lists& l, int E, int e, int t, float gate) {
+    const int tid = threadIdx.x;
+    const bool is = (unsigned)e < (unsigned)E;
+    if (is) atomicOr(&l.bits[e][t >> 5], 1u << (t & 31));
     __syncthreads();
     if (tid < 64) {
-        unsigned rows = 0, act = 0;      // of the experts before
-#pragma unroll
-        for (int j = 0; j < MAXE / 64; ++j) {
-            const int x = j * 64 + tid;
-            const unsigned n = __popc(l.bits[x][0]) + __popc(l.bits[x][1]), up = moe_wave_scan_u32(n);
+        unsigned rows = 0, act = 0, cost = 0;    // of the experts before
+        for (int x = tid; x - tid < E; x += 64) {
+            const unsigned n = __popc(l.bits[x][0]) + __popc(l.bits[x][1]), c = n ? (unsigned)line_cost((int)n) : 0u;
+            // (both sums in one scan: at most 512 rows, and 256 experts' costs of at most 10)
+            const unsigned up = moe_wave_scan_u32(n | c << 16);
             const unsigned long long on = __ballot(n != 0);
-            l.first[x] = (int)(rows + up - n);
-            if (n) l.active[act + __popcll(on & ((1ull << tid) - 1ull))] = x;
-            rows += (unsigned)__builtin_amdgcn_readlane((int)up, 63);
+            l.first[x] = (int)(rows + (up & 0xffffu) - n);
+            if (n) {
+                const int at = (int)act + __popcll(on & ((1ull << tid) - 1ull));
+                l.active[at] = x;
+                l.cost[at] = (int)(cost + (up >> 16) - c);
+            }
+            const unsigned all = (unsigned)__builtin_amdgcn_readlane((int)up, 63);
+            rows += all & 0xffffu;
+            cost += all >> 16;
             act += (unsigned)__popcll(on);
         }
-        if (tid == 0) { l.first[MAXE] = (int)rows; l.n_active = (int)act; }
+        if (tid == 0) {
+            l.first[(E + 63) & ~63] = (int)rows;
+            l.cost[act] = (int)cost;
+            l.n_active = (int)act;
+        }
     }
     __syncthreads();
-    if ((unsigned)e < (unsigned)E) {
+    if (is) {
         const unsigned lo = l.bits[e][0], hi = l.bits[e][1], below = (1u << (t & 31)) - 1u;
-        l.a[l.first[e] + (t < 32 ? __popc(lo & below) : __popc(lo) + __popc(hi & below))] = (unsigned short)tid;
+        const int r = l.first[e] + (t < 32 ? __popc(lo & below) : __popc(lo) + __popc(hi & below));
+        l.t[r] = (unsigned char)t;
+        l.gate[r] = gate;
     }
     __syncthreads();
-}
-
-// ---- acc[g] += 16 weight rows (A) x the 16 activation rows of group g (B) over the 128-byte lines [l0, l1)
-// WL: weight loads of eight rows (1: rows 8 - 15 of the product mean nothing), XL: loads of a group's activation rows, U: lines in
-// flight.  w0, w1: the two eights of weight rows; x_at: byte offsets of the lane's rows, beyond the buffer for rows that are not there.
-template <int TY, int G, int XL, int WL, int U>
-__device__ __forceinline__ void lines_product(const unsigned char* w0, const unsigned char* w1, unsigned w_off, __amdgpu_buffer_rsrc_t x,
-                                              const unsigned (&x_at)[4][2], int l0, int l1, f32x4 (&acc)[4], u32x4* turn) {
-    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
-    // (rows of eight pieces, piece p of row r at place p ^ (r & 7): no bank conflicts either way)
-    const int st_at = (lane >> 3) * 8 + ((lane & 7) ^ (lane >> 3)), rd_at = l16 * 8 + (lq ^ (l16 & 7));
-    u32x4* const xturn = turn + 16 * 8;
-    for (int l = l0; l < l1; l += U) {
-        u32x4 w[U][WL], b[U][G][XL];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int at = (l + u < l1 ? l + u : l1 - 1) * 128;          // (past the end: the last line again, not multiplied)
-            w[u][0] = *(gpiece)((gptr)(uintptr_t)(w0 + at) + w_off);
-            if constexpr (WL == 2) w[u][1] = *(gpiece)((gptr)(uintptr_t)(w1 + at) + w_off);
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int i = 0; i < XL; ++i) b[u][g][i] = __builtin_amdgcn_raw_buffer_load_b128(x, (int)x_at[g][i], at, 0);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (l + u < l1) {
-#pragma unroll
-                for (int i = 0; i < WL; ++i) turn[i * 64 + st_at] = w[u][i];
-                u32x4 wf[2] = {turn[rd_at], turn[rd_at ^ 4]};
-#pragma unroll
-                for (int g = 0; g < G; ++g) {
-#pragma unroll
-                    for (int i = 0; i < XL; ++i) xturn[i * 64 + st_at] = b[u][g][i];
-#pragma unroll
-                    for (int v = 0; v < 2; ++v) acc[g] = mma<TY>(wf[v], xturn[rd_at ^ (4 * v)], acc[g]);
-                }
-            }
-        }
-    }
-}
-// the same for m rows (m <= 64), as many groups as they need
-template <int TY, int WL>
-__device__ __forceinline__ int lines_product_rows(int m, const unsigned char* w0, const unsigned char* w1, unsigned w_off, __amdgpu_buffer_rsrc_t x,
-                                                  const unsigned (&x_at)[4][2], int l0, int l1, f32x4 (&acc)[4], u32x4* turn) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (m <= 8) lines_product<TY, 1, 1, WL, WL == 2 ? 6 : 8>(w0, w1, w_off, x, x_at, l0, l1, acc, turn);
-    else if (m <= 16) lines_product<TY, 1, 2, WL, WL == 2 ? 4 : 6>(w0, w1, w_off, x, x_at, l0, l1, acc, turn);
-    else if (m <= 32) lines_product<TY, 2, 2, WL, WL == 2 ? 3 : 4>(w0, w1, w_off, x, x_at, l0, l1, acc, turn);
-    else if (m <= 48) lines_product<TY, 3, 2, WL, 2>(w0, w1, w_off, x, x_at, l0, l1, acc, turn);
-    else lines_product<TY, 4, 2, WL, 2>(w0, w1, w_off, x, x_at, l0, l1, acc, turn);
-    // (the last matrix instructions stand before a branch, across which the compiler does not keep the distance to the use of
-    // their results: sixteen cycles and more here)
-    asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc[0]), "+v"(acc[1]), "+v"(acc[2]), "+v"(acc[3]));
-    return (m + 15) >> 4;
 }
 
 constexpr unsigned NOWHERE = 0x80000000u;        // beyond every buffer here (they are smaller than 2 GiB)
+
+// Where a product's activations come from: LDS, where they all lie in it (rows in order, 16-byte piece p of row r of every 128 bytes at
+// place p ^ (r & 7)); or memory, as fragments, or in whole lines that are turned into fragments in LDS.  (Rows in lines cost
+// the vector cache 16 look-ups a load, as fragments 4 for every row: lines are the choice for more than 16 rows that lie in order.)
+enum { IN_LDS = 0, FRAGMENTS = 1, LINES = 2 };
+
+// ---- products.  A segment: 16 weight rows times an expert's m <= 64 rows over the 128-byte lines [l0, l1) of the contraction.
+struct Segment {
+    __amdgpu_buffer_rsrc_t w, x;
+    unsigned w_at[2];                    // byte offsets of the lane's two weight rows (eight rows a load)
+    // and of its activations: its 16 bytes of group g in the first 64 bytes of a row, or (LINES) its 16 bytes of the first 128 of rows
+    // 16 g + 8 i ... at [2 g + i]; beyond the buffer for rows that are not there (in LDS: of any row).  IN_LDS, rows taken one by one: see dots()
+    unsigned x_at[8];
+    int x_step;                          // from one 64 bytes to the next (FRAGMENTS)
+    int l0, l1, m;
+};
+
+// Eight weight rows a load, a lane's 16 bytes of them times the same 16 bytes of every activation row, in fp32: for a few rows, where the
+// matrix instruction's 16 columns would be nearly empty (fp32: eight of 32 cycles a line).  acc[i][r]: row 8 i + lane / 8, activation row r.
+template <int WL, int M>
+__device__ __forceinline__ void dots(const u32x4 (&w)[WL], const unsigned char* xl, const unsigned (&x_at)[8], int line, float (&acc)[WL][M]) {
+#pragma unroll
+    for (int r = 0; r < M; ++r) {
+        const u32x4 x = *(const u32x4*)(xl + x_at[r] + line * 128);
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[i][r] = fmaf(__uint_as_float(w[i][j]), __uint_as_float(x[j]), acc[i][r]);
+    }
+}
+// their sums over the eight lanes of a row, in the matrix instruction's places: lane holds activation row lane % 16, weight rows 4 (lane / 16) + r
+template <int WL, int M> __device__ __forceinline__ f32x4 dots_total(float (&acc)[WL][M]) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    float mine[2] = {0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < WL; ++i)
+#pragma unroll
+        for (int r = 0; r < M; ++r) {
+            float v = acc[i][r];
+            v += dpp_xchg<0>(v);
+            v += dpp_xchg<1>(v);
+            v += dpp_xchg<2>(v);
+            mine[i] = (lane & 7) == r ? v : mine[i];
+        }
+    f32x4 out;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int from = (4 * (lq & 1) + r) * 8 + (l16 & 7);
+        const float lo = __shfl(mine[0], from), hi = WL == 2 ? __shfl(mine[1], from) : 0.f;
+        out[r] = lq & 2 ? hi : lo;
+    }
+    return out;
+}
+
+// A wavefront's run of segments with G groups of 16 rows: acc[g] = weight rows (A) x rows of group g (B), D lines in flight.
+//   WL     weight loads of eight rows (1: rows 8 - 15 of the product mean nothing)
+//   M      > 0: at most M rows, by dots() (IN_LDS, fp32)
+//   next(Segment&)  the segment behind the present one, false if there is none of this kind;   done(Segment const&, acc)
+// The loads run on from one segment into the next: in the last D lines of one the next one's first are fetched; a segment takes its lines'
+// number rounded up to D.  The weights of a line go through one half of the turning place while the line before is multiplied.
+template <int TY, int WL, int G, int M, int D, int X, typename Next, typename Done>
+__device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned char* xl, Next next, Done done) {
+    static_assert(D % 2 == 0, "the turning place's halves alternate");
+    static_assert(M == 0 || (X == IN_LDS && TY == FP && G == 1), "");
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    // (rows of eight pieces, piece p of row r at place p ^ (r & 7): no bank conflicts either way)
+    const int st_at = (lane >> 3) * 8 + ((lane & 7) ^ (lane >> 3)), rd_at = l16 * 8 + (lq ^ (l16 & 7));
+    u32x4 a[D][WL], b[X == IN_LDS ? 1 : D][G][2];
+    auto fetch = [&](const Segment& from, int u, int l) __attribute__((always_inline)) {
+        const bool in = l < from.l1;
+        const int at = in ? l : 0;
+#pragma unroll
+        for (int i = 0; i < WL; ++i) a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(from.w, (int)(in ? from.w_at[i] : NOWHERE), at * 128, 0);
+        if constexpr (X != IN_LDS) {
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int v = 0; v < 2; ++v)
+                    b[u][g][v] = __builtin_amdgcn_raw_buffer_load_b128(from.x, (int)(in ? from.x_at[X == LINES ? 2 * g + v : g] : NOWHERE),
+                                                                       X == LINES ? at * 128 : (2 * at + v) * from.x_step, 0);
+        }
+    };
+    u32x4 wf[2][2], xf[2][G][2];
+    // line l of segment s, fetched at u, becomes fragments
+    auto turned = [&](const Segment& s, int u, int l) __attribute__((always_inline)) {
+        if constexpr (M == 0) {
+            u32x4* const half = turn + (u & 1) * 128;
+#pragma unroll
+            for (int i = 0; i < WL; ++i) half[i * 64 + st_at] = a[u % D][i];
+            wf[u & 1][0] = half[rd_at];
+            wf[u & 1][1] = half[rd_at ^ 4];
+            if constexpr (X == IN_LDS) {
+                const int at = l < s.l1 ? l * 128 : 0;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) xf[u & 1][g][v] = *(const u32x4*)(xl + (s.x_at[g] ^ (64u * v)) + at);
+            }
+        }
+    };
+    f32x4 acc[G];
+    float dot[WL][M ? M : 1];
+    auto multiply = [&](const Segment& s, int u, int l) __attribute__((always_inline)) {
+        if constexpr (M > 0) {
+            dots<WL, M>(a[u], xl, s.x_at, l, dot);
+        } else {
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                if constexpr (X == LINES) {
+                    u32x4* const third = turn + 256;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) third[v * 64 + st_at] = b[u][g][v];
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) acc[g] = mma<TY>(wf[u & 1][v], third[rd_at ^ (4 * v)], acc[g]);
+                } else {
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) acc[g] = mma<TY>(wf[u & 1][v], X == IN_LDS ? xf[u & 1][g][v] : b[X == IN_LDS ? 0 : u][g][v], acc[g]);
+                }
+            }
+        }
+    };
+#pragma unroll
+    for (int u = 0; u < D; ++u) fetch(seg, u, seg.l0 + u);
+    turned(seg, 0, seg.l0);
+    for (;;) {
+        Segment nxt = seg;
+        const bool more = next(nxt);
+        if (!more) nxt.l1 = nxt.l0;
+#pragma unroll
+        for (int g = 0; g < G; ++g) acc[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+#pragma unroll
+            for (int r = 0; r < (M ? M : 1); ++r) dot[i][r] = 0.f;
+        int l = seg.l0;
+        for (; l + D < seg.l1 || (more && l < seg.l1); l += D) {
+            const bool last = l + D >= seg.l1;
+            Segment from = seg;
+            int at = l + D;
+            if (last) {
+                from = nxt;
+                at = nxt.l0;
+            }
+#pragma unroll
+            for (int u = 0; u < D; ++u) {
+                if (u + 1 < D) turned(seg, u + 1, l + u + 1);
+                else turned(from, D, at);                // (the next D's first, fetched at u = 0)
+                if (l + u < seg.l1) multiply(seg, u, l + u);
+                fetch(from, u, at + u);
+                __builtin_amdgcn_sched_barrier(0);       // (lines stay apart: mixed, they need more registers than there are)
+            }
+        }
+        if (!more) {                     // the run's last lines: nothing to fetch
+#pragma unroll
+            for (int u = 0; u < D; ++u) {
+                if (l + u < seg.l1) {
+                    if (u + 1 < D) turned(seg, u + 1, l + u + 1);
+                    multiply(seg, u, l + u);
+                }
+            }
+        }
+        if constexpr (M > 0) acc[0] = dots_total<WL, M>(dot);
+        // (the last matrix instructions stand before a branch, across which the compiler does not keep the distance to the use of
+        // their results: sixteen cycles and more here)
+#pragma unroll
+        for (int g = 0; g < G; ++g) asm volatile("s_nop 15\n\ts_nop 3" : "+v"(acc[g]));
+        done(seg, acc);
+        if (!more) return;
+        seg = nxt;
+    }
+}
+// what decides which instance of stream() multiplies m rows
+template <int TY, int X> __device__ __forceinline__ int kind_of(int m) {
+    if (TY == FP && X == IN_LDS && m <= 8) return m <= 2 ? -2 : -8;
+    return (m + 15) >> 4;
+}
+// Runs of segments one behind the other, whatever their rows.  current: false if there is none; few: there are few lines in all.
+template <int TY, int WL, int X, int X_TALL, typename Current, typename Next, typename Done>
+__device__ __forceinline__ void stream_all(u32x4* turn, const unsigned char* xl, bool few, Current current, Next next, Done done) {
+    Segment seg;
+    constexpr int DEEP = X == IN_LDS ? (WL == 2 ? 10 : 16) : (WL == 2 ? 8 : 12);
+    while (current(seg)) {
+        const int kind = kind_of<TY, X>(seg.m);
+        auto same = [&](Segment& s) __attribute__((always_inline)) { return next(s) && kind_of<TY, X>(s.m) == kind; };
+        if constexpr (TY == FP && X == IN_LDS) {
+            if (kind == -2) {
+                stream<TY, WL, 1, 2, DEEP, X>(seg, turn, xl, same, done);
+                continue;
+            }
+            if (kind == -8) {
+                stream<TY, WL, 1, 8, 8, X>(seg, turn, xl, same, done);
+                continue;
+            }
+        }
+        if (kind == 1 && few) stream<TY, WL, 1, 0, 4, X>(seg, turn, xl, same, done);
+        else if (kind == 1) stream<TY, WL, 1, 0, DEEP, X>(seg, turn, xl, same, done);
+        else if (kind == 2) stream<TY, WL, 2, 0, 6, X_TALL>(seg, turn, xl, same, done);
+        else if (kind == 3) stream<TY, WL, 3, 0, 4, X_TALL>(seg, turn, xl, same, done);
+        else stream<TY, WL, 4, 0, X == IN_LDS ? 4 : 2, X_TALL>(seg, turn, xl, same, done);
+    }
+}
+// what a line of an expert with m rows costs a wavefront, in loads
+__device__ __forceinline__ int line_cost(int m) { return 2 + (m + 15) / 16 * 2; }
+
+// The lane's place in rows that lie in LDS: its 16 bytes of row r for a fragment, and of row r for dots().
+__device__ __forceinline__ unsigned fragment_at(int r, unsigned row_bytes) {
+    const int lq = (threadIdx.x & 63) >> 4;
+    return (unsigned)r * row_bytes + (unsigned)(lq ^ (r & 7)) * 16u;
+}
+__device__ __forceinline__ unsigned piece_at(int r, unsigned row_bytes) { return (unsigned)r * row_bytes + (unsigned)((threadIdx.x & 7) ^ (r & 7)) * 16u; }
+// `rows` rows of row_bytes (a multiple of 128) from memory into LDS in that order: all wavefronts, a row each; to be waited for (vmcnt) and
+// shown to the others by a barrier
+__device__ __forceinline__ void rows_to_lds(const void* from, int rows, unsigned row_bytes, unsigned char* to) {
+    const int lane = threadIdx.x & 63, wave = sgpr(threadIdx.x >> 6);
+    const __amdgpu_buffer_rsrc_t src = make_rsrc(from, (unsigned)rows * row_bytes);
+    for (int r = wave; r < rows; r += NW)
+        for (unsigned at = 0; at < row_bytes; at += 1024) {
+            const unsigned mine = at + (unsigned)((lane & ~7) | ((lane & 7) ^ (r & 7))) * 16u;
+            if (mine < row_bytes)        // (the row's end is a multiple of 128 bytes: the place is inside where the source is)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(src, (lds_void_t*)(to + (unsigned)r * row_bytes + at), 16, (unsigned)r * row_bytes + mine, 0, 0, 0);
+        }
+}
 
 // ---- routing
 struct Route {
@@ -165,13 +341,22 @@ struct Route {
     float* gate;
     int T, d, E, k, renorm;
 };
-template <int TT> struct RouteLds {      // TT: groups of 16 tokens
-    double part[NW * 16][TT * 16 + 1];   // [contraction part, expert][token]
-    float xsq[NW][TT * 16];
+// How T tokens are routed: TT groups of 16, x in LDS or not; a wavefront takes EB blocks of 16 experts, D lines in flight.
+// (More experts a wavefront fetch x less often, but their sums take LDS: 128 KB for four blocks and 32 tokens.)
+template <int TT_, bool LDS_> struct How {
+    static constexpr int TT = TT_, EB = TT_ <= 1 || (TT_ == 2 && !LDS_) ? 4 : 2, D = TT_ == 1 ? 3 : 2;
+    static constexpr bool LDS = LDS_;
+};
+template <bool LDS> using Routed = How<0, LDS>;          // the choice is there already
+template <typename H> struct RouteLds {
+    double part[NW * H::EB * 16][H::TT * 16 + 1];        // [contraction part, expert][token]; the lines' turning places before
+    float xsq[NW][H::TT * 16];
+    float bias[MAXE];
     float most[NW];
 };
+template <bool LDS> struct RouteLds<How<0, LDS>> {};
 
-constexpr int TERMS = 32;                // terms summed up in fp32, by one matrix instruction
+constexpr int TERMS = 64;                // terms summed up in fp32: a line, by two matrix instructions
 
 // fp64 product of token row and expert row by a wavefront
 __device__ __forceinline__ double exact_dot(const uint16_t* xr, const uint16_t* wr, int d) {
@@ -195,255 +380,536 @@ __device__ __forceinline__ double exact_dot(const uint16_t* xr, const uint16_t* 
     return wave_sum_f64(s0 + s1);
 }
 
-// exp(v) for v <= 0 in 64 bits: what the rounding of v to fp32 took away is put back
-__device__ __forceinline__ float exp_of(double v) {
-    const float hi = (float)v, e = expf(hi);
-    return e > 0.f ? fmaf(e, (float)(v - (double)hi), e) : e;
+// unsigned numbers in the floats' order; 0 for what is no number
+__device__ __forceinline__ unsigned order_of(float v) {
+    const unsigned u = __float_as_uint(v);
+    return v == v ? u ^ (u >> 31 ? 0xffffffffu : 0x80000000u) : 0u;
 }
 
-template <int TT>
-__device__ __forceinline__ void route_all(const Route& p, RouteLds<TT>& s, Lists& l, bool write) {
+// A token whose choice (the wavefront's lanes `from` on, expert ids by falling logit) is not certain: the logits that are close to a chosen
+// one's are computed again in fp64, and the choice is made again among exact and well separated ones.  A wavefront; returns the choice
+// of number lane % 16.
+template <typename L>
+__device__ __forceinline__ int choose_again(const Route& p, L& s, int t, int se, double tau, int from, int rounds) {
+    const int lane = threadIdx.x & 63, E = p.E, k = p.k, d = p.d;
+    constexpr int NJ = MAXE / 64;
+    constexpr double NONE = -__builtin_huge_val();
+    auto close = [&](double a, double b) __attribute__((always_inline)) { return !(fabs(a - b) >= tau + 3e-7 * fabs(a)); };
+    const int last_e = __builtin_amdgcn_readlane(se, from + k - 1);
+    const double last = last_e == INT_MAX ? NONE : s.part[last_e][t], least = last - (tau + 3e-7 * fabs(last));
+    double v[NJ];
+    unsigned again = 0;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const int e = lane + 64 * j;
+        v[j] = e < E ? s.part[e][t] : NONE;
+        bool near = false;
+        for (int r = 0; r < rounds; ++r) {
+            const int oe = __builtin_amdgcn_readlane(se, from + r);
+            if (oe != INT_MAX) near = near || (oe != e && close(s.part[oe][t], v[j]));
+        }
+        if (e < E && near && !(v[j] < least)) again |= 1u << j;
+    }
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+        for (unsigned long long m = __ballot(again >> j & 1); m; m &= m - 1) {
+            const int src = __builtin_ctzll(m), e = src + 64 * j;
+            const double dot = exact_dot(p.x + (size_t)t * d, p.w + (size_t)e * d, d) + (p.bias ? (double)p.bias[e] : 0.0);
+            if (lane == src) {
+                v[j] = dot;
+                s.part[e][t] = dot;
+            }
+        }
+    unsigned taken = 0;                  // of this lane's experts
+    int chosen = INT_MAX;
+    for (int r = 0; r < rounds; ++r) {
+        double bv = NONE;
+        int be = INT_MAX;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+            if (!(taken >> j & 1) && lane + 64 * j < E && beats(v[j], lane + 64 * j, bv, be)) { bv = v[j]; be = lane + 64 * j; }
+        row_best_f64(bv, be, true);
+        if (be != INT_MAX && (be & 63) == lane) taken |= 1u << (be >> 6);
+        if ((lane & 15) == r) chosen = be;
+    }
+    return chosen;
+}
+
+// Sixteen lanes choose for a token, four tokens a wavefront from t0 on; lane `sub` of them holds experts sub, sub + 16, ... (NI of them) as
+// numbers in the order of the logits rounded to fp32.
+template <int NI, typename L>
+__device__ __forceinline__ void choose(const Route& p, L& s, Lists& l, int t0, float wn, int KS, bool write) {
+    const int lane = threadIdx.x & 63, sub = lane & 15, T = p.T, E = p.E, k = p.k, rounds = k + 1 < E ? k + 1 : E;
+    const int t = t0 + (lane >> 4), tt = t < T ? t : T - 1;
+    double v[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) v[i] = s.part[sub + 16 * i < E ? sub + 16 * i : E - 1][tt];
+    unsigned key[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) key[i] = sub + 16 * i < E ? order_of((float)v[i]) : 0u;
+    float xs = 0.f;
+#pragma unroll
+    for (int q = 0; q < NW; ++q) xs += q < KS ? s.xsq[q][tt] : 0.f;
+    // A logit is off by two roundings per term of a matrix instruction at most (the order inside it is not known); twice that is
+    // what two logits may be wrong by against one another.  The choice compares them rounded to fp32.
+    const double tau = 2.1f * 5.9604645e-8f * (2 * TERMS + 6) * (sqrtf(xs) * 1.0001f) * (sqrtf(wn) * 1.0001f);
+    int se = INT_MAX;                    // lane `sub`: the choice of that number
+    for (int r = 0; r < rounds; ++r) {
+        unsigned best = key[0];
+#pragma unroll
+        for (int i = 1; i < NI; ++i) best = max(best, key[i]);
+        unsigned top = best;
+        top = max(top, (unsigned)dpp_xchg<0>((int)top));
+        top = max(top, (unsigned)dpp_xchg<1>((int)top));
+        top = max(top, (unsigned)dpp_xchg<2>((int)top));
+        top = max(top, (unsigned)dpp_xchg<3>((int)top));
+        // (equal ones: any of them, the exact choice sees to it)
+        const int winner = __builtin_ctz((unsigned)(__ballot(best == top) >> (lane & 48)) & 0xffffu);
+        int e = 0;
+#pragma unroll
+        for (int i = NI - 1; i >= 0; --i) e = key[i] == top ? sub + 16 * i : e;
+        e = __shfl(e, (lane & 48) + winner);
+        se = sub == r && top ? e : se;
+#pragma unroll
+        for (int i = 0; i < NI; ++i) key[i] = e == sub + 16 * i ? 0u : key[i];
+    }
+    double sv = se != INT_MAX ? s.part[se][tt] : -__builtin_huge_val();
+    const double next = __shfl(sv, lane + 1 < 64 ? lane + 1 : lane);
+    // (written so that a bound or a difference that is no number counts as close; a token with a NaN has nothing to be looked at again)
+    const unsigned long long look = __ballot(t < T && sub + 1 < rounds && !(fabs(sv - next) >= tau + 3e-7 * fabs(sv)) && xs == xs);
+    if (look) {
+#pragma nounroll
+        for (int q = 0; q < 4; ++q)
+            if (look >> (16 * q) & 0xffffu) {
+                const int again = choose_again(p, s, t0 + q, se, lane_f64(tau, 16 * q), 16 * q, rounds);
+                if ((lane >> 4) == q) se = again;
+            }
+        sv = se != INT_MAX ? s.part[se][tt] : -__builtin_huge_val();
+#pragma unroll
+        for (int i = 0; i < NI; ++i) v[i] = s.part[sub + 16 * i < E ? sub + 16 * i : E - 1][tt];
+    }
+    const double top = __shfl(sv, lane & 48);
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < NI; ++i) sum += sub + 16 * i < E ? __expf((float)(v[i] - top)) : 0.f;
+    sum += dpp_xchg<0>(sum);
+    sum += dpp_xchg<1>(sum);
+    sum += dpp_xchg<2>(sum);
+    sum += dpp_xchg<3>(sum);
+    const float mine = se == INT_MAX ? __builtin_nanf("") : __expf((float)(sv - top));
+    float chosen = sub < k ? mine : 0.f;
+    chosen += dpp_xchg<0>(chosen);
+    chosen += dpp_xchg<1>(chosen);
+    chosen += dpp_xchg<2>(chosen);
+    chosen += dpp_xchg<3>(chosen);
+    if (t < T && sub < k) {
+        const float over = p.renorm && sum == sum ? chosen : sum;        // (a logit that is no number: nor is any gate)
+        l.id[t * k + sub] = se;
+        if (write) {
+            p.idx[t * k + sub] = se;
+            p.gate[t * k + sub] = mine / over;
+        }
+    }
+}
+
+template <typename H>
+__device__ __forceinline__ void route_all(const Route& p, unsigned char* smem, const unsigned char* xl, Lists& l, bool write) {
+    constexpr int TT = H::TT, XL = 2, EB = H::EB, D = H::D, PLACE = (EB + (H::LDS ? 0 : TT)) * 128;
+    RouteLds<H>& s = *(RouteLds<H>*)smem;
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int T = p.T, d = p.d, E = p.E, k = p.k;
-    // NB blocks of 16 experts, the contraction in KS parts; wavefront = block + NB part
-    const int blocks = (E + 15) >> 4, NB = blocks <= 1 ? 1 : blocks <= 2 ? 2 : blocks <= 4 ? 4 : blocks <= 8 ? 8 : 16, KS = NW / NB;
-    const int block = wave % NB, part = wave / NB;
-    const float my_norm = tid < E ? p.norm2[tid] : 0.f;
-    double acc[TT][4];
+    const int T = p.T, d = p.d, E = p.E;
+    // NB groups of EB blocks of 16 experts, the contraction in KS parts; wavefront = group + NB part
+    const int groups = (E + 16 * EB - 1) / (16 * EB), NB = groups <= 1 ? 1 : groups <= 2 ? 2 : groups <= 4 ? 4 : 8, KS = NW / NB;
+    const int group = wave % NB, part = wave / NB;
+    // (fetched before the product, so that their latency passes under it)
+    const float my_norm = tid < E ? p.norm2[tid] : 0.f, my_bias = tid < E && p.bias ? p.bias[tid] : 0.f;
+    double acc[EB][TT][4];
 #pragma unroll
-    for (int g = 0; g < TT; ++g)
+    for (int b = 0; b < EB; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[g][r] = 0.0;
-    float xsq[TT] = {};
-    if (block < blocks) {
-        const int e = block * 16 + l16 < E ? block * 16 + l16 : E - 1;
-        const uint16_t* wr = p.w + (size_t)e * d + lq * 8;
-        const uint16_t* xr[TT];
+        for (int g = 0; g < TT; ++g)
 #pragma unroll
-        for (int g = 0; g < TT; ++g) xr[g] = p.x + (size_t)(g * 16 + l16 < T ? g * 16 + l16 : T - 1) * d + lq * 8;
-        constexpr int U = TT == 1 ? 6 : TT == 2 ? 4 : TT == 3 ? 3 : 2;   // 32-term steps in flight
-        const int steps = d / TERMS;
-        for (int c = part; c < steps; c += KS * U) {
-            u32x4 w[U], x[U][TT];
+            for (int r = 0; r < 4; ++r) acc[b][g][r] = 0.0;
+    float xsq[TT][XL] = {};
+    if (group < groups) {
+        // whole lines, eight rows a load, turned into fragments in LDS, as in stream()
+        const __amdgpu_buffer_rsrc_t w = make_rsrc(p.w, (unsigned)(E * d) * 2u), x = make_rsrc(p.x, (unsigned)(T * d) * 2u);
+        u32x4* const turn = (u32x4*)smem + wave * PLACE;
+        const int st_at = (lane >> 3) * 8 + ((lane & 7) ^ (lane >> 3)), rd_at = l16 * 8 + (lq ^ (l16 & 7));
+        const unsigned piece = (unsigned)(lane & 7) * 16u;
+        unsigned w_at[EB][2], x_at[TT][XL];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int at = (c + u * KS < steps ? c + u * KS : c) * TERMS;
-                w[u] = *(const u32x4*)(wr + at);
+        for (int b = 0; b < EB; ++b)
 #pragma unroll
-                for (int g = 0; g < TT; ++g) x[u][g] = *(const u32x4*)(xr[g] + at);
+            for (int i = 0; i < 2; ++i) {
+                const int e = (group * EB + b) * 16 + i * 8 + (lane >> 3);
+                w_at[b][i] = e < E ? (unsigned)e * (unsigned)d * 2u + piece : NOWHERE;
             }
-            if (block == 0) {
 #pragma unroll
-                for (int u = 0; u < U; ++u)
-                    if (c + u * KS < steps) {
+        for (int g = 0; g < TT; ++g)
 #pragma unroll
-                        for (int g = 0; g < TT; ++g)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float a = __uint_as_float(x[u][g][j] << 16), b = __uint_as_float(x[u][g][j] & 0xffff0000u);
-                                xsq[g] = fmaf(a, a, fmaf(b, b, xsq[g]));
-                            }
-                    }
+            for (int i = 0; i < XL; ++i) {
+                const int t = g * 16 + i * 8 + (lane >> 3);
+                x_at[g][i] = t < T ? (unsigned)t * (unsigned)d * 2u + piece : NOWHERE;
             }
-            // (no branch between a matrix instruction and the use of its result: the compiler does not keep
-            // their distance across one.  Steps past the end give zeros.)
+        unsigned x_in[TT];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const bool in = c + u * KS < steps;
-                f32x4 v[TT];
-#pragma unroll
-                for (int g = 0; g < TT; ++g) v[g] = mma<BF>(w[u], x[u][g], f32x4{0.f, 0.f, 0.f, 0.f});
+        for (int g = 0; g < TT; ++g) x_in[g] = fragment_at(g * 16 + l16 < T ? g * 16 + l16 : T - 1, (unsigned)d * 2u);
+        const int lines = d / 64;
+        u32x4 a[D][EB][2], c[H::LDS ? 1 : D][TT][XL];
+        auto fetch = [&](int u, int line) __attribute__((always_inline)) {
+            const bool in = line < lines;
+            const int at = in ? line * 128 : 0;
+            if constexpr (!H::LDS) {
 #pragma unroll
                 for (int g = 0; g < TT; ++g)
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[g][r] += (double)(in ? v[g][r] : 0.f);
+                    for (int i = 0; i < XL; ++i) c[u][g][i] = __builtin_amdgcn_raw_buffer_load_b128(x, (int)(in ? x_at[g][i] : NOWHERE), at, 0);
+            }
+#pragma unroll
+            for (int b = 0; b < EB; ++b)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) a[u][b][i] = __builtin_amdgcn_raw_buffer_load_b128(w, (int)(in ? w_at[b][i] : NOWHERE), at, 0);
+        };
+#pragma unroll
+        for (int u = 0; u < D; ++u) fetch(u, part + u * KS);
+        if constexpr (H::LDS) {
+            MOE_WAIT_VMCNT(0);           // (x, and the first lines of W_g, which are next anyway)
+            __syncthreads();
+        }
+        for (int line = part; line < lines; line += D * KS) {
+#pragma unroll
+            for (int u = 0; u < D; ++u) {
+                if constexpr (!H::LDS) {
+#pragma unroll
+                    for (int g = 0; g < TT; ++g)
+#pragma unroll
+                        for (int i = 0; i < XL; ++i) turn[(EB + g) * 128 + i * 64 + st_at] = c[u][g][i];
+                }
+#pragma unroll
+                for (int b = 0; b < EB; ++b)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) turn[b * 128 + i * 64 + st_at] = a[u][b][i];
+                if (!H::LDS && group == 0) {
+#pragma unroll
+                    for (int g = 0; g < TT; ++g)
+#pragma unroll
+                        for (int i = 0; i < XL; ++i)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const unsigned v = c[H::LDS ? 0 : u][g][i][j];
+                                const float lo = __uint_as_float(v << 16), hi = __uint_as_float(v & 0xffff0000u);
+                                xsq[g][i] = fmaf(lo, lo, fmaf(hi, hi, xsq[g][i]));
+                            }
+                }
+                u32x4 xf[TT][2];
+#pragma unroll
+                for (int g = 0; g < TT; ++g)
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+                        xf[g][v] = H::LDS ? *(const u32x4*)(xl + (x_in[g] ^ (64u * v)) + (line + u * KS < lines ? line + u * KS : 0) * 128)
+                                          : turn[(EB + g) * 128 + (rd_at ^ (4 * v))];
+                // (no branch between a matrix instruction and the use of its result: the compiler does not keep their
+                // distance across one)
+#pragma unroll
+                for (int b = 0; b < EB; ++b) {
+                    const u32x4 wf[2] = {turn[b * 128 + rd_at], turn[b * 128 + (rd_at ^ 4)]};
+                    f32x4 q[TT];
+#pragma unroll
+                    for (int g = 0; g < TT; ++g) q[g] = mma<BF>(wf[1], xf[g][1], mma<BF>(wf[0], xf[g][0], f32x4{0.f, 0.f, 0.f, 0.f}));
+#pragma unroll
+                    for (int g = 0; g < TT; ++g)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) acc[b][g][r] += H::LDS && line + u * KS >= lines ? 0.0 : (double)q[g][r];
+                }
+                fetch(u, line + (u + D) * KS);
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
+    } else if constexpr (H::LDS) {
+        __syncthreads();
     }
+    __syncthreads();                     // (the sums take the turning places' memory)
     // D[i][j]: lane holds token j = l16, experts i = 4 lq + r
 #pragma unroll
-    for (int g = 0; g < TT; ++g) {
+    for (int g = 0; g < TT; ++g)
+        if (g * 16 + l16 < T) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s.part[wave * 16 + 4 * lq + r][g * 16 + l16] = acc[g][r];
-        float q = xsq[g];
-        q += __shfl_xor(q, 16);
-        q += __shfl_xor(q, 32);
-        if (block == 0 && lq == 0) s.xsq[part][g * 16 + l16] = q;
+            for (int b = 0; b < EB; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) s.part[(wave * EB + b) * 16 + 4 * lq + r][g * 16 + l16] = acc[b][g][r];
+        }
+    if constexpr (H::LDS) {
+        for (int t = wave; t < T; t += NW) {
+            float q = 0.f;
+            for (int at = lane * 16; at < d * 2; at += 1024) {
+                const u32x4 v = *(const u32x4*)(xl + t * d * 2 + at);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float lo = __uint_as_float(v[j] << 16), hi = __uint_as_float(v[j] & 0xffff0000u);
+                    q = fmaf(lo, lo, fmaf(hi, hi, q));
+                }
+            }
+            q = (float)wave_sum_f64((double)q);
+            if (lane < KS) s.xsq[lane][t] = lane == 0 ? q : 0.f;
+        }
+    } else if (group == 0) {
+#pragma unroll
+        for (int g = 0; g < TT; ++g)
+#pragma unroll
+            for (int i = 0; i < XL; ++i) {
+                float q = xsq[g][i];     // the eight lanes of a row
+                q += dpp_xchg<0>(q);
+                q += dpp_xchg<1>(q);
+                q += dpp_xchg<2>(q);
+                if ((lane & 7) == 0) s.xsq[part][g * 16 + i * 8 + (lane >> 3)] = q;
+            }
     }
+    if (tid < E) s.bias[tid] = my_bias;
     const float most = moe_wave_max_nonneg(my_norm);
     if (lane == 0) s.most[wave] = most;
     __syncthreads();
+    // the logits, in the first part's place
+    const int bits = T <= 1 ? 0 : 32 - __builtin_clz((unsigned)(T - 1));
+    for (int i = tid; i < E << bits; i += NTH) {
+        const int t = i & ((1 << bits) - 1), e = i >> bits;
+        if (t < T) {
+            double v[NW];
+#pragma unroll
+            for (int q = 0; q < NW; ++q) v[q] = s.part[((q < KS ? q : 0) * NB * EB + (e >> 4)) * 16 + (e & 15)][t];
+            double sum = (double)s.bias[e];
+#pragma unroll
+            for (int q = 0; q < NW; ++q) sum += q < KS ? v[q] : 0.0;
+            s.part[e][t] = sum;
+        }
+    }
     float wn = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) wn = fmaxf(wn, s.most[w]);
-
-    // a wavefront chooses for a token; lane holds experts lane, lane + 64, ...
-    constexpr int NJ = MAXE / 64;
-    constexpr double NONE = -__builtin_huge_val();
-    for (int t = wave; t < T; t += NW) {
-        double v[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            const int e = lane + 64 * j;
-            v[j] = NONE;
-            if (e < E) {
-                v[j] = p.bias ? (double)p.bias[e] : 0.0;
-                for (int q = 0; q < KS; ++q) v[j] += s.part[(q * NB + (e >> 4)) * 16 + (e & 15)][t];
-            }
-        }
-        float xs = 0.f;
-        for (int q = 0; q < KS; ++q) xs += s.xsq[q][t];
-        // |error| of a logit: two roundings per term of a matrix instruction (the order inside it is not known), the
-        // sums of norms rounded up; twice that is what two logits may be wrong by against one another
-        const float tau = 2.1f * 5.9604645e-8f * (2 * TERMS + 6) * (sqrtf(xs) * 1.0001f) * (sqrtf(wn) * 1.0001f);
-        const int rounds = k + 1 < E ? k + 1 : E;
-        double sv = NONE;                // lane r: the r-th choice
-        int se = INT_MAX;
-        auto choose = [&]() __attribute__((always_inline)) {
-            unsigned taken = 0;          // of this lane's experts
-            for (int r = 0; r < rounds; ++r) {
-                double bv = NONE;
-                int be = INT_MAX;
-#pragma unroll
-                for (int j = 0; j < NJ; ++j)
-                    if (j * 64 < E && !(taken >> j & 1) && lane + 64 * j < E && beats(v[j], lane + 64 * j, bv, be)) { bv = v[j]; be = lane + 64 * j; }
-                row_best_f64(bv, be, true);
-                if (be != INT_MAX && (be & 63) == lane) taken |= 1u << (be >> 6);
-                if (lane == r) { sv = bv; se = be; }
-            }
-        };
-        choose();
-        const double next = __shfl(sv, lane + 1 < 64 ? lane + 1 : lane);
-        // (written so that a bound or a difference that is no number counts as near)
-        if (__ballot(lane + 1 < rounds && !(sv - next >= (double)tau))) {
-            // near one another: these logits again, in fp64
-            const double last = lane_f64(sv, k - 1) - (double)tau;
-            unsigned again = 0;
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const int e = lane + 64 * j;
-                bool near = false;
-                if (j * 64 < E)
-                    for (int r = 0; r < rounds; ++r) {
-                        const double o = lane_f64(sv, r);
-                        const int oe = __builtin_amdgcn_readlane(se, r);
-                        near = near || (oe != e && !(fabs(v[j] - o) >= (double)tau));
-                    }
-                if (e < E && near && !(v[j] < last)) again |= 1u << j;
-            }
-#pragma unroll
-            for (int j = 0; j < NJ; ++j)
-                for (unsigned long long m = __ballot(again >> j & 1); m; m &= m - 1) {
-                    const int src = __builtin_ctzll(m), e = src + 64 * j;
-                    const double dot = exact_dot(p.x + (size_t)t * d, p.w + (size_t)e * d, d) + (p.bias ? (double)p.bias[e] : 0.0);
-                    if (lane == src) v[j] = dot;
-                }
-            choose();
-        }
-        const double top = lane_f64(sv, 0);
-        float e = 0.f;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j)
-            if (lane + 64 * j < E) e += exp_of(v[j] - top);
-        e += dpp_xchg<0>(e);
-        e += dpp_xchg<1>(e);
-        e += dpp_xchg<2>(e);
-        e += dpp_xchg<3>(e);
-        const float all = (__int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), 0)) + __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), 16))) +
-                          (__int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), 32)) + __int_as_float(__builtin_amdgcn_readlane(__float_as_int(e), 48)));
-        const float mine = se == INT_MAX ? __builtin_nanf("") : exp_of(sv - top);
-        float chosen = 0.f;
-        for (int r = 0; r < k; ++r) chosen += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(mine), r));
-        if (lane < k) {
-            const float over = p.renorm && all == all ? chosen : all;    // (a logit that is no number: nor is any gate)
-            l.id[t * k + lane] = se;
-            if (write) {
-                p.idx[t * k + lane] = se;
-                p.gate[t * k + lane] = mine / over;
-            }
-        }
+    __syncthreads();
+    for (int t0 = wave * 4; t0 < T; t0 += NW * 4) {
+        if (E <= 64) choose<4>(p, s, l, t0, wn, KS, write);
+        else if (E <= 128) choose<8>(p, s, l, t0, wn, KS, write);
+        else choose<16>(p, s, l, t0, wn, KS, write);
     }
     __syncthreads();
 }
 
 // ---- launch 1
+constexpr unsigned X_BYTES = 64 << 10, H_BYTES = 80 << 10;       // of LDS for x, and for the hidden activations in launch 2
 struct Hidden {
     Route route;
     const void* x;
     const void* const *w_in, *const *s_w_in;
-    unsigned char *h, *s_h;              // hidden activations of the rows [A,F] and of the shared expert [T,shared_F]
-    int F, shared_F, glu;
+    unsigned char *h, *s_h;              // hidden activations of the rows (A of F) and of the shared expert (T of shared_F)
+    int F, shared_F, glu, h_rows;        // h_rows: H row by row, else an expert's rows piece by piece (see finish)
 };
 __device__ __forceinline__ uint16_t half_of(float v) {           // saturating, nearest-even
     return __builtin_bit_cast(uint16_t, (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f));
 }
 
-// TT: groups of 16 tokens that every work-group routes itself; 0: idx is there already
-template <bool F32, int TT>
+template <bool F32, typename H>
 __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : BF;
-    constexpr size_t TURNS = sizeof(u32x4) * TURN_PIECES * NW, ROUTE = TT ? sizeof(RouteLds<TT ? TT : 1>) : 0;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[TURNS > ROUTE ? TURNS : ROUTE];
+    constexpr size_t PLACE = H::LDS ? 256 : 384, PLACES = sizeof(u32x4) * (PLACE + 256) * NW, ROUTE = sizeof(RouteLds<H>);
+    __shared__ __attribute__((aligned(16))) unsigned char smem[PLACES > ROUTE ? PLACES : ROUTE];
+    static_assert(sizeof smem >= sizeof(u32x4) * NW * (H::EB + (H::LDS ? 0 : H::TT)) * 128, "the routing's turning places");
+    __shared__ __attribute__((aligned(16))) unsigned char xl[H::LDS ? X_BYTES : 16];
     __shared__ Lists l;
+    __shared__ int head_lines[NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const int T = p.route.T, d = p.route.d, E = p.route.E, k = p.route.k;
-    if constexpr (TT > 0) {
-        route_all<TT>(p.route, *(RouteLds<TT>*)smem, l, blockIdx.x == 0);
+    const unsigned row_bytes = (unsigned)d * ES;
+    if constexpr (H::LDS) rows_to_lds(p.x, T, row_bytes, xl);
+    const void* const mine_w = tid < E ? p.w_in[tid] : nullptr;
+    if (tid < 2 * MAXE) (&l.bits[0][0])[tid] = 0u;
+    int e = -1;
+    if constexpr (H::TT > 0) {
+        route_all<H>(p.route, smem, xl, l, blockIdx.x == 0);
+        if (tid < T * k) e = l.id[tid];
     } else {
-        if (tid < T * k) l.id[tid] = p.route.idx[tid];
+        if (tid < T * k) e = p.route.idx[tid];
+        if constexpr (H::LDS) MOE_WAIT_VMCNT(0);
         __syncthreads();
     }
-    make_lists(l, T, E, k);
-    u32x4* const turn = (u32x4*)smem + wave * TURN_PIECES;
-    const __amdgpu_buffer_rsrc_t x = make_rsrc(p.x, (unsigned)(T * d) * ES);
-    const unsigned w_off = (unsigned)(lane >> 3) * (unsigned)d * ES + (unsigned)(lane & 7) * 16u, piece = (unsigned)(lane & 7) * 16u;
-    const size_t row_bytes = (size_t)d * ES;
-    // items of 16 weight rows: the shared expert's first (they have the most rows), then the active experts'
-    const int s_items = p.shared_F / 8, per = p.F / (p.glu ? 8 : 16), items = s_items + sgpr(l.n_active) * per;
-    for (int item = wave * (int)gridDim.x + (int)blockIdx.x; item < items; item += NW * (int)gridDim.x) {
-        const bool shared = item < s_items, glu = shared || p.glu;
-        const int rest = item - s_items, ai = shared ? 0 : rest / per, q = shared ? item : rest - ai * per;
-        const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? 0 : sgpr(l.first[e]);
-        const int m = shared ? T : sgpr(l.first[e + 1]) - r0;
-        const unsigned char* w = (const unsigned char*)sgpr_ptr(shared ? p.s_w_in[0] : p.w_in[e]);
+    if (tid < E) l.w[tid] = mine_w;
+    make_lists(l, E, e, tid / k, 0.f);
+    u32x4* const turn = (u32x4*)smem + wave * PLACE;
+    f32x4* const heads = (f32x4*)((u32x4*)smem + NW * PLACE);            // [wavefront][group][lane]
+    const __amdgpu_buffer_rsrc_t x = make_rsrc(p.x, (unsigned)T * row_bytes);
+    const int lines = d * ES / 128, grid = (int)gridDim.x, block = (int)blockIdx.x;
+    // Items of 16 weight rows: the shared expert's first, then the active experts'.  The work-group has every grid-th of them, and its
+    // wavefronts equal shares of their lines by what these cost: whole items, and an item's head or tail at either end.
+    const int s_items = p.shared_F / 8, per = p.F / (p.glu ? 8 : 16), n_active = sgpr(l.n_active), items = s_items + n_active * per;
+    const int mine = items > block ? (items - block + grid - 1) / grid : 0;
+    auto cost_of = [&](int n) __attribute__((always_inline)) {           // of a line of the work-group's item n
+        const int item = n * grid + block - s_items, e = l.active[item < 0 || n >= mine ? 0 : item / per];
+        return n >= mine ? 0u : (unsigned)line_cost(item < 0 ? T : l.first[e + 1] - l.first[e]);
+    };
+    const unsigned c0 = cost_of(lane), up0 = moe_wave_scan_u32(c0);
+    unsigned all = (unsigned)__builtin_amdgcn_readlane((int)up0, 63);
+    for (int n0 = 64; n0 < mine; n0 += 64) all += moe_wave_sum_u32(cost_of(n0 + lane));
+    const int total = (int)(all * (unsigned)lines), lo = sgpr((int)((unsigned long long)total * (unsigned)wave / NW)),
+              hi = sgpr((int)((unsigned long long)total * (unsigned)(wave + 1) / NW));
+    // the first item of the share, and where it begins
+    int n = 0, base = 0;
+    for (int n0 = 0; n0 < mine; n0 += 64) {
+        const unsigned up = n0 ? moe_wave_scan_u32(cost_of(n0 + lane)) : up0;
+        const int count = (int)__popcll(__ballot(n0 + lane < mine && (base + (int)up) * lines <= lo));
+        if (count) base += __builtin_amdgcn_readlane((int)up, count - 1);
+        n += count;
+        if (count < 64) break;
+    }
+    base = sgpr(base) * lines;
+    // Where item n is: expert number ai of the active ones (-1: the shared one), item q of its.
+    struct Place { int n, ai, q; };
+    auto place_of = [&](int n) __attribute__((always_inline)) {
+        const int item = n * grid + block, rest = item - s_items;
+        Place c = {n, -1, item};
+        if (rest >= 0) {
+            c.ai = rest / per;
+            c.q = rest - c.ai * per;
+        }
+        return c;
+    };
+    auto behind = [&](Place c) __attribute__((always_inline)) {
+        ++c.n;
+        c.q += grid;
+        while (c.q >= (c.ai < 0 ? s_items : per) && c.ai < n_active) {
+            c.q -= c.ai < 0 ? s_items : per;
+            ++c.ai;
+        }
+        return c;
+    };
+    struct Item {
+        int r0, m, width, out0;
+        bool glu;
+        unsigned char* h;
+    };
+    auto item_of = [&](const Place& c) __attribute__((always_inline)) {
+        Item it;
+        const bool shared = c.ai < 0;
+        const int e = shared ? 0 : sgpr(l.active[c.ai]), q = c.q;
+        it.glu = shared || p.glu;
+        it.r0 = shared ? 0 : sgpr(l.first[e]);
+        it.m = shared ? T : sgpr(l.first[e + 1]) - it.r0;
+        it.width = shared ? p.shared_F : p.F;
+        it.h = shared ? p.s_h : p.h;
+        it.out0 = F32 ? (it.glu ? (q >> 2) * 32 + (q & 3) * 8 : q * 16)
+                      : (it.glu ? (q >> 2) * 32 + (q & 1) * 16 + ((q >> 1) & 1) : (q >> 1) * 32 + (q & 1));
+        return it;
+    };
+    auto finish = [&](const Item& it, f32x4 a, int g) __attribute__((always_inline)) {
+        const int r = g * 16 + l16;
+        float v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float up = __shfl_xor(a[i], 32);
+            v[i] = it.glu ? silu_f(a[i]) * up : fmaxf(a[i], 0.f);
+        }
+        if (r < it.m && (!it.glu || lq < 2)) {
+            // H row by row; or an expert's rows piece by piece, 16 bytes of every row behind one another, so that a fragment of any rows is
+            // one run of bytes.  The lane's four outputs are in one piece (16 bits: every other one of its eight).
+            const int col = it.out0 + 4 * lq * (F32 ? 1 : 2), piece = col * ES / 16;
+            unsigned char* to = it.h + (size_t)it.r0 * it.width * ES + (p.h_rows ? (size_t)r * it.width * ES + piece * 16 : ((size_t)piece * it.m + r) * 16);
+            if constexpr (F32) {
+                *(f32x4*)to = f32x4{v[0], v[1], v[2], v[3]};
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) ((uint16_t*)to)[(col & 1) + 2 * i] = half_of(v[i]);
+            }
+        }
+    };
+    // the segment of an item that lies in the share; false behind its end
+    auto segment = [&](Segment& s, const Place& c, int base) __attribute__((always_inline)) {
+        if (c.n >= mine || base >= hi) return false;
+        const bool shared = c.ai < 0, glu = shared || p.glu;
+        const int e = shared ? 0 : sgpr(l.active[c.ai]), r0 = shared ? 0 : sgpr(l.first[e]), q = c.q;
+        s.m = shared ? T : sgpr(l.first[e + 1]) - r0;
+        const int cost = line_cost(s.m);
+        s.l0 = 0;
+        s.l1 = lines;
+        if (lo > base) s.l0 = (lo - base + cost - 1) / cost;
+        if (hi < base + lines * cost) s.l1 = (hi - base + cost - 1) / cost;
         // Packed rows (moe_pack_weights): 16-bit rows 16 h + j of a block of 32 are outputs 2 j + h, fp32 rows are in order; with SwiGLU
         // blocks of 32 gate and 32 up rows alternate.  An item is 16 rows of a block, or 8 gate rows and their 8 up rows.
         const int p0 = glu ? (q >> 2) * 64 + (q & 3) * 8 : q * 16;
-        const int out0 = F32 ? (glu ? (q >> 2) * 32 + (q & 3) * 8 : q * 16)
-                             : (glu ? (q >> 2) * 32 + (q & 1) * 16 + ((q >> 1) & 1) : (q >> 1) * 32 + (q & 1));
-        constexpr int out_step = F32 ? 1 : 2;
-        unsigned x_at[4][2];
+        const unsigned char* w = (const unsigned char*)sgpr_ptr(shared ? p.s_w_in[0] : l.w[e]) + (size_t)p0 * row_bytes;
+        const unsigned up = (glu ? 32u : 8u) * row_bytes, at = (unsigned)(lane >> 3) * row_bytes + (unsigned)(lane & 7) * 16u;
+        s.w = make_rsrc(w, up + 8u * row_bytes);
+        s.w_at[0] = at;
+        s.w_at[1] = up + at;
+        s.x = x;
+        s.x_step = 64;
+        auto token = [&](int r) __attribute__((always_inline)) { return shared ? r : (int)l.t[r0 + r]; };
+        if constexpr (H::LDS) {
+            if (kind_of<TY, IN_LDS>(s.m) < 0) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+                for (int r = 0; r < 8; ++r) s.x_at[r] = piece_at(token(r < s.m ? r : s.m - 1), row_bytes);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = g * 16 + i * 8 + (lane >> 3);
-                x_at[g][i] = NOWHERE;
-                if (r < m) x_at[g][i] = (unsigned)(shared ? r : (int)l.a[r0 + r] / k) * (unsigned)row_bytes + piece;
+                for (int g = 0; g < 4; ++g) s.x_at[g] = fragment_at(token(g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
             }
-        f32x4 acc[4];
-        const unsigned char* w0 = w + p0 * row_bytes;
-        const int groups = lines_product_rows<TY, 2>(m, w0, w0 + (glu ? 32 : 8) * row_bytes, w_off, x, x_at, 0, d * ES / 128, acc, turn);
-        const int width = shared ? p.shared_F : p.F;
-        unsigned char* h = shared ? p.s_h : p.h;
-        for (int g = 0; g < groups; ++g) {
-            f32x4 a = g == 0 ? acc[0] : g == 1 ? acc[1] : g == 2 ? acc[2] : acc[3];
-            const int r = g * 16 + l16;
-            float v[4];
+        } else if (s.m <= 16) {
+            s.x_at[0] = NOWHERE;
+            if (l16 < s.m) s.x_at[0] = (unsigned)token(l16) * row_bytes + (unsigned)lq * 16u;
+        } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float up = __shfl_xor(a[i], 32);
-                v[i] = glu ? silu_f(a[i]) * up : fmaxf(a[i], 0.f);
+            for (int i = 0; i < 8; ++i) {
+                const int r = i * 8 + (lane >> 3);
+                s.x_at[i] = NOWHERE;
+                if (r < s.m) s.x_at[i] = (unsigned)token(r) * row_bytes + (unsigned)(lane & 7) * 16u;
             }
-            if (r < m && (!glu || lq < 2)) {
-                unsigned char* to = h + ((size_t)(r0 + r) * width + out0 + 4 * lq * out_step) * ES;
-                if constexpr (F32) {
-                    *(f32x4*)to = f32x4{v[0], v[1], v[2], v[3]};
+        }
+        return true;
+    };
+    Place here = place_of(n), tail = {};
+    int tail_lines = 0;                  // > 0: of an item whose rest is with the wavefronts behind
+    if (lane == 0) head_lines[wave] = 0;
+    stream_all<TY, 2, H::LDS ? IN_LDS : FRAGMENTS, H::LDS ? IN_LDS : LINES>(
+        turn, xl, hi - lo <= 16,
+        [&](Segment& s) __attribute__((always_inline)) {
+            while (segment(s, here, base)) {
+                if (s.l0 < s.l1) return true;
+                base += line_cost(s.m) * lines;
+                here = behind(here);
+            }
+            return false;
+        },
+        [&](Segment& s) __attribute__((always_inline)) { return segment(s, behind(here), base + line_cost(s.m) * lines) && s.l0 < s.l1; },
+        [&](const Segment& s, auto& acc) __attribute__((always_inline)) {
+            constexpr int G = sizeof(acc) / sizeof(acc[0]);
+            if (s.l0 == 0 && s.l1 == lines) {
+                const Item it = item_of(here);
+#pragma unroll
+                for (int g = 0; g < G; ++g) finish(it, acc[g], g);
+            } else {
+                // (the turning place is free only behind the last segment, which a tail is)
+                f32x4* const to = s.l0 ? heads + wave * 256 : (f32x4*)turn;
+#pragma unroll
+                for (int g = 0; g < G; ++g) to[g * 64 + lane] = acc[g];
+                if (s.l0) {
+                    if (lane == 0) head_lines[wave] = s.l1 - s.l0;
                 } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) ((uint16_t*)to)[2 * i] = half_of(v[i]);
+                    tail = here;
+                    tail_lines = s.l1;
                 }
             }
+            base += line_cost(s.m) * lines;
+            here = behind(here);
+        });
+    __syncthreads();
+    if (tail_lines) {
+        const Item it = item_of(tail);
+        for (int g = 0; g < (it.m + 15) >> 4; ++g) {
+            f32x4 a = ((const f32x4*)turn)[g * 64 + lane];
+            int have = tail_lines;
+            for (int w = wave + 1; have < lines; ++w) {
+                const int more = sgpr(head_lines[w]);
+                if (more) a += heads[w * 256 + g * 64 + lane];
+                have += more;
+            }
+            finish(it, a, g);
         }
     }
 }
@@ -455,85 +921,149 @@ struct Out {
     const void* const *w_out, *const *s_w_out;
     const unsigned char *h, *s_h;
     void* y;
-    int T, d, E, k, F, shared_F, y_f32;
+    int T, d, E, k, F, shared_F, y_f32, splits;
 };
 
-// WL: 1 for 8 columns of a work-group, 2 for 16
-template <bool F32, int WL>
+// WL: 1 for 8 columns of a work-group, 2 for 16.  LDS: the hidden activations go there first.  splits > 1 (one choice per token, no shared
+// expert): the work-groups of a column block share the experts, and each writes its experts' tokens.
+template <bool F32, int WL, bool LDS>
 __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : HF, COLS = WL * 8;
-    __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(u32x4) * TURN_PIECES * NW];
+    __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(u32x4) * 256 * NW];
+    __shared__ __attribute__((aligned(16))) unsigned char hl[LDS ? H_BYTES : 16];
     __shared__ __attribute__((aligned(16))) float sums[NW][MAXT][COLS];
     __shared__ Lists l;
-    __shared__ int lost[MAXT];           // tokens with an assignment to no expert
+    __shared__ int state[MAXT];          // of a token: 0 not this work-group's, 1 to be written, 2 with an assignment to no expert
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6), l16 = lane & 15, lq = lane >> 4;
-    const int T = p.T, d = p.d, E = p.E, k = p.k, F = p.F;
-    if (tid < T) lost[tid] = 0;
+    const int T = p.T, d = p.d, E = p.E, k = p.k, F = p.F, splits = p.splits;
+    const int split = (int)blockIdx.x % splits, p0 = (int)blockIdx.x / splits * COLS;
+    const unsigned f_bytes = (unsigned)F * ES, s_bytes = (unsigned)p.shared_F * ES, s_base = (unsigned)(T * k) * f_bytes;
+    int e = -1;
+    float gate = 0.f;
     if (tid < T * k) {
-        l.id[tid] = p.idx[tid];
-        l.gate[tid] = p.gate[tid];
+        e = p.idx[tid];
+        gate = p.gate[tid];
     }
+    const void* const mine_w = tid < E ? p.w_out[tid] : nullptr;
+    if constexpr (LDS) {
+        rows_to_lds(p.h, T * k, f_bytes, hl);
+        if (p.shared_F) rows_to_lds(p.s_h, T, s_bytes, hl + s_base);
+    }
+    if (tid < 2 * MAXE) (&l.bits[0][0])[tid] = 0u;
+    if (tid < T) state[tid] = splits == 1;
     for (int i = lane; i < T * COLS; i += 64) (&sums[wave][0][0])[i] = 0.f;
     __syncthreads();
-    if (tid < T * k && (unsigned)l.id[tid] >= (unsigned)E) lost[tid / k] = 1;
-    make_lists(l, T, E, k);
-    u32x4* const turn = (u32x4*)smem + wave * TURN_PIECES;
-    const int n_active = sgpr(l.n_active), rows = sgpr(l.first[MAXE]);
-    const __amdgpu_buffer_rsrc_t h = make_rsrc(p.h, (unsigned)(rows * F) * ES), s_h = make_rsrc(p.s_h, (unsigned)(T * p.shared_F) * ES);
-    const int p0 = (int)blockIdx.x * COLS;
-    // (expert, line) pairs, the shared expert's behind the others'
-    const int L = F * ES / 128, s_L = p.shared_F * ES / 128, units = n_active * L + s_L;
-    const int u1 = (int)((long long)units * (wave + 1) / NW);
-    for (int u = (int)((long long)units * wave / NW); u < u1;) {
-        const int ai = u / L;
-        const bool shared = ai >= n_active;
-        const int base = shared ? n_active * L : ai * L, l0 = u - base, have = shared ? s_L : L;
-        const int l1 = u1 - base < have ? u1 - base : have;
-        u = base + l1;
-        const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? 0 : sgpr(l.first[e]), m = shared ? T : sgpr(l.first[e + 1]) - r0;
-        const size_t row_bytes = (size_t)(shared ? p.shared_F : F) * ES;
-        const unsigned char* w = (const unsigned char*)sgpr_ptr(shared ? p.s_w_out[0] : p.w_out[e]) + p0 * row_bytes;
-        const unsigned piece = (unsigned)(lane & 7) * 16u, w_off = (unsigned)(lane >> 3) * (unsigned)row_bytes + piece;
-        unsigned x_at[4][2];
+    if (tid < E) l.w[tid] = mine_w;
+    if (tid < T * k && (unsigned)e >= (unsigned)E && split == 0) state[tid / k] = 2;
+    if constexpr (LDS) MOE_WAIT_VMCNT(0);
+    make_lists(l, E, e, tid / k, gate);
+    u32x4* const turn = (u32x4*)smem + wave * 256;
+    const int n_active = sgpr(l.n_active), rows = sgpr(l.first[(E + 63) & ~63]);
+    const __amdgpu_buffer_rsrc_t h = make_rsrc(p.h, (unsigned)rows * f_bytes), s_h = make_rsrc(p.s_h, (unsigned)T * s_bytes);
+    // The lines of the active experts' contractions, the shared expert's behind, by what they cost: a wavefront's share of that.
+    const int L = F * ES / 128, s_L = p.shared_F * ES / 128, s_cost = line_cost(T);
+    int ai0 = 0, ai1 = n_active;         // the work-group's experts
+    if (splits > 1) {
+        const int all = l.cost[n_active];
+        int below = 0, upto = 0;
+        for (int x = lane; x - lane < n_active; x += 64) {
+            const int owner = x < n_active ? l.cost[x] * splits / all : splits;
+            below += __popcll(__ballot(owner < split));
+            upto += __popcll(__ballot(owner <= split));
+        }
+        ai0 = below;
+        ai1 = upto;
+    }
+    const int base = sgpr(L * l.cost[ai0]), all = sgpr(L * l.cost[ai1]) - base + s_L * s_cost;
+    const int lo = (int)((unsigned long long)all * (unsigned)wave / NW), hi = (int)((unsigned long long)all * (unsigned)(wave + 1) / NW);
+    int ai = ai0;
+    for (int x = ai0 + lane; x - lane < ai1; x += 64) ai += __popcll(__ballot(x < ai1 && L * l.cost[x + 1] - base <= lo));
+    ai = sgpr(ai);
+    auto segment = [&](Segment& s, int ai) __attribute__((always_inline)) {
+        const bool shared = ai == ai1;
+        if (ai > ai1 || (shared && !s_L)) return false;
+        const int at = sgpr(L * l.cost[ai]) - base;
+        if (at >= hi) return false;
+        const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? 0 : sgpr(l.first[e]), have = shared ? s_L : L;
+        s.m = shared ? T : sgpr(l.first[e + 1]) - r0;
+        const int c = line_cost(s.m);
+        s.l0 = 0;
+        s.l1 = have;
+        if (lo > at) s.l0 = (lo - at + c - 1) / c;
+        if (hi < at + have * c) s.l1 = (hi - at + c - 1) / c;
+        const unsigned row_bytes = shared ? s_bytes : f_bytes, at8 = (unsigned)(lane >> 3) * row_bytes + (unsigned)(lane & 7) * 16u;
+        s.w = make_rsrc((const unsigned char*)sgpr_ptr(shared ? p.s_w_out[0] : l.w[e]) + (size_t)p0 * row_bytes, COLS * row_bytes);
+        s.w_at[0] = at8;
+        s.w_at[1] = at8 + 8u * row_bytes;
+        s.x = shared ? s_h : h;
+        s.x_step = 64 * s.m;
+        if constexpr (LDS) {
+            const unsigned from = shared ? s_base : (unsigned)r0 * row_bytes;
+            // (places in rows counted from the first: r0 need not be a multiple of 8)
+            const int first = shared ? 0 : r0;
+            const unsigned start = from - (unsigned)first * row_bytes;
+            if (kind_of<TY, IN_LDS>(s.m) < 0) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g)
+                for (int r = 0; r < 8; ++r) s.x_at[r] = start + piece_at(first + (r < s.m ? r : s.m - 1), row_bytes);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = g * 16 + i * 8 + (lane >> 3);
-                x_at[g][i] = r < m ? (unsigned)(r0 + r) * (unsigned)row_bytes + piece : NOWHERE;
+                for (int g = 0; g < 4; ++g) s.x_at[g] = start + fragment_at(first + (g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
             }
-        f32x4 acc[4];
-        const int groups = lines_product_rows<TY, WL>(m, w, w + 8 * row_bytes, w_off, shared ? s_h : h, x_at, l0, l1, acc, turn);
-        for (int g = 0; g < groups; ++g) {
-            const f32x4 a = g == 0 ? acc[0] : g == 1 ? acc[1] : g == 2 ? acc[2] : acc[3];
-            const int r = g * 16 + l16;
-            if (r < m && (WL == 2 || lq < 2)) {
-                const int as = shared ? 0 : l.a[r0 + r], t = shared ? r : as / k;
-                const float gate = shared ? 1.f : l.gate[as];
-                f32x4* to = (f32x4*)&sums[wave][t][4 * lq];      // (an expert's rows are different tokens)
-                f32x4 s = *to;
+        } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = fmaf(gate, a[i], s[i]);
-                *to = s;
+            for (int g = 0; g < 4; ++g) {
+                const int r = g * 16 + l16;
+                s.x_at[g] = r < s.m ? (unsigned)r0 * row_bytes + (unsigned)(lq * s.m + r) * 16u : NOWHERE;
             }
         }
-    }
+        return true;
+    };
+    stream_all<TY, WL, LDS ? IN_LDS : FRAGMENTS, LDS ? IN_LDS : FRAGMENTS>(
+        turn, hl, hi - lo <= 16,
+        [&](Segment& s) __attribute__((always_inline)) {
+            while (segment(s, ai)) {
+                if (s.l0 < s.l1) return true;
+                ++ai;
+            }
+            return false;
+        },
+        [&](Segment& s) __attribute__((always_inline)) { return segment(s, ai + 1) && s.l0 < s.l1; },
+        [&](const Segment& s, auto& acc) __attribute__((always_inline)) {
+            constexpr int G = sizeof(acc) / sizeof(acc[0]);
+            const bool shared = ai == ai1;
+            const int r0 = shared ? 0 : sgpr(l.first[sgpr(l.active[ai])]);
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int r = g * 16 + l16;
+                if (r < s.m && (WL == 2 || lq < 2)) {
+                    const int t = shared ? r : l.t[r0 + r];
+                    const float gate = shared ? 1.f : l.gate[r0 + r];
+                    f32x4* to = (f32x4*)&sums[wave][t][4 * lq];          // (an expert's rows are different tokens)
+                    f32x4 sum = *to;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[i] = fmaf(gate, acc[g][i], sum[i]);
+                    *to = sum;
+                    if (splits > 1) state[t] = 1;
+                }
+            }
+            ++ai;
+        });
     __syncthreads();
-    if (tid < T * COLS) {
-        const int t = tid / COLS, c = tid - t * COLS, row = p0 + c;
+    for (int i = tid; i < T * COLS; i += NTH) {
+        const int t = i / COLS, c = i - t * COLS, row = p0 + c, st = state[t];
         float v = 0.f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) v += sums[w][t][c];
-        if (lost[t]) v = __builtin_nanf("");                      // (its gates are NaN)
+        if (st == 2) v = __builtin_nanf("");                      // (its gates are NaN)
         const int col = F32 ? row : (row & ~31) + 2 * (row & 15) + ((row >> 4) & 1);
-        if (p.y_f32) ((float*)p.y)[(size_t)t * d + col] = v;
-        else ((uint16_t*)p.y)[(size_t)t * d + col] = f32_to_bf16(v);
+        if (st) {
+            if (p.y_f32) ((float*)p.y)[(size_t)t * d + col] = v;
+            else ((uint16_t*)p.y)[(size_t)t * d + col] = f32_to_bf16(v);
+        }
     }
 }
-static_assert(MAXT * 16 <= NTH, "a thread per output of a work-group");
-
-template <bool F32, int TT> void launch_hidden(const Hidden& a, hipStream_t st) {
-    hipLaunchKernelGGL((few_hidden_kernel<F32, TT>), dim3(MOE_GEMM_GRID), dim3(NTH), 0, st, a);
+template <bool F32, typename H> void launch_hidden(const Hidden& a, hipStream_t st) {
+    hipLaunchKernelGGL((few_hidden_kernel<F32, H>), dim3(MOE_GEMM_GRID), dim3(NTH), 0, st, a);
 }
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -558,7 +1088,7 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     MOE_REQUIRE(d % 64 == 0 && F % 64 == 0 && shared_F % 64 == 0, MOE_ERR_UNSUPPORTED, "moe_layer_few: d=%d F=%d shared_F=%d are not all multiples of 64",
                 d, F, shared_F);
     const size_t es = moe_elem_size(dt), two_gib = (size_t)1 << 31;
-    MOE_REQUIRE((size_t)8 * d * es < two_gib && (size_t)8 * F * es < two_gib && (size_t)8 * shared_F * es < two_gib && (size_t)T * d * es < two_gib && (size_t)T * k * F * es < two_gib && (size_t)T * shared_F * es < two_gib, MOE_ERR_UNSUPPORTED,
+    MOE_REQUIRE((size_t)8 * d * es < two_gib && (size_t)8 * F * es < two_gib && (size_t)8 * shared_F * es < two_gib && (size_t)T * d * es < two_gib && (size_t)E * d * es < two_gib && (size_t)T * k * F * es < two_gib && (size_t)T * shared_F * es < two_gib, MOE_ERR_UNSUPPORTED,
                 "moe_layer_few: rows of %d, %d and %d values are too long", d, F, shared_F);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(x && w_gate && w_in && w_out && expert_idx && gate_w && y && (dt == MOE_F32 || w_norm2) && (!shared_F || (s_w_in && s_w_out)),
@@ -574,26 +1104,35 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     a.x = x; a.w_in = w_in; a.s_w_in = s_w_in; a.F = F; a.shared_F = shared_F; a.glu = act == MOE_SWIGLU;
     a.h = (unsigned char*)ws;
     a.s_h = a.h + (size_t)T * k * F * es;
+    // x and the hidden activations go to LDS first where they fit (T <= 32: beyond, the routing's sums take it)
+    const bool x_lds = (size_t)T * d * es <= X_BYTES && T <= 32, h_lds = need <= H_BYTES;
+    a.h_rows = h_lds;
     if (dt == MOE_F32) {
         const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
         if (rc != MOE_OK) return rc;
-        launch_hidden<true, 0>(a, st);
+        x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
     } else if (T <= 16) {
-        launch_hidden<false, 1>(a, st);
+        x_lds ? launch_hidden<false, How<1, true>>(a, st) : launch_hidden<false, How<1, false>>(a, st);
     } else if (T <= 32) {
-        launch_hidden<false, 2>(a, st);
+        x_lds ? launch_hidden<false, How<2, true>>(a, st) : launch_hidden<false, How<2, false>>(a, st);
     } else if (T <= 48) {
-        launch_hidden<false, 3>(a, st);
+        launch_hidden<false, How<3, false>>(a, st);
     } else {
-        launch_hidden<false, 4>(a, st);
+        launch_hidden<false, How<4, false>>(a, st);
     }
     MOE_CHECK_LAUNCH("moe_layer_few (routing and first product)");
-    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32};
-    // Sixteen columns where they make a work-group per CU, else eight (a matrix instruction half empty, twice the work-groups)
-    const bool wide = d / 16 >= MOE_GEMM_GRID;
-    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(d / (wide ? 16 : 8))), dim3(NTH), 0, st, o); };
-    if (dt == MOE_F32) wide ? go(few_out_kernel<true, 2>) : go(few_out_kernel<true, 1>);
-    else wide ? go(few_out_kernel<false, 2>) : go(few_out_kernel<false, 1>);
+    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1};
+    // With one choice per token and no shared expert up to T work-groups share a column block's experts.  Sixteen columns where they
+    // make a work-group per CU, else eight (a matrix instruction half empty, twice the work-groups).
+    const int most = k == 1 && !shared_F ? T : 1;
+    const bool wide = (long long)(d / 16) * most >= MOE_GEMM_GRID;
+    const int blocks = d / (wide ? 16 : 8);
+    while (o.splits < most && blocks * (o.splits + 1) <= MOE_GEMM_GRID) ++o.splits;
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * o.splits)), dim3(NTH), 0, st, o); };
+    if (dt == MOE_F32 && h_lds) wide ? go(few_out_kernel<true, 2, true>) : go(few_out_kernel<true, 1, true>);
+    else if (dt == MOE_F32) wide ? go(few_out_kernel<true, 2, false>) : go(few_out_kernel<true, 1, false>);
+    else if (h_lds) wide ? go(few_out_kernel<false, 2, true>) : go(few_out_kernel<false, 1, true>);
+    else wide ? go(few_out_kernel<false, 2, false>) : go(few_out_kernel<false, 1, false>);
     MOE_CHECK_LAUNCH("moe_layer_few (second product and combine)");
     return MOE_OK;
 }
