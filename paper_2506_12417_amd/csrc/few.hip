@@ -120,9 +120,10 @@ enum { IN_LDS = 0, FRAGMENTS = 1, LINES = 2 };
 struct Segment {
     __amdgpu_buffer_rsrc_t w, x;
     unsigned w_at[2];                    // byte offsets of the lane's two weight rows (eight rows a load)
-    // and of its activations: its 16 bytes of group g in the first 64 bytes of a row, or (LINES) its 16 bytes of the first 128 of rows
-    // 16 g + 8 i ... at [2 g + i]; beyond the buffer for rows that are not there (in LDS: of any row).  IN_LDS, rows taken one by one: see dots()
-    unsigned x_at[8];
+    // and of its activations: its 16 bytes of group g in the first 64 bytes of a row; beyond the buffer for rows that are not there (in
+    // LDS: of any row)
+    unsigned x_at[4];
+    unsigned row_at[8];                  // LINES: its 16 bytes of the first 128 of row 8 i + lane / 8; IN_LDS, fp32: of row i, for dots()
     int x_step;                          // from one 64 bytes to the next (FRAGMENTS)
     int l0, l1, m;
 };
@@ -188,7 +189,7 @@ __device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned 
             for (int g = 0; g < G; ++g)
 #pragma unroll
                 for (int v = 0; v < 2; ++v)
-                    b[u][g][v] = __builtin_amdgcn_raw_buffer_load_b128(from.x, (int)(in ? from.x_at[X == LINES ? 2 * g + v : g] : NOWHERE),
+                    b[u][g][v] = __builtin_amdgcn_raw_buffer_load_b128(from.x, (int)(in ? (X == LINES ? from.row_at[2 * g + v] : from.x_at[g]) : NOWHERE),
                                                                        X == LINES ? at * 128 : (2 * at + v) * from.x_step, 0);
         }
     };
@@ -214,7 +215,7 @@ __device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned 
     float dot[WL][M ? M : 1];
     auto multiply = [&](const Segment& s, int u, int l) __attribute__((always_inline)) {
         if constexpr (M > 0) {
-            dots<WL, M>(a[u], xl, s.x_at, l, dot);
+            dots<WL, M>(a[u], xl, s.row_at, l, dot);
         } else {
 #pragma unroll
             for (int g = 0; g < G; ++g) {
@@ -761,35 +762,23 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
         if (count < 64) break;
     }
     base = sgpr(base) * lines;
-    // Where item n is: expert number ai of the active ones (-1: the shared one), item q of its.
-    struct Place { int n, ai, q; };
-    auto place_of = [&](int n) __attribute__((always_inline)) {
-        const int item = n * grid + block, rest = item - s_items;
-        Place c = {n, -1, item};
-        if (rest >= 0) {
-            c.ai = rest / per;
-            c.q = rest - c.ai * per;
+    // Where the item is: number `ai` of the active experts (-1: the shared one), item q of its.
+    auto step = [&](int& ai, int& q) __attribute__((always_inline)) {    // the work-group's next
+        q += grid;
+        while (q >= (ai < 0 ? s_items : per) && ai < n_active) {
+            q -= ai < 0 ? s_items : per;
+            ++ai;
         }
-        return c;
-    };
-    auto behind = [&](Place c) __attribute__((always_inline)) {
-        ++c.n;
-        c.q += grid;
-        while (c.q >= (c.ai < 0 ? s_items : per) && c.ai < n_active) {
-            c.q -= c.ai < 0 ? s_items : per;
-            ++c.ai;
-        }
-        return c;
     };
     struct Item {
         int r0, m, width, out0;
         bool glu;
         unsigned char* h;
     };
-    auto item_of = [&](const Place& c) __attribute__((always_inline)) {
+    auto item_of = [&](int ai, int q) __attribute__((always_inline)) {
         Item it;
-        const bool shared = c.ai < 0;
-        const int e = shared ? 0 : sgpr(l.active[c.ai]), q = c.q;
+        const bool shared = ai < 0;
+        const int e = shared ? 0 : sgpr(l.active[ai]);
         it.glu = shared || p.glu;
         it.r0 = shared ? 0 : sgpr(l.first[e]);
         it.m = shared ? T : sgpr(l.first[e + 1]) - it.r0;
@@ -821,10 +810,10 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
         }
     };
     // the segment of an item that lies in the share; false behind its end
-    auto segment = [&](Segment& s, const Place& c, int base) __attribute__((always_inline)) {
-        if (c.n >= mine || base >= hi) return false;
-        const bool shared = c.ai < 0, glu = shared || p.glu;
-        const int e = shared ? 0 : sgpr(l.active[c.ai]), r0 = shared ? 0 : sgpr(l.first[e]), q = c.q;
+    auto segment = [&](Segment& s, int ai, int q, int base) __attribute__((always_inline)) {
+        if (base >= hi) return false;    // (the items' costs end where the last share does)
+        const bool shared = ai < 0, glu = shared || p.glu;
+        const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? 0 : sgpr(l.first[e]);
         s.m = shared ? T : sgpr(l.first[e + 1]) - r0;
         const int cost = line_cost(s.m);
         s.l0 = 0;
@@ -843,44 +832,49 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
         s.x_step = 64;
         auto token = [&](int r) __attribute__((always_inline)) { return shared ? r : (int)l.t[r0 + r]; };
         if constexpr (H::LDS) {
-            if (kind_of<TY, IN_LDS>(s.m) < 0) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) s.x_at[r] = piece_at(token(r < s.m ? r : s.m - 1), row_bytes);
-            } else {
+            for (int g = 0; g < 4; ++g) s.x_at[g] = fragment_at(token(g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
+            if constexpr (F32) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) s.x_at[g] = fragment_at(token(g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
+                for (int r = 0; r < 8; ++r) s.row_at[r] = piece_at(token(r < s.m ? r : s.m - 1), row_bytes);
             }
-        } else if (s.m <= 16) {
-            s.x_at[0] = NOWHERE;
-            if (l16 < s.m) s.x_at[0] = (unsigned)token(l16) * row_bytes + (unsigned)lq * 16u;
-        } else {
+        } else {                         // (up to 16 rows as fragments, more in lines)
+            s.x_at[1] = s.x_at[2] = s.x_at[3] = NOWHERE;         // (members without a value end up in scratch memory when copied)
+            s.x_at[0] = l16 < s.m ? (unsigned)token(l16 < s.m ? l16 : 0) * row_bytes + (unsigned)lq * 16u : NOWHERE;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const int r = i * 8 + (lane >> 3);
-                s.x_at[i] = NOWHERE;
-                if (r < s.m) s.x_at[i] = (unsigned)token(r) * row_bytes + (unsigned)(lane & 7) * 16u;
+                s.row_at[i] = r < s.m ? (unsigned)token(r < s.m ? r : 0) * row_bytes + (unsigned)(lane & 7) * 16u : NOWHERE;
             }
         }
         return true;
     };
-    Place here = place_of(n), tail = {};
-    int tail_lines = 0;                  // > 0: of an item whose rest is with the wavefronts behind
+    int ai = -1, q = n * grid + block;
+    if (q >= s_items) {
+        ai = (q - s_items) / per;
+        q = q - s_items - ai * per;
+    }
+    int tail_ai = 0, tail_q = 0, tail_lines = 0;         // tail_lines > 0: of an item whose rest is with the wavefronts behind
     if (lane == 0) head_lines[wave] = 0;
     stream_all<TY, 2, H::LDS ? IN_LDS : FRAGMENTS, H::LDS ? IN_LDS : LINES>(
         turn, xl, hi - lo <= 16,
         [&](Segment& s) __attribute__((always_inline)) {
-            while (segment(s, here, base)) {
+            while (segment(s, ai, q, base)) {
                 if (s.l0 < s.l1) return true;
                 base += line_cost(s.m) * lines;
-                here = behind(here);
+                step(ai, q);
             }
             return false;
         },
-        [&](Segment& s) __attribute__((always_inline)) { return segment(s, behind(here), base + line_cost(s.m) * lines) && s.l0 < s.l1; },
+        [&](Segment& s) __attribute__((always_inline)) {
+            int next_ai = ai, next_q = q;
+            step(next_ai, next_q);
+            return segment(s, next_ai, next_q, base + line_cost(s.m) * lines) && s.l0 < s.l1;
+        },
         [&](const Segment& s, auto& acc) __attribute__((always_inline)) {
             constexpr int G = sizeof(acc) / sizeof(acc[0]);
             if (s.l0 == 0 && s.l1 == lines) {
-                const Item it = item_of(here);
+                const Item it = item_of(ai, q);
 #pragma unroll
                 for (int g = 0; g < G; ++g) finish(it, acc[g], g);
             } else {
@@ -891,16 +885,17 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
                 if (s.l0) {
                     if (lane == 0) head_lines[wave] = s.l1 - s.l0;
                 } else {
-                    tail = here;
+                    tail_ai = ai;
+                    tail_q = q;
                     tail_lines = s.l1;
                 }
             }
             base += line_cost(s.m) * lines;
-            here = behind(here);
+            step(ai, q);
         });
     __syncthreads();
     if (tail_lines) {
-        const Item it = item_of(tail);
+        const Item it = item_of(tail_ai, tail_q);
         for (int g = 0; g < (it.m + 15) >> 4; ++g) {
             f32x4 a = ((const f32x4*)turn)[g * 64 + lane];
             int have = tail_lines;
@@ -1002,12 +997,11 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
             // (places in rows counted from the first: r0 need not be a multiple of 8)
             const int first = shared ? 0 : r0;
             const unsigned start = from - (unsigned)first * row_bytes;
-            if (kind_of<TY, IN_LDS>(s.m) < 0) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) s.x_at[r] = start + piece_at(first + (r < s.m ? r : s.m - 1), row_bytes);
-            } else {
+            for (int g = 0; g < 4; ++g) s.x_at[g] = start + fragment_at(first + (g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
+            if constexpr (F32) {
 #pragma unroll
-                for (int g = 0; g < 4; ++g) s.x_at[g] = start + fragment_at(first + (g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
+                for (int r = 0; r < 8; ++r) s.row_at[r] = start + piece_at(first + (r < s.m ? r : s.m - 1), row_bytes);
             }
         } else {
 #pragma unroll
