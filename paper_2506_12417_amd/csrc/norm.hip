@@ -242,7 +242,8 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         float y[V];
         float m = 0.f, r = 0.f;
         Held<float, VEC> own_gate;
-        if (SRC != SRC_NONE && p.gate_rows > 1) own_gate.fetch(p.gate + at, d);
+        const bool own = SRC != SRC_NONE && p.gate_rows > 1;
+        if (own) own_gate.fetch(p.gate + at, d);
         if constexpr (SRC == SRC_ROWS) combine_row<G, VEC>(p, t, y);
         if (KEEP && t + step < p.T) fetch(t + step);
         if constexpr (SRC == SRC_NONE) {
@@ -261,11 +262,12 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
             }
             if (p.stats && threadIdx.x == 0) { p.stats[(size_t)t * 4] = m; p.stats[(size_t)t * 4 + 1] = r; }
             if (!KEEP) gate_params();
+            if (own) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float g = p.gate_rows > 1 ? own_gate.at(i) : gate[i];
-                y[i] = column<VEC>(i) < d ? fmaf(p.alpha, h.at(i), g * y[i]) : 0.f;
+                for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
             }
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = fmaf(p.alpha, h.at(i), gate[i] * y[i]);       // (past d: v, h and post_b are zero)
             store<VEC>((HT*)p.y + at, d, y);
         }
         if (p.next_kind != MOE_NORM_NONE) {
@@ -373,68 +375,108 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         if (HAS_V && p.gate_rows > 1) own_gate.fetch(p.gate + at, d);
         if (KEEP && t + step < p.T) fetch(t + step);
         float vn[V], y[V], gy[V];
+        const bool next_layer = p.next_kind == MOE_NORM_LAYER, post_layer = p.post_kind == MOE_NORM_LAYER;
+        // (Past d everything is zero, but for what LAYER subtracts the mean from.)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            y[i] = h.at(i);
-            if constexpr (HAS_V) {
-                vn[i] = v.at(i);
-                if (p.post_kind != MOE_NORM_NONE) vn[i] = (vn[i] - st[0]) * st[1];
-                const float g = p.gate_rows > 1 ? own_gate.at(i) : gate[i];
-                y[i] = fmaf(p.alpha, y[i], g * fmaf(vn[i], pw[i], pb[i]));     // (without a norm pw is 1 and pb 0)
+        for (int i = 0; i < V; ++i) y[i] = h.at(i);
+        if constexpr (HAS_V) {
+            if (p.gate_rows > 1) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
             }
-            gy[i] = q.dy ? dy.at(i) : 0.f;
+#pragma unroll
+            for (int i = 0; i < V; ++i) vn[i] = v.at(i);
+            if (post_layer) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) vn[i] = column<VEC>(i) < d ? vn[i] - st[0] : 0.f;
+            }
+            if (p.post_kind != MOE_NORM_NONE) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) vn[i] *= st[1];
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) y[i] = fmaf(p.alpha, y[i], gate[i] * fmaf(vn[i], pw[i], pb[i]));     // (without a norm pw is 1 and pb 0)
+        }
+#pragma unroll
+        for (int i = 0; i < V; ++i) gy[i] = 0.f;
+        if (q.dy) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) gy[i] = dy.at(i);
         }
         if (q.du) {
-            float a = 0.f, b = 0.f;
+            float a = 0.f, b = 0.f, gn[V];
             if (!KEEP) next_params();
+            if (next_layer) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) y[i] = column<VEC>(i) < d ? y[i] - st[S - 2] : 0.f;
+            }
 #pragma unroll
             for (int i = 0; i < V; ++i) {
-                const bool in = column<VEC>(i) < d;
-                y[i] = in ? (y[i] - st[S - 2]) * st[S - 1] : 0.f;
-                const float gn = du.at(i) * nw[i];
-                a = fmaf(gn, y[i], a);
-                b += in ? gn : 0.f;
+                y[i] *= st[S - 1];
+                gn[i] = du.at(i) * nw[i];
+                a = fmaf(gn[i], y[i], a);
             }
-            acc.template add<D_NEXT_W>([&](int i, float s) __attribute__((always_inline)) { return fmaf(du.at(i), y[i], s); });
-            acc.template add<D_NEXT_B>([&](int i, float s) __attribute__((always_inline)) { return s + du.at(i); });
-            const bool layer = p.next_kind == MOE_NORM_LAYER;
-            sum(a, b, layer);
+            if (next_layer) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) b += gn[i];
+            }
+            if (q.slot[D_NEXT_W] >= 0) acc.template add<D_NEXT_W>([&](int i, float s) __attribute__((always_inline)) { return fmaf(du.at(i), y[i], s); });
+            if (q.slot[D_NEXT_B] >= 0) acc.template add<D_NEXT_B>([&](int i, float s) __attribute__((always_inline)) { return s + du.at(i); });
+            sum(a, b, next_layer);
             a *= p.inv_d;
-            b = layer ? b * p.inv_d : 0.f;
+            if (next_layer) {
+                b *= p.inv_d;
 #pragma unroll
-            for (int i = 0; i < V; ++i) gy[i] = fmaf(st[S - 1], fmaf(-y[i], a, du.at(i) * nw[i] - b), gy[i]);
+                for (int i = 0; i < V; ++i) gn[i] -= b;
+            }
+#pragma unroll
+            for (int i = 0; i < V; ++i) gy[i] = fmaf(st[S - 1], fmaf(-y[i], a, gn[i]), gy[i]);
         }
-        float out[V];
+        if (q.dh) {
+            float out[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) out[i] = HAS_V ? p.alpha * gy[i] : gy[i];
-        if (q.dh) store<VEC>((HT*)q.dh + at, d, out);
+            for (int i = 0; i < V; ++i) out[i] = HAS_V ? p.alpha * gy[i] : gy[i];
+            store<VEC>((HT*)q.dh + at, d, out);
+        }
         if constexpr (HAS_V) {
             float a = 0.f, b = 0.f;
             if (!KEEP) { post_params(); gate_params(); }
-            if (!KEEP && p.gate_rows > 1) own_gate.fetch(p.gate + at, d);
+            if (!KEEP && p.gate_rows > 1) {
+                own_gate.fetch(p.gate + at, d);
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                out[i] = gy[i] * fmaf(vn[i], pw[i], pb[i]);
-                gy[i] *= p.gate_rows > 1 ? own_gate.at(i) : gate[i];         // dp
+                for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
             }
-            acc.template add<D_GATE>([&](int i, float s) __attribute__((always_inline)) { return s + out[i]; });
-            acc.template add<D_POST_W>([&](int i, float s) __attribute__((always_inline)) { return fmaf(gy[i], vn[i], s); });
-            acc.template add<D_POST_B>([&](int i, float s) __attribute__((always_inline)) { return s + gy[i]; });
+            if (q.slot[D_GATE] >= 0)
+                acc.template add<D_GATE>([&](int i, float s) __attribute__((always_inline)) { return fmaf(gy[i], fmaf(vn[i], pw[i], pb[i]), s); });
+            if (q.dgate) {
+                float out[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const bool in = column<VEC>(i) < d;
-                gy[i] *= pw[i];
-                a = in ? fmaf(gy[i], vn[i], a) : a;
-                b += in ? gy[i] : 0.f;
+                for (int i = 0; i < V; ++i) out[i] = gy[i] * fmaf(vn[i], pw[i], pb[i]);
+                store<VEC>(q.dgate + at, d, out);
             }
-            if (q.dgate) store<VEC>(q.dgate + at, d, out);
+#pragma unroll
+            for (int i = 0; i < V; ++i) gy[i] *= gate[i];        // dp
+            if (q.slot[D_POST_W] >= 0) acc.template add<D_POST_W>([&](int i, float s) __attribute__((always_inline)) { return fmaf(gy[i], vn[i], s); });
+            if (q.slot[D_POST_B] >= 0) acc.template add<D_POST_B>([&](int i, float s) __attribute__((always_inline)) { return s + gy[i]; });
             if (p.post_kind != MOE_NORM_NONE) {
-                const bool layer = p.post_kind == MOE_NORM_LAYER;
-                sum(a, b, layer);
-                a *= p.inv_d;
-                b = layer ? b * p.inv_d : 0.f;
 #pragma unroll
-                for (int i = 0; i < V; ++i) gy[i] = st[1] * fmaf(-vn[i], a, gy[i] - b);
+                for (int i = 0; i < V; ++i) {
+                    gy[i] *= pw[i];
+                    a = fmaf(gy[i], vn[i], a);
+                }
+                if (post_layer) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) b += column<VEC>(i) < d ? gy[i] : 0.f;
+                }
+                sum(a, b, post_layer);
+                a *= p.inv_d;
+                if (post_layer) {
+                    b *= p.inv_d;
+#pragma unroll
+                    for (int i = 0; i < V; ++i) gy[i] -= b;
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) gy[i] = st[1] * fmaf(-vn[i], a, gy[i]);
             }
             if (q.dv) store<VEC>((VT*)q.dv + at, d, gy);
         }
@@ -494,7 +536,7 @@ Shape shape(int T, int d, int waves, int parts) {
     if (blocks > most) blocks = most;
     return {dim3((unsigned)(blocks < 1 ? 1 : blocks)), dim3((unsigned)g, (unsigned)rows)};
 }
-Shape forward_shape(int T, int d) { return shape(T, d, 16, 1 << 30); }
+Shape forward_shape(int T, int d) { return shape(T, d, 32, 1 << 30); }
 // (a row in work is a row of partial sums)
 Shape backward_shape(int T, int d, bool has_v) { return shape(T, d, has_v ? 8 : 16, 1024); }
 
