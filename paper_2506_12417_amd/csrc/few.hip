@@ -63,14 +63,18 @@ struct Lists {
     const void* w[MAXE];                 // the experts' matrices
     int id[MAXA];                        // the choice, by assignment
     float gate[MAXA];                    // by row
-    unsigned char t[MAXA];               // a row's token
+    unsigned short pair[MAXA];           // a row's assignment: token * k + choice
+    unsigned char t[MAXA];               // and its token
 };
 
 __device__ __forceinline__ int line_cost(int m);
 
-// Every thread's assignment (expert e of token t with weight gate; e outside [0,E): none) -> lists.  The bits are clear.  A barrier before
-// and behind.
-__device__ __forceinline__ void make_lists(Lists& l, int E, int e, int t, float gate) {
+__device__ __forceinline__ int rows_in(const Lists& l, int x, unsigned long long range) {
+    return __popc(l.bits[x][0] & (unsigned)range) + __popc(l.bits[x][1] & (unsigned)(range >> 32));
+}
+// Every thread's assignment (expert e of token t with weight gate; e outside [0,E): none) -> lists; active and cost of the experts and rows of
+// the tokens in `range` only.  The bits are clear.  A barrier before and behind.
+__device__ __forceinline__ void make_lists(Lists& l, int E, int e, int t, float gate, unsigned long long range) {
     const int tid = threadIdx.x;
     const bool is = (unsigned)e < (unsigned)E;
     if (is) atomicOr(&l.bits[e][t >> 5], 1u << (t & 31));
@@ -78,12 +82,12 @@ __device__ __forceinline__ void make_lists(Lists& l, int E, int e, int t, float 
     if (tid < 64) {
         unsigned rows = 0, act = 0, cost = 0;    // of the experts before
         for (int x = tid; x - tid < E; x += 64) {
-            const unsigned n = __popc(l.bits[x][0]) + __popc(l.bits[x][1]), c = n ? (unsigned)line_cost((int)n) : 0u;
+            const unsigned n = (unsigned)rows_in(l, x, ~0ull), in = (unsigned)rows_in(l, x, range), c = in ? (unsigned)line_cost((int)in) : 0u;
             // (both sums in one scan: at most 512 rows, and 256 experts' costs of at most 10)
             const unsigned up = moe_wave_scan_u32(n | c << 16);
-            const unsigned long long on = __ballot(n != 0);
+            const unsigned long long on = __ballot(in != 0);
             l.first[x] = (int)(rows + (up & 0xffffu) - n);
-            if (n) {
+            if (in) {
                 const int at = (int)act + __popcll(on & ((1ull << tid) - 1ull));
                 l.active[at] = x;
                 l.cost[at] = (int)(cost + (up >> 16) - c);
@@ -103,6 +107,7 @@ __device__ __forceinline__ void make_lists(Lists& l, int E, int e, int t, float 
     if (is) {
         const unsigned lo = l.bits[e][0], hi = l.bits[e][1], below = (1u << (t & 31)) - 1u;
         const int r = l.first[e] + (t < 32 ? __popc(lo & below) : __popc(lo) + __popc(hi & below));
+        l.pair[r] = (unsigned short)tid;
         l.t[r] = (unsigned char)t;
         l.gate[r] = gate;
     }
@@ -113,7 +118,7 @@ constexpr unsigned NOWHERE = 0x80000000u;        // beyond every buffer here (th
 
 // Where a product's activations come from: LDS, where they all lie in it (rows in order, 16-byte piece p of row r of every 128 bytes at
 // place p ^ (r & 7)); or memory, as fragments, or in whole lines that are turned into fragments in LDS.  (Rows in lines cost
-// the vector cache 16 look-ups a load, as fragments 4 for every row: lines are the choice for more than 16 rows that lie in order.)
+// the vector cache 16 look-ups a load, as fragments 4 for every row: lines are the choice for more than 4 rows that lie in order.)
 enum { IN_LDS = 0, FRAGMENTS = 1, LINES = 2 };
 
 // ---- products.  A segment: 16 weight rows times an expert's m <= 64 rows over the 128-byte lines [l0, l1) of the contraction.
@@ -283,8 +288,9 @@ __device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned 
     }
 }
 // what decides which instance of stream() multiplies m rows
-template <int TY, int X> __device__ __forceinline__ int kind_of(int m) {
+template <int TY, int X, int X_TALL> __device__ __forceinline__ int kind_of(int m) {
     if (TY == FP && X == IN_LDS && m <= 8) return m <= 2 ? -2 : -8;
+    if (X_TALL == LINES && m <= 4) return 0;
     return (m + 15) >> 4;
 }
 // Runs of segments one behind the other, whatever their rows.  current: false if there is none; few: there are few lines in all.
@@ -293,8 +299,8 @@ __device__ __forceinline__ void stream_all(u32x4* turn, const unsigned char* xl,
     Segment seg;
     constexpr int DEEP = X == IN_LDS ? (WL == 2 ? 10 : 16) : (WL == 2 ? 8 : 12);
     while (current(seg)) {
-        const int kind = kind_of<TY, X>(seg.m);
-        auto same = [&](Segment& s) __attribute__((always_inline)) { return next(s) && kind_of<TY, X>(s.m) == kind; };
+        const int kind = kind_of<TY, X, X_TALL>(seg.m);
+        auto same = [&](Segment& s) __attribute__((always_inline)) { return next(s) && kind_of<TY, X, X_TALL>(s.m) == kind; };
         if constexpr (TY == FP && X == IN_LDS) {
             if (kind == -2) {
                 stream<TY, WL, 1, 2, DEEP, X>(seg, turn, xl, same, done);
@@ -305,8 +311,9 @@ __device__ __forceinline__ void stream_all(u32x4* turn, const unsigned char* xl,
                 continue;
             }
         }
-        if (kind == 1 && few) stream<TY, WL, 1, 0, 4, X>(seg, turn, xl, same, done);
-        else if (kind == 1) stream<TY, WL, 1, 0, DEEP, X>(seg, turn, xl, same, done);
+        if (kind <= 1 && few) stream<TY, WL, 1, 0, 4, X>(seg, turn, xl, same, done);
+        else if (kind == 0) stream<TY, WL, 1, 0, DEEP, X>(seg, turn, xl, same, done);
+        else if (kind == 1) stream<TY, WL, 1, 0, DEEP, X_TALL>(seg, turn, xl, same, done);
         else if (kind == 2) stream<TY, WL, 2, 0, 6, X_TALL>(seg, turn, xl, same, done);
         else if (kind == 3) stream<TY, WL, 3, 0, 4, X_TALL>(seg, turn, xl, same, done);
         else stream<TY, WL, 4, 0, X == IN_LDS ? 4 : 2, X_TALL>(seg, turn, xl, same, done);
@@ -703,7 +710,7 @@ struct Hidden {
     const void* x;
     const void* const *w_in, *const *s_w_in;
     unsigned char *h, *s_h;              // hidden activations of the rows (A of F) and of the shared expert (T of shared_F)
-    int F, shared_F, glu, h_rows;        // h_rows: H row by row, else an expert's rows piece by piece (see finish)
+    int F, shared_F, glu, h_rows;        // h_rows: H in rows, else an expert's rows piece by piece (see finish)
 };
 __device__ __forceinline__ uint16_t half_of(float v) {           // saturating, nearest-even
     return __builtin_bit_cast(uint16_t, (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f));
@@ -734,7 +741,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
         __syncthreads();
     }
     if (tid < E) l.w[tid] = mine_w;
-    make_lists(l, E, e, tid / k, 0.f);
+    make_lists(l, E, e, tid / k, 0.f, ~0ull);
     u32x4* const turn = (u32x4*)smem + wave * PLACE;
     f32x4* const heads = (f32x4*)((u32x4*)smem + NW * PLACE);            // [wavefront][group][lane]
     const __amdgpu_buffer_rsrc_t x = make_rsrc(p.x, (unsigned)T * row_bytes);
@@ -772,13 +779,14 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
     };
     struct Item {
         int r0, m, width, out0;
-        bool glu;
+        bool shared, glu;
         unsigned char* h;
     };
     auto item_of = [&](int ai, int q) __attribute__((always_inline)) {
         Item it;
         const bool shared = ai < 0;
         const int e = shared ? 0 : sgpr(l.active[ai]);
+        it.shared = shared;
         it.glu = shared || p.glu;
         it.r0 = shared ? 0 : sgpr(l.first[e]);
         it.m = shared ? T : sgpr(l.first[e + 1]) - it.r0;
@@ -797,10 +805,11 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
             v[i] = it.glu ? silu_f(a[i]) * up : fmaxf(a[i], 0.f);
         }
         if (r < it.m && (!it.glu || lq < 2)) {
-            // H row by row; or an expert's rows piece by piece, 16 bytes of every row behind one another, so that a fragment of any rows is
-            // one run of bytes.  The lane's four outputs are in one piece (16 bits: every other one of its eight).
+            // H in rows by token and choice; or an expert's rows piece by piece, 16 bytes of every row behind one another, so that a fragment
+            // of any rows is one run of bytes.  The lane's four outputs are in one piece (16 bits: every other one of its eight).
             const int col = it.out0 + 4 * lq * (F32 ? 1 : 2), piece = col * ES / 16;
-            unsigned char* to = it.h + (size_t)it.r0 * it.width * ES + (p.h_rows ? (size_t)r * it.width * ES + piece * 16 : ((size_t)piece * it.m + r) * 16);
+            const size_t row = it.width * ES;
+            unsigned char* to = it.h + (p.h_rows ? (it.shared ? r : (int)l.pair[it.r0 + r]) * row + piece * 16 : it.r0 * row + ((size_t)piece * it.m + r) * 16);
             if constexpr (F32) {
                 *(f32x4*)to = f32x4{v[0], v[1], v[2], v[3]};
             } else {
@@ -838,7 +847,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
 #pragma unroll
                 for (int r = 0; r < 8; ++r) s.row_at[r] = piece_at(token(r < s.m ? r : s.m - 1), row_bytes);
             }
-        } else {                         // (up to 16 rows as fragments, more in lines)
+        } else {
             s.x_at[1] = s.x_at[2] = s.x_at[3] = NOWHERE;         // (members without a value end up in scratch memory when copied)
             s.x_at[0] = l16 < s.m ? (unsigned)token(l16 < s.m ? l16 : 0) * row_bytes + (unsigned)lq * 16u : NOWHERE;
 #pragma unroll
@@ -916,11 +925,12 @@ struct Out {
     const void* const *w_out, *const *s_w_out;
     const unsigned char *h, *s_h;
     void* y;
-    int T, d, E, k, F, shared_F, y_f32, splits;
+    int T, d, E, k, F, shared_F, y_f32, splits, by_token, pairs;
 };
 
-// WL: 1 for 8 columns of a work-group, 2 for 16.  LDS: the hidden activations go there first.  splits > 1 (one choice per token, no shared
-// expert): the work-groups of a column block share the experts, and each writes its experts' tokens.
+// WL: 1 for 8 columns of a work-group, 2 for 16.  LDS: the hidden activations (of its tokens) go there first.  splits > 1: that many
+// work-groups share a column block: a range of the tokens each (by_token), or, with one choice per token and no shared expert, the experts.
+// pairs (LDS): every assignment of the range for itself, so that a token's sums do not depend on what other tokens chose.
 template <bool F32, int WL, bool LDS>
 __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : HF, COLS = WL * 8;
@@ -931,8 +941,11 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     __shared__ int state[MAXT];          // of a token: 0 not this work-group's, 1 to be written, 2 with an assignment to no expert
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const int T = p.T, d = p.d, E = p.E, k = p.k, F = p.F, splits = p.splits;
-    const int split = (int)blockIdx.x % splits, p0 = (int)blockIdx.x / splits * COLS;
-    const unsigned f_bytes = (unsigned)F * ES, s_bytes = (unsigned)p.shared_F * ES, s_base = (unsigned)(T * k) * f_bytes;
+    // (the work-groups of a column block on one XCD where the number of blocks is a multiple of eight)
+    const int blocks = d / COLS, split = (int)blockIdx.x / blocks, p0 = ((int)blockIdx.x - split * blocks) * COLS;
+    const int t0 = p.by_token ? T * split / splits : 0, t1 = p.by_token ? T * (split + 1) / splits : T;
+    const unsigned long long range = (t1 < 64 ? (1ull << t1) : 0ull) - (1ull << t0);
+    const unsigned f_bytes = (unsigned)F * ES, s_bytes = (unsigned)p.shared_F * ES, s_base = (unsigned)((t1 - t0) * k) * f_bytes;
     int e = -1;
     float gate = 0.f;
     if (tid < T * k) {
@@ -941,24 +954,38 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     }
     const void* const mine_w = tid < E ? p.w_out[tid] : nullptr;
     if constexpr (LDS) {
-        rows_to_lds(p.h, T * k, f_bytes, hl);
-        if (p.shared_F) rows_to_lds(p.s_h, T, s_bytes, hl + s_base);
+        rows_to_lds(p.h + (size_t)(t0 * k) * f_bytes, (t1 - t0) * k, f_bytes, hl);
+        if (p.shared_F) rows_to_lds(p.s_h + (size_t)t0 * s_bytes, t1 - t0, s_bytes, hl + s_base);
     }
     if (tid < 2 * MAXE) (&l.bits[0][0])[tid] = 0u;
-    if (tid < T) state[tid] = splits == 1;
+    if (tid < T) state[tid] = splits == 1 || (p.by_token && tid >= t0 && tid < t1);
     for (int i = lane; i < T * COLS; i += 64) (&sums[wave][0][0])[i] = 0.f;
     __syncthreads();
     if (tid < E) l.w[tid] = mine_w;
-    if (tid < T * k && (unsigned)e >= (unsigned)E && split == 0) state[tid / k] = 2;
+    if (tid < T * k && (unsigned)e >= (unsigned)E && (p.by_token ? state[tid / k] : split == 0)) state[tid / k] = 2;
     if constexpr (LDS) MOE_WAIT_VMCNT(0);
-    make_lists(l, E, e, tid / k, gate);
+    const bool pairs = LDS && p.pairs;
+    if (pairs) {
+        const int i = tid - t0 * k, n = (t1 - t0) * k;
+        if (i >= 0 && i < n) {
+            l.active[i] = (unsigned)e < (unsigned)E ? e : -1;
+            l.pair[i] = (unsigned short)tid;
+            l.t[i] = (unsigned char)(tid / k);
+            l.gate[i] = gate;
+        }
+        if (tid <= n) l.cost[tid] = tid * line_cost(1);
+        if (tid == 0) l.n_active = n;
+        __syncthreads();
+    } else {
+        make_lists(l, E, e, tid / k, gate, range);
+    }
     u32x4* const turn = (u32x4*)smem + wave * 256;
-    const int n_active = sgpr(l.n_active), rows = sgpr(l.first[(E + 63) & ~63]);
-    const __amdgpu_buffer_rsrc_t h = make_rsrc(p.h, (unsigned)rows * f_bytes), s_h = make_rsrc(p.s_h, (unsigned)T * s_bytes);
+    const int n_active = sgpr(l.n_active), all_rows = LDS ? 0 : sgpr(l.first[(E + 63) & ~63]);
+    const __amdgpu_buffer_rsrc_t h = make_rsrc(p.h, (unsigned)all_rows * f_bytes), s_h = make_rsrc(p.s_h, (unsigned)T * s_bytes);
     // The lines of the active experts' contractions, the shared expert's behind, by what they cost: a wavefront's share of that.
-    const int L = F * ES / 128, s_L = p.shared_F * ES / 128, s_cost = line_cost(T);
+    const int L = F * ES / 128, s_L = p.shared_F * ES / 128, s_cost = line_cost(t1 - t0);
     int ai0 = 0, ai1 = n_active;         // the work-group's experts
-    if (splits > 1) {
+    if (splits > 1 && !p.by_token) {
         const int all = l.cost[n_active];
         int below = 0, upto = 0;
         for (int x = lane; x - lane < n_active; x += 64) {
@@ -979,8 +1006,11 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         if (ai > ai1 || (shared && !s_L)) return false;
         const int at = sgpr(L * l.cost[ai]) - base;
         if (at >= hi) return false;
-        const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? 0 : sgpr(l.first[e]), have = shared ? s_L : L;
-        s.m = shared ? T : sgpr(l.first[e + 1]) - r0;
+        // the expert's rows (all tokens') begin at `begin` and are `rows`; the work-group's are s.m, `off` behind
+        const int chosen = shared ? 0 : sgpr(l.active[ai]), e = pairs && chosen < 0 ? 0 : chosen, have = shared ? s_L : chosen < 0 ? 0 : L;
+        const int begin = shared ? 0 : pairs ? ai : sgpr(l.first[e]), rows = shared ? T : pairs ? 1 : sgpr(l.first[e + 1]) - begin;
+        const int off = shared ? t0 : pairs ? 0 : sgpr(rows_in(l, e, (1ull << t0) - 1ull)), r0 = begin + off;
+        s.m = shared ? t1 - t0 : pairs ? 1 : sgpr(rows_in(l, e, range));
         const int c = line_cost(s.m);
         s.l0 = 0;
         s.l1 = have;
@@ -991,23 +1021,24 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         s.w_at[0] = at8;
         s.w_at[1] = at8 + 8u * row_bytes;
         s.x = shared ? s_h : h;
-        s.x_step = 64 * s.m;
+        s.x_step = 64 * rows;
         if constexpr (LDS) {
-            const unsigned from = shared ? s_base : (unsigned)r0 * row_bytes;
-            // (places in rows counted from the first: r0 need not be a multiple of 8)
-            const int first = shared ? 0 : r0;
-            const unsigned start = from - (unsigned)first * row_bytes;
+            const unsigned start = shared ? s_base : 0u;
+            auto place = [&](int r) __attribute__((always_inline)) {     // of row r (of the last one, beyond)
+                const int at = r < s.m ? r : s.m - 1;
+                return shared ? at : (int)l.pair[r0 + at] - t0 * k;
+            };
 #pragma unroll
-            for (int g = 0; g < 4; ++g) s.x_at[g] = start + fragment_at(first + (g * 16 + l16 < s.m ? g * 16 + l16 : s.m - 1), row_bytes);
+            for (int g = 0; g < 4; ++g) s.x_at[g] = start + fragment_at(place(g * 16 + l16), row_bytes);
             if constexpr (F32) {
 #pragma unroll
-                for (int r = 0; r < 8; ++r) s.row_at[r] = start + piece_at(first + (r < s.m ? r : s.m - 1), row_bytes);
+                for (int r = 0; r < 8; ++r) s.row_at[r] = start + piece_at(place(r), row_bytes);
             }
         } else {
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const int r = g * 16 + l16;
-                s.x_at[g] = r < s.m ? (unsigned)r0 * row_bytes + (unsigned)(lq * s.m + r) * 16u : NOWHERE;
+                s.x_at[g] = r < s.m ? (unsigned)begin * row_bytes + (unsigned)(lq * rows + off + r) * 16u : NOWHERE;
             }
         }
         return true;
@@ -1025,19 +1056,19 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         [&](const Segment& s, auto& acc) __attribute__((always_inline)) {
             constexpr int G = sizeof(acc) / sizeof(acc[0]);
             const bool shared = ai == ai1;
-            const int r0 = shared ? 0 : sgpr(l.first[sgpr(l.active[ai])]);
+            const int e = shared ? 0 : sgpr(l.active[ai]), r0 = shared ? t0 : pairs ? ai : sgpr(l.first[e] + rows_in(l, e, (1ull << t0) - 1ull));
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int r = g * 16 + l16;
                 if (r < s.m && (WL == 2 || lq < 2)) {
-                    const int t = shared ? r : l.t[r0 + r];
+                    const int t = shared ? r0 + r : l.t[r0 + r];
                     const float gate = shared ? 1.f : l.gate[r0 + r];
                     f32x4* to = (f32x4*)&sums[wave][t][4 * lq];          // (an expert's rows are different tokens)
                     f32x4 sum = *to;
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] = fmaf(gate, acc[g][i], sum[i]);
                     *to = sum;
-                    if (splits > 1) state[t] = 1;
+                    if (splits > 1 && !p.by_token) state[t] = 1;
                 }
             }
             ++ai;
@@ -1098,9 +1129,25 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     a.x = x; a.w_in = w_in; a.s_w_in = s_w_in; a.F = F; a.shared_F = shared_F; a.glu = act == MOE_SWIGLU;
     a.h = (unsigned char*)ws;
     a.s_h = a.h + (size_t)T * k * F * es;
-    // x and the hidden activations go to LDS first where they fit (T <= 32: beyond, the routing's sums take it)
-    const bool x_lds = (size_t)T * d * es <= X_BYTES && T <= 32, h_lds = need <= H_BYTES;
+    // The second launch's work-groups: sixteen columns where they make one per CU, else eight (a matrix instruction half empty, twice the
+    // work-groups); where these are few, several share a column block.  With one choice per token they share the experts, and nothing is
+    // fetched twice.  Else they share the tokens, and an expert is fetched for every range of tokens that chose it, from the L2 then, while
+    // most CUs would have no work.  Ranges of at most four tokens take every assignment for itself (few experts are met twice).
+    const bool apart = k == 1 && !shared_F;
+    const bool wide = (long long)(d / 16) * (apart ? T : 1) >= MOE_GEMM_GRID;
+    const int blocks = d / (wide ? 16 : 8);
+    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1, !apart, 0};
+    while (o.splits < T && blocks * (o.splits + 1) <= MOE_GEMM_GRID) ++o.splits;
+    int range = (T + o.splits - 1) / o.splits;
+    o.pairs = !apart && o.splits > 1 && range <= 4;
+    if (!apart && !o.pairs && T < 16) {
+        o.splits = 1;
+        range = T;
+    }
+    // x and the hidden activations go to LDS first where they fit (x: T <= 32, beyond the routing's sums take it)
+    const bool x_lds = (size_t)T * d * es <= X_BYTES && T <= 32, h_lds = (size_t)(apart ? T : range) * (need / T) <= H_BYTES;
     a.h_rows = h_lds;
+    o.pairs &= h_lds;
     if (dt == MOE_F32) {
         const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
         if (rc != MOE_OK) return rc;
@@ -1115,13 +1162,6 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
         launch_hidden<false, How<4, false>>(a, st);
     }
     MOE_CHECK_LAUNCH("moe_layer_few (routing and first product)");
-    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1};
-    // With one choice per token and no shared expert up to T work-groups share a column block's experts.  Sixteen columns where they
-    // make a work-group per CU, else eight (a matrix instruction half empty, twice the work-groups).
-    const int most = k == 1 && !shared_F ? T : 1;
-    const bool wide = (long long)(d / 16) * most >= MOE_GEMM_GRID;
-    const int blocks = d / (wide ? 16 : 8);
-    while (o.splits < most && blocks * (o.splits + 1) <= MOE_GEMM_GRID) ++o.splits;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * o.splits)), dim3(NTH), 0, st, o); };
     if (dt == MOE_F32 && h_lds) wide ? go(few_out_kernel<true, 2, true>) : go(few_out_kernel<true, 1, true>);
     else if (dt == MOE_F32) wide ? go(few_out_kernel<true, 2, false>) : go(few_out_kernel<true, 1, false>);
