@@ -1,4 +1,4 @@
-// moe_layer_few: a whole MoE layer for a few tokens (T <= 64) in two launches.
+// moe_layer_few: a whole MoE layer for a few tokens (T <= 64) in two launches (three: fp32, and more than 32 tokens).
 //
 //   launch 1   routing, then   H[r,:] = act(x[token of r] . W_in^T)            for every row r = (expert, token)
 //   launch 2   y[t,:] = sum_j gate[t,j] H[row of (t,j)] . W_out^T  (+ shared expert)
@@ -10,13 +10,13 @@
 //
 // Launch 1, one work-group of eight wavefronts per CU.  Every work-group routes all tokens for itself (what it reads for
 // that, W_g and x, comes from the L2s; waiting for another work-group's answer, or another launch, costs more): logits on the matrix
-// cores in fp32 over 32 terms at a time, added up in fp64, with a rigorous error bound; logits closer than the bound are
-// computed again in fp64, so that the choice is that of exact arithmetic.  Then its wavefronts take items of 16 weight rows, each
-// alone over the whole contraction: no barrier, no partial sums.
-// Launch 2: a work-group owns 8 or 16 output columns for all tokens and all experts.  The (expert, 128-byte line) pairs of its
-// contraction are dealt out to its wavefronts in runs of equal cost; a wavefront adds each expert's products, times the gates, to
+// cores in fp32 over 64 terms at a time, added up in fp64, with a rigorous error bound; a token whose logits are closer than the bound
+// has those computed again in fp64, so that the choice is that of exact arithmetic.  Then its items of 16 weight rows are shared
+// out to its wavefronts in runs of equal cost; an item that several of them have part of is added up in LDS.
+// Launch 2: a work-group owns 8 or 16 output columns, for all tokens and experts or, in narrow layers, some of them.  The (expert,
+// 128-byte line) pairs of its contraction are shared out in the same way; a wavefront adds each expert's products, times the gates, to
 // sums per token of its own in LDS, and these are added in a fixed order.  So the combine costs no pass over memory, no atomics and no
-// second launch, and all CUs read equal shares of the weights whatever the routing.
+// launch of its own, and all CUs read equal shares of the weights whatever the routing.
 //
 // Weights and rows come in whole 128-byte lines, eight rows a load, several lines in flight per wavefront, and
 // are turned into the matrix instruction's fragments in a piece of LDS of the wavefront's own (fragments straight from global memory touch 16
@@ -355,6 +355,11 @@ template <int TT_, bool LDS_> struct How {
     static constexpr int TT = TT_, EB = TT_ <= 1 || (TT_ == 2 && !LDS_) ? 4 : 2, D = TT_ == 1 ? 3 : 2;
     static constexpr bool LDS = LDS_;
 };
+// Beyond that many tokens MOE_BF16 routes in a launch of its own: what every work-group does for itself takes longer than that then (64
+// tokens: d=320 F=512 E=24 k=4 38.2 us against 34.9, d=2048 F=1408 E=60 k=4 227 against 220; 17 to 32 tokens: up to 3 us less than with
+// a launch).
+constexpr int ROUTE_MAXT = 32;
+static_assert(ROUTE_MAXT <= NW * 4, "choose: four tokens a wavefront");
 template <bool LDS> using Routed = How<0, LDS>;          // the choice is there already
 template <typename H> struct RouteLds {
     double part[NW * H::EB * 16][H::TT * 16 + 1];        // [contraction part, expert][token]; the lines' turning places before
@@ -695,16 +700,17 @@ __device__ __forceinline__ void route_all(const Route& p, unsigned char* smem, c
 #pragma unroll
     for (int w = 0; w < NW; ++w) wn = fmaxf(wn, s.most[w]);
     __syncthreads();
-    for (int t0 = wave * 4; t0 < T; t0 += NW * 4) {
-        if (E <= 64) choose<4>(p, s, l, t0, wn, KS, write);
-        else if (E <= 128) choose<8>(p, s, l, t0, wn, KS, write);
-        else choose<16>(p, s, l, t0, wn, KS, write);
+    if (wave * 4 < T) {                  // (four tokens a wavefront, ROUTE_MAXT in all)
+        if (E <= 64) choose<4>(p, s, l, wave * 4, wn, KS, write);
+        else if (E <= 128) choose<8>(p, s, l, wave * 4, wn, KS, write);
+        else choose<16>(p, s, l, wave * 4, wn, KS, write);
     }
     __syncthreads();
 }
 
 // ---- launch 1
-constexpr unsigned X_BYTES = 64 << 10, H_BYTES = 80 << 10;       // of LDS for x, and for the hidden activations in launch 2
+constexpr unsigned X_BYTES = 64 << 10;           // of LDS for x
+constexpr unsigned h_bytes(int WL) { return WL == 2 ? 80u << 10 : 93u << 10; }     // and for the hidden activations in launch 2
 struct Hidden {
     Route route;
     const void* x;
@@ -935,7 +941,7 @@ template <bool F32, int WL, bool LDS>
 __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : HF, COLS = WL * 8;
     __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(u32x4) * 256 * NW];
-    __shared__ __attribute__((aligned(16))) unsigned char hl[LDS ? H_BYTES : 16];
+    __shared__ __attribute__((aligned(16))) unsigned char hl[LDS ? h_bytes(WL) : 16];
     __shared__ __attribute__((aligned(16))) float sums[NW][MAXT][COLS];
     __shared__ Lists l;
     __shared__ int state[MAXT];          // of a token: 0 not this work-group's, 1 to be written, 2 with an assignment to no expert
@@ -1132,34 +1138,29 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     // The second launch's work-groups: sixteen columns where they make one per CU, else eight (a matrix instruction half empty, twice the
     // work-groups); where these are few, several share a column block.  With one choice per token they share the experts, and nothing is
     // fetched twice.  Else they share the tokens, and an expert is fetched for every range of tokens that chose it, from the L2 then, while
-    // most CUs would have no work.  Ranges of at most four tokens take every assignment for itself (few experts are met twice).
+    // most CUs would have no work.  Ranges of at most eight tokens take every assignment for itself, as few experts are met twice there.
+    // (us, unshared / ranges / of assignments: 8 tokens, fp32 d=320 F=1984 E=16 k=2: 51.9 / - / 32.1; 12 tokens, 16-bit d=320 F=512
+    // E=24 k=4: 28.7 / 24.8 / 22.1, d=640 F=768 E=24 k=2: - / 28.7 / 26.3; 32 tokens, d=512 F=512 E=24 k=4: - / 31.5 / 32.9)
     const bool apart = k == 1 && !shared_F;
     const bool wide = (long long)(d / 16) * (apart ? T : 1) >= MOE_GEMM_GRID;
     const int blocks = d / (wide ? 16 : 8);
     Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1, !apart, 0};
     while (o.splits < T && blocks * (o.splits + 1) <= MOE_GEMM_GRID) ++o.splits;
-    int range = (T + o.splits - 1) / o.splits;
-    o.pairs = !apart && o.splits > 1 && range <= 4;
-    if (!apart && !o.pairs && T < 16) {
-        o.splits = 1;
-        range = T;
-    }
-    // x and the hidden activations go to LDS first where they fit (x: T <= 32, beyond the routing's sums take it)
-    const bool x_lds = (size_t)T * d * es <= X_BYTES && T <= 32, h_lds = (size_t)(apart ? T : range) * (need / T) <= H_BYTES;
+    const int range = apart ? T : (T + o.splits - 1) / o.splits;
+    // x and the work-group's hidden activations go to LDS first where they fit
+    const bool x_lds = (size_t)T * d * es <= X_BYTES, h_lds = (size_t)range * (need / T) <= h_bytes(wide ? 2 : 1);
     a.h_rows = h_lds;
-    o.pairs &= h_lds;
-    if (dt == MOE_F32) {
-        const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
+    o.pairs = h_lds && !apart && o.splits > 1 && range <= 8;
+    if (dt == MOE_F32 || T > ROUTE_MAXT) {
+        const int rc = dt == MOE_F32 ? moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream)
+                                     : moe_route_topk_packed(x, w_gate, w_norm2, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
         if (rc != MOE_OK) return rc;
-        x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
+        if (dt == MOE_F32) x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
+        else x_lds ? launch_hidden<false, Routed<true>>(a, st) : launch_hidden<false, Routed<false>>(a, st);
     } else if (T <= 16) {
         x_lds ? launch_hidden<false, How<1, true>>(a, st) : launch_hidden<false, How<1, false>>(a, st);
-    } else if (T <= 32) {
-        x_lds ? launch_hidden<false, How<2, true>>(a, st) : launch_hidden<false, How<2, false>>(a, st);
-    } else if (T <= 48) {
-        launch_hidden<false, How<3, false>>(a, st);
     } else {
-        launch_hidden<false, How<4, false>>(a, st);
+        x_lds ? launch_hidden<false, How<2, true>>(a, st) : launch_hidden<false, How<2, false>>(a, st);
     }
     MOE_CHECK_LAUNCH("moe_layer_few (routing and first product)");
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * o.splits)), dim3(NTH), 0, st, o); };

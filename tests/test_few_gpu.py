@@ -151,6 +151,32 @@ def test_widths(d, F, shared_F, dt, act, T):
     check(Case(T, d, F, 4, 2, act, dt, shared_F=shared_F, renorm=1), y_dts=(1,))
 
 
+@pytest.mark.parametrize("T,d,F,E,k,shared_F", [(5, 320, 512, 24, 4, 0), (12, 64, 128, 9, 3, 64), (20, 256, 192, 16, 8, 128), (23, 768, 256, 6, 2, 0),
+                                                (33, 640, 320, 12, 3, 64), (47, 512, 448, 24, 6, 0), (64, 960, 1472, 8, 2, 0), (64, 64, 64, 3, 1, 64)])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_narrow_layers(T, d, F, E, k, shared_F, dt):
+    """Few output columns and many tokens: those who share the columns take ranges of the tokens, of odd lengths here."""
+    print("[case] few narrow T=%d d=%d F=%d E=%d k=%d shared=%d %s" % (T, d, F, E, k, shared_F, dt), flush=True)
+    check(Case(T, d, F, E, k, "swiglu" if T % 2 else "relu", dt, shared_F=shared_F, renorm=T % 2))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,shared_F", [(9, 0), (40, 64), (64, 0)])
+def test_tokens_that_are_no_numbers_in_narrow_layers(T, shared_F, dt):
+    """First, last and some in between are NaN: their rows are, no other is, and the others keep their values to the tolerance."""
+    c = Case(T, 128, 192, 7, 3, "swiglu", dt, shared_F=shared_F)
+    dev = Device(c)
+    idx, _, y, m1, m2 = reference(c)
+    x = dev.x.clone()
+    bad = sorted({0, T // 2, T // 2 + 1, T - 1})
+    keep = [t for t in range(T) if t not in bad]
+    x[bad] = float("nan")
+    got = dev.run(x=x).cpu().numpy()
+    assert np.isnan(got[bad]).all() and np.array_equal(dev.idx.cpu().numpy()[keep], idx[keep])
+    bound = 600 * 2.0 ** -24 * m1 + (600 * 2.0 ** -24 + 4e-6) * m2 + (2.0 ** -12 * m2 if dt == "bf16" else 0.0)
+    assert (np.abs(got - y) <= bound)[keep].all()
+
+
 def test_all_tokens_on_one_expert():
     """A bias that leaves one expert: 64 rows there, none elsewhere."""
     for dt in ("bf16", "f32"):
