@@ -2,6 +2,7 @@
 
 `paper_2506_12417_amd.binding` is the ctypes face of libmoe.so: same names as include/moe.h,
 argument marshalling only.  `paper_2506_12417_amd.layer` chains the calls into one layer
-forward.  Importing either raises if the built library is missing -- there is no fallback.
+forward, `paper_2506_12417_amd.block` that layer with the norms, the gate and the residual addition
+around it.  Importing any of them raises if the built library is missing -- there is no fallback.
 """
-__all__ = ["binding", "layer", "build"]
+__all__ = ["binding", "layer", "block", "build"]

@@ -1,0 +1,106 @@
+"""A MoE layer as it stands in a model, between two residual additions:
+
+    u = pre(h),   v = layer(u),   y = alpha * h + gate * post(v),   u' = next(y)
+
+Like the layer, this owns buffers and marshals arguments; every value is computed in the library's kernels."""
+from __future__ import annotations
+
+from typing import Dict, Optional, Tuple
+
+import numpy as np
+import torch
+
+from . import binding as B
+from .layer import MoELayer, to_device
+
+KINDS = {"none": B.MOE_NORM_NONE, "rms": B.MOE_NORM_RMS, "layer": B.MOE_NORM_LAYER}
+NAMES = ("pre_w", "pre_b", "post_w", "post_b", "gate", "next_w", "next_b")
+
+
+def prefers_few(layer: MoELayer) -> bool:
+    """Whether one call serves the layer's tokens best.  Up to 32 bf16 tokens it takes 0.97 to 1.4 times fewer microseconds than the separate
+    calls (one token of d=768 F=3072 21 us against 25; 32 tokens of d=2048 F=1408 E=60 k=4 168 against 171); with more, whole tiles of rows
+    are worth a plan (64 tokens 220 against 207).  In fp32 the matrix instruction bounds both, and the line is at 16 (5 tokens of d=320
+    F=1984 26 against 31, 32 tokens 49 against 44)."""
+    return layer.few_ok and (layer.T <= 32 and layer.packed_router if layer.dt == B.MOE_BF16 else layer.T <= 16)
+
+
+class MoEBlock:
+    """pre, post, next: "rms", "layer" or "none" (pre always is one; next is the norm of the block behind, whose u' comes out here).
+    h_dtype: the residual stream's type; the layer's own is u's.  gate: "none", "shared" (one row of d factors) or "token" (a row for every
+    token).  train: forward() keeps what the backward calls read, and v is stored for them."""
+
+    def __init__(self, layer: MoELayer, pre: str = "rms", post: str = "none", next: str = "none", eps: float = 1e-5, alpha: float = 1.0,
+                 gate: str = "none", h_dtype: str = "bf16", train: bool = False):
+        assert pre != "none" and layer.d <= B.MOE_NORM_MAX_D
+        self.layer, self.eps, self.alpha, self.train = layer, eps, alpha, train
+        self.T, self.d, dev = layer.T, layer.d, layer.device
+        self.pre, self.post, self.next = KINDS[pre], KINDS[post], KINDS[next]
+        self.gate_rows = {"none": 0, "shared": 1, "token": self.T}[gate]
+        self.h_dt = B.MOE_BF16 if h_dtype == "bf16" else B.MOE_F32
+        self.h_tdt = torch.bfloat16 if h_dtype == "bf16" else torch.float32
+        self.param: Dict[str, Optional[torch.Tensor]] = {n: None for n in NAMES}
+        T, d, f32 = self.T, self.d, torch.float32
+        self.u = torch.empty((T, d), dtype=layer.tdt, device=dev)
+        self.y = torch.empty((T, d), dtype=self.h_tdt, device=dev)
+        self.u_next = torch.empty((T, d), dtype=layer.tdt, device=dev) if self.next else None
+        if train:
+            self.pre_stats = torch.empty((T, 2), dtype=f32, device=dev)
+            self.end_stats = torch.empty((T, 4), dtype=f32, device=dev)
+            self.grad: Dict[str, torch.Tensor] = {}
+            n = max(B.moe_workspace_bytes(op, T, d, 0, 0, 0, layer.dt) for op in (B.MOE_OP_NORM_BACKWARD, B.MOE_OP_BLOCK_END_BACKWARD))
+            self.ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
+            self.dv = torch.empty((T, d), dtype=f32, device=dev)
+            self.dh = torch.empty((T, d), dtype=self.h_tdt, device=dev)
+
+    def load(self, **arrays: np.ndarray):
+        """Parameters by name (NAMES), fp32: [d], and the gate [d] or [T,d].  What is not loaded counts as ones (weights) or zeros."""
+        for name, a in arrays.items():
+            assert name in NAMES and np.shape(a) in (((self.d,), (1, self.d)) if name != "gate" or self.gate_rows < 2 else ((self.T, self.d),)), name
+            self.param[name] = to_device(np.asarray(a, dtype=np.float32).reshape(-1, self.d), self.layer.device)
+            if self.train:
+                self.grad["d" + name] = torch.empty_like(self.param[name])
+        assert self.gate_rows == 0 or "gate" not in arrays or self.param["gate"].shape[0] == self.gate_rows
+
+    def _end(self) -> Tuple:
+        p = self.param
+        assert self.gate_rows == 0 or p["gate"] is not None, "the gate is not loaded"
+        return (self.T, self.d, self.post, self.eps, p["post_w"], p["post_b"], p["gate"] if self.gate_rows else None, self.gate_rows, self.alpha,
+                self.next, self.eps, p["next_w"], p["next_b"], self.y, self.u_next, self.layer.dt)
+
+    def forward(self, h: torch.Tensor, u: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        """Enqueues the block; returns y and u' (None without a next norm), buffers of the block's own.  u: pre(h), where the block before has
+        made it as its u'."""
+        L, p = self.layer, self.param
+        assert not (self.train and u is not None), "the pre norm's statistics come from its own call"
+        if u is None:
+            B.moe_norm(h, self.h_dt, p["pre_w"], p["pre_b"], self.T, self.d, self.pre, self.eps, self.u, L.dt, self.pre_stats if self.train else None,
+                       stream)
+            u = self.u
+        if prefers_few(L):
+            L.forward_few(u, stream=stream)
+        elif self.train or L.fold_combine:
+            L.forward(u, stream=stream)
+        else:
+            # the layer's combine in the same pass as what follows it: v is never stored
+            L.forward(u, stream=stream, rows=True)
+            B.moe_block_end_rows(L.y_perm, L.inv_perm, L.gate_w, L.s_y if L.shared_F else None, L.k, h, self.h_dt, *self._end(), stream)
+            return self.y, self.u_next
+        B.moe_block_end(L.y, B.MOE_F32, h, self.h_dt, *self._end(), self.end_stats if self.train else None, stream)
+        return self.y, self.u_next
+
+    def end_backward(self, h: torch.Tensor, dy: Optional[torch.Tensor], du_next: Optional[torch.Tensor], stream=None):
+        """From the gradients of y and u' to those of v (fp32) and, by the residual connection, of h; the parameters' go to `grad`."""
+        p, g = self.param, self.grad
+        B.moe_block_end_backward(dy, du_next, self.layer.dt, self.layer.y, B.MOE_F32, h, self.h_dt, self.T, self.d, self.post, p["post_w"], p["post_b"],
+                                 p["gate"] if self.gate_rows else None, self.gate_rows, self.alpha, self.next, p["next_w"], self.end_stats, self.dv, self.dh,
+                                 *[g.get(n) for n in ("dpost_w", "dpost_b", "dgate", "dnext_w", "dnext_b")], self.ws, self.ws.numel(), stream)
+        return self.dv, self.dh
+
+    def pre_backward(self, h: torch.Tensor, du: torch.Tensor, stream=None) -> torch.Tensor:
+        """From the gradient of u, as the layer's own backward gives it for dv, to h's whole gradient: end_backward's dh is added, in
+        place."""
+        p, g = self.param, self.grad
+        B.moe_norm_backward(du, self.layer.dt, h, self.h_dt, p["pre_w"], self.pre_stats, self.T, self.d, self.pre, self.dh, self.dh, g.get("dpre_w"),
+                            g.get("dpre_b"), self.ws, self.ws.numel(), stream)
+        return self.dh

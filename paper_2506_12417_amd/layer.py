@@ -117,6 +117,10 @@ class MoELayer:
         # in fp32 the first product can gather as well (moe_grouped_ffn_gather)
         can_fuse = can_fuse or (self.dt == B.MOE_F32 and T >= 1)
         self.fuse_gather = can_fuse if fuse_gather is None else (fuse_gather and can_fuse)
+        # a decode step's sizes: the whole layer in one call (forward_few)
+        self.few_ok = (1 <= T <= B.MOE_FEW_MAX_T and d % 64 == 0 and F % 64 == 0 and shared_F % 64 == 0)
+        if self.few_ok:
+            self.few_ws = torch.empty(B.moe_layer_few_workspace(T, F, k, shared_F, self.dt), dtype=torch.uint8, device=dev)
         if shared_F:
             # the always-on shared expert is one more group: E = 1, every token, rows in place
             self.shared = ExpertGroup(1, d, shared_F, B.MOE_SWIGLU, self.dt, dev)
@@ -227,7 +231,20 @@ class MoELayer:
         return (B.moe_grouped_ffn, B.moe_grouped_ffn_phase,
                 (self.x_perm, self.A, *shape[1:], *kinds, *table, self.y_perm, stream), ("g1", "g2"))
 
-    def forward(self, x: torch.Tensor, stream=None, marks=None, routed: bool = False, stages=None) -> torch.Tensor:
+    def forward_few(self, x: torch.Tensor, y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """The whole layer in one call, for a decode step's few tokens (few_ok says whether the sizes fit; a bf16 router has to be
+        packed).  y: [T,d] fp32 or bf16, None = the layer's own fp32 buffer.  The choice is forward()'s; the sums are added in
+        another order, so the last bits differ."""
+        assert self.few_ok and (self.packed_router or self.dt == B.MOE_F32), "sizes or router are not moe_layer_few's"
+        y = self.y if y is None else y
+        g, s = self.experts, self.shared if self.shared_F else None
+        w, norm2 = (self.W_gt, self.w_norm2) if self.dt == B.MOE_BF16 else (self.W_g, None)
+        B.moe_layer_few(x, self.T, self.d, self.F, self.E, self.k, self.act, self.dt, self.renorm, w, norm2, self.bias, g.in_ptrs, g.out_ptrs,
+                        self.shared_F, s.in_ptrs if s else None, s.out_ptrs if s else None, self.expert_idx, self.gate_w,
+                        self.few_ws, self.few_ws.numel(), y, B.MOE_F32 if y.dtype == torch.float32 else B.MOE_BF16, stream)
+        return y
+
+    def forward(self, x: torch.Tensor, stream=None, marks=None, routed: bool = False, stages=None, rows: bool = False) -> torch.Tensor:
         """Enqueues the whole layer on the current (or given) stream; returns the output buffer.
         A bf16 token's last bits depend on the number of tokens the layer is made for: calls with a
         handful of rows per expert run by kernels that add the contraction in another order
@@ -238,7 +255,10 @@ class MoELayer:
         stages: optional list that receives (name, event) after every stage of the path, starting
         with ("start", event) (per-stage timing; the events are recorded on the current stream).  With
         either the same launches run in the same order, the products by their *_phase calls; in calls
-        with few rows the shared expert's products share the launches of g1 and g2."""
+        with few rows the shared expert's products share the launches of g1 and g2.
+        rows: step 6 is left to the caller (moe_block_end_rows): y_perm, inv_perm, gate_w and s_y are what it adds up.  Not with
+        fold_combine, where the second product has done it."""
+        assert not (rows and self.fold_combine), "the second product makes y here"
         mark = None
         if stages is not None:
             stream = None
@@ -283,6 +303,8 @@ class MoELayer:
             self.shared_ffn(x, stream)
             if mark:
                 mark("shared")
+        if rows:
+            return self.y_perm
         self.combine(True, stream)
         if mark:
             mark("combine")
