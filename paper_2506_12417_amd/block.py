@@ -18,10 +18,11 @@ NAMES = ("pre_w", "pre_b", "post_w", "post_b", "gate", "next_w", "next_b")
 
 
 def prefers_few(layer: MoELayer) -> bool:
-    """Whether one call serves the layer's tokens best.  Up to 32 bf16 tokens it takes 0.97 to 1.4 times fewer microseconds than the separate
-    calls (one token of d=768 F=3072 21 us against 25; 32 tokens of d=2048 F=1408 E=60 k=4 168 against 171); with more, whole tiles of rows
-    are worth a plan (64 tokens 220 against 207).  In fp32 the matrix instruction bounds both, and the line is at 16 (5 tokens of d=320
-    F=1984 26 against 31, 32 tokens 49 against 44)."""
+    """Whether one call serves the layer's tokens better than the separate ones.  Up to 32 bf16 tokens (us, this call / those): d=768 F=3072 E=128
+    k=1 one token 21 / 25, 16 tokens 44 / 51; d=2048 F=1408 E=60 k=4 with a shared expert 8 tokens 99 / 110; d=4096 F=14336 E=8 k=2 3 tokens
+    249 / 290; but narrow layers, from 20 tokens on: d=320 F=512 E=24 k=4 32 tokens 28 / 26.  Beyond, whole tiles of rows are worth a plan
+    (64 tokens of the last 35 / 29, of d=4096 522 / 491).  In fp32 the matrix instruction bounds both, and the line is at 16 (5 tokens of
+    d=320 F=1984 E=16 k=2 26 / 31, 16 tokens 38 / 40, 64 tokens 68 / 49)."""
     return layer.few_ok and (layer.T <= 32 and layer.packed_router if layer.dt == B.MOE_BF16 else layer.T <= 16)
 
 

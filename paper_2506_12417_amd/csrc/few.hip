@@ -22,6 +22,7 @@
 // are turned into the matrix instruction's fragments in a piece of LDS of the wavefront's own (fragments straight from global memory touch 16
 // lines per quarter wavefront instead of 2, and the vector cache is then what a CU waits for).
 #include <climits>
+#include <type_traits>
 #include "common.h"
 #include "ffn_kernels.h"
 #include "gemm_util.h"
@@ -173,10 +174,13 @@ template <int WL, int M> __device__ __forceinline__ f32x4 dots_total(float (&acc
 // A wavefront's run of segments with G groups of 16 rows: acc[g] = weight rows (A) x rows of group g (B), D lines in flight.
 //   WL     weight loads of eight rows (1: rows 8 - 15 of the product mean nothing)
 //   M      > 0: at most M rows, by dots() (IN_LDS, fp32)
+//   CACHE  CACHE_NT for weights that are fetched once: streamed past what the caches hold they come 5 - 12 % faster (d=4096 F=14336 E=8
+//          k=2, 3 tokens 272 - 278 us against 244 - 256, d=2048 F=1408 E=60 k=4, 8 tokens 105 against 99); fetched for several ranges of
+//          tokens they are better off in the L2 (fp32 d=320 F=1984, 33 tokens 50 us against 53)
 //   next(Segment&)  the segment behind the present one, false if there is none of this kind;   done(Segment const&, acc)
 // The loads run on from one segment into the next: in the last D lines of one the next one's first are fetched; a segment takes its lines'
 // number rounded up to D.  The weights of a line go through one half of the turning place while the line before is multiplied.
-template <int TY, int WL, int G, int M, int D, int X, typename Next, typename Done>
+template <int TY, int WL, int G, int M, int D, int X, int CACHE, typename Next, typename Done>
 __device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned char* xl, Next next, Done done) {
     static_assert(D % 2 == 0, "the turning place's halves alternate");
     static_assert(M == 0 || (X == IN_LDS && TY == FP && G == 1), "");
@@ -188,7 +192,7 @@ __device__ __forceinline__ void stream(Segment seg, u32x4* turn, const unsigned 
         const bool in = l < from.l1;
         const int at = in ? l : 0;
 #pragma unroll
-        for (int i = 0; i < WL; ++i) a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(from.w, (int)(in ? from.w_at[i] : NOWHERE), at * 128, 0);
+        for (int i = 0; i < WL; ++i) a[u][i] = __builtin_amdgcn_raw_buffer_load_b128(from.w, (int)(in ? from.w_at[i] : NOWHERE), at * 128, CACHE);
         if constexpr (X != IN_LDS) {
 #pragma unroll
             for (int g = 0; g < G; ++g)
@@ -294,7 +298,7 @@ template <int TY, int X, int X_TALL> __device__ __forceinline__ int kind_of(int 
     return (m + 15) >> 4;
 }
 // Runs of segments one behind the other, whatever their rows.  current: false if there is none; few: there are few lines in all.
-template <int TY, int WL, int X, int X_TALL, typename Current, typename Next, typename Done>
+template <int TY, int WL, int X, int X_TALL, int CACHE, typename Current, typename Next, typename Done>
 __device__ __forceinline__ void stream_all(u32x4* turn, const unsigned char* xl, bool few, Current current, Next next, Done done) {
     Segment seg;
     constexpr int DEEP = X == IN_LDS ? (WL == 2 ? 10 : 16) : (WL == 2 ? 8 : 12);
@@ -303,20 +307,20 @@ __device__ __forceinline__ void stream_all(u32x4* turn, const unsigned char* xl,
         auto same = [&](Segment& s) __attribute__((always_inline)) { return next(s) && kind_of<TY, X, X_TALL>(s.m) == kind; };
         if constexpr (TY == FP && X == IN_LDS) {
             if (kind == -2) {
-                stream<TY, WL, 1, 2, DEEP, X>(seg, turn, xl, same, done);
+                stream<TY, WL, 1, 2, DEEP, X, CACHE>(seg, turn, xl, same, done);
                 continue;
             }
             if (kind == -8) {
-                stream<TY, WL, 1, 8, 8, X>(seg, turn, xl, same, done);
+                stream<TY, WL, 1, 8, 8, X, CACHE>(seg, turn, xl, same, done);
                 continue;
             }
         }
-        if (kind <= 1 && few) stream<TY, WL, 1, 0, 4, X>(seg, turn, xl, same, done);
-        else if (kind == 0) stream<TY, WL, 1, 0, DEEP, X>(seg, turn, xl, same, done);
-        else if (kind == 1) stream<TY, WL, 1, 0, DEEP, X_TALL>(seg, turn, xl, same, done);
-        else if (kind == 2) stream<TY, WL, 2, 0, 6, X_TALL>(seg, turn, xl, same, done);
-        else if (kind == 3) stream<TY, WL, 3, 0, 4, X_TALL>(seg, turn, xl, same, done);
-        else stream<TY, WL, 4, 0, X == IN_LDS ? 4 : 2, X_TALL>(seg, turn, xl, same, done);
+        if (kind <= 1 && few) stream<TY, WL, 1, 0, 4, X, CACHE>(seg, turn, xl, same, done);
+        else if (kind == 0) stream<TY, WL, 1, 0, DEEP, X, CACHE>(seg, turn, xl, same, done);
+        else if (kind == 1) stream<TY, WL, 1, 0, DEEP, X_TALL, CACHE>(seg, turn, xl, same, done);
+        else if (kind == 2) stream<TY, WL, 2, 0, 6, X_TALL, CACHE>(seg, turn, xl, same, done);
+        else if (kind == 3) stream<TY, WL, 3, 0, 4, X_TALL, CACHE>(seg, turn, xl, same, done);
+        else stream<TY, WL, 4, 0, X == IN_LDS ? 4 : 2, X_TALL, CACHE>(seg, turn, xl, same, done);
     }
 }
 // what a line of an expert with m rows costs a wavefront, in loads
@@ -871,7 +875,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
     }
     int tail_ai = 0, tail_q = 0, tail_lines = 0;         // tail_lines > 0: of an item whose rest is with the wavefronts behind
     if (lane == 0) head_lines[wave] = 0;
-    stream_all<TY, 2, H::LDS ? IN_LDS : FRAGMENTS, H::LDS ? IN_LDS : LINES>(
+    stream_all<TY, 2, H::LDS ? IN_LDS : FRAGMENTS, H::LDS ? IN_LDS : LINES, CACHE_NT>(
         turn, xl, hi - lo <= 16,
         [&](Segment& s) __attribute__((always_inline)) {
             while (segment(s, ai, q, base)) {
@@ -931,13 +935,13 @@ struct Out {
     const void* const *w_out, *const *s_w_out;
     const unsigned char *h, *s_h;
     void* y;
-    int T, d, E, k, F, shared_F, y_f32, splits, by_token, pairs;
+    int T, d, E, k, F, shared_F, y_f32, splits, pairs;
 };
 
 // WL: 1 for 8 columns of a work-group, 2 for 16.  LDS: the hidden activations (of its tokens) go there first.  splits > 1: that many
-// work-groups share a column block: a range of the tokens each (by_token), or, with one choice per token and no shared expert, the experts.
-// pairs (LDS): every assignment of the range for itself, so that a token's sums do not depend on what other tokens chose.
-template <bool F32, int WL, bool LDS>
+// work-groups share a column block: a range of the tokens each (RANGES), or, with one choice per token and no shared expert, the experts.
+// pairs (RANGES, LDS): every assignment of the range for itself, so that a token's sums do not depend on what other tokens chose.
+template <bool F32, int WL, bool LDS, bool RANGES>
 __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : HF, COLS = WL * 8;
     __shared__ __attribute__((aligned(16))) unsigned char smem[sizeof(u32x4) * 256 * NW];
@@ -949,7 +953,7 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     const int T = p.T, d = p.d, E = p.E, k = p.k, F = p.F, splits = p.splits;
     // (the work-groups of a column block on one XCD where the number of blocks is a multiple of eight)
     const int blocks = d / COLS, split = (int)blockIdx.x / blocks, p0 = ((int)blockIdx.x - split * blocks) * COLS;
-    const int t0 = p.by_token ? T * split / splits : 0, t1 = p.by_token ? T * (split + 1) / splits : T;
+    const int t0 = RANGES ? T * split / splits : 0, t1 = RANGES ? T * (split + 1) / splits : T;
     const unsigned long long range = (t1 < 64 ? (1ull << t1) : 0ull) - (1ull << t0);
     const unsigned f_bytes = (unsigned)F * ES, s_bytes = (unsigned)p.shared_F * ES, s_base = (unsigned)((t1 - t0) * k) * f_bytes;
     int e = -1;
@@ -964,13 +968,13 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         if (p.shared_F) rows_to_lds(p.s_h + (size_t)t0 * s_bytes, t1 - t0, s_bytes, hl + s_base);
     }
     if (tid < 2 * MAXE) (&l.bits[0][0])[tid] = 0u;
-    if (tid < T) state[tid] = splits == 1 || (p.by_token && tid >= t0 && tid < t1);
+    if (tid < T) state[tid] = RANGES ? tid >= t0 && tid < t1 : splits == 1;
     for (int i = lane; i < T * COLS; i += 64) (&sums[wave][0][0])[i] = 0.f;
     __syncthreads();
     if (tid < E) l.w[tid] = mine_w;
-    if (tid < T * k && (unsigned)e >= (unsigned)E && (p.by_token ? state[tid / k] : split == 0)) state[tid / k] = 2;
+    if (tid < T * k && (unsigned)e >= (unsigned)E && (RANGES ? state[tid / k] : split == 0)) state[tid / k] = 2;
     if constexpr (LDS) MOE_WAIT_VMCNT(0);
-    const bool pairs = LDS && p.pairs;
+    const bool pairs = RANGES && LDS && p.pairs;
     if (pairs) {
         const int i = tid - t0 * k, n = (t1 - t0) * k;
         if (i >= 0 && i < n) {
@@ -991,7 +995,7 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
     // The lines of the active experts' contractions, the shared expert's behind, by what they cost: a wavefront's share of that.
     const int L = F * ES / 128, s_L = p.shared_F * ES / 128, s_cost = line_cost(t1 - t0);
     int ai0 = 0, ai1 = n_active;         // the work-group's experts
-    if (splits > 1 && !p.by_token) {
+    if (!RANGES && splits > 1) {
         const int all = l.cost[n_active];
         int below = 0, upto = 0;
         for (int x = lane; x - lane < n_active; x += 64) {
@@ -1049,7 +1053,7 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         }
         return true;
     };
-    stream_all<TY, WL, LDS ? IN_LDS : FRAGMENTS, LDS ? IN_LDS : FRAGMENTS>(
+    stream_all<TY, WL, LDS ? IN_LDS : FRAGMENTS, LDS ? IN_LDS : FRAGMENTS, RANGES ? 0 : CACHE_NT>(
         turn, hl, hi - lo <= 16,
         [&](Segment& s) __attribute__((always_inline)) {
             while (segment(s, ai)) {
@@ -1074,7 +1078,7 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) sum[i] = fmaf(gate, acc[g][i], sum[i]);
                     *to = sum;
-                    if (splits > 1 && !p.by_token) state[t] = 1;
+                    if (!RANGES && splits > 1) state[t] = 1;
                 }
             }
             ++ai;
@@ -1144,13 +1148,14 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     const bool apart = k == 1 && !shared_F;
     const bool wide = (long long)(d / 16) * (apart ? T : 1) >= MOE_GEMM_GRID;
     const int blocks = d / (wide ? 16 : 8);
-    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1, !apart, 0};
+    Out o = {expert_idx, gate_w, w_out, s_w_out, a.h, a.s_h, y, T, d, E, k, F, shared_F, y_dt == MOE_F32, 1, 0};
     while (o.splits < T && blocks * (o.splits + 1) <= MOE_GEMM_GRID) ++o.splits;
     const int range = apart ? T : (T + o.splits - 1) / o.splits;
     // x and the work-group's hidden activations go to LDS first where they fit
     const bool x_lds = (size_t)T * d * es <= X_BYTES, h_lds = (size_t)range * (need / T) <= h_bytes(wide ? 2 : 1);
     a.h_rows = h_lds;
-    o.pairs = h_lds && !apart && o.splits > 1 && range <= 8;
+    const bool ranges = !apart && o.splits > 1;      // (then d <= 1024, and eight columns)
+    o.pairs = ranges && h_lds && range <= 8;
     if (dt == MOE_F32 || T > ROUTE_MAXT) {
         const int rc = dt == MOE_F32 ? moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream)
                                      : moe_route_topk_packed(x, w_gate, w_norm2, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
@@ -1164,10 +1169,13 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     }
     MOE_CHECK_LAUNCH("moe_layer_few (routing and first product)");
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)(blocks * o.splits)), dim3(NTH), 0, st, o); };
-    if (dt == MOE_F32 && h_lds) wide ? go(few_out_kernel<true, 2, true>) : go(few_out_kernel<true, 1, true>);
-    else if (dt == MOE_F32) wide ? go(few_out_kernel<true, 2, false>) : go(few_out_kernel<true, 1, false>);
-    else if (h_lds) wide ? go(few_out_kernel<false, 2, true>) : go(few_out_kernel<false, 1, true>);
-    else wide ? go(few_out_kernel<false, 2, false>) : go(few_out_kernel<false, 1, false>);
+    auto typed = [&](auto f32, auto lds) {
+        if (ranges) go(few_out_kernel<f32(), 1, lds(), true>);
+        else if (wide) go(few_out_kernel<f32(), 2, lds(), false>);
+        else go(few_out_kernel<f32(), 1, lds(), false>);
+    };
+    if (dt == MOE_F32) h_lds ? typed(std::true_type{}, std::true_type{}) : typed(std::true_type{}, std::false_type{});
+    else h_lds ? typed(std::false_type{}, std::true_type{}) : typed(std::false_type{}, std::false_type{});
     MOE_CHECK_LAUNCH("moe_layer_few (second product and combine)");
     return MOE_OK;
 }
