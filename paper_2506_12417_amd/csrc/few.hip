@@ -712,8 +712,25 @@ __device__ __forceinline__ void route_all(const Route& p, unsigned char* smem, c
     __syncthreads();
 }
 
-// ---- launch 1
 constexpr unsigned X_BYTES = 64 << 10;           // of LDS for x
+
+// The routing alone, ROUTE_EACH tokens a work-group.
+constexpr int ROUTE_EACH = 8;
+template <typename H> __global__ __launch_bounds__(NTH) void few_route_kernel(Route p) {
+    constexpr size_t PLACES = sizeof(u32x4) * NW * (H::EB + (H::LDS ? 0 : H::TT)) * 128, ROUTE = sizeof(RouteLds<H>);
+    __shared__ __attribute__((aligned(16))) unsigned char smem[PLACES > ROUTE ? PLACES : ROUTE];
+    __shared__ __attribute__((aligned(16))) unsigned char xl[H::LDS ? X_BYTES : 16];
+    __shared__ Lists l;
+    const int t0 = (int)blockIdx.x * ROUTE_EACH;
+    p.x += (size_t)t0 * p.d;
+    p.idx += t0 * p.k;
+    p.gate += t0 * p.k;
+    p.T = p.T - t0 < ROUTE_EACH ? p.T - t0 : ROUTE_EACH;
+    if constexpr (H::LDS) rows_to_lds(p.x, p.T, (unsigned)p.d * 2u, xl);
+    route_all<H>(p, smem, xl, l, true);
+}
+
+// ---- launch 1
 constexpr unsigned h_bytes(int WL) { return WL == 2 ? 80u << 10 : 93u << 10; }     // and for the hidden activations in launch 2
 struct Hidden {
     Route route;
@@ -1156,12 +1173,16 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     a.h_rows = h_lds;
     const bool ranges = !apart && o.splits > 1;      // (then d <= 1024, and eight columns)
     o.pairs = ranges && h_lds && range <= 8;
-    if (dt == MOE_F32 || T > ROUTE_MAXT) {
-        const int rc = dt == MOE_F32 ? moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream)
-                                     : moe_route_topk_packed(x, w_gate, w_norm2, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
+    if (dt == MOE_F32) {
+        const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
         if (rc != MOE_OK) return rc;
-        if (dt == MOE_F32) x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
-        else x_lds ? launch_hidden<false, Routed<true>>(a, st) : launch_hidden<false, Routed<false>>(a, st);
+        x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
+    } else if (T > ROUTE_MAXT) {
+        const dim3 grid((unsigned)((T + ROUTE_EACH - 1) / ROUTE_EACH));
+        if ((size_t)ROUTE_EACH * d * es <= X_BYTES) hipLaunchKernelGGL((few_route_kernel<How<1, true>>), grid, dim3(NTH), 0, st, a.route);
+        else hipLaunchKernelGGL((few_route_kernel<How<1, false>>), grid, dim3(NTH), 0, st, a.route);
+        MOE_CHECK_LAUNCH("moe_layer_few (routing)");
+        x_lds ? launch_hidden<false, Routed<true>>(a, st) : launch_hidden<false, Routed<false>>(a, st);
     } else if (T <= 16) {
         x_lds ? launch_hidden<false, How<1, true>>(a, st) : launch_hidden<false, How<1, false>>(a, st);
     } else {
