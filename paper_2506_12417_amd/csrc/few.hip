@@ -1,4 +1,4 @@
-// moe_layer_few: a whole MoE layer for a few tokens (T <= 64) in two launches (three: fp32, and more than 32 tokens).
+// moe_layer_few: a whole MoE layer for a few tokens (T <= 64) in two launches (three: fp32, more than 32 tokens, and a large shared expert).
 //
 //   launch 1   routing, then   H[r,:] = act(x[token of r] . W_in^T)            for every row r = (expert, token)
 //   launch 2   y[t,:] = sum_j gate[t,j] H[row of (t,j)] . W_out^T  (+ shared expert)
@@ -714,23 +714,8 @@ __device__ __forceinline__ void route_all(const Route& p, unsigned char* smem, c
 
 constexpr unsigned X_BYTES = 64 << 10;           // of LDS for x
 
-// The routing alone, ROUTE_EACH tokens a work-group.
-constexpr int ROUTE_EACH = 8;
-template <typename H> __global__ __launch_bounds__(NTH) void few_route_kernel(Route p) {
-    constexpr size_t PLACES = sizeof(u32x4) * NW * (H::EB + (H::LDS ? 0 : H::TT)) * 128, ROUTE = sizeof(RouteLds<H>);
-    __shared__ __attribute__((aligned(16))) unsigned char smem[PLACES > ROUTE ? PLACES : ROUTE];
-    __shared__ __attribute__((aligned(16))) unsigned char xl[H::LDS ? X_BYTES : 16];
-    __shared__ Lists l;
-    const int t0 = (int)blockIdx.x * ROUTE_EACH;
-    p.x += (size_t)t0 * p.d;
-    p.idx += t0 * p.k;
-    p.gate += t0 * p.k;
-    p.T = p.T - t0 < ROUTE_EACH ? p.T - t0 : ROUTE_EACH;
-    if constexpr (H::LDS) rows_to_lds(p.x, p.T, (unsigned)p.d * 2u, xl);
-    route_all<H>(p, smem, xl, l, true);
-}
-
 // ---- launch 1
+constexpr int ROUTE_EACH = 8;
 constexpr unsigned h_bytes(int WL) { return WL == 2 ? 80u << 10 : 93u << 10; }     // and for the hidden activations in launch 2
 struct Hidden {
     Route route;
@@ -738,23 +723,44 @@ struct Hidden {
     const void* const *w_in, *const *s_w_in;
     unsigned char *h, *s_h;              // hidden activations of the rows (A of F) and of the shared expert (T of shared_F)
     int F, shared_F, glu, h_rows;        // h_rows: H in rows, else an expert's rows piece by piece (see finish)
+    int route_blocks;                    // R: so many work-groups route
 };
 __device__ __forceinline__ uint16_t half_of(float v) {           // saturating, nearest-even
     return __builtin_bit_cast(uint16_t, (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f));
 }
 
-template <bool F32, typename H>
+// H: how the tokens are routed first, by every work-group; or not at all (Routed).  R (a How; with Routed): a launch of its own for the
+// routing, ROUTE_EACH tokens a work-group, and beside it the shared expert's first product, by the other work-groups.
+template <bool F32, typename H, typename R>
 __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
+    constexpr bool FIRST = !std::is_void<R>::value;
+    typedef typename std::conditional<FIRST, R, H>::type Router;
     constexpr int ES = F32 ? 4 : 2, TY = F32 ? FP : BF;
-    constexpr size_t PLACE = H::LDS ? 256 : 384, PLACES = sizeof(u32x4) * (PLACE + 256) * NW, ROUTE = sizeof(RouteLds<H>);
-    __shared__ __attribute__((aligned(16))) unsigned char smem[PLACES > ROUTE ? PLACES : ROUTE];
-    static_assert(sizeof smem >= sizeof(u32x4) * NW * (H::EB + (H::LDS ? 0 : H::TT)) * 128, "the routing's turning places");
-    __shared__ __attribute__((aligned(16))) unsigned char xl[H::LDS ? X_BYTES : 16];
+    constexpr size_t PLACE = H::LDS ? 256 : 384, PLACES = sizeof(u32x4) * (PLACE + 256) * NW, ROUTE = sizeof(RouteLds<Router>);
+    constexpr size_t TURN = sizeof(u32x4) * NW * (Router::EB + (Router::LDS ? 0 : Router::TT)) * 128, SMEM = PLACES > ROUTE ? PLACES : ROUTE;
+    __shared__ __attribute__((aligned(16))) unsigned char smem[SMEM > TURN ? SMEM : TURN];
+    __shared__ __attribute__((aligned(16))) unsigned char xl[H::LDS || Router::LDS ? X_BYTES : 16];
     __shared__ Lists l;
     __shared__ int head_lines[NW];
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6), l16 = lane & 15, lq = lane >> 4;
     const int T = p.route.T, d = p.route.d, E = p.route.E, k = p.route.k;
     const unsigned row_bytes = (unsigned)d * ES;
+    int grid = (int)gridDim.x, block = (int)blockIdx.x;
+    if constexpr (FIRST) {
+        if (block < p.route_blocks) {
+            Route r = p.route;
+            const int t0 = block * ROUTE_EACH;
+            r.x += (size_t)t0 * d;
+            r.idx += t0 * k;
+            r.gate += t0 * k;
+            r.T = T - t0 < ROUTE_EACH ? T - t0 : ROUTE_EACH;
+            if constexpr (R::LDS) rows_to_lds(r.x, r.T, row_bytes, xl);
+            route_all<R>(r, smem, xl, l, true);
+            return;
+        }
+        grid -= p.route_blocks;
+        block -= p.route_blocks;
+    }
     if constexpr (H::LDS) rows_to_lds(p.x, T, row_bytes, xl);
     const void* const mine_w = tid < E ? p.w_in[tid] : nullptr;
     if (tid < 2 * MAXE) (&l.bits[0][0])[tid] = 0u;
@@ -763,7 +769,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
         route_all<H>(p.route, smem, xl, l, blockIdx.x == 0);
         if (tid < T * k) e = l.id[tid];
     } else {
-        if (tid < T * k) e = p.route.idx[tid];
+        if (!FIRST && tid < T * k) e = p.route.idx[tid];
         if constexpr (H::LDS) MOE_WAIT_VMCNT(0);
         __syncthreads();
     }
@@ -772,7 +778,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
     u32x4* const turn = (u32x4*)smem + wave * PLACE;
     f32x4* const heads = (f32x4*)((u32x4*)smem + NW * PLACE);            // [wavefront][group][lane]
     const __amdgpu_buffer_rsrc_t x = make_rsrc(p.x, (unsigned)T * row_bytes);
-    const int lines = d * ES / 128, grid = (int)gridDim.x, block = (int)blockIdx.x;
+    const int lines = d * ES / 128;
     // Items of 16 weight rows: the shared expert's first, then the active experts'.  The work-group has every grid-th of them, and its
     // wavefronts equal shares of their lines by what these cost: whole items, and an item's head or tail at either end.
     const int s_items = p.shared_F / 8, per = p.F / (p.glu ? 8 : 16), n_active = sgpr(l.n_active), items = s_items + n_active * per;
@@ -1114,8 +1120,8 @@ __global__ __launch_bounds__(NTH) void few_out_kernel(Out p) {
         }
     }
 }
-template <bool F32, typename H> void launch_hidden(const Hidden& a, hipStream_t st) {
-    hipLaunchKernelGGL((few_hidden_kernel<F32, H>), dim3(MOE_GEMM_GRID), dim3(NTH), 0, st, a);
+template <bool F32, typename H, typename R = void> void launch_hidden(const Hidden& a, hipStream_t st, int grid = MOE_GEMM_GRID) {
+    hipLaunchKernelGGL((few_hidden_kernel<F32, H, R>), dim3((unsigned)grid), dim3(NTH), 0, st, a);
 }
 
 bool aligned(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -1173,15 +1179,22 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     a.h_rows = h_lds;
     const bool ranges = !apart && o.splits > 1;      // (then d <= 1024, and eight columns)
     o.pairs = ranges && h_lds && range <= 8;
+    // A shared expert whose first matrices take as long to fetch as a launch (16 MB, three microseconds) is worked on while a few work-groups
+    // route: d=2048 F=1408 E=60 k=4 shared 5632 (46 MB), us without / with: 1 token 42.9 / 39.7, 9 tokens 106 / 101, 16 tokens 134 / 133, 24
+    // tokens 149 / 153 (the routing's loads wait behind the others); d=1152 shared 1600 (7 MB), 4 tokens 29.9 / 31.0.
+    const bool beside = T <= 16 && (size_t)shared_F * 2 * d * es >= (16u << 20);
     if (dt == MOE_F32) {
         const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);
         if (rc != MOE_OK) return rc;
         x_lds ? launch_hidden<true, Routed<true>>(a, st) : launch_hidden<true, Routed<false>>(a, st);
-    } else if (T > ROUTE_MAXT) {
-        const dim3 grid((unsigned)((T + ROUTE_EACH - 1) / ROUTE_EACH));
-        if ((size_t)ROUTE_EACH * d * es <= X_BYTES) hipLaunchKernelGGL((few_route_kernel<How<1, true>>), grid, dim3(NTH), 0, st, a.route);
-        else hipLaunchKernelGGL((few_route_kernel<How<1, false>>), grid, dim3(NTH), 0, st, a.route);
+    } else if (T > ROUTE_MAXT || beside) {
+        a.route_blocks = (T + ROUTE_EACH - 1) / ROUTE_EACH;
+        const int grid = beside ? MOE_GEMM_GRID : a.route_blocks;
+        if (x_lds) launch_hidden<false, Routed<true>, How<1, true>>(a, st, grid);
+        else if ((size_t)(T < ROUTE_EACH ? T : ROUTE_EACH) * d * es <= X_BYTES) launch_hidden<false, Routed<false>, How<1, true>>(a, st, grid);
+        else launch_hidden<false, Routed<false>, How<1, false>>(a, st, grid);
         MOE_CHECK_LAUNCH("moe_layer_few (routing)");
+        if (beside) a.shared_F = 0;      // (its first product is done)
         x_lds ? launch_hidden<false, Routed<true>>(a, st) : launch_hidden<false, Routed<false>>(a, st);
     } else if (T <= 16) {
         x_lds ? launch_hidden<false, How<1, true>>(a, st) : launch_hidden<false, How<1, false>>(a, st);

@@ -160,6 +160,14 @@ def test_narrow_layers(T, d, F, E, k, shared_F, dt):
     check(Case(T, d, F, E, k, "swiglu" if T % 2 else "relu", dt, shared_F=shared_F, renorm=T % 2))
 
 
+@pytest.mark.parametrize("T,d,F,E,k,shared_F", [(1, 2048, 64, 5, 2, 2048), (9, 2048, 128, 20, 3, 2112), (16, 2048, 64, 7, 1, 2048), (16, 8192, 64, 4, 2, 512),
+                                                (3, 8192, 64, 4, 2, 576), (33, 8192, 64, 4, 2, 0), (40, 4096, 64, 3, 1, 64)])
+def test_large_shared_experts_and_wide_tokens(T, d, F, E, k, shared_F):
+    """The shared expert's first product beside the routing, eight tokens a work-group there; tokens that do not fit LDS."""
+    print("[case] few beside T=%d d=%d F=%d E=%d k=%d shared=%d" % (T, d, F, E, k, shared_F), flush=True)
+    check(Case(T, d, F, E, k, "swiglu", "bf16", shared_F=shared_F, renorm=1), y_dts=(0,))
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("T,shared_F", [(9, 0), (40, 64), (64, 0)])
 def test_tokens_that_are_no_numbers_in_narrow_layers(T, shared_F, dt):
