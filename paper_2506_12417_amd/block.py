@@ -57,11 +57,11 @@ class MoEBlock:
     def load(self, **arrays: np.ndarray):
         """Parameters by name (NAMES), fp32: [d], and the gate [d] or [T,d].  What is not loaded counts as ones (weights) or zeros."""
         for name, a in arrays.items():
-            assert name in NAMES and np.shape(a) in (((self.d,), (1, self.d)) if name != "gate" or self.gate_rows < 2 else ((self.T, self.d),)), name
+            rows = self.gate_rows if name == "gate" else 1
+            assert name in NAMES and rows and np.shape(a) in (((self.d,), (1, self.d)) if rows == 1 else ((rows, self.d),)), name
             self.param[name] = to_device(np.asarray(a, dtype=np.float32).reshape(-1, self.d), self.layer.device)
             if self.train:
                 self.grad["d" + name] = torch.empty_like(self.param[name])
-        assert self.gate_rows == 0 or "gate" not in arrays or self.param["gate"].shape[0] == self.gate_rows
 
     def _end(self) -> Tuple:
         p = self.param

@@ -22,12 +22,14 @@
 // stream's gradient (268 MB, 5.5); 8192 x 4096, both norms, 61 forward (268 MB, 4.4) and 91 + 6 backward (402 MB, 4.4); the rows form,
 // 8192 x 2048 with four experts' rows and a shared one each, 89 (438 MB, 4.9); 1501 x 777 fp32 4.4, 7.5 + 3.6; 33 x 2048 3 - 4.
 #include "common.h"
+#include "gemm_util.h"
 #include <type_traits>
 
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned int u32x2;
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 
@@ -39,25 +41,28 @@ static_assert(MAXT_LONG * V == MOE_NORM_MAX_D && MAXT * V == MOE_NORM_ANY_D, "")
 enum { SRC_NONE = 0, SRC_TENSOR = 1, SRC_ROWS = 2 };
 
 // ---- a thread's values of a row: neighbours (VEC, one or two 16-byte pieces) where rows are whole 16-byte pieces, else
-// one of every blockDim.x
-template <bool VEC> __device__ __forceinline__ int column(int i) { return VEC ? (int)threadIdx.x * V + i : i * (int)blockDim.x + (int)threadIdx.x; }
+// every 64th of its wavefront's
+template <bool VEC> __device__ __forceinline__ int column(int i) {
+    return VEC ? (int)threadIdx.x * V + i : ((int)threadIdx.x & ~63) * V + i * 64 + ((int)threadIdx.x & 63);
+}
 
+// All goes through buffer loads and stores: what lies past the row's d values, or in a row that is not there (`on` false), reads as zero or
+// is not written, without a branch; behind branches with loads in them the compiler waits for all that is under way, the next row's
+// loads included (8192 x 4096, both norms: 61 forward + 91 us backward, against 50 + 76).
 template <typename E, bool VEC> struct Held;
 template <> struct Held<float, true> {
     f32x4 a, b;
-    __device__ __forceinline__ void fetch(const float* row, int d) {
-        const int c = column<true>(0);
-        a = b = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (c < d) { a = *(const f32x4*)(row + c); b = *(const f32x4*)(row + c + 4); }
+    __device__ __forceinline__ void fetch(const float* row, int d, bool on) {
+        const __amdgpu_buffer_rsrc_t r = make_rsrc(row, on ? (unsigned)d * 4u : 0u);
+        a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, column<true>(0) * 4, 0, 0));
+        b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(r, column<true>(4) * 4, 0, 0));
     }
     __device__ __forceinline__ float at(int i) const { return i < 4 ? a[i & 3] : b[i & 3]; }
 };
 template <> struct Held<uint16_t, true> {
     u32x4 a;
-    __device__ __forceinline__ void fetch(const uint16_t* row, int d) {
-        const int c = column<true>(0);
-        a = u32x4{0u, 0u, 0u, 0u};
-        if (c < d) a = *(const u32x4*)(row + c);
+    __device__ __forceinline__ void fetch(const uint16_t* row, int d, bool on) {
+        a = __builtin_amdgcn_raw_buffer_load_b128(make_rsrc(row, on ? (unsigned)d * 2u : 0u), column<true>(0) * 2, 0, 0);
     }
     __device__ __forceinline__ float at(int i) const {
         const unsigned w = a[i >> 1];
@@ -66,42 +71,44 @@ template <> struct Held<uint16_t, true> {
 };
 template <typename E> struct Held<E, false> {
     E a[V];
-    __device__ __forceinline__ void fetch(const E* row, int d) {
+    __device__ __forceinline__ void fetch(const E* row, int d, bool on) {
+        const __amdgpu_buffer_rsrc_t r = make_rsrc(row, on ? (unsigned)d * (unsigned)sizeof(E) : 0u);
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            a[i] = 0;
-            if (column<false>(i) < d) a[i] = row[column<false>(i)];
+            if constexpr (sizeof(E) == 4) a[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, column<false>(i) * 4, 0, 0));
+            else a[i] = __builtin_amdgcn_raw_buffer_load_b16(r, column<false>(i) * 2, 0, 0);
         }
     }
     __device__ __forceinline__ float at(int i) const { return load_as_f32(&a[i]); }
 };
 
-template <bool VEC> __device__ __forceinline__ void store(float* row, int d, const float (&x)[V]) {
+template <bool VEC> __device__ __forceinline__ void store(float* row, int d, const float (&x)[V], bool on) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(row, on ? (unsigned)d * 4u : 0u);
     if constexpr (VEC) {
-        if (column<true>(0) < d) {
-            *(f32x4*)(row + column<true>(0)) = f32x4{x[0], x[1], x[2], x[3]};
-            *(f32x4*)(row + column<true>(4)) = f32x4{x[4], x[5], x[6], x[7]};
-        }
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x[0], x[1], x[2], x[3]}), r, column<true>(0) * 4, 0, 0);
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, f32x4{x[4], x[5], x[6], x[7]}), r, column<true>(4) * 4, 0, 0);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (column<false>(i) < d) row[column<false>(i)] = x[i];
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[i]), r, column<false>(i) * 4, 0, 0);
     }
 }
-template <bool VEC> __device__ __forceinline__ void store(uint16_t* row, int d, const float (&x)[V]) {
+template <bool VEC> __device__ __forceinline__ void store(uint16_t* row, int d, const float (&x)[V], bool on) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(row, on ? (unsigned)d * 2u : 0u);
     if constexpr (VEC) {
         const f32x8 f = {x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]};
-        if (column<true>(0) < d) *(bf16x8*)(row + column<true>(0)) = __builtin_convertvector(f, bf16x8);   // to nearest, ties to even
+        const bf16x8 to = __builtin_convertvector(f, bf16x8);    // to nearest, ties to even
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, to), r, column<true>(0) * 2, 0, 0);
     } else {
 #pragma unroll
         for (int i = 0; i < V; ++i)
-            if (column<false>(i) < d) row[column<false>(i)] = __builtin_bit_cast(uint16_t, (__bf16)x[i]);
+            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, (__bf16)x[i]), r, column<false>(i) * 2, 0, 0);
     }
 }
 // a parameter's columns; `none` where there is no such parameter
 template <bool VEC> __device__ __forceinline__ void params(const float* p, int d, float none, float (&to)[V]) {
     Held<float, VEC> t;
-    if (p) t.fetch(p, d);
+    t.fetch(p, d, p != nullptr);
 #pragma unroll
     for (int i = 0; i < V; ++i) to[i] = p ? t.at(i) : none;
 }
@@ -123,17 +130,21 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 struct RowSum {
     float (*red)[2][MAXW];               // [buffer][value][wavefront]
-    int turn;
+    int waves, turn;
     __device__ __forceinline__ void operator()(float& a, float& b, bool both) {
         a = wave_sum(a);
         if (both) b = wave_sum(b);
-        if (blockDim.x > 64) {
-            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, n = blockDim.x >> 6;
+        if (waves > 1) {
+            const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
             if (lane == 0) { red[turn][0][wave] = a; red[turn][1][wave] = b; }
             __syncthreads();
             const int at = lane & 15;
-            a = lanes16_sum(at < n ? red[turn][0][at] : 0.f);
-            if (both) b = lanes16_sum(at < n ? red[turn][1][at] : 0.f);
+            a = red[turn][0][at];        // (past the wavefronts: whatever is there)
+            a = lanes16_sum(at < waves ? a : 0.f);
+            if (both) {
+                b = red[turn][1][at];
+                b = lanes16_sum(at < waves ? b : 0.f);
+            }
             turn ^= 1;
         }
     }
@@ -167,6 +178,7 @@ struct Args {
     const void* h;                       // [T,d]
     const float *post_w, *post_b, *gate, *next_w, *next_b;
     int T, d, post_kind, next_kind, gate_rows, k;
+    int waves, step;                     // of a row; rows in work at a time
     float post_eps, next_eps, alpha, inv_d;
     const int32_t* inv_perm;             // experts' rows only, as gate_w and shared
     const float *gate_w, *shared;
@@ -182,7 +194,7 @@ __device__ __forceinline__ void combine_row(const Args& p, int t, float (&x)[V])
 #pragma unroll
     for (int i = 0; i < V; ++i) x[i] = 0.f;
     Held<float, VEC> s;
-    if (p.shared) s.fetch(p.shared + (size_t)t * p.d, p.d);
+    s.fetch(p.shared + (size_t)t * p.d, p.d, p.shared != nullptr);
     for (int j0 = 0; j0 < p.k; j0 += G) {
         Held<float, VEC> r[G];
         float w[G];
@@ -192,7 +204,7 @@ __device__ __forceinline__ void combine_row(const Args& p, int t, float (&x)[V])
             const int jj = j0 + j < p.k ? j0 + j : p.k - 1;
             w[j] = p.gate_w ? p.gate_w[a0 + jj] : 1.f;
             at[j] = p.inv_perm[a0 + jj];
-            r[j].fetch(rows + (size_t)(at[j] < 0 ? 0 : at[j]) * p.d, p.d);
+            r[j].fetch(rows + (size_t)(at[j] < 0 ? 0 : at[j]) * p.d, p.d, true);
         }
 #pragma unroll
         for (int j = 0; j < G; ++j)
@@ -215,8 +227,8 @@ template <typename VT, typename HT, typename UT, bool VEC, int SRC, int G, bool 
 __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
     constexpr bool KEEP = !LONG;
     __shared__ float red[2][2][MAXW];
-    RowSum sum = {red, 0};
-    const int d = p.d, step = (int)(gridDim.x * blockDim.y);
+    RowSum sum = {red, p.waves, 0};
+    const int d = p.d, step = p.step;
     float pw[V], pb[V], gate[V], nw[V], nb[V];
     auto post_params = [&]() __attribute__((always_inline)) {
         params<VEC>(SRC == SRC_NONE ? nullptr : p.post_w, d, 1.f, pw);
@@ -229,14 +241,25 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         params<VEC>(p.next_w, d, 1.f, nw);
         params<VEC>(p.next_b, d, 0.f, nb);
     };
+    const bool own = SRC != SRC_NONE && p.gate_rows > 1;
     Held<VT, VEC> v_next;
     Held<HT, VEC> h_next;
+    Held<float, VEC> gate_next;
     auto fetch = [&](int t) __attribute__((always_inline)) {
-        if constexpr (SRC == SRC_TENSOR) v_next.fetch((const VT*)p.v + (size_t)t * d, d);
-        h_next.fetch((const HT*)p.h + (size_t)t * d, d);
+        const bool on = t < p.T;
+        const size_t at = (size_t)t * d;
+        if constexpr (SRC == SRC_TENSOR) v_next.fetch((const VT*)p.v + at, d, on);
+        h_next.fetch((const HT*)p.h + at, d, on);
+        if constexpr (SRC != SRC_NONE) gate_next.fetch(p.gate + at, d, on && own);
     };
-    int t = (int)(blockIdx.x * blockDim.y + threadIdx.y);        // (a wavefront for itself, or one row for all)
-    if (KEEP && t < p.T) fetch(t);
+    // a row's mean and factor, by one thread
+    auto keep = [&](int t, int which, float m, float r) __attribute__((always_inline)) {
+        constexpr int S = SRC == SRC_NONE ? 2 : 4;
+        const __amdgpu_buffer_rsrc_t to = make_rsrc(p.stats + (size_t)t * S, p.stats ? S * 4u : 0u);
+        __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(r)}, to, threadIdx.x == 0 ? which * 8 : S * 4, 0, 0);
+    };
+    int t = sgpr((int)(blockIdx.x * blockDim.y + threadIdx.y));  // (a wavefront for itself, or one row for all)
+    if (KEEP) fetch(t);
     if (KEEP) { post_params(); gate_params(); next_params(); }
     for (; t < p.T; t += step) {
         if (!KEEP) fetch(t);
@@ -245,11 +268,9 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         const size_t at = (size_t)t * d;
         float y[V];
         float m = 0.f, r = 0.f;
-        Held<float, VEC> own_gate;
-        const bool own = SRC != SRC_NONE && p.gate_rows > 1;
-        if (own) own_gate.fetch(p.gate + at, d);
+        const Held<float, VEC> own_gate = gate_next;
         if constexpr (SRC == SRC_ROWS) combine_row<G, VEC>(p, t, y);
-        if (KEEP && t + step < p.T) fetch(t + step);
+        if (KEEP) fetch(t + step);
         if constexpr (SRC == SRC_NONE) {
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = h.at(i);
@@ -264,7 +285,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = fmaf(y[i], pw[i], pb[i]);
             }
-            if (p.stats && threadIdx.x == 0) { p.stats[(size_t)t * 4] = m; p.stats[(size_t)t * 4 + 1] = r; }
+            if constexpr (SRC == SRC_TENSOR) keep(t, 0, m, r);
             if (!KEEP) gate_params();
             if (own) {
 #pragma unroll
@@ -272,16 +293,15 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = fmaf(p.alpha, h.at(i), gate[i] * y[i]);       // (past d: v, h and post_b are zero)
-            store<VEC>((HT*)p.y + at, d, y);
+            store<VEC>((HT*)p.y + at, d, y, true);
         }
         if (p.next_kind != MOE_NORM_NONE) {
             normalise<VEC>(y, p.next_kind, p.next_eps, d, p.inv_d, sum, m, r);
-            constexpr int S = SRC == SRC_NONE ? 2 : 4;
-            if (p.stats && threadIdx.x == 0) { p.stats[(size_t)t * S + S - 2] = m; p.stats[(size_t)t * S + S - 1] = r; }
+            if constexpr (SRC != SRC_ROWS) keep(t, SRC == SRC_NONE ? 0 : 1, m, r);
             if (!KEEP) next_params();
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = fmaf(y[i], nw[i], nb[i]);
-            store<VEC>((UT*)p.u + at, d, y);
+            store<VEC>((UT*)p.u + at, d, y, true);
         }
     }
 }
@@ -342,8 +362,10 @@ template <typename VT, typename HT, typename UT, bool VEC, bool HAS_V, bool LONG
 __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args p, Grads q) {
     constexpr bool KEEP = !LONG;
     __shared__ float red[2][2][MAXW];
-    RowSum sum = {red, 0};
-    const int d = p.d, step = (int)(gridDim.x * blockDim.y), first = (int)(blockIdx.x * blockDim.y + threadIdx.y);
+    RowSum sum = {red, p.waves, 0};
+    const int d = p.d, step = p.step, first = sgpr((int)(blockIdx.x * blockDim.y + threadIdx.y));
+    constexpr int S = HAS_V ? 4 : 2;
+    const bool own = HAS_V && p.gate_rows > 1;
     float pw[V], pb[V], gate[V], nw[V];
     auto post_params = [&]() __attribute__((always_inline)) {
         params<VEC>(HAS_V ? p.post_w : nullptr, d, 1.f, pw);
@@ -356,14 +378,25 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
     Held<VT, VEC> v_next;
     Held<HT, VEC> h_next, dy_next;
     Held<UT, VEC> du_next;
+    Held<float, VEC> gate_next;
+    u32x4 st_next = {};
     auto fetch = [&](int t) __attribute__((always_inline)) {
+        const bool on = t < p.T;
         const size_t at = (size_t)t * d;
-        if constexpr (HAS_V) v_next.fetch((const VT*)p.v + at, d);
-        h_next.fetch((const HT*)p.h + at, d);
-        if (q.dy) dy_next.fetch((const HT*)q.dy + at, d);
-        if (q.du) du_next.fetch((const UT*)q.du + at, d);
+        const __amdgpu_buffer_rsrc_t stats = make_rsrc(p.stats + (size_t)t * S, on ? S * 4u : 0u);
+        if constexpr (HAS_V) {
+            st_next = __builtin_amdgcn_raw_buffer_load_b128(stats, 0, 0, 0);
+        } else {
+            const u32x2 two = __builtin_amdgcn_raw_buffer_load_b64(stats, 0, 0, 0);
+            st_next = u32x4{two[0], two[1], 0u, 0u};
+        }
+        if constexpr (HAS_V) v_next.fetch((const VT*)p.v + at, d, on);
+        h_next.fetch((const HT*)p.h + at, d, on);
+        dy_next.fetch((const HT*)q.dy + at, d, on && q.dy);
+        du_next.fetch((const UT*)q.du + at, d, on && q.du);
+        if constexpr (HAS_V) gate_next.fetch(p.gate + at, d, on && own);
     };
-    if (KEEP && first < p.T) fetch(first);
+    if (KEEP) fetch(first);
     if (KEEP) { post_params(); gate_params(); next_params(); }
     for (int t = first; t < p.T; t += step) {
         if (!KEEP) { fetch(t); post_params(); gate_params(); }
@@ -371,20 +404,18 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         const Held<HT, VEC> h = h_next, dy = dy_next;
         const Held<UT, VEC> du = du_next;
         const size_t at = (size_t)t * d;
-        constexpr int S = HAS_V ? 4 : 2;
+        const Held<float, VEC> own_gate = gate_next;
         float st[S];
 #pragma unroll
-        for (int i = 0; i < S; ++i) st[i] = p.stats[(size_t)t * S + i];
-        Held<float, VEC> own_gate;
-        if (HAS_V && p.gate_rows > 1) own_gate.fetch(p.gate + at, d);
-        if (KEEP && t + step < p.T) fetch(t + step);
+        for (int i = 0; i < S; ++i) st[i] = __uint_as_float(st_next[i]);
+        if (KEEP) fetch(t + step);
         float vn[V], y[V], gy[V];
         const bool next_layer = p.next_kind == MOE_NORM_LAYER, post_layer = p.post_kind == MOE_NORM_LAYER;
         // (Past d everything is zero, but for what LAYER subtracts the mean from.)
 #pragma unroll
         for (int i = 0; i < V; ++i) y[i] = h.at(i);
         if constexpr (HAS_V) {
-            if (p.gate_rows > 1) {
+            if (own) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
             }
@@ -436,27 +467,25 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
 #pragma unroll
             for (int i = 0; i < V; ++i) gy[i] = fmaf(st[S - 1], fmaf(-y[i], a, gn[i]), gy[i]);
         }
-        if (q.dh) {
-            float out[V];
+        float out[V];
 #pragma unroll
-            for (int i = 0; i < V; ++i) out[i] = HAS_V ? p.alpha * gy[i] : gy[i];
-            store<VEC>((HT*)q.dh + at, d, out);
-        }
+        for (int i = 0; i < V; ++i) out[i] = HAS_V ? p.alpha * gy[i] : gy[i];
+        store<VEC>((HT*)q.dh + at, d, out, q.dh != nullptr);
         if constexpr (HAS_V) {
             float a = 0.f, b = 0.f;
             if (!KEEP) { post_params(); gate_params(); }
-            if (!KEEP && p.gate_rows > 1) {
-                own_gate.fetch(p.gate + at, d);
+            if (!KEEP && own) {
+                Held<float, VEC> again;
+                again.fetch(p.gate + at, d, true);
 #pragma unroll
-                for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
+                for (int i = 0; i < V; ++i) gate[i] = again.at(i);
             }
             if (q.slot[D_GATE] >= 0)
                 acc.template add<D_GATE>([&](int i, float s) __attribute__((always_inline)) { return fmaf(gy[i], fmaf(vn[i], pw[i], pb[i]), s); });
             if (q.dgate) {
-                float out[V];
 #pragma unroll
                 for (int i = 0; i < V; ++i) out[i] = gy[i] * fmaf(vn[i], pw[i], pb[i]);
-                store<VEC>(q.dgate + at, d, out);
+                store<VEC>(q.dgate + at, d, out, true);
             }
 #pragma unroll
             for (int i = 0; i < V; ++i) gy[i] *= gate[i];        // dp
@@ -482,7 +511,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
 #pragma unroll
                 for (int i = 0; i < V; ++i) gy[i] = st[1] * fmaf(-vn[i], a, gy[i]);
             }
-            if (q.dv) store<VEC>((VT*)q.dv + at, d, gy);
+            store<VEC>((VT*)q.dv + at, d, gy, q.dv != nullptr);
         }
     }
     auto put = [&](auto which) __attribute__((always_inline)) {
@@ -490,7 +519,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         if (q.slot[W] < 0) return;
         float s[V];
         acc.template add<W>([&](int i, float v) __attribute__((always_inline)) { return s[i] = v; });
-        store<VEC>(q.part + ((size_t)first * q.slots + q.slot[W]) * d, d, s);
+        store<VEC>(q.part + ((size_t)first * q.slots + q.slot[W]) * d, d, s, true);
     };
     put(std::integral_constant<int, D_NEXT_W>{});
     put(std::integral_constant<int, D_NEXT_B>{});
@@ -554,10 +583,12 @@ template <typename F> void by_type(int dt, F f) {
 }
 
 template <int SRC, int G>
-int launch_forward(const char* who, const Args& a, int v_dt, int h_dt, int u_dt, bool vec, hipStream_t st) {
+int launch_forward(const char* who, Args a, int v_dt, int h_dt, int u_dt, bool vec, hipStream_t st) {
     MOE_REQUIRE(vec || a.d <= MOE_NORM_ANY_D, MOE_ERR_UNSUPPORTED, "%s: d=%d beyond %d needs multiples of 8 and pointers aligned to 16 bytes", who,
                 a.d, MOE_NORM_ANY_D);
     const Shape s = forward_shape(a.T, a.d);
+    a.waves = (int)s.block.x / 64;
+    a.step = (int)(s.grid.x * s.block.y);
     by_type(SRC == SRC_TENSOR ? v_dt : MOE_F32, [&](auto vt) {
         by_type(h_dt, [&](auto ht) {
             by_type(u_dt, [&](auto ut) {
@@ -577,7 +608,7 @@ int launch_forward(const char* who, const Args& a, int v_dt, int h_dt, int u_dt,
 }
 
 template <bool HAS_V>
-int launch_backward(const char* who, const Args& a, Grads q, float* const (&want)[N_GRADS], int v_dt, int h_dt, int u_dt, bool vec, hipStream_t st) {
+int launch_backward(const char* who, Args a, Grads q, float* const (&want)[N_GRADS], int v_dt, int h_dt, int u_dt, bool vec, hipStream_t st) {
     MOE_REQUIRE(vec || a.d <= MOE_NORM_ANY_D, MOE_ERR_UNSUPPORTED, "%s: d=%d beyond %d needs multiples of 8 and pointers aligned to 16 bytes", who,
                 a.d, MOE_NORM_ANY_D);
     Outs o = {};
@@ -587,6 +618,8 @@ int launch_backward(const char* who, const Args& a, Grads q, float* const (&want
         if (want[g]) o.out[q.slots++] = want[g];
     }
     const Shape s = backward_shape(a.T, a.d, HAS_V);
+    a.waves = (int)s.block.x / 64;
+    a.step = (int)(s.grid.x * s.block.y);
     if (a.T)
         by_type(HAS_V ? v_dt : MOE_F32, [&](auto vt) {
             by_type(h_dt, [&](auto ht) {

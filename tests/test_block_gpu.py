@@ -158,6 +158,8 @@ def test_refusals():
         block.load(pre_w=np.zeros(191))
     with pytest.raises(AssertionError):
         block.load(scale=np.zeros(192))
+    with pytest.raises(AssertionError):
+        block.load(gate=np.zeros(192))                 # (it has none)
     from paper_2506_12417_amd.block import MoEBlock
     gated = MoEBlock(block.layer, gate="shared")
     with pytest.raises(AssertionError):
