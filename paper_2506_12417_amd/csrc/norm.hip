@@ -13,14 +13,14 @@
 // What bounds it: HBM; in calls of few rows the launch and one chain of load, sums over the row, store.  A row is
 // held in registers, eight values a thread, so that every tensor is read once and the statistics take two passes over registers
 // (mean first, then squares of the differences).  A work-group keeps its columns of the parameters in registers and goes over
-// rows, the next row's loads under way while the present one is summed up (rows of more than 4096 values leave a
+// rows, the next row's loads under way while the present one is summed up (backward, rows of more than 4096 values leave a
 // thread no registers for either: they fetch the parameters again for every row).  All arithmetic is fp32; the outputs are rounded
 // once, and u is made of the unrounded y.  The parameters' gradients are summed over a work-group's rows in registers, written
 // to the workspace and added up by a second launch in a fixed order: no atomics.
 //
-// Measured: 16384 x 2048, 16-bit, LAYER, 28 us forward (134 MB, 4.8 TB/s; a copy of 1 GiB reaches 5.2) and 48 + 6 backward with the residual
-// stream's gradient (268 MB, 5.5); 8192 x 4096, both norms, 61 forward (268 MB, 4.4) and 91 + 6 backward (402 MB, 4.4); the rows form,
-// 8192 x 2048 with four experts' rows and a shared one each, 89 (438 MB, 4.9); 1501 x 777 fp32 4.4, 7.5 + 3.6; 33 x 2048 3 - 4.
+// Measured: 16384 x 2048, 16-bit, LAYER, 26 us forward (134 MB, 5.2 TB/s; a copy of 1 GiB reaches 5.2) and 47 + 6 backward with the residual
+// stream's gradient (268 MB, 5.7); 8192 x 4096, both norms, 50 forward (268 MB, 5.4) and 75 + 6 backward (402 MB, 5.4); the rows form,
+// 8192 x 2048 with four experts' rows and a shared one each, 85 (438 MB, 5.2); 1501 x 777 fp32 4.2, 5.7 + 3.6; 33 x 2048 3 - 4.
 #include "common.h"
 #include "gemm_util.h"
 #include <type_traits>
@@ -225,22 +225,10 @@ __device__ __forceinline__ void combine_row(const Args& p, int t, float (&x)[V])
 
 template <typename VT, typename HT, typename UT, bool VEC, int SRC, int G, bool LONG>
 __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
-    constexpr bool KEEP = !LONG;
     __shared__ float red[2][2][MAXW];
     RowSum sum = {red, p.waves, 0};
     const int d = p.d, step = p.step;
     float pw[V], pb[V], gate[V], nw[V], nb[V];
-    auto post_params = [&]() __attribute__((always_inline)) {
-        params<VEC>(SRC == SRC_NONE ? nullptr : p.post_w, d, 1.f, pw);
-        params<VEC>(SRC == SRC_NONE ? nullptr : p.post_b, d, 0.f, pb);
-    };
-    auto gate_params = [&]() __attribute__((always_inline)) {
-        params<VEC>(SRC == SRC_NONE || p.gate_rows != 1 ? nullptr : p.gate, d, 1.f, gate);
-    };
-    auto next_params = [&]() __attribute__((always_inline)) {
-        params<VEC>(p.next_w, d, 1.f, nw);
-        params<VEC>(p.next_b, d, 0.f, nb);
-    };
     const bool own = SRC != SRC_NONE && p.gate_rows > 1;
     Held<VT, VEC> v_next;
     Held<HT, VEC> h_next;
@@ -259,10 +247,13 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         __builtin_amdgcn_raw_buffer_store_b64(u32x2{__float_as_uint(m), __float_as_uint(r)}, to, threadIdx.x == 0 ? which * 8 : S * 4, 0, 0);
     };
     int t = sgpr((int)(blockIdx.x * blockDim.y + threadIdx.y));  // (a wavefront for itself, or one row for all)
-    if (KEEP) fetch(t);
-    if (KEEP) { post_params(); gate_params(); next_params(); }
+    fetch(t);
+    params<VEC>(SRC == SRC_NONE ? nullptr : p.post_w, d, 1.f, pw);
+    params<VEC>(SRC == SRC_NONE ? nullptr : p.post_b, d, 0.f, pb);
+    params<VEC>(SRC == SRC_NONE || p.gate_rows != 1 ? nullptr : p.gate, d, 1.f, gate);
+    params<VEC>(p.next_w, d, 1.f, nw);
+    params<VEC>(p.next_b, d, 0.f, nb);
     for (; t < p.T; t += step) {
-        if (!KEEP) fetch(t);
         const Held<VT, VEC> v = v_next;
         const Held<HT, VEC> h = h_next;
         const size_t at = (size_t)t * d;
@@ -270,7 +261,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         float m = 0.f, r = 0.f;
         const Held<float, VEC> own_gate = gate_next;
         if constexpr (SRC == SRC_ROWS) combine_row<G, VEC>(p, t, y);
-        if (KEEP) fetch(t + step);
+        fetch(t + step);
         if constexpr (SRC == SRC_NONE) {
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = h.at(i);
@@ -281,12 +272,10 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
             }
             if (p.post_kind != MOE_NORM_NONE) {
                 normalise<VEC>(y, p.post_kind, p.post_eps, d, p.inv_d, sum, m, r);
-                if (!KEEP) post_params();
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = fmaf(y[i], pw[i], pb[i]);
             }
             if constexpr (SRC == SRC_TENSOR) keep(t, 0, m, r);
-            if (!KEEP) gate_params();
             if (own) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) gate[i] = own_gate.at(i);
@@ -298,7 +287,6 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_kernel(Args p) {
         if (p.next_kind != MOE_NORM_NONE) {
             normalise<VEC>(y, p.next_kind, p.next_eps, d, p.inv_d, sum, m, r);
             if constexpr (SRC != SRC_ROWS) keep(t, SRC == SRC_NONE ? 0 : 1, m, r);
-            if (!KEEP) next_params();
 #pragma unroll
             for (int i = 0; i < V; ++i) y[i] = fmaf(y[i], nw[i], nb[i]);
             store<VEC>((UT*)p.u + at, d, y, true);
