@@ -13,8 +13,8 @@
 // What bounds it: HBM; in calls of few rows the launch and one chain of load, sums over the row, store.  A row is
 // held in registers, eight values a thread, so that every tensor is read once and the statistics take two passes over registers
 // (mean first, then squares of the differences).  A work-group keeps its columns of the parameters in registers and goes over
-// rows, the next row's loads under way while the present one is summed up (backward, rows of more than 4096 values leave a
-// thread no registers for either: they fetch the parameters again for every row).  All arithmetic is fp32; the outputs are rounded
+// rows, the next row's loads under way while the present one is summed up (at a block's end, backward, rows of more than 4096
+// values leave a thread no registers for either: they fetch the parameters again for every row, 4096 x 8192 in 195 us).  All arithmetic is fp32; the outputs are rounded
 // once, and u is made of the unrounded y.  The parameters' gradients are summed over a work-group's rows in registers, written
 // to the workspace and added up by a second launch in a fixed order: no atomics.
 //
@@ -348,7 +348,7 @@ template <> struct Sums<true> {
 
 template <typename VT, typename HT, typename UT, bool VEC, bool HAS_V, bool LONG>
 __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args p, Grads q) {
-    constexpr bool KEEP = !LONG;
+    constexpr bool TIGHT = LONG && HAS_V;        // too few registers for parameters, sums and the next row
     __shared__ float red[2][2][MAXW];
     RowSum sum = {red, p.waves, 0};
     const int d = p.d, step = p.step, first = sgpr((int)(blockIdx.x * blockDim.y + threadIdx.y));
@@ -361,7 +361,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
     };
     auto gate_params = [&]() __attribute__((always_inline)) { params<VEC>(!HAS_V || p.gate_rows != 1 ? nullptr : p.gate, d, 1.f, gate); };
     auto next_params = [&]() __attribute__((always_inline)) { params<VEC>(p.next_w, d, 1.f, nw); };
-    Sums<LONG> acc;
+    Sums<TIGHT> acc;
     acc.clear();
     Held<VT, VEC> v_next;
     Held<HT, VEC> h_next, dy_next;
@@ -384,10 +384,9 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         du_next.fetch((const UT*)q.du + at, d, on && q.du);
         if constexpr (HAS_V) gate_next.fetch(p.gate + at, d, on && own);
     };
-    if (KEEP) fetch(first);
-    if (KEEP) { post_params(); gate_params(); next_params(); }
+    if (!TIGHT) { fetch(first); post_params(); gate_params(); next_params(); }
     for (int t = first; t < p.T; t += step) {
-        if (!KEEP) { fetch(t); post_params(); gate_params(); }
+        if (TIGHT) { fetch(t); post_params(); gate_params(); }
         const Held<VT, VEC> v = v_next;
         const Held<HT, VEC> h = h_next, dy = dy_next;
         const Held<UT, VEC> du = du_next;
@@ -396,7 +395,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         float st[S];
 #pragma unroll
         for (int i = 0; i < S; ++i) st[i] = __uint_as_float(st_next[i]);
-        if (KEEP) fetch(t + step);
+        if (!TIGHT) fetch(t + step);
         float vn[V], y[V], gy[V];
         const bool next_layer = p.next_kind == MOE_NORM_LAYER, post_layer = p.post_kind == MOE_NORM_LAYER;
         // (Past d everything is zero, but for what LAYER subtracts the mean from.)
@@ -428,7 +427,7 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         }
         if (q.du) {
             float a = 0.f, b = 0.f, gn[V];
-            if (!KEEP) next_params();
+            if (TIGHT) next_params();
             if (next_layer) {
 #pragma unroll
                 for (int i = 0; i < V; ++i) y[i] = column<VEC>(i) < d ? y[i] - st[S - 2] : 0.f;
@@ -461,8 +460,8 @@ __global__ __launch_bounds__(LONG ? MAXT_LONG : MAXT) void norm_back_kernel(Args
         store<VEC>((HT*)q.dh + at, d, out, q.dh != nullptr);
         if constexpr (HAS_V) {
             float a = 0.f, b = 0.f;
-            if (!KEEP) { post_params(); gate_params(); }
-            if (!KEEP && own) {
+            if (TIGHT) { post_params(); gate_params(); }
+            if (TIGHT && own) {
                 Held<float, VEC> again;
                 again.fetch(p.gate + at, d, true);
 #pragma unroll
