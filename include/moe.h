@@ -505,7 +505,7 @@ MOE_API int moe_layer_few(const void* x, int T, int d, int F, int E, int k, moe_
  *   gate [gate_rows,d] fp32: gate_rows 1 (the same for all tokens) or T (a row for every token); NULL with gate_rows 0
  *   stats: what the backward call reads, [T,2] fp32 of moe_norm, [T,4] of moe_block_end (which takes no rows form); may be NULL
  *   y may be h itself, u may be x itself (of one type); no other output may overlap an input
- * Requires d <= MOE_NORM_MAX_D.  Up to MOE_NORM_ANY_D any d and any alignment will do (widths that are no multiples of 8, or
+ * Requires d <= MOE_NORM_MAX_D, T < 2^31 - 2^20.  Up to MOE_NORM_ANY_D any d and any alignment will do (widths that are no multiples of 8, or
  * pointers not aligned to 16 bytes, go value by value); beyond, both are needed.  T = 0 is a no-op.
  */
 typedef enum { MOE_NORM_NONE = 0, MOE_NORM_RMS = 1, MOE_NORM_LAYER = 2 } moe_norm_kind;

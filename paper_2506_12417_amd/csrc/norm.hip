@@ -23,6 +23,7 @@
 // 8192 x 2048 with four experts' rows and a shared one each, 85 (438 MB, 5.2); 1501 x 777 fp32 4.2, 5.7 + 3.6; 33 x 2048 3 - 4.
 #include "common.h"
 #include "gemm_util.h"
+#include <climits>
 #include <type_traits>
 
 namespace {
@@ -637,6 +638,8 @@ bool kind_ok(int kind, bool none) { return kind == MOE_NORM_RMS || kind == MOE_N
 int check_shape(const char* who, int T, int d) {
     MOE_REQUIRE(T >= 0 && d >= 1, MOE_ERR_ARG, "%s: T=%d d=%d", who, T, d);
     MOE_REQUIRE(d <= MOE_NORM_MAX_D, MOE_ERR_UNSUPPORTED, "%s: d=%d is beyond %d", who, d, MOE_NORM_MAX_D);
+    // (a row's number and the rows in work at a time add up to an int)
+    MOE_REQUIRE(T <= INT_MAX - (1 << 20), MOE_ERR_UNSUPPORTED, "%s: T=%d is beyond %d", who, T, INT_MAX - (1 << 20));
     return MOE_OK;
 }
 int check_norms(const char* who, int T, int post_kind, float post_eps, const float* post_w, const float* post_b, const float* gate, int gate_rows,

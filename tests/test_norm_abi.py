@@ -51,6 +51,11 @@ def test_shapes_and_types(call):
     assert call(**bad) == B.MOE_ERR_UNSUPPORTED
 
 
+@pytest.mark.parametrize("call", [norm, norm_back, end, rows, end_back])
+def test_more_rows_than_an_int_can_step_over(call):
+    assert call(T=2 ** 31 - 1) == B.MOE_ERR_UNSUPPORTED and "T=" in str(B.moe_last_error())
+
+
 def test_long_rows_want_aligned_pointers():
     assert norm(d=8192, x=ODD) == B.MOE_ERR_UNSUPPORTED
     assert end(d=8192, v=ODD) == B.MOE_ERR_UNSUPPORTED
