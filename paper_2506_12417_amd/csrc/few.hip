@@ -36,8 +36,6 @@
 namespace {
 
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
-typedef const __attribute__((address_space(1))) unsigned char* gptr;
-typedef const __attribute__((address_space(1))) u32x4* gpiece;
 
 constexpr int NW = 8, NTH = NW * 64;            // wavefronts and threads of a work-group
 constexpr int MAXT = MOE_FEW_MAX_T, MAXE = MOE_MAX_EXPERTS, MAXA = MAXT * MOE_MAX_TOPK;
@@ -1151,7 +1149,8 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     MOE_REQUIRE(d % 64 == 0 && F % 64 == 0 && shared_F % 64 == 0, MOE_ERR_UNSUPPORTED, "moe_layer_few: d=%d F=%d shared_F=%d are not all multiples of 64",
                 d, F, shared_F);
     const size_t es = moe_elem_size(dt), two_gib = (size_t)1 << 31;
-    MOE_REQUIRE((size_t)8 * d * es < two_gib && (size_t)8 * F * es < two_gib && (size_t)8 * shared_F * es < two_gib && (size_t)T * d * es < two_gib && (size_t)E * d * es < two_gib && (size_t)T * k * F * es < two_gib && (size_t)T * shared_F * es < two_gib, MOE_ERR_UNSUPPORTED,
+    MOE_REQUIRE((size_t)8 * d * es < two_gib && (size_t)8 * F * es < two_gib && (size_t)8 * shared_F * es < two_gib && (size_t)T * d * es < two_gib &&
+                    (size_t)E * d * es < two_gib && (size_t)T * k * F * es < two_gib && (size_t)T * shared_F * es < two_gib, MOE_ERR_UNSUPPORTED,
                 "moe_layer_few: rows of %d, %d and %d values are too long", d, F, shared_F);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(x && w_gate && w_in && w_out && expert_idx && gate_w && y && (dt == MOE_F32 || w_norm2) && (!shared_F || (s_w_in && s_w_out)),
