@@ -647,6 +647,7 @@ __device__ __forceinline__ void route_all(const Route& p, unsigned char* smem, c
             }
         }
     } else if constexpr (H::LDS) {
+        MOE_WAIT_VMCNT(0);               // (a wavefront without experts has copied rows of x as well)
         __syncthreads();
     }
     __syncthreads();                     // (the sums take the turning places' memory)

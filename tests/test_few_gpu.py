@@ -144,6 +144,15 @@ def test_experts_and_choices(E, k, dt, act, T):
     check(Case(T, 128, 64, E, k, act, dt, renorm=k % 2, bias=E % 2 == 0), y_dts=(0,))
 
 
+@pytest.mark.parametrize("T,d,E,k,shared_F", [(5, 256, 160, 4, 0), (16, 2048, 144, 2, 0), (16, 2048, 160, 2, 2048), (20, 256, 80, 3, 0), (31, 1024, 90, 2, 0),
+                                              (32, 960, 200, 4, 64), (40, 256, 160, 2, 0), (64, 4096, 150, 1, 0)])
+def test_wavefronts_without_experts(T, d, E, k, shared_F):
+    """Numbers of experts that leave wavefronts of the routing none: these copy their rows of x into LDS like the others, and
+    those rows have to be there before anybody reads them (beside the first product, too, and in a launch of its own)."""
+    print("[case] few idle wavefronts T=%d d=%d E=%d k=%d shared=%d" % (T, d, E, k, shared_F), flush=True)
+    check(Case(T, d, 64, E, k, "relu", "bf16", shared_F=shared_F, renorm=1), y_dts=(0,))
+
+
 @pytest.mark.parametrize("d,F,shared_F", [(64, 64, 0), (64, 128, 64), (320, 1984, 0), (768, 512, 192), (1088, 704, 0), (4096, 64, 64), (4160, 128, 0), (8192, 192, 0)])
 @pytest.mark.parametrize("dt,act,T", [("bf16", "swiglu", 3), ("bf16", "relu", 21), ("f32", "swiglu", 9)])
 def test_widths(d, F, shared_F, dt, act, T):
