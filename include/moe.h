@@ -473,7 +473,9 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
  *   ws: scratch of moe_layer_few_workspace() bytes: the hidden activations, which are rounded once, to IEEE half, and saturate, in MOE_BF16
  *           (as in moe_grouped_ffn); everything else is summed in fp32
  *   y [T,d] y_dt (MOE_F32 or MOE_BF16: rounded once) out
- * Requires T <= MOE_FEW_MAX_T, d, F and shared_F multiples of 64, x, w_gate, ws and the matrices aligned to 16 bytes.  T = 0 is a no-op.
+ * Requires T <= MOE_FEW_MAX_T, d, F and shared_F multiples of 64, x, w_gate, ws and the matrices aligned to 16 bytes, and less than 2 GiB
+ * in x, in w_gate, in 40 rows of w_in (16 with MOE_RELU and no shared expert), in 16 of w_out and s_w_out and in either half of ws.  T = 0 is
+ * a no-op.
  * It adds in an order of its own: the last bits differ from those of the separate calls, and a token's may depend on the other tokens of
  * the call (which experts take part decides how sums are shared out).  The same call gives the same bits.
  */

@@ -1150,7 +1150,9 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     MOE_REQUIRE(d % 64 == 0 && F % 64 == 0 && shared_F % 64 == 0, MOE_ERR_UNSUPPORTED, "moe_layer_few: d=%d F=%d shared_F=%d are not all multiples of 64",
                 d, F, shared_F);
     const size_t es = moe_elem_size(dt), two_gib = (size_t)1 << 31;
-    MOE_REQUIRE((size_t)8 * d * es < two_gib && (size_t)8 * F * es < two_gib && (size_t)8 * shared_F * es < two_gib && (size_t)T * d * es < two_gib &&
+    // (offsets inside a buffer are 31 bits: a segment of the first matrix spans 16 rows, with SwiGLU the 8 up rows end 40 rows on; one of the second 16)
+    const size_t in_rows = act == MOE_SWIGLU || shared_F ? 40 : 16;
+    MOE_REQUIRE(in_rows * d * es < two_gib && (size_t)16 * F * es < two_gib && (size_t)16 * shared_F * es < two_gib && (size_t)T * d * es < two_gib &&
                     (size_t)E * d * es < two_gib && (size_t)T * k * F * es < two_gib && (size_t)T * shared_F * es < two_gib, MOE_ERR_UNSUPPORTED,
                 "moe_layer_few: rows of %d, %d and %d values are too long", d, F, shared_F);
     if (T == 0) return MOE_OK;

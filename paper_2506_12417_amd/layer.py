@@ -118,7 +118,10 @@ class MoELayer:
         can_fuse = can_fuse or (self.dt == B.MOE_F32 and T >= 1)
         self.fuse_gather = can_fuse if fuse_gather is None else (fuse_gather and can_fuse)
         # a decode step's sizes: the whole layer in one call (forward_few)
-        self.few_ok = (1 <= T <= B.MOE_FEW_MAX_T and d % 64 == 0 and F % 64 == 0 and shared_F % 64 == 0)
+        # (the library's limits: 31-bit offsets in what it reads through one descriptor)
+        in_rows = 40 if self.act == B.MOE_SWIGLU or shared_F else 16
+        most = max(in_rows * d, 16 * F, 16 * shared_F, T * d, E * d, A * F, T * shared_F) * self.tdt.itemsize
+        self.few_ok = (1 <= T <= B.MOE_FEW_MAX_T and d % 64 == 0 and F % 64 == 0 and shared_F % 64 == 0 and most < 2 ** 31)
         if self.few_ok:
             self.few_ws = torch.empty(B.moe_layer_few_workspace(T, F, k, shared_F, self.dt), dtype=torch.uint8, device=dev)
         if shared_F:

@@ -37,3 +37,32 @@ def test_workspace():
     assert call(T=5, F=192, k=3, shared_F=128, s_w_in=FAKE, s_w_out=FAKE, ws_bytes=need - 1) == B.MOE_ERR_WORKSPACE
     assert call(ws=None) == B.MOE_ERR_WORKSPACE
     assert B.moe_layer_few_workspace(-1, 64, 1, 0, 0) == 0 and B.moe_layer_few_workspace(1, 64, 1, 0, 9) == 0
+
+
+def test_rows_that_offsets_do_not_reach():
+    """The first width past each limit is refused and the last one inside passes on to the workspace check: 40 rows of a first matrix with
+    SwiGLU (its own or the shared expert's) or 16 without, 16 of a second one, are less than 2 GiB."""
+    def first_past(rows, es):
+        n = -(-2 ** 31 // (rows * es))
+        return -(-n // 64) * 64
+
+    for dt, es in ((B.MOE_BF16, 2), (B.MOE_F32, 4)):
+        one = dict(T=1, E=1, k=1, dt=dt, ws_bytes=0)
+        shared = dict(shared_F=64, s_w_in=FAKE, s_w_out=FAKE)
+        for rows, size, kw in ((40, "d", dict(act=B.MOE_SWIGLU)), (40, "d", shared), (16, "d", dict(act=B.MOE_RELU)), (16, "F", {}), (16, "F", dict(act=B.MOE_SWIGLU)),
+                               (16, "shared_F", shared)):
+            n = first_past(rows, es)
+            assert call(**{**one, **kw, size: n}) == B.MOE_ERR_UNSUPPORTED, (dt, size, kw, n)
+            assert call(**{**one, **kw, size: n - 64}) == B.MOE_ERR_WORKSPACE, (dt, size, kw, n)
+    assert call(T=1, E=1, k=1, d=1 << 26, act=B.MOE_SWIGLU, ws_bytes=0) == B.MOE_ERR_UNSUPPORTED     # (32 rows of it are 2^32 bytes)
+
+
+def test_layers_know_what_is_refused():
+    """MoELayer.few_ok agrees with the library (tensors without memory: only sizes count)."""
+    from paper_2506_12417_amd.layer import MoELayer
+    for T, d, F, act in ((1, 64, 64, "relu"), (64, 128, 192, "swiglu"), (65, 64, 64, "relu"), (1, 96, 64, "relu"), (1, 64, 32, "relu"),
+                         (1, 1 << 26, 64, "swiglu"), (1, 1 << 25, 64, "relu"), (1, 1 << 25, 64, "swiglu"), (1, 64, 1 << 26, "relu"),
+                         (1, 64, (1 << 26) - 64, "relu"), (64, 64, 1 << 24, "relu")):
+        L = MoELayer(T, d, F, 1, 1, act, "bf16", 0, device="meta")
+        status = call(T=T, d=d, F=F, E=1, k=1, act=B.MOE_SWIGLU if act == "swiglu" else B.MOE_RELU, ws_bytes=0)
+        assert L.few_ok == (status == B.MOE_ERR_WORKSPACE) and (L.few_ok or status == B.MOE_ERR_UNSUPPORTED), (T, d, F, act, status)
