@@ -608,7 +608,7 @@ int launch_backward(const char* who, Args a, Grads q, float* const (&want)[N_GRA
     const Shape s = backward_shape(a.T, a.d, HAS_V);
     a.waves = (int)s.block.x / 64;
     a.step = (int)(s.grid.x * s.block.y);
-    if (a.T)
+    if (a.T) {
         by_type(HAS_V ? v_dt : MOE_F32, [&](auto vt) {
             by_type(h_dt, [&](auto ht) {
                 by_type(u_dt, [&](auto ut) {
@@ -623,7 +623,8 @@ int launch_backward(const char* who, Args a, Grads q, float* const (&want)[N_GRA
                 });
             });
         });
-    MOE_CHECK_LAUNCH(who);
+        MOE_CHECK_LAUNCH(who);
+    }
     if (q.slots) {
         hipLaunchKernelGGL(sum_parts_kernel, dim3((unsigned)((a.d + 15) / 16), (unsigned)q.slots), dim3(1024), 0, st, q.part,
                            a.T ? (int)(s.grid.x * s.block.y) : 0, q.slots, a.d, o);
@@ -755,7 +756,7 @@ extern "C" int moe_block_end_backward(const void* dy, const void* du, moe_dtype 
     MOE_REQUIRE(gate || !dgate, MOE_ERR_ARG, "%s: gradient of a gate that is none", who);
     MOE_REQUIRE(du || (!dnext_w && !dnext_b), MOE_ERR_ARG, "%s: parameters' gradients without du", who);
     MOE_REQUIRE(T == 0 || (v && h && stats && (dy || du)), MOE_ERR_ARG, "%s: null pointer", who);
-    const bool own = gate_rows > 1;
+    const bool own = gate_rows != 1;     // (a row for every token; no tokens: dgate has no rows)
     float* const want[N_GRADS] = {dnext_w, dnext_b, own ? nullptr : dgate, dpost_w, dpost_b};
     int n = 0;
     for (float* w : want) n += w != nullptr;

@@ -104,6 +104,12 @@ def test_block_end_backward_arguments():
     assert end_back(gate=FAKE, gate_rows=1, dgate=FAKE) == B.MOE_ERR_WORKSPACE
 
 
+def test_no_tokens_have_no_gate_gradient():
+    """A gate for every token of none: dgate has no rows, so that nothing is enqueued, let alone written there (d zeros were)."""
+    none = dict(T=0, dy=None, du=None, v=None, h=None, stats=None, ws=None, ws_bytes=0)
+    assert end_back(**none, gate=FAKE, gate_rows=0, dgate=FAKE) == B.MOE_OK
+
+
 def test_workspace_sizes():
     for op in (B.MOE_OP_NORM_BACKWARD, B.MOE_OP_BLOCK_END_BACKWARD):
         ask = lambda T, d: B.moe_workspace_bytes(op, T, d, 0, 0, 0, 0)    # noqa: E731

@@ -371,6 +371,17 @@ def test_no_rows():
     assert not dw.any() and not db.any() and not dg.any()
 
 
+def test_no_rows_of_a_token_gate():
+    """No tokens and a gate for every token: dgate has no rows, and what lies at its address stays; the others are zero."""
+    torch, B = _torch()
+    d = 264
+    dpw, dpb, other = (torch.full((d,), 7.0, device="cuda") for _ in range(3))
+    B.moe_block_end_backward(None, None, BF16, None, BF16, None, BF16, 0, d, RMS, None, None, torch.ones(d, device="cuda"), 0, 1.0, NONE, None, None, None,
+                             None, dpw, dpb, other, None, None, None, 0)
+    torch.cuda.synchronize()
+    assert not dpw.any() and not dpb.any() and (other == 7.0).all()
+
+
 def test_stream_and_graph():
     """The calls go to the stream that they are given, and a graph of them replays on new inputs."""
     torch, B = _torch()
