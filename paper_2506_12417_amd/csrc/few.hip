@@ -511,12 +511,12 @@ __device__ __forceinline__ void choose(const Route& p, L& s, Lists& l, int t0, f
     const double top = __shfl(sv, lane & 48);
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < NI; ++i) sum += sub + 16 * i < E ? __expf((float)(v[i] - top)) : 0.f;
+    for (int i = 0; i < NI; ++i) sum += sub + 16 * i < E ? gate_exp((float)(v[i] - top)) : 0.f;
     sum += dpp_xchg<0>(sum);
     sum += dpp_xchg<1>(sum);
     sum += dpp_xchg<2>(sum);
     sum += dpp_xchg<3>(sum);
-    const float mine = se == INT_MAX ? __builtin_nanf("") : __expf((float)(sv - top));
+    const float mine = se == INT_MAX ? __builtin_nanf("") : gate_exp((float)(sv - top));
     float chosen = sub < k ? mine : 0.f;
     chosen += dpp_xchg<0>(chosen);
     chosen += dpp_xchg<1>(chosen);

@@ -1,4 +1,4 @@
-// Exchanges between lanes and what the routers build on them: comparisons, sums and the best of a wavefront in 64 bits.
+// Exchanges between lanes and what the routers build on them: comparisons, sums and the best of a wavefront in 64 bits; the gates' exponential.
 #pragma once
 #include "common.h"
 
@@ -55,6 +55,14 @@ __device__ __forceinline__ void row_best_f64(double& v, int& e, bool all) {
             if (beats(ov, oe, v, e)) { v = ov; e = oe; }
         }
     }
+}
+
+// exp(v) = 2^t for t = v log2(e), with what the rounding of t took away put back (v is up to tens, so t alone costs several
+// units in the last place of the result).
+__device__ __forceinline__ float gate_exp(float v) {
+    constexpr float L = 1.44269504088896340736f, L_REST = (float)(1.44269504088896340736 - (double)L), LN2 = 0.69314718055994530942f;
+    const float t = v * L, rest = fmaf(v, L_REST, fmaf(v, L, -t)), e = __builtin_amdgcn_exp2f(t);
+    return e > 0.f ? fmaf(e, rest * LN2, e) : e;     // (rest is no number for an infinite v)
 }
 
 }  // namespace

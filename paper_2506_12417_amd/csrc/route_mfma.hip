@@ -66,14 +66,6 @@ template <int TPT> __device__ __forceinline__ void group_best(float& v, int& e) 
     if (TPT == 16) { ov = dpp_xchg<3>(v); oe = dpp_xchg<3>(e); if (beats(ov, oe, v, e)) { v = ov; e = oe; } }
 }
 
-// exp(v) = 2^t for t = v log2(e), with what the rounding of t took away put back (v is up to tens, so t alone costs several
-// units in the last place of the result).
-__device__ __forceinline__ float gate_exp(float v) {
-    constexpr float L = 1.44269504088896340736f, L_REST = (float)(1.44269504088896340736 - (double)L), LN2 = 0.69314718055994530942f;
-    const float t = v * L, rest = fmaf(v, L_REST, fmaf(v, L, -t)), e = __builtin_amdgcn_exp2f(t);
-    return e > 0.f ? fmaf(e, rest * LN2, e) : e;     // (rest is no number for an infinite v)
-}
-
 // LDS of the phases after the product (it reuses the memory of the operand staging).
 template <int NB, int KSP>
 struct RouteLds {

@@ -254,6 +254,31 @@ def test_masked_experts():
         check(Case(19, 128, 64, 12, 3, "relu", "bf16", b=b), y_dts=(0,))
 
 
+@pytest.mark.parametrize("T,shared_F", [(5, 0), (20, 0), (40, 0), (9, 2048)])
+@pytest.mark.parametrize("renorm", [0, 1])
+def test_gates_keep_their_bits(T, shared_F, renorm):
+    """Gates to fp32's precision relative to themselves, small ones too.  Tokens of a single one make the logits weights of W_g, so that they and
+    their differences are exact.  In units of 2^-24: an exponential is off by 3 (an instruction's last place, a correction's rounding), the
+    sum of positive terms by the terms' 3 and 8 additions, the quotient by 1; 3 + 3 + 8 + 1 < 16.  (A rounded product with log2(e) alone
+    would be off by 2^-18 ln 2 at 2^-115, 44 units.)"""
+    print("[case] few gates T=%d shared=%d renorm=%d" % (T, shared_F, renorm), flush=True)
+    d, E, k = 2048 if shared_F else 128, 16, 8
+    r = np.random.default_rng(T)
+    x, W_g = np.zeros((T, d)), np.zeros((d, E))
+    x[np.arange(T), 3 * np.arange(T)] = 1.0
+    for t in range(T):
+        low = -80.0 * r.random(E)
+        low[r.integers(E)] = 0.0
+        W_g[3 * t] = low
+    c = Case(T, d, 64, E, k, "relu", "bf16", shared_F=shared_F, renorm=renorm, bias=False, x=x, W_g=W_g)
+    dev = Device(c)
+    dev.run()
+    idx, gate, _, _, _ = reference(c)
+    assert np.array_equal(dev.idx.cpu().numpy(), idx)
+    off = np.abs(dev.gate.cpu().numpy().astype(np.float64) / gate - 1.0)
+    assert off.max() <= 16 * 2.0 ** -24, off.max() * 2.0 ** 24
+
+
 def test_hidden_activations_saturate():
     c = Case(4, 64, 64, 2, 1, "relu", "bf16", bias=False)
     c.x = rounded(wide(c.x) * 3e4, "bf16")
