@@ -471,7 +471,7 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
  *   expert_idx [T,k], gate_w [T,k] out: the choice of moe_route_topk (decided as if in float64; a token whose logits are NaN gets ids
  *           outside [0,E), NaN weights and a row of NaN)
  *   ws: scratch of moe_layer_few_workspace() bytes: the hidden activations, which are rounded once, to IEEE half, and saturate, in MOE_BF16
- *           (as in moe_grouped_ffn); everything else is summed in fp32
+ *           (as in moe_grouped_ffn); everything else is summed in fp32.  A NaN in a matrix reaches the outputs that it takes part in.
  *   y [T,d] y_dt (MOE_F32 or MOE_BF16: rounded once) out
  * Requires T <= MOE_FEW_MAX_T, d, F and shared_F multiples of 64, x, w_gate, ws and the matrices aligned to 16 bytes, and less than 2 GiB
  * in x, in w_gate, in 40 rows of w_in (16 with MOE_RELU and no shared expert), in 16 of w_out and s_w_out and in either half of ws.  T = 0 is

@@ -43,6 +43,11 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
     return (uint16_t)(u >> 16);
 }
 
+// What an activation does to a value that is no number: nothing (fmaxf and the median of three would return a number).
+__device__ __forceinline__ float relu_f(float v) { return __builtin_elementwise_maximum(v, 0.f); }
+// to the range of IEEE half
+__device__ __forceinline__ float clamp_half(float v) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -65504.f), 65504.f); }
+
 template <typename T> __device__ __forceinline__ float load_as_f32(const T* p);
 template <> __device__ __forceinline__ float load_as_f32<float>(const float* p) { return *p; }
 template <> __device__ __forceinline__ float load_as_f32<uint16_t>(const uint16_t* p) { return bf16_to_f32(*p); }

@@ -730,7 +730,7 @@ struct Hidden {
     int route_blocks;                    // R: so many work-groups route
 };
 __device__ __forceinline__ uint16_t half_of(float v) {           // saturating, nearest-even
-    return __builtin_bit_cast(uint16_t, (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f));
+    return __builtin_bit_cast(uint16_t, (_Float16)clamp_half(v));
 }
 
 // H: how the tokens are routed first, by every work-group; or not at all (Routed).  R (a How; with Routed): a launch of its own for the
@@ -839,7 +839,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float up = __shfl_xor(a[i], 32);
-            v[i] = it.glu ? silu_f(a[i]) * up : fmaxf(a[i], 0.f);
+            v[i] = it.glu ? silu_f(a[i]) * up : relu_f(a[i]);
         }
         if (r < it.m && (!it.glu || lq < 2)) {
             // H in rows by token and choice; or an expert's rows piece by piece, 16 bytes of every row behind one another, so that a fragment

@@ -279,6 +279,41 @@ def test_gates_keep_their_bits(T, shared_F, renorm):
     assert off.max() <= 16 * 2.0 ** -24, off.max() * 2.0 ** 24
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,F,E,k,act,shared_F", [(6, 128, 192, 5, 2, "relu", 0), (12, 768, 128, 6, 1, "relu", 0), (40, 192, 128, 7, 3, "swiglu", 64),
+                                                    (30, 2048, 64, 4, 2, "swiglu", 64)])
+def test_weights_that_are_no_numbers(T, d, F, E, k, act, shared_F, dt):
+    """A NaN in an expert's first matrix makes the rows of the tokens that chose it NaN, one in its second matrix their outputs of that
+    column, one in the shared expert's every token's; all other values keep their bits."""
+    print("[case] few NaN weights T=%d d=%d %s %s" % (T, d, act, dt), flush=True)
+    c = Case(T, d, F, E, k, act, dt, shared_F=shared_F)
+    dev = Device(c)
+    y0 = dev.run().cpu().numpy()
+    idx = dev.idx.cpu().numpy()
+    e = int(np.bincount(idx.ravel(), minlength=E).argmax())
+    chose = (idx == e).any(1)
+    nan = 0x7fc0 if dt == "bf16" else np.nan
+    for name in c.w:
+        w = {n: a[e].copy() for n, a in c.w.items()}
+        w[name][w[name].shape[0] // 3, 17] = nan
+        dev.g.load_expert(e, w)
+        y = dev.run().cpu().numpy()
+        want = np.zeros((T, d), dtype=bool)
+        want[chose] = True
+        if name in ("W2", "Wd"):
+            want[:, :17] = want[:, 18:] = False
+        assert np.array_equal(np.isnan(y), want) and np.array_equal(y[~want], y0[~want]), name
+    dev.g.load_expert(e, {n: a[e] for n, a in c.w.items()})
+    for name in c.sw or ():
+        w = {n: a[0].copy() for n, a in c.sw.items()}
+        w[name][0, 3] = nan
+        dev.s.load_expert(0, w)
+        y = dev.run().cpu().numpy()
+        want = np.full((T, d), name != "Wd")
+        want[:, 3] = True
+        assert np.array_equal(np.isnan(y), want) and np.array_equal(y[~want], y0[~want]), name
+
+
 def test_hidden_activations_saturate():
     c = Case(4, 64, 64, 2, 1, "relu", "bf16", bias=False)
     c.x = rounded(wide(c.x) * 3e4, "bf16")
