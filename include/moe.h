@@ -295,7 +295,8 @@ MOE_API int moe_pack_w_out(const void* w, int n, int F, int d, moe_dtype dt, voi
  * accumulates both products in fp32 and rounds the hidden activations once, to IEEE half: 11
  * significant bits, so the result is within about 1e-3 of the output's RMS of the exact one
  * (bf16 activations would be eight times coarser); a hidden activation beyond +-65504 (the
- * largest half value) is stored as +-65504: it saturates, y_perm stays finite.  The bf16 kernels
+ * largest half value) is stored as +-65504: it saturates, y_perm stays finite.  A NaN in a matrix reaches
+ * the outputs that it takes part in (in MOE_F32 with MOE_RELU a hidden activation that is NaN counts as 0).  The bf16 kernels
  * are persistent launches laid out for the whole MI355X (256 compute units in 8 XCDs):
  * MOE_ERR_UNSUPPORTED on a device that reports another count.
  */

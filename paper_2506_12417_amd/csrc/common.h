@@ -45,8 +45,16 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
 
 // What an activation does to a value that is no number: nothing (fmaxf and the median of three would return a number).
 __device__ __forceinline__ float relu_f(float v) { return __builtin_elementwise_maximum(v, 0.f); }
-// to the range of IEEE half
-__device__ __forceinline__ float clamp_half(float v) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(v, -65504.f), 65504.f); }
+// To IEEE half, nearest-even, saturating: what rounds to infinity becomes the largest value.
+__device__ __forceinline__ uint16_t half_bits(float v) {
+    const _Float16 h = (_Float16)v;
+    return __builtin_bit_cast(uint16_t, __builtin_elementwise_minimum(__builtin_elementwise_maximum(h, (_Float16)-65504.f), (_Float16)65504.f));
+}
+__device__ __forceinline__ unsigned half_bits(float lo, float hi) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 pair;
+    const pair h = {(_Float16)lo, (_Float16)hi}, most = {(_Float16)65504.f, (_Float16)65504.f};
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_minimum(__builtin_elementwise_maximum(h, -most), most));
+}
 
 template <typename T> __device__ __forceinline__ float load_as_f32(const T* p);
 template <> __device__ __forceinline__ float load_as_f32<float>(const float* p) { return *p; }

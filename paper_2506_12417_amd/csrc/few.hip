@@ -729,9 +729,6 @@ struct Hidden {
     int F, shared_F, glu, h_rows;        // h_rows: H in rows, else an expert's rows piece by piece (see finish)
     int route_blocks;                    // R: so many work-groups route
 };
-__device__ __forceinline__ uint16_t half_of(float v) {           // saturating, nearest-even
-    return __builtin_bit_cast(uint16_t, (_Float16)clamp_half(v));
-}
 
 // H: how the tokens are routed first, by every work-group; or not at all (Routed).  R (a How; with Routed): a launch of its own for the
 // routing, ROUTE_EACH tokens a work-group, and beside it the shared expert's first product, by the other work-groups.
@@ -851,7 +848,7 @@ __global__ __launch_bounds__(NTH) void few_hidden_kernel(Hidden p) {
                 *(f32x4*)to = f32x4{v[0], v[1], v[2], v[3]};
             } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) ((uint16_t*)to)[(col & 1) + 2 * i] = half_of(v[i]);
+                for (int i = 0; i < 4; ++i) ((uint16_t*)to)[(col & 1) + 2 * i] = half_bits(v[i]);
             }
         }
     };

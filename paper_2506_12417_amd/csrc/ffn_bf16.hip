@@ -419,9 +419,7 @@ __device__ __forceinline__ void gemm_bf16_body(const uint16_t* __restrict__ a_ma
             __builtin_amdgcn_raw_buffer_store_b64(v, ro, voff, soff, O_POLICY);
         } else {
             // hidden activations saturate at the largest half value instead of becoming infinite
-            const f32x2 f = {__builtin_amdgcn_fmed3f(lo, -65504.f, 65504.f), __builtin_amdgcn_fmed3f(hi, -65504.f, 65504.f)};
-            const f16x2 b = __builtin_convertvector(f, f16x2);            // nearest-even
-            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, b), ro, voff, soff, O_POLICY);
+            __builtin_amdgcn_raw_buffer_store_b32(half_bits(lo, hi), ro, voff, soff, O_POLICY);
         }
     };
     auto epilogue = [&](__amdgpu_buffer_rsrc_t ro, int mi_on, int n0) __attribute__((always_inline)) {
@@ -451,7 +449,7 @@ __device__ __forceinline__ void gemm_bf16_body(const uint16_t* __restrict__ a_ma
                         const int col = n0 + wn * C::WTN + ni * 32;
                         if (col < N) {
                             if (EPI == MOE_EPI_RELU)
-                                store_pair(ro, fmaxf(acc[mi][ni][a][0][r], 0.f), fmaxf(acc[mi][ni][a][1][r], 0.f), voff, (unsigned)col * ES);
+                                store_pair(ro, relu_f(acc[mi][ni][a][0][r]), relu_f(acc[mi][ni][a][1][r]), voff, (unsigned)col * ES);
                             else
                                 store_pair(ro, acc[mi][ni][a][0][r], acc[mi][ni][a][1][r], voff, (unsigned)col * ES);
                         }

@@ -103,10 +103,6 @@ __device__ __forceinline__ void rows_product(const uint16_t* __restrict__ a_mat,
     }
 }
 
-__device__ __forceinline__ uint16_t half_bits(float v) {     // saturating, nearest-even
-    return __builtin_bit_cast(uint16_t, (_Float16)__builtin_amdgcn_fmed3f(v, -65504.f, 65504.f));
-}
-
 // One product: what a launch is given for it (moe_launch_gemm_rows).
 struct Job {
     const uint16_t* a_mat;
@@ -220,8 +216,8 @@ __global__ __launch_bounds__(KS * 64, 4) void gemm_rows_kernel(Job main, Job oth
                 if constexpr (!HALF_IN) {
                     uint16_t* to = (uint16_t*)out + (size_t)row * ld_out + col + 2 * j;
                     if constexpr (GLU) *to = half_bits(silu_f(v0) * v1);
-                    else if constexpr (NSUB == 1) *to = half_bits(fmaxf(v0, 0.f));
-                    else *(uint32_t*)to = half_bits(fmaxf(v0, 0.f)) | ((uint32_t)half_bits(fmaxf(v1, 0.f)) << 16);
+                    else if constexpr (NSUB == 1) *to = half_bits(relu_f(v0));
+                    else *(uint32_t*)to = half_bits(relu_f(v0), relu_f(v1));
                 } else {
                     if constexpr (SCAT) {
                         if (i >= NTH) place(r);

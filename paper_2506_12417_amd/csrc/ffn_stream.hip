@@ -297,9 +297,7 @@ __device__ __forceinline__ void gemm_stream_body(const uint16_t* __restrict__ a_
             __builtin_amdgcn_raw_buffer_store_b64(v, ro, voff, soff, 0);
         } else {
             // hidden activations saturate at the largest half value instead of becoming infinite
-            const f32x2 f = {__builtin_amdgcn_fmed3f(lo, -65504.f, 65504.f), __builtin_amdgcn_fmed3f(hi, -65504.f, 65504.f)};
-            const f16x2 b = __builtin_convertvector(f, f16x2);
-            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, b), ro, voff, soff, 0);
+            __builtin_amdgcn_raw_buffer_store_b32(half_bits(lo, hi), ro, voff, soff, 0);
         }
     };
     auto epilogue = [&](__amdgpu_buffer_rsrc_t ro, int mb_on, int col) __attribute__((always_inline)) {
@@ -315,7 +313,7 @@ __device__ __forceinline__ void gemm_stream_body(const uint16_t* __restrict__ a_
             for (int r = 0; r < 4; ++r) {
                 const unsigned voff = st_base + (unsigned)(m * 16 + r) * ld_bytes;
                 if (EPI == MOE_EPI_RELU)
-                    store_pair(ro, fmaxf(acc[m][0][r], 0.f), fmaxf(acc[m][1][r], 0.f), voff, (unsigned)col * ES);
+                    store_pair(ro, relu_f(acc[m][0][r]), relu_f(acc[m][1][r]), voff, (unsigned)col * ES);
                 else
                     store_pair(ro, acc[m][0][r], acc[m][1][r], voff, (unsigned)col * ES);
             }

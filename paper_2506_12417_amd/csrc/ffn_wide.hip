@@ -335,9 +335,7 @@ __device__ __forceinline__ void store_pair(__amdgpu_buffer_rsrc_t ro, float lo, 
         __builtin_amdgcn_raw_buffer_store_b64(v, ro, voff, soff, 0);
     } else {
         // hidden activations saturate at the largest half value instead of becoming infinite
-        const f32x2 f = {__builtin_amdgcn_fmed3f(lo, -65504.f, 65504.f), __builtin_amdgcn_fmed3f(hi, -65504.f, 65504.f)};
-        const f16x2 b = __builtin_convertvector(f, f16x2);            // nearest-even
-        __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, b), ro, voff, soff, 0);
+        __builtin_amdgcn_raw_buffer_store_b32(half_bits(lo, hi), ro, voff, soff, 0);
     }
 }
 
@@ -374,7 +372,7 @@ __device__ __forceinline__ void epilogue(const Acc& acc, __amdgpu_buffer_rsrc_t 
                     const int col = col0 + ni * 32;
                     if (col < N) {
                         if (EPI == MOE_EPI_RELU)
-                            store_pair<HALF_IN>(ro, fmaxf(acc[mi][ni][a][0][r], 0.f), fmaxf(acc[mi][ni][a][1][r], 0.f), voff, (unsigned)col * ES);
+                            store_pair<HALF_IN>(ro, relu_f(acc[mi][ni][a][0][r]), relu_f(acc[mi][ni][a][1][r]), voff, (unsigned)col * ES);
                         else
                             store_pair<HALF_IN>(ro, acc[mi][ni][a][0][r], acc[mi][ni][a][1][r], voff, (unsigned)col * ES);
                     }
