@@ -216,6 +216,67 @@ def test_block_end_and_its_gradients(T, d, post, nxt, gate):
     compare(*run(torch, B, dict(a, post_b=None, next_b=None), (F32, F32, F32)))
 
 
+# More rows than a launch has work-groups (wavefronts, up to 512 columns) for, and no multiple of them: the second and later rows of one, whose
+# loads are under way while the row before is worked on, whose sums take the LDS buffers in turn and whose parameters' gradients are added to
+# those of the rows before.  Rows in work: 8192 up to 512 columns, 2048 up to 2048, 512 up to 8192 forward; 1024 at most backward.
+MANY = [(9001, 256), (4500, 777), (2500, 2048), (1100, 4104), (1100, 8192)]
+
+
+@pytest.mark.parametrize("T,d", MANY)
+@pytest.mark.parametrize("kind,dt", [(RMS, BF16), (LAYER, F32)])
+def test_norm_of_many_rows(T, d, kind, dt):
+    torch, B = _torch()
+    print("[case] norm of many rows", T, d, kind, dt, flush=True)
+    compare(*run(torch, B, make(T, d, T + d, nxt=kind, with_v=False), (dt, dt, dt)))
+
+
+@pytest.mark.parametrize("T,d", [(8700, 136), (2500, 1032), (1300, 4096), (1100, 4104), (600, 8192)])
+@pytest.mark.parametrize("post,nxt,gate,dt", [(RMS, LAYER, "token", BF16), (LAYER, RMS, "token", F32), (RMS, RMS, "channel", BF16)])
+def test_block_end_of_many_rows(T, d, post, nxt, gate, dt):
+    torch, B = _torch()
+    print("[case] block end of many rows", T, d, post, nxt, gate, dt, flush=True)
+    compare(*run(torch, B, make(T, d, T + d, post, nxt, gate), (dt, dt, dt)))
+
+
+@pytest.mark.parametrize("T,d,k", [(8200, 264, 3), (2500, 2048, 2), (1300, 4096, 4), (1000, 4104, 2), (700, 8192, 5)])
+def test_rows_form_of_many_rows(T, d, k):
+    """The rows form, bit for bit against combine and block end, which are compared with the formula above."""
+    torch, B = _torch()
+    print("[case] rows form of many rows", T, d, k, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(T)
+    new = lambda *shape: torch.empty(shape, device="cuda").normal_(generator=g)     # noqa: E731
+    rows, shared, h, gate = new(T * k, d), new(T, d), new(T, d).bfloat16(), new(T, d)
+    inv, gw = torch.randperm(T * k, generator=g, device="cuda").int(), new(T, k)
+    par = [new(d) for _ in range(4)]
+    norms = (LAYER, EPS, par[0], par[1], gate, T, 0.75, RMS, EPS, par[2], par[3])
+    v = torch.empty((T, d), device="cuda")
+    y, u, y2, u2 = (torch.full((T, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    torch.cuda.synchronize()
+    B.moe_block_end_rows(rows, inv, gw, shared, k, h, BF16, T, d, *norms, y, u, BF16)
+    B.moe_unpermute_combine(rows, inv, gw, shared, T, d, k, v)
+    B.moe_block_end(v, F32, h, BF16, T, d, *norms, y2, u2, BF16)
+    torch.cuda.synchronize()
+    assert torch.isfinite(y).all() and torch.isfinite(u).all() and torch.equal(y, y2) and torch.equal(u, u2)
+
+
+def test_many_rows_do_not_touch_one_another():
+    """A row of NaN, of infinities or of zeros between others that the same work-group goes over leaves these alone."""
+    torch, B = _torch()
+    for T, d in ((9001, 128), (1100, 4104)):
+        a = make(T, d, 77, LAYER, RMS, "token", dy=False, du=False)
+        base, _, _ = run(torch, B, a)
+        bad = dict(a, h=a["h"].copy(), v=a["v"].copy())
+        hit = np.arange(3, T, 7)
+        bad["h"][hit[0::3]], bad["v"][hit[1::3]], bad["v"][hit[2::3], d - 1] = np.nan, 0.0, np.inf
+        got, _, _ = run(torch, B, bad)
+        keep = torch.ones(T, dtype=torch.bool)
+        keep[torch.from_numpy(hit)] = False
+        keep = keep.cuda()
+        for n in ("y", "u"):
+            assert torch.equal(base[n][keep], got[n][keep]), n
+            assert got[n][torch.from_numpy(hit[0::3]).cuda()].isnan().all() and torch.isfinite(got[n][torch.from_numpy(hit[1::3]).cuda()]).all()
+
+
 @pytest.mark.parametrize("dts", [(v, h, u) for v in (F32, BF16) for h in (F32, BF16) for u in (F32, BF16)])
 @pytest.mark.parametrize("d,shift", [(264, 0), (264, 1), (8192, 0), (101, 3)])
 def test_types_alignment_and_missing_parameters(dts, d, shift):
