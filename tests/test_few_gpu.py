@@ -280,6 +280,33 @@ def test_gates_keep_their_bits(T, shared_F, renorm):
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("low", [-np.inf, float(np.finfo(np.float32).min)])
+@pytest.mark.parametrize("T", [7, 29, 45])
+def test_masked_experts_that_are_chosen_and_that_are_not(T, low, dt):
+    """More choices than experts that are left: the masked ones follow by their index with weight zero, and the rows are those of the experts that
+    are left.  As many choices as are left: the masked ones' matrices of infinities and NaN take part in nothing."""
+    print("[case] few masked T=%d %g %s" % (T, low, dt), flush=True)
+    E, k, left = 9, 4, [1, 6]
+    b = np.full(E, low, dtype=np.float32)
+    b[left] = [0.25, 0.0]
+    c = Case(T, 128, 64, E, k, "relu", dt, b=b, renorm=T % 2)
+    check(c, y_dts=(0,))
+    dev = Device(c)
+    y = dev.run()
+    idx, gate = dev.idx.cpu().numpy(), dev.gate.cpu().numpy()
+    assert (np.sort(idx[:, :2], 1) == left).all() and (idx[:, 2:] == [0, 2]).all() and (gate[:, 2:] == 0).all() and (gate[:, :2] > 0).all()
+    for only in (1, 2):                                       # as many as are left, or fewer
+        c = Case(T, 128, 64, E, only, "relu", dt, b=b, renorm=T % 2)
+        dev = Device(c)
+        y = dev.run()
+        for e in sorted(set(range(E)) - set(left)):
+            for name, w in ((n, a[e].copy()) for n, a in c.w.items()):
+                w[:] = (0x7f80, 0x7fc0)[e % 2] if dt == "bf16" else (np.inf, np.nan)[e % 2]
+                dev.g.load_expert(e, {n: w if n == name else a[e] for n, a in c.w.items()})
+            assert dev.torch.equal(dev.run(), y), (only, e)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("T,d,F,E,k,act,shared_F", [(6, 128, 192, 5, 2, "relu", 0), (12, 768, 128, 6, 1, "relu", 0), (40, 192, 128, 7, 3, "swiglu", 64),
                                                     (30, 2048, 64, 4, 2, "swiglu", 64)])
 def test_weights_that_are_no_numbers(T, d, F, E, k, act, shared_F, dt):
