@@ -124,6 +124,17 @@ def _d(t) -> Optional[int]:
     return t.data_ptr()
 
 
+def check_rows(name: str, t, rows: int, d: int, dtypes, device):
+    """A tensor that a call reads or writes as `rows` contiguous rows of d values: refused unless it is one of these types, there, and that
+    many (the library sees an address only)."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in dtypes or t.device != device or t.numel() != rows * d or (t.dim() > 1 and t.shape[-1] != d):
+        raise MoeError(MOE_ERR_ARG, "%s: %s; wanted %d rows of %d values, %s on %s" % (
+            name, "%s %s on %s" % (tuple(t.shape), t.dtype, t.device) if isinstance(t, torch.Tensor) else type(t).__name__, rows, d,
+            " or ".join(map(str, dtypes)), device))
+    if not t.is_contiguous():
+        raise MoeError(MOE_ERR_UNSUPPORTED, "%s: strides %s: rows have to be contiguous" % (name, tuple(t.stride())))
+
+
 _raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 
 

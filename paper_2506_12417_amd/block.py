@@ -63,6 +63,11 @@ class MoEBlock:
             if self.train:
                 self.grad["d" + name] = torch.empty_like(self.param[name])
 
+    def _check(self, dtype: torch.dtype, **tensors: Optional[torch.Tensor]):
+        for name, t in tensors.items():
+            if t is not None:
+                B.check_rows(name, t, self.T, self.d, (dtype,), self.y.device)
+
     def _end(self) -> Tuple:
         p = self.param
         assert self.gate_rows == 0 or p["gate"] is not None, "the gate is not loaded"
@@ -74,6 +79,8 @@ class MoEBlock:
         made it as its u'."""
         L, p = self.layer, self.param
         assert not (self.train and u is not None), "the pre norm's statistics come from its own call"
+        self._check(self.h_tdt, h=h)
+        self._check(L.tdt, u=u)
         if u is None:
             B.moe_norm(h, self.h_dt, p["pre_w"], p["pre_b"], self.T, self.d, self.pre, self.eps, self.u, L.dt, self.pre_stats if self.train else None,
                        stream)
@@ -93,6 +100,8 @@ class MoEBlock:
     def end_backward(self, h: torch.Tensor, dy: Optional[torch.Tensor], du_next: Optional[torch.Tensor], stream=None):
         """From the gradients of y and u' to those of v (fp32) and, by the residual connection, of h; the parameters' go to `grad`."""
         p, g = self.param, self.grad
+        self._check(self.h_tdt, h=h, dy=dy)
+        self._check(self.layer.tdt, du_next=du_next)
         B.moe_block_end_backward(dy, du_next, self.layer.dt, self.layer.y, B.MOE_F32, h, self.h_dt, self.T, self.d, self.post, p["post_w"], p["post_b"],
                                  p["gate"] if self.gate_rows else None, self.gate_rows, self.alpha, self.next, p["next_w"], self.end_stats, self.dv, self.dh,
                                  *[g.get(n) for n in ("dpost_w", "dpost_b", "dgate", "dnext_w", "dnext_b")], self.ws, self.ws.numel(), stream)
@@ -102,6 +111,8 @@ class MoEBlock:
         """From the gradient of u, as the layer's own backward gives it for dv, to h's whole gradient: end_backward's dh is added, in
         place."""
         p, g = self.param, self.grad
+        self._check(self.h_tdt, h=h)
+        self._check(self.layer.tdt, du=du)
         B.moe_norm_backward(du, self.layer.dt, h, self.h_dt, p["pre_w"], self.pre_stats, self.T, self.d, self.pre, self.dh, self.dh, g.get("dpre_w"),
                             g.get("dpre_b"), self.ws, self.ws.numel(), stream)
         return self.dh

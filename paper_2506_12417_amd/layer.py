@@ -240,6 +240,8 @@ class MoELayer:
         another order, so the last bits differ."""
         assert self.few_ok and (self.packed_router or self.dt == B.MOE_F32), "sizes or router are not moe_layer_few's"
         y = self.y if y is None else y
+        B.check_rows("x", x, self.T, self.d, (self.tdt,), self.y.device)
+        B.check_rows("y", y, self.T, self.d, (torch.float32, torch.bfloat16), self.y.device)
         g, s = self.experts, self.shared if self.shared_F else None
         w, norm2 = (self.W_gt, self.w_norm2) if self.dt == B.MOE_BF16 else (self.W_g, None)
         B.moe_layer_few(x, self.T, self.d, self.F, self.E, self.k, self.act, self.dt, self.renorm, w, norm2, self.bias, g.in_ptrs, g.out_ptrs,
