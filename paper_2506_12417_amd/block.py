@@ -98,13 +98,18 @@ class MoEBlock:
         return self.y, self.u_next
 
     def end_backward(self, h: torch.Tensor, dy: Optional[torch.Tensor], du_next: Optional[torch.Tensor], stream=None):
-        """From the gradients of y and u' to those of v (fp32) and, by the residual connection, of h; the parameters' go to `grad`."""
+        """From the gradients of y and u' to those of v (fp32) and, by the residual connection, of h; the parameters' go to `grad`.  Either of dy
+        and du_next may be None, which is zero: without du_next the gradients of the next norm's parameters are."""
         p, g = self.param, self.grad
         self._check(self.h_tdt, h=h, dy=dy)
         self._check(self.layer.tdt, du_next=du_next)
+        of_next = g.get("dnext_w"), g.get("dnext_b")
         B.moe_block_end_backward(dy, du_next, self.layer.dt, self.layer.y, B.MOE_F32, h, self.h_dt, self.T, self.d, self.post, p["post_w"], p["post_b"],
                                  p["gate"] if self.gate_rows else None, self.gate_rows, self.alpha, self.next, p["next_w"], self.end_stats, self.dv, self.dh,
-                                 *[g.get(n) for n in ("dpost_w", "dpost_b", "dgate", "dnext_w", "dnext_b")], self.ws, self.ws.numel(), stream)
+                                 *[g.get(n) for n in ("dpost_w", "dpost_b", "dgate")], *((None, None) if du_next is None else of_next), self.ws, self.ws.numel(), stream)
+        if du_next is None and of_next != (None, None):
+            # (gradients over no tokens: zero)
+            B.moe_norm_backward(None, self.layer.dt, None, self.h_dt, None, None, 0, self.d, self.next, None, None, *of_next, None, 0, stream)
         return self.dv, self.dh
 
     def pre_backward(self, h: torch.Tensor, du: torch.Tensor, stream=None) -> torch.Tensor:

@@ -151,6 +151,29 @@ def test_training_step(T, dt, h_dtype, post, next, gate):
     N.check("dpre_b", block.grad["dpre_b"], ref["dnext_b"])
 
 
+@pytest.mark.parametrize("T,post,next,gate", [(9, "rms", "rms", "token"), (130, "layer", "layer", "shared"), (40, "none", "rms", "none")])
+def test_training_step_without_a_gradient_of_the_next_norms_output(T, post, next, gate):
+    """du_next None is zero: all gradients as the formulas have them, those of the next norm's parameters zero."""
+    torch, B = N._torch()
+    print("[case] block training without du", T, post, next, gate, flush=True)
+    block, r = make_block(T, 192, 128, 6, 2, "bf16", T, 64, gate, post, next, train=True)
+    h, _ = N.to_dev(torch, 2.0 * r.standard_normal((T, 192)) + 0.2, block.h_dt)
+    dy, _ = N.to_dev(torch, r.standard_normal((T, 192)), block.h_dt)
+    block.forward(h)
+    for g in block.grad.values():
+        g.fill_(7.0)
+    dv, dh = block.end_backward(h, dy, None)
+    torch.cuda.synchronize()
+    ref = N.reference(dict(arguments(block, h, block.layer.y), dy=dy.float().cpu().numpy().astype(np.float64)))
+    N.check("dv", dv, ref["dv"])
+    N.check("dh", dh, ref["dh"], block.h_dt)
+    for n in ("dpost_w", "dpost_b", "dgate"):
+        assert (n in block.grad) == (n in ref)
+        if n in ref:
+            N.check(n, block.grad[n], ref[n])
+    assert not block.grad["dnext_w"].any() and not block.grad["dnext_b"].any()
+
+
 def test_refusals():
     torch, B = N._torch()
     block, _ = make_block(5, 192, 128, 6, 2, "bf16", 1)
