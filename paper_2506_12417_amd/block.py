@@ -53,6 +53,7 @@ class MoEBlock:
             self.ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
             self.dv = torch.empty((T, d), dtype=f32, device=dev)
             self.dh = torch.empty((T, d), dtype=self.h_tdt, device=dev)
+            self.pre_own = True              # whether the last forward() has run the pre norm
 
     def load(self, **arrays: np.ndarray):
         """Parameters by name (NAMES), fp32: [d], and the gate [d] or [T,d].  What is not loaded counts as ones (weights) or zeros."""
@@ -76,11 +77,12 @@ class MoEBlock:
 
     def forward(self, h: torch.Tensor, u: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """Enqueues the block; returns y and u' (None without a next norm), buffers of the block's own.  u: pre(h), where the block before has
-        made it as its u'."""
+        made it as its u' (its next norm stands in for this one's pre norm, and so it is in the backward calls: the gradient of u goes to that
+        block's end_backward as du_next, this one's dh as dy, and there is no pre_backward)."""
         L, p = self.layer, self.param
-        assert not (self.train and u is not None), "the pre norm's statistics come from its own call"
         self._check(self.h_tdt, h=h)
         self._check(L.tdt, u=u)
+        self.pre_own = u is None
         if u is None:
             B.moe_norm(h, self.h_dt, p["pre_w"], p["pre_b"], self.T, self.d, self.pre, self.eps, self.u, L.dt, self.pre_stats if self.train else None,
                        stream)
@@ -116,6 +118,8 @@ class MoEBlock:
         """From the gradient of u, as the layer's own backward gives it for dv, to h's whole gradient: end_backward's dh is added, in
         place."""
         p, g = self.param, self.grad
+        if not self.pre_own:
+            raise B.MoeError(B.MOE_ERR_ARG, "forward() was given u: its gradient is du_next of the block that has made it")
         self._check(self.h_tdt, h=h)
         self._check(self.layer.tdt, du=du)
         B.moe_norm_backward(du, self.layer.dt, h, self.h_dt, p["pre_w"], self.pre_stats, self.T, self.d, self.pre, self.dh, self.dh, g.get("dpre_w"),

@@ -174,6 +174,48 @@ def test_training_step_without_a_gradient_of_the_next_norms_output(T, post, next
     assert not block.grad["dnext_w"].any() and not block.grad["dnext_b"].any()
 
 
+@pytest.mark.parametrize("T,dt,h_dtype", [(9, "bf16", "bf16"), (333, "bf16", "f32"), (40, "f32", "f32")])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_two_trained_blocks(T, dt, h_dtype, norm):
+    """The first block's next norm is the second one's pre norm, forward and backward: dh and the gradient of u go back to the first block's end.
+    (Any gradients stand in for what the layers' own backward would give for dv.)"""
+    torch, B = N._torch()
+    d = 192
+    print("[case] two trained blocks", T, dt, h_dtype, norm, flush=True)
+    b1, r = make_block(T, d, 128, 6, 2, dt, T, 64, "shared", "rms", norm, train=True, h_dtype=h_dtype)
+    b2, _ = make_block(T, d, 64, 4, 2, dt, T + 1, 0, "token", "layer", "rms", train=True, h_dtype=h_dtype)
+    rows = lambda t: N.to_dev(torch, r.standard_normal((T, d)), t)[0]     # noqa: E731
+    np64 = lambda t: t.float().cpu().numpy().astype(np.float64)   # noqa: E731
+    h, dy2, du2, du_pre2, du_pre1 = rows(b1.h_dt), rows(b1.h_dt), *(rows(b1.layer.dt) for _ in range(3))
+    y1, u1 = b1.forward(h)
+    y2, u2 = b2.forward(y1, u=u1)
+    dv2, dh2 = b2.end_backward(y1, dy2, du2)
+    with pytest.raises(B.MoeError):
+        b2.pre_backward(y1, du_pre2)
+    dv1, dh1 = b1.end_backward(h, dh2, du_pre2)
+    torch.cuda.synchronize()
+    for b, into, dy, du, dv, dh in ((b2, y1, dy2, du2, dv2, dh2), (b1, h, dh2, du_pre2, dv1, dh1)):
+        ref = N.reference(dict(arguments(b, into, b.layer.y), dy=np64(dy), du=np64(du)))
+        N.check("y", b.y, ref["y"], b.h_dt)
+        N.check("dv", dv, ref["dv"])
+        N.check("dh", dh, ref["dh"], b.h_dt)
+        for n in ("dpost_w", "dpost_b", "dgate", "dnext_w", "dnext_b"):
+            N.check(n, b.grad[n], ref[n])
+    # the second block took u as it was given, and the first one has a pre norm of its own
+    v2 = b2.layer.y.clone()
+    assert torch.equal(v2, b2.layer.forward_few(u1) if T == 9 else b2.layer.forward(u1))
+    dh = dh1.clone()
+    dx = b1.pre_backward(h, du_pre1)
+    torch.cuda.synchronize()
+    a = arguments(b1, h, None)
+    ref = N.reference(dict(a, gate=None, next=b1.pre, next_w=a["pre_w"], next_b=a["pre_b"], dy=np64(dh), du=np64(du_pre1)))
+    N.check("dx", dx, ref["dh"], b1.h_dt)
+    N.check("dpre_w", b1.grad["dpre_w"], ref["dnext_w"])
+    b2.forward(y1)                                    # (a forward of its own again: pre_backward is there)
+    b2.pre_backward(y1, du_pre2)
+    torch.cuda.synchronize()
+
+
 def test_refusals():
     torch, B = N._torch()
     block, _ = make_block(5, 192, 128, 6, 2, "bf16", 1)
