@@ -45,6 +45,8 @@ class MoEBlock:
         self.u = torch.empty((T, d), dtype=layer.tdt, device=dev)
         self.y = torch.empty((T, d), dtype=self.h_tdt, device=dev)
         self.u_next = torch.empty((T, d), dtype=layer.tdt, device=dev) if self.next else None
+        # (trained, the block keeps v itself: the layer may run again, for another block or alone, before the backward calls)
+        self.v = torch.empty((T, d), dtype=f32, device=dev) if train else None
         if train:
             self.pre_stats = torch.empty((T, 2), dtype=f32, device=dev)
             self.end_stats = torch.empty((T, 4), dtype=f32, device=dev)
@@ -88,9 +90,9 @@ class MoEBlock:
                        stream)
             u = self.u
         if prefers_few(L):
-            L.forward_few(u, stream=stream)
+            L.forward_few(u, self.v, stream)
         elif self.train or L.fold_combine:
-            L.forward(u, stream=stream)
+            L.forward(u, stream, y=self.v)
         else:
             # the layer's combine in the same pass as what follows it: v is never stored
             L.forward(u, stream=stream, rows=True)
@@ -106,7 +108,7 @@ class MoEBlock:
         self._check(self.h_tdt, h=h, dy=dy)
         self._check(self.layer.tdt, du_next=du_next)
         of_next = g.get("dnext_w"), g.get("dnext_b")
-        B.moe_block_end_backward(dy, du_next, self.layer.dt, self.layer.y, B.MOE_F32, h, self.h_dt, self.T, self.d, self.post, p["post_w"], p["post_b"],
+        B.moe_block_end_backward(dy, du_next, self.layer.dt, self.v, B.MOE_F32, h, self.h_dt, self.T, self.d, self.post, p["post_w"], p["post_b"],
                                  p["gate"] if self.gate_rows else None, self.gate_rows, self.alpha, self.next, p["next_w"], self.end_stats, self.dv, self.dh,
                                  *[g.get(n) for n in ("dpost_w", "dpost_b", "dgate")], *((None, None) if du_next is None else of_next), self.ws, self.ws.numel(), stream)
         if du_next is None and of_next != (None, None):

@@ -104,7 +104,8 @@ class MoELayer:
         self.sched = torch.empty((E, n_bins), dtype=i32, device=dev)
         self.h = torch.empty((A, F), dtype=self.tdt, device=dev)
         self.y_perm = torch.empty((A, d), dtype=f32, device=dev)
-        self.y = torch.empty((T, d), dtype=f32, device=dev)
+        self.own_y = torch.empty((T, d), dtype=f32, device=dev)
+        self.y = self.own_y                  # the last call's output
         self.shared_F = shared_F
         # 256-row tiles: the library folds the gather and the scatter into the products of its
         # four-wavefront kernels (its default); its eight-wavefront kernels have no gather at this height
@@ -239,9 +240,11 @@ class MoELayer:
         packed).  y: [T,d] fp32 or bf16, None = the layer's own fp32 buffer.  The choice is forward()'s; the sums are added in
         another order, so the last bits differ."""
         assert self.few_ok and (self.packed_router or self.dt == B.MOE_F32), "sizes or router are not moe_layer_few's"
-        y = self.y if y is None else y
-        B.check_rows("x", x, self.T, self.d, (self.tdt,), self.y.device)
-        B.check_rows("y", y, self.T, self.d, (torch.float32, torch.bfloat16), self.y.device)
+        y = self.own_y if y is None else y
+        B.check_rows("x", x, self.T, self.d, (self.tdt,), self.own_y.device)
+        B.check_rows("y", y, self.T, self.d, (torch.float32, torch.bfloat16), self.own_y.device)
+        if y.dtype == torch.float32:
+            self.y = y
         g, s = self.experts, self.shared if self.shared_F else None
         w, norm2 = (self.W_gt, self.w_norm2) if self.dt == B.MOE_BF16 else (self.W_g, None)
         B.moe_layer_few(x, self.T, self.d, self.F, self.E, self.k, self.act, self.dt, self.renorm, w, norm2, self.bias, g.in_ptrs, g.out_ptrs,
@@ -249,8 +252,9 @@ class MoELayer:
                         self.few_ws, self.few_ws.numel(), y, B.MOE_F32 if y.dtype == torch.float32 else B.MOE_BF16, stream)
         return y
 
-    def forward(self, x: torch.Tensor, stream=None, marks=None, routed: bool = False, stages=None, rows: bool = False) -> torch.Tensor:
-        """Enqueues the whole layer on the current (or given) stream; returns the output buffer.
+    def forward(self, x: torch.Tensor, stream=None, marks=None, routed: bool = False, stages=None, rows: bool = False,
+                y: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Enqueues the whole layer on the current (or given) stream; returns the output buffer: y ([T,d] fp32), or the layer's own.
         A bf16 token's last bits depend on the number of tokens the layer is made for: calls with a
         handful of rows per expert run by kernels that add the contraction in another order
         (moe_ffn_kernel_mode 1 keeps to one order; it also gives up the four-wavefront kernels).
@@ -264,6 +268,9 @@ class MoELayer:
         rows: step 6 is left to the caller (moe_block_end_rows): y_perm, inv_perm, gate_w and s_y are what it adds up.  Not with
         fold_combine, where the second product has done it."""
         assert not (rows and self.fold_combine), "the second product makes y here"
+        if y is not None:
+            B.check_rows("y", y, self.T, self.d, (torch.float32,), self.own_y.device)
+        self.y = self.own_y if y is None else y
         mark = None
         if stages is not None:
             stream = None

@@ -216,6 +216,39 @@ def test_two_trained_blocks(T, dt, h_dtype, norm):
     torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("T,F,k,shared_F,dt", [(9, 128, 2, 64, "bf16"), (150, 128, 2, 64, "bf16"), (700, 512, 1, 0, "bf16"), (40, 128, 2, 0, "f32")])
+def test_a_layer_runs_again_before_the_backward_calls(T, F, k, shared_F, dt):
+    """The same layer in another trained block, and alone, by every form of its calls: the first block's gradients stay."""
+    torch, B = N._torch()
+    d = 256
+    print("[case] tied layer", T, F, k, shared_F, dt, flush=True)
+    b1, r = make_block(T, d, F, 6, k, dt, T, shared_F, "shared", "rms", "rms", train=True)
+    from paper_2506_12417_amd.block import MoEBlock
+    b2 = MoEBlock(b1.layer, post="rms", train=True)
+    L = b1.layer
+    rows = lambda t: N.to_dev(torch, r.standard_normal((T, d)), t)[0]     # noqa: E731
+    h, other, dy, du = rows(b1.h_dt), rows(b1.h_dt), rows(b1.h_dt), rows(L.dt)
+    b1.forward(h)
+    want = [t.clone() for t in (*b1.end_backward(h, dy, du), *(b1.grad[n] for n in ("dpost_w", "dgate", "dnext_w")))]
+    b1.forward(h)
+    y = L.y.clone()
+    b2.forward(other)
+    x = rows(L.dt)
+    alone = L.forward(x)
+    assert alone is L.y and alone is not b1.v and alone is not b2.v
+    if L.few_ok:
+        assert L.forward_few(x) is alone
+    got = [t.clone() for t in (*b1.end_backward(h, dy, du), *(b1.grad[n] for n in ("dpost_w", "dgate", "dnext_w")))]
+    torch.cuda.synchronize()
+    assert torch.equal(b1.v, y) and not torch.equal(b2.v, y) and not torch.equal(alone, y)
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    mine = torch.full((T, d), float("nan"), device="cuda")
+    assert L.forward(x, y=mine) is mine and L.y is mine
+    got = mine.clone()
+    torch.cuda.synchronize()
+    assert torch.equal(got, L.forward(x))
+
+
 def test_refusals():
     torch, B = N._torch()
     block, _ = make_block(5, 192, 128, 6, 2, "bf16", 1)
