@@ -18,12 +18,24 @@ NAMES = ("pre_w", "pre_b", "post_w", "post_b", "gate", "next_w", "next_b")
 
 
 def prefers_few(layer: MoELayer) -> bool:
-    """Whether one call serves the layer's tokens better than the separate ones.  Up to 32 bf16 tokens (us, this call / those): d=768 F=3072 E=128
-    k=1 one token 21 / 25, 16 tokens 44 / 51; d=2048 F=1408 E=60 k=4 with a shared expert 8 tokens 99 / 110; d=4096 F=14336 E=8 k=2 3 tokens
-    249 / 290; but narrow layers, from 20 tokens on: d=320 F=512 E=24 k=4 32 tokens 28 / 26.  Beyond, whole tiles of rows are worth a plan
-    (64 tokens of the last 35 / 29, of d=4096 522 / 491).  In fp32 the matrix instruction bounds both, and the line is at 16 (5 tokens of
-    d=320 F=1984 E=16 k=2 26 / 31, 16 tokens 38 / 40, 64 tokens 68 / 49)."""
-    return layer.few_ok and (layer.T <= 32 and layer.packed_router if layer.dt == B.MOE_BF16 else layer.T <= 16)
+    """Whether one call serves the layer's tokens better than the separate ones.  Measured: a block with the next norm, us by this call / by
+    those, in graphs over enough layers that no weight is in a cache.
+
+    16 bits, up to 16 tokens: d=768 F=3072 E=128 k=1 one token 27 / 32, 16 tokens 48 / 55; d=2048 F=1408 E=60 k=4 with a shared expert 8 tokens 103 / 119;
+    d=320 F=512 E=24 k=4 16 tokens 31 / 32, d=960 F=1472 E=8 k=2 41 / 39.  Up to 32 where they choose one expert each or d is beyond 1536: d=768 F=3072
+    62 / 71, d=1024 F=2048 E=4 k=1 28 / 32, d=2048 F=2048 E=8 k=2 52 / 58, d=2048 F=1408 164 / 177.  Not in narrower layers, where an expert's matrices
+    are fetched, or its rows multiplied, once for every range of tokens: d=512 F=512 E=24 k=4 39 / 36, d=512 F=2048 E=4 k=2 38 / 33, d=1536 F=768
+    E=32 k=4 72 / 69.  Beyond, whole tiles of rows are worth a plan.
+
+    fp32, up to 16 tokens: d=320 F=1984 E=16 k=2 5 tokens 30 / 35, 16 tokens 38 / 40; d=1536 F=1024 E=6 k=2 16 tokens 39 / 42.  The matrix instruction
+    bounds both, and where ranges of tokens share the columns (d up to 1024, more choices than one) that many products are the line: d=768 F=1536 E=16
+    k=4 6 tokens 51 / 53, 8 tokens 58 / 54; d=1024 F=2048 E=8 k=2 4 tokens 40 / 46, 8 tokens 50 / 50, 12 tokens 58 / 51."""
+    T, d, k = layer.T, layer.d, layer.k
+    if not layer.few_ok:
+        return False
+    if layer.dt == B.MOE_BF16:
+        return layer.packed_router and T <= (32 if k == 1 or d > 1536 else 16)
+    return T <= 16 and (k == 1 or d > 1024 or T * k * d * layer.F < 2 ** 25)
 
 
 class MoEBlock:

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from paper_2506_12417_amd import binding as B
-from paper_2506_12417_amd.block import MoEBlock
+from paper_2506_12417_amd.block import MoEBlock, prefers_few
 from paper_2506_12417_amd.layer import MoELayer
 
 T, D = 6, 64
@@ -64,3 +64,20 @@ def test_more_dimensions_and_one():
     b = block()
     for shape in ((2, 3, D), (T * D,), (T, D)):
         refused(b.forward, torch.zeros(shape), status=B.MOE_ERR_HIP)
+
+
+def test_the_choice_follows_what_was_measured():
+    """Sizes at which one form took at least 3 % longer than the other: that one is not chosen."""
+    for few, sizes in ((True, ((1, 320, 512, 24, 4, "bf16"), (8, 320, 512, 24, 4, "bf16"), (8, 512, 512, 24, 4, "bf16"), (32, 768, 3072, 128, 1, "bf16"),
+                               (24, 1024, 2048, 4, 1, "bf16"), (32, 2048, 2048, 8, 2, "bf16"), (32, 2048, 1408, 60, 4, "bf16"), (16, 1536, 768, 32, 4, "bf16"),
+                               (16, 320, 1984, 16, 2, "f32"), (16, 1536, 1024, 6, 2, "f32"), (16, 1024, 2048, 8, 1, "f32"), (4, 1024, 2048, 8, 2, "f32"),
+                               (6, 768, 1536, 16, 4, "f32"))),
+                       (False, ((32, 320, 512, 24, 4, "bf16"), (32, 512, 512, 24, 4, "bf16"), (32, 768, 512, 16, 2, "bf16"), (24, 1088, 704, 24, 4, "bf16"),
+                                (32, 1536, 768, 32, 4, "bf16"), (32, 512, 2048, 4, 2, "bf16"), (64, 4096, 14336, 8, 2, "bf16"), (64, 320, 512, 24, 4, "bf16"),
+                                (12, 1024, 2048, 8, 2, "f32"), (16, 1024, 2048, 32, 2, "f32"), (8, 768, 1536, 16, 4, "f32"), (64, 320, 1984, 16, 2, "f32")))):
+        for T, d, F, E, k, dtype in sizes:
+            layer = MoELayer(T, d, F, E, k, "swiglu", dtype, 0, device="meta")
+            layer.packed_router = dtype == "bf16"
+            assert prefers_few(layer) == few, (T, d, F, E, k, dtype)
+    layer = MoELayer(4, 320, 512, 8, 2, "swiglu", "bf16", 0, device="meta")
+    assert not prefers_few(layer)                     # (its router is not packed)
