@@ -28,8 +28,8 @@ def prefers_few(layer: MoELayer) -> bool:
     E=32 k=4 72 / 69.  Beyond, whole tiles of rows are worth a plan.
 
     fp32, up to 16 tokens: d=320 F=1984 E=16 k=2 5 tokens 30 / 35, 16 tokens 38 / 40; d=1536 F=1024 E=6 k=2 16 tokens 39 / 42.  The matrix instruction
-    bounds both, and where ranges of tokens share the columns (d up to 1024, more choices than one) that many products are the line: d=768 F=1536 E=16
-    k=4 6 tokens 51 / 53, 8 tokens 58 / 54; d=1024 F=2048 E=8 k=2 4 tokens 40 / 46, 8 tokens 50 / 50, 12 tokens 58 / 51."""
+    bounds both, and where ranges of tokens share the columns (d up to 1024, more choices than one) 2^25 multiply-adds a matrix, all rows counted, are
+    the line: d=768 F=1536 E=16 k=4 6 tokens 51 / 53, 8 tokens 58 / 54; d=1024 F=2048 E=8 k=2 4 tokens 40 / 46, 8 tokens 50 / 50, 12 tokens 58 / 51."""
     T, d, k = layer.T, layer.d, layer.k
     if not layer.few_ok:
         return False

@@ -18,13 +18,16 @@
 // sums per token of its own in LDS, and these are added in a fixed order.  So the combine costs no pass over memory, no atomics and no
 // launch of its own, and all CUs read equal shares of the weights whatever the routing.
 //
+// The hidden activations are the second product's operands, and so IEEE half in 16 bits (11 significant bits; bf16 would be eight times coarser): that
+// rounding is 2.0e-4 of y's norm, and changes the last bit of one bf16 output in thirty (whose own rounding is 1.65e-3 of the norm).
+//
 // Weights and rows come in whole 128-byte lines, eight rows a load, several lines in flight per wavefront, and
 // are turned into the matrix instruction's fragments in a piece of LDS of the wavefront's own (fragments straight from global memory touch 16
 // lines per quarter wavefront instead of 2, and the vector cache is then what a CU waits for).
 //
-// Measured, us for launches 1 and 2 (weights of the chosen experts, TB/s): d=768 F=3072 E=128 k=1 one token 14.1 + 6.0 (9.4 MB), 8 tokens
-// 19.1 + 11.1 (69 MB, 2.3); d=4096 F=14336 E=8 k=2, 3 tokens 150 + 69 (1.4 GB, 6.4; 5.6 where they lie elsewhere); d=2048 F=1408 E=60 k=4 with a
-// shared expert of 5632, 33 tokens 11.3 + 88 + 53 with the routing (825 MB, 5.4); fp32 d=320 F=1984 E=16 k=2, 5 tokens 4.6 + 12.7 + 7.3.
+// Measured, us for launches 1 and 2 (medians of 50; weights of the chosen experts, TB/s): d=768 F=3072 E=128 k=1 one token 14.4 + 6.6 (9.4 MB), 8 tokens
+// 19.5 + 11.6 (69 MB, 2.2); d=4096 F=14336 E=8 k=2, 3 tokens 153 + 70 (1.4 GB, 6.3; 5.6 where they lie elsewhere); d=2048 F=1408 E=60 k=4 with a
+// shared expert of 5632, 33 tokens 12 + 92 + 56 with the routing (825 MB, 5.2); fp32 d=320 F=1984 E=16 k=2, 5 tokens 4.7 + 13.6 + 7.8.
 // One token, launch 1: logits 4.9, their sums and the choice 3.5, lists 0.7, product 3.
 #include <climits>
 #include <type_traits>
@@ -1185,7 +1188,8 @@ extern "C" int moe_layer_few(const void* x, int T, int d, int F, int E, int k, m
     o.pairs = ranges && h_lds && range <= 8;
     // A shared expert whose first matrices take as long to fetch as a launch (16 MB, three microseconds) is worked on while a few work-groups
     // route: d=2048 F=1408 E=60 k=4 shared 5632 (46 MB), us without / with: 1 token 42.9 / 39.7, 9 tokens 106 / 101, 16 tokens 134 / 133, 24
-    // tokens 149 / 153 (the routing's loads wait behind the others); d=1152 shared 1600 (7 MB), 4 tokens 29.9 / 31.0.
+    // tokens 149 / 153 (the routing's loads wait behind the others); d=1152 shared 1600 (7 MB), 4 tokens 29.9 / 31.0.  Eight layers of 17 to 168 MB and
+    // d=1024 to 7168, 1 to 16 tokens: with / without 0.96 on the average, 0.80 to 1.06 (d=1024 1.03, d=7168 0.90).
     const bool beside = T <= 16 && (size_t)shared_F * 2 * d * es >= (16u << 20);
     if (dt == MOE_F32) {
         const int rc = moe_route_topk(x, w_gate, bias, T, d, E, k, renorm, dt, expert_idx, gate_w, nullptr, stream);

@@ -14,13 +14,15 @@
 // held in registers, eight values a thread, so that every tensor is read once and the statistics take two passes over registers
 // (mean first, then squares of the differences).  A work-group keeps its columns of the parameters in registers and goes over
 // rows, the next row's loads under way while the present one is summed up (at a block's end, backward, rows of more than 4096
-// values leave a thread no registers for either: they fetch the parameters again for every row, 4096 x 8192 in 195 us).  All
+// values leave a thread no registers for either: they fetch the parameters again for every row, 4096 x 8192 in 200 us).  All
 // arithmetic is fp32; the outputs are rounded once, and u is made of the unrounded y.  The parameters' gradients are summed over a work-group's rows in registers, written
 // to the workspace and added up by a second launch in a fixed order: no atomics.
 //
-// Measured: 16384 x 2048, 16-bit, LAYER, 26 us forward (134 MB, 5.2 TB/s; a copy of 1 GiB reaches 5.2) and 47 + 6 backward with the residual
-// stream's gradient (268 MB, 5.7); 8192 x 4096, both norms, 50 forward (268 MB, 5.4) and 75 + 6 backward (402 MB, 5.4); the rows form,
-// 8192 x 2048 with four experts' rows and a shared one each, 85 (438 MB, 5.2); 1501 x 777 fp32 4.2, 5.7 + 3.6; 33 x 2048 3 - 4.
+// Measured (medians of 50 launches, each by itself; the least are up to a fifth shorter): 16384 x 2048, 16-bit, LAYER, 29 us forward (134 MB, 4.6 TB/s; a copy
+// of 1 GiB reaches 5.2) and 51 + 7 backward with the residual stream's gradient (268 MB, 5.3); 8192 x 4096, both norms, 58 forward (268 MB, 4.7) and
+// 78 + 7 backward (402 MB, 5.2); the rows form with four experts' rows and a shared one each, 8192 x 2048 88 (438 MB, 5.0), 2048 x 8192 the
+// same, 33 x 2048 4.2; 1501 x 777 fp32 4.2, 5.8 + 4.4; 33 x 2048 3 - 3.5.  Beyond 4096 columns, 8192 x 5120, 7168 and 8192 forward 47, 64, 61 and
+// backward 67, 133, 102 (+ 8); both norms, 4096 rows of these, 50, 52, 56 and 104, 170, 200 (+ 6).
 #include "common.h"
 #include "gemm_util.h"
 #include <climits>
@@ -49,7 +51,7 @@ template <bool VEC> __device__ __forceinline__ int column(int i) {
 
 // All goes through buffer loads and stores: what lies past the row's d values, or in a row that is not there (`on` false), reads as zero or
 // is not written, without a branch; behind branches with loads in them the compiler waits for all that is under way, the next row's
-// loads included (8192 x 4096, both norms: 61 forward + 91 us backward, against 50 + 76).
+// loads included (8192 x 4096, both norms, the least of 50: 61 forward + 91 us backward, against 50 + 76).
 template <typename E, bool VEC> struct Held;
 template <> struct Held<float, true> {
     f32x4 a, b;
