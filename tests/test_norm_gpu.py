@@ -259,6 +259,55 @@ def test_rows_form_of_many_rows(T, d, k):
     assert torch.isfinite(y).all() and torch.isfinite(u).all() and torch.equal(y, y2) and torch.equal(u, u2)
 
 
+def test_rows_beyond_what_32_bits_reach():
+    """Tensors of more than 2^31 values and 4 GiB: the last rows' bits, and those of the first, are those of a call on these rows alone."""
+    torch, B = _torch()
+    T, d, n = 1 << 20, 2056, 5
+    print("[case] long tensors", T, d, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    new = lambda *shape, dt=torch.bfloat16: torch.empty(shape, dtype=dt, device="cuda").normal_(generator=g)    # noqa: E731
+    w, b = new(d, dt=torch.float32), new(d, dt=torch.float32)
+    ws = torch.empty(B.moe_workspace_bytes(B.MOE_OP_NORM_BACKWARD, T, d, 0, 0, 0, 0), dtype=torch.uint8, device="cuda")
+    x, du = new(T, d), new(T, d)
+    assert x.numel() > 2 ** 31 and x.numel() * 2 > 2 ** 32
+
+    def norms(x, du):
+        t = x.shape[0]
+        u, dx, stats, db = torch.empty_like(x), torch.empty_like(x), torch.empty((t, 2), device="cuda"), torch.empty(d, device="cuda")
+        B.moe_norm(x, BF16, w, b, t, d, LAYER, EPS, u, BF16, stats)
+        B.moe_norm_backward(du, BF16, x, BF16, w, stats, t, d, LAYER, du, dx, None, db, ws, ws.numel())
+        torch.cuda.synchronize()
+        return u, dx, stats, db
+
+    whole = norms(x, du)
+    for part in (slice(0, n), slice(T - n, T)):
+        alone = norms(x[part].clone(), du[part].clone())
+        assert all(torch.equal(a[part], p) for a, p in zip(whole[:3], alone[:3]))
+    # (a thread adds up T / 1024 rows, then 64 + 16 parts follow: as many roundings in a row)
+    total = sum(du[i:i + 65536].double().sum(0) for i in range(0, T, 65536))
+    size = sum(du[i:i + 65536].double().abs().sum(0) for i in range(0, T, 65536))
+    assert ((whole[3].double() - total).abs() <= (T // 1024 + 80) * 2.0 ** -24 * size).all()
+    del whole, du
+    # the rows form: experts' rows of 8 GiB, those of the last tokens anywhere in them
+    k, tokens = 2, T // 2
+    rows, inv = new(T, d, dt=torch.float32), torch.randperm(T, generator=g, device="cuda").int()
+    inv[-2 * n:] = torch.arange(T - 2 * n, T, device="cuda").int()
+    gw, h = new(tokens, k, dt=torch.float32), x[:tokens]
+
+    def ends(inv, gw, h, shared):
+        t = h.shape[0]
+        y, u = torch.empty_like(h), torch.empty_like(h)
+        B.moe_block_end_rows(rows, inv, gw, shared, k, h, BF16, t, d, RMS, EPS, w, None, None, 0, 0.5, LAYER, EPS, w, b, y, u, BF16)
+        torch.cuda.synchronize()
+        return y, u
+
+    shared = new(tokens, d, dt=torch.float32)
+    whole = ends(inv, gw, h, shared)
+    for part in (slice(0, n), slice(tokens - n, tokens)):
+        alone = ends(inv[part.start * k:part.stop * k].clone(), gw[part].clone(), h[part].clone(), shared[part].clone())
+        assert all(torch.equal(a[part], p) and torch.isfinite(p).all() for a, p in zip(whole, alone))
+
+
 def test_many_rows_do_not_touch_one_another():
     """A row of NaN, of infinities or of zeros between others that the same work-group goes over leaves these alone."""
     torch, B = _torch()
