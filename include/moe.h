@@ -461,6 +461,102 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
                           const float* shared, int T, int d, int k, float* y, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * A training step of the layer: activations kept in 8 bits for the backward pass, and the gradients of steps 1, 4, 5 and 6.
+ *
+ *   forward    moe_route_topk* (with logits_out), the sort, moe_grouped_ffn_keep, moe_grouped_ffn_phase(2) (or its top-1 form), moe_unpermute_combine
+ *   backward   moe_grouped_ffn_backward, moe_permute_backward, moe_route_topk_backward; where the experts run elsewhere
+ *              moe_unpermute_combine_backward gives the gradients of their outputs
+ *
+ * Gradients are summed in a fixed order: the same call gives the same bits.
+ *
+ * Kept in 8 bits: 64 neighbouring columns of a row (fewer at its end) share a scale,
+ *
+ *   m = the largest |v| of the 64      scale = m / 127      q = 127 v / m to the nearest integer      read back: q * scale
+ *
+ * so that a value is off by at most m / 254.  Where one of the 64 is NaN or infinite all of them read back as NaN; where m is below 2^-100
+ * as 0.
+ *   x [rows,n] dt, any n and any alignment      q [rows,n] int8      scale [rows, ceil(n / 64)] fp32
+ * rows = 0 is a no-op.  No output may overlap an input.
+ */
+MOE_API int moe_keep_rows(const void* x, moe_dtype dt, long long rows, int n, int8_t* q, float* scale, void* stream);
+MOE_API int moe_keep_restore(const int8_t* q, const float* scale, long long rows, int n, void* x, moe_dtype dt, void* stream);
+
+/* The first product of moe_grouped_ffn, which keeps its result z for the backward pass.  With r, e, t as there and Z = F (MOE_RELU) or 2F (MOE_SWIGLU):
+ *
+ *   z[r] = x[perm[r] / k] W_in_e  (MOE_SWIGLU: F gates, then F ups)      h_scratch[r] = relu(z), or silu(gate) * up, as moe_grouped_ffn has it
+ *   z_q, z_scale = z in 8 bits as above; with MOE_RELU relu(z), where a value above zero is kept as at least one step of its scale, so that the
+ *   activation's slope is not lost (in a block whose largest value is at least 2^-100)
+ *
+ *   x [T,d] dt      w_in: as moe_grouped_ffn      offsets [E+1], perm [A]: from the sort      h_scratch [A,F] 2 bytes a value, out: what
+ *   moe_grouped_ffn_phase(2) reads      z_q [A,Z] int8 out      z_scale [A,Z/64] fp32 out
+ * No plan is needed.  Rows behind offsets[E] are left as they were.  MOE_BF16 only, d and F multiples of 64, x, h_scratch, z_q and
+ * matrices aligned to 16 bytes, x smaller than 4 GiB.  T = 0 is a no-op.
+ */
+MOE_API int moe_grouped_ffn_keep(const void* x, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt,
+                                 const void* const* w_in, const int32_t* offsets, const int32_t* perm,
+                                 void* h_scratch, int8_t* z_q, float* z_scale, void* stream);
+
+/* The gradients of steps 5 and 6 together: y[t] = sum_j gate_w[t,j] FFN_e(x[t]), given dy and what moe_grouped_ffn_keep has kept.  Row r of expert e is
+ * assignment a = perm[r] of token t = a / k:
+ *
+ *   s = dy[t] W_out_e^T                            dgate_w[a] = sum_f h[f] s[f]     (h: formed again from z)
+ *   dz = gate_w[a] s times the activation's slope    dx_perm[r] = dz W_in_e^T
+ *   dW_in_e = sum_r x[t]^T dz[r]                   dW_out_e = sum_r (gate_w[a] h[r])^T dy[t]
+ *
+ *   dy [T,d] dy_dt      x [T,d] dt      gate_w [T,k] fp32 or NULL (all ones)
+ *   w_a, w_b [E,d,F], w_o [E,F,d] dt: the matrices as given to moe_pack_weights and moe_pack_w_out (w_b NULL with MOE_RELU)
+ *   dx_perm [A,d] fp32 out or NULL: moe_permute_backward adds a token's rows up
+ *   dgate_w [T,k] fp32 out or NULL (0 where inv_perm is negative: that assignment has no row)
+ *   dw_a, dw_b, dw_o dw_dt out, or all NULL; experts without rows get zeros.  accumulate != 0: added to what is there (a bf16 gradient
+ *           is then rounded once a call)
+ *   ws: moe_workspace_bytes(MOE_OP_FFN_BACKWARD, T, d, F, E, k, dt) bytes at most (MOE_RELU and dy in bf16 take less): dz and gate_w h, which
+ *           are rounded once, to bf16, as dy is where it is fp32, and sums
+ * Rows of dx_perm behind offsets[E] are left as they were.  MOE_BF16 only (dy_dt and dw_dt may be MOE_F32), d and F multiples of 64, pointers aligned to 16
+ * bytes (index arrays, gate_w and scales to 4), x smaller than 4 GiB.  T = 0 sets the matrices' gradients to zero, unless it accumulates.
+ */
+MOE_API int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const void* x, int T, int d, int F, int E, int k,
+                                     moe_act act, moe_dtype dt, const void* w_a, const void* w_b, const void* w_o,
+                                     const int32_t* offsets, const int32_t* perm, const int32_t* inv_perm,
+                                     const float* gate_w, const int8_t* z_q, const float* z_scale,
+                                     float* dx_perm, float* dgate_w, void* dw_a, void* dw_b, void* dw_o, moe_dtype dw_dt,
+                                     int accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/* The gradients of moe_unpermute_combine (those of `shared` are dy itself) and of moe_permute's row gather, r = inv_perm[t k + j]:
+ *
+ *   dy_perm[r] = gate_w[t,j] dy[t]      dgate_w[t,j] = sum_c dy[t,c] y_perm[r,c]      dx[t] = dx_add[t] + sum_j dx_perm[r]
+ *
+ *   dy [T,d] dy_dt      y_perm [A,d] fp32 (NULL without dgate_w)      gate_w [T,k] fp32 or NULL (all ones)
+ *   dy_perm [A,d] perm_dt out or NULL      dgate_w [T,k] fp32 out or NULL      dx_add [T,d] fp32 or NULL      dx [T,d] dx_dt out
+ * A negative inv_perm entry has no row: dgate_w is 0 there, and it adds nothing to dx.  Any d, any alignment.  dx may be dx_add (both fp32); no
+ * other output may overlap an input.  T = 0 is a no-op.
+ */
+MOE_API int moe_unpermute_combine_backward(const void* dy, moe_dtype dy_dt, const float* y_perm, const int32_t* inv_perm,
+                                           const float* gate_w, int T, int d, int k, void* dy_perm, moe_dtype perm_dt,
+                                           float* dgate_w, void* stream);
+MOE_API int moe_permute_backward(const float* dx_perm, const int32_t* inv_perm, int T, int d, int k, const float* dx_add,
+                                 void* dx, moe_dtype dx_dt, void* stream);
+
+/* The gradients of moe_route_topk, the choice itself being constant: with D = sum_j gate_w[t,j] dgate_w[t,j],
+ *
+ *   renorm == 0: dlogits[t,e] = p_e ([e chosen as j] dgate_w[t,j] - D),  p = softmax of logits[t]
+ *   renorm != 0: dlogits[t,e] = gate_w[t,j] (dgate_w[t,j] - D) for the chosen, 0 for the others
+ *   dlogits += dlogits_add  (the gradient of a loss on the logits themselves)
+ *   dx = dx_add + dlogits w_gate^T      dw_gate = x^T dlogits      dbias = sum_t dlogits
+ *
+ *   dgate_w, gate_w [T,k] fp32      expert_idx [T,k]      logits [T,E] fp32: logits_out of moe_route_topk (NULL with renorm)
+ *   dlogits_add [T,E] fp32 or NULL      x [T,d] dt (NULL without dw_gate)      w_gate [d,E] dt as given (NULL without dx)
+ *   dlogits [T,E] fp32 out      dx_add [T,d] fp32 or NULL      dx [T,d] fp32 out or NULL (may be dx_add)
+ *   dw_gate [d,E] fp32 out or NULL      dbias [E] fp32 out or NULL
+ *   ws: moe_workspace_bytes(MOE_OP_ROUTE_BACKWARD, T, d, 0, E, 0, dt) bytes; none and NULL without dw_gate and dbias
+ * Both products are fp32 throughout.  A token with an expert_idx outside [0,E) has a row of NaN.
+ * Requires what moe_route_topk requires, dx and dx_add aligned to 16 bytes, T <= 64 * 65535.  T = 0 sets dw_gate and dbias to zero.
+ */
+MOE_API int moe_route_topk_backward(const float* dgate_w, const float* gate_w, const int32_t* expert_idx, const float* logits,
+                                    const float* dlogits_add, const void* x, const void* w_gate, int T, int d, int E, int k,
+                                    int renorm, moe_dtype dt, float* dlogits, const float* dx_add, float* dx,
+                                    float* dw_gate, float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * The whole layer for a few tokens (a decode step), in two or three launches: routing, expert FFNs, the shared expert and the
  * weighted sum, all that moe_route_topk ... moe_unpermute_combine compute, without a sort, a plan or rows in between.
  *
@@ -607,7 +703,7 @@ MOE_API int moe_set_expert_pointers(const void** w_in, const void** w_out, int E
 MOE_API int moe_token_threshold(double phi, int d_type, double beta);
 
 /* Scratch sizes.  op selects the call. */
-enum { MOE_OP_PERMUTE = 1, MOE_OP_NORM_BACKWARD = 2, MOE_OP_BLOCK_END_BACKWARD = 3 };
+enum { MOE_OP_PERMUTE = 1, MOE_OP_NORM_BACKWARD = 2, MOE_OP_BLOCK_END_BACKWARD = 3, MOE_OP_FFN_BACKWARD = 4, MOE_OP_ROUTE_BACKWARD = 5 };
 MOE_API size_t moe_workspace_bytes(int op, int T, int d, int F, int E, int k, moe_dtype dt);
 
 /* Diagnostic: a plain device-to-device copy of `bytes` bytes (a multiple of 16; src and dst

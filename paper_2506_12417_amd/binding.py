@@ -26,7 +26,7 @@ MOE_PLAN_BALANCED, MOE_PLAN_HARMOENY, MOE_PLAN_STATIC, MOE_PLAN_EVEN_SPLIT, MOE_
 MOE_MAX_EXPERTS, MOE_MAX_TOPK, MOE_MAX_BINS = 256, 8, 16
 MOE_PLAN_HDR_CTR = 4 + 2 * (MOE_MAX_BINS + 1)
 MOE_PLAN_HDR_INTS = MOE_PLAN_HDR_CTR + MOE_MAX_BINS + 1
-MOE_OP_PERMUTE, MOE_OP_NORM_BACKWARD, MOE_OP_BLOCK_END_BACKWARD = 1, 2, 3
+MOE_OP_PERMUTE, MOE_OP_NORM_BACKWARD, MOE_OP_BLOCK_END_BACKWARD, MOE_OP_FFN_BACKWARD, MOE_OP_ROUTE_BACKWARD = 1, 2, 3, 4, 5
 MOE_FEW_MAX_T = 64
 MOE_NORM_NONE, MOE_NORM_RMS, MOE_NORM_LAYER = 0, 1, 2
 MOE_NORM_MAX_D, MOE_NORM_ANY_D = 8192, 4096
@@ -37,7 +37,9 @@ MOE_TILE_WHOLE_PLAN = 0x10000
 EXPORTS = [
     "moe_route_topk", "moe_pack_router", "moe_route_topk_packed", "moe_permute", "moe_permute_static", "moe_plan_capacity", "moe_plan_tiles", "moe_permute_plan", "moe_plan_tiles_subset", "moe_rebalance", "moe_pack_weights", "moe_pack_w_out",
     "moe_ffn_tile_m", "moe_ffn_pick_tile_m", "moe_ffn_kernel_mode", "moe_ffn_pairs", "moe_grouped_ffn", "moe_grouped_ffn_phase", "moe_grouped_ffn_top1", "moe_grouped_ffn_top1_phase", "moe_grouped_ffn_fused", "moe_grouped_ffn_fused_phase", "moe_grouped_ffn_shared", "moe_grouped_ffn_shared_phase", "moe_grouped_ffn_gather", "moe_grouped_ffn_gather_phase", "moe_unpermute_combine",
-    "moe_layer_few", "moe_layer_few_workspace", "moe_norm", "moe_norm_backward", "moe_block_end", "moe_block_end_rows", "moe_block_end_backward", "moe_prefetch_create",
+    "moe_layer_few", "moe_layer_few_workspace", "moe_norm", "moe_norm_backward", "moe_block_end", "moe_block_end_rows", "moe_block_end_backward",
+    "moe_keep_rows", "moe_keep_restore", "moe_grouped_ffn_keep", "moe_grouped_ffn_backward", "moe_unpermute_combine_backward", "moe_permute_backward",
+    "moe_route_topk_backward", "moe_prefetch_create",
     "moe_prefetch_experts", "moe_set_expert_pointers", "moe_prefetch_wait", "moe_prefetch_release", "moe_prefetch_reset", "moe_prefetch_destroy",
     "moe_token_threshold", "moe_workspace_bytes", "moe_copy_bytes", "moe_last_error", "moe_version",
 ]
@@ -79,6 +81,13 @@ _norms = [_i, _f, _vp, _vp, _vp, _i, _f, _i, _f, _vp, _vp]
 lib.moe_block_end.argtypes = [_vp, _i, _vp, _i, _i, _i] + _norms + [_vp, _vp, _i, _vp, _vp]
 lib.moe_block_end_rows.argtypes = [_vp, _vp, _vp, _vp, _i, _vp, _i, _i, _i] + _norms + [_vp, _vp, _i, _vp]
 lib.moe_block_end_backward.argtypes = [_vp, _vp, _i, _vp, _i, _vp, _i, _i, _i, _i, _vp, _vp, _vp, _i, _f, _i] + [_vp] * 10 + [_sz, _vp]
+lib.moe_keep_rows.argtypes = [_vp, _i, C.c_longlong, _i, _vp, _vp, _vp]
+lib.moe_keep_restore.argtypes = [_vp, _vp, C.c_longlong, _i, _vp, _i, _vp]
+lib.moe_grouped_ffn_keep.argtypes = [_vp] + [_i] * 7 + [_vp] * 7
+lib.moe_grouped_ffn_backward.argtypes = [_vp, _i, _vp] + [_i] * 7 + [_vp] * 14 + [_i, _i, _vp, _sz, _vp]
+lib.moe_unpermute_combine_backward.argtypes = [_vp, _i, _vp, _vp, _vp, _i, _i, _i, _vp, _i, _vp, _vp]
+lib.moe_permute_backward.argtypes = [_vp, _vp, _i, _i, _i, _vp, _vp, _i, _vp]
+lib.moe_route_topk_backward.argtypes = [_vp] * 7 + [_i] * 6 + [_vp] * 6 + [_sz, _vp]
 lib.moe_prefetch_create.argtypes = [C.POINTER(_vp), _i, _sz, _vp]
 lib.moe_prefetch_experts.argtypes = [_vp, C.POINTER(C.c_int32), _i, C.POINTER(_vp), _sz, C.POINTER(_vp)]
 lib.moe_set_expert_pointers.argtypes = [_vp, _vp, _i, C.POINTER(C.c_int32), _i, C.POINTER(_vp), _sz, _vp]
@@ -359,6 +368,41 @@ def moe_block_end_backward(dy, du, u_dt, v, v_dt, h, h_dt, T, d, post_kind, post
     _check(lib.moe_block_end_backward(_d(dy), _d(du), u_dt, _d(v), v_dt, _d(h), h_dt, T, d, post_kind, _d(post_w), _d(post_b), _d(gate),
                                       gate_rows, alpha, next_kind, _d(next_w), _d(stats), _d(dv), _d(dh), _d(dpost_w), _d(dpost_b),
                                       _d(dgate), _d(dnext_w), _d(dnext_b), _d(ws), ws_bytes, _stream(stream)))
+
+
+def moe_keep_rows(x, dt, rows, n, q, scale, stream=None):
+    _check(lib.moe_keep_rows(_d(x), dt, rows, n, _d(q), _d(scale), _stream(stream)))
+
+
+def moe_keep_restore(q, scale, rows, n, x, dt, stream=None):
+    _check(lib.moe_keep_restore(_d(q), _d(scale), rows, n, _d(x), dt, _stream(stream)))
+
+
+def moe_grouped_ffn_keep(x, T, d, F, E, k, act, dt, w_in, offsets, perm, h_scratch, z_q, z_scale, stream=None):
+    _check(lib.moe_grouped_ffn_keep(_d(x), T, d, F, E, k, act, dt, _d(w_in), _d(offsets), _d(perm), _d(h_scratch), _d(z_q), _d(z_scale),
+                                    _stream(stream)))
+
+
+def moe_grouped_ffn_backward(dy, dy_dt, x, T, d, F, E, k, act, dt, w_a, w_b, w_o, offsets, perm, inv_perm, gate_w, z_q, z_scale, dx_perm, dgate_w,
+                             dw_a, dw_b, dw_o, dw_dt, accumulate, ws, ws_bytes, stream=None):
+    _check(lib.moe_grouped_ffn_backward(_d(dy), dy_dt, _d(x), T, d, F, E, k, act, dt, _d(w_a), _d(w_b), _d(w_o), _d(offsets), _d(perm), _d(inv_perm),
+                                        _d(gate_w), _d(z_q), _d(z_scale), _d(dx_perm), _d(dgate_w), _d(dw_a), _d(dw_b), _d(dw_o), dw_dt, accumulate,
+                                        _d(ws), ws_bytes, _stream(stream)))
+
+
+def moe_unpermute_combine_backward(dy, dy_dt, y_perm, inv_perm, gate_w, T, d, k, dy_perm, perm_dt, dgate_w, stream=None):
+    _check(lib.moe_unpermute_combine_backward(_d(dy), dy_dt, _d(y_perm), _d(inv_perm), _d(gate_w), T, d, k, _d(dy_perm), perm_dt, _d(dgate_w),
+                                              _stream(stream)))
+
+
+def moe_permute_backward(dx_perm, inv_perm, T, d, k, dx_add, dx, dx_dt, stream=None):
+    _check(lib.moe_permute_backward(_d(dx_perm), _d(inv_perm), T, d, k, _d(dx_add), _d(dx), dx_dt, _stream(stream)))
+
+
+def moe_route_topk_backward(dgate_w, gate_w, expert_idx, logits, dlogits_add, x, w_gate, T, d, E, k, renorm, dt, dlogits, dx_add, dx, dw_gate, dbias,
+                            ws, ws_bytes, stream=None):
+    _check(lib.moe_route_topk_backward(_d(dgate_w), _d(gate_w), _d(expert_idx), _d(logits), _d(dlogits_add), _d(x), _d(w_gate), T, d, E, k, renorm, dt,
+                                       _d(dlogits), _d(dx_add), _d(dx), _d(dw_gate), _d(dbias), _d(ws), ws_bytes, _stream(stream)))
 
 
 def moe_copy_bytes(src, dst, nbytes: int, stream=None):

@@ -41,7 +41,7 @@ def prefers_few(layer: MoELayer) -> bool:
 class MoEBlock:
     """pre, post, next: "rms", "layer" or "none" (pre always is one; next is the norm of the block behind, whose u' comes out here).
     h_dtype: the residual stream's type; the layer's own is u's.  gate: "none", "shared" (one row of d factors) or "token" (a row for every
-    token).  train: forward() keeps what the backward calls read, and v is stored for them."""
+    token).  train: forward() keeps what the backward calls read, and v is stored for them; with a layer that trains, backward() makes all gradients."""
 
     def __init__(self, layer: MoELayer, pre: str = "rms", post: str = "none", next: str = "none", eps: float = 1e-5, alpha: float = 1.0,
                  gate: str = "none", h_dtype: str = "bf16", train: bool = False):
@@ -101,7 +101,8 @@ class MoEBlock:
             B.moe_norm(h, self.h_dt, p["pre_w"], p["pre_b"], self.T, self.d, self.pre, self.eps, self.u, L.dt, self.pre_stats if self.train else None,
                        stream)
             u = self.u
-        if prefers_few(L):
+        self.u_in = u
+        if prefers_few(L) and not L.train:
             L.forward_few(u, self.v, stream)
         elif self.train or L.fold_combine:
             L.forward(u, stream, y=self.v)
@@ -139,3 +140,12 @@ class MoEBlock:
         B.moe_norm_backward(du, self.layer.dt, h, self.h_dt, p["pre_w"], self.pre_stats, self.T, self.d, self.pre, self.dh, self.dh, g.get("dpre_w"),
                             g.get("dpre_b"), self.ws, self.ws.numel(), stream)
         return self.dh
+
+    def backward(self, h: torch.Tensor, dy: Optional[torch.Tensor], du_next: Optional[torch.Tensor], accumulate: bool = False,
+                 stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
+        """The whole block's gradients, with a layer that trains (MoELayer(train=True)): from those of y and u' to h's (a buffer of the block's) and
+        None; or, where forward() was given u, to what the residual connection passes on to h and the gradient of u (du_next of the block that
+        has made it).  Parameters' gradients go to `grad` and the layer's `grad`.  It belongs to the layer's last forward()."""
+        dv, dh = self.end_backward(h, dy, du_next, stream)
+        du = self.layer.backward(dv, self.u_in, None, accumulate, stream)
+        return (self.pre_backward(h, du, stream), None) if self.pre_own else (dh, du)

@@ -31,6 +31,9 @@ static inline bool moe_dtype_ok(int dt) { return dt == MOE_F32 || dt == MOE_BF16
 
 // norm.hip: workspace of moe_norm_backward or moe_block_end_backward for the gradients of `grads` parameters of d values
 size_t moe_norm_back_bytes(int T, int d, bool block_end, int grads);
+// ffn_train.hip and route_backward.hip: workspaces of the gradients
+size_t moe_ffn_back_bytes(int T, int d, int F, int k);
+size_t moe_route_back_bytes(int T, int d, int E);
 
 #define MOE_WAVE 64
 

@@ -28,7 +28,7 @@ extern "C" int moe_token_threshold(double phi, int d_type, double beta) {
 
 // permute scratch: one histogram of E counters per block of PERMUTE_BLOCK_ITEMS assignments
 extern "C" size_t moe_workspace_bytes(int op, int T, int d, int F, int E, int k, moe_dtype dt) {
-    (void)F; (void)dt;
+    (void)dt;
     if (op == MOE_OP_PERMUTE) {
         if (T < 0 || k < 1 || E < 1) return 0;
         size_t A = (size_t)T * (size_t)k;
@@ -38,6 +38,8 @@ extern "C" size_t moe_workspace_bytes(int op, int T, int d, int F, int E, int k,
     }
     if (op == MOE_OP_NORM_BACKWARD) return moe_norm_back_bytes(T, d, false, 2);
     if (op == MOE_OP_BLOCK_END_BACKWARD) return moe_norm_back_bytes(T, d, true, 5);
+    if (op == MOE_OP_FFN_BACKWARD) return moe_ffn_back_bytes(T, d, F, k);
+    if (op == MOE_OP_ROUTE_BACKWARD) return moe_route_back_bytes(T, d, E);
     return 0;
 }
 

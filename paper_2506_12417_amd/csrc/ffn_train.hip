@@ -1,0 +1,941 @@
+// The experts' part of a training step (moe_grouped_ffn_keep, moe_grouped_ffn_backward).  Row r of expert e (offsets[e] <= r < offsets[e+1]) is
+// assignment a = perm[r] of token t = a / k with weight w = gate_w[a]:
+//
+//   keep       z = x[t] W_in     h = relu(z), or silu(g) u of z = (g, u)     z kept in 8 bits (keep.h), h in half
+//   backward   s = dy[t] W_out^T     dgate_w[a] = sum_f h s     dh = w s     dz = dh [z > 0], or (dh u sig(g) (1 + g (1 - sig(g))), dh silu(g))
+//              dx_perm[r] = dz W_in^T     dW_in = sum_r x[t]^T dz     dW_out = sum_r (w h)^T dy[t]
+//
+// Three products over an expert's rows (z, s, dx_perm: nt_kernel, which differ in their operands and in what is done with the result) and two over
+// the rows themselves (dW_in, dW_out: tn_kernel).  What bounds them: arithmetic where experts hold many rows, the fetch of the matrices and the
+// stores of their gradients where they hold few.
+//
+// Both kernels: a work-group of four wavefronts per CU, persistent, takes items (256 outputs of 256, 128 or 64 rows; 256 x 256 values of a gradient).
+// The contraction goes in stages of 64 terms through two buffers of LDS, filled by loads that go there directly; a stage is two
+// halves of 32 terms, the fragments of a half are in registers when its multiplications start, the next half's are read
+// meanwhile.  An item's first two stages are fetched while the item before is finished and stored.
+//
+// Rounded on the way: dz and w h, once, to bf16 (the matrix instruction's type), and what is kept in 8 bits.  Sums are fp32.
+#include <type_traits>
+#include "common.h"
+#include "ffn_kernels.h"
+#include "gemm_util.h"
+#include "keep.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr int NTH = 256;
+[[maybe_unused]] constexpr int XCD = 8;
+constexpr int GROUP_ROWS = 8;              // row tiles of an expert that are taken together, column block after column block
+
+// (nothing may move across: neither memory operations nor matrix-core work)
+__device__ __forceinline__ void wg_barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("" ::: "memory");
+}
+
+// Sum and largest over the four lanes l16, l16 + 16, l16 + 32, l16 + 48; all four get it.
+__device__ __forceinline__ float quarter_sum(float v) {
+    const unsigned b = __float_as_uint(v);
+    const u32x2 p = __builtin_amdgcn_permlane16_swap(b, b, false, false);
+    const unsigned c = __float_as_uint(__uint_as_float(p[0]) + __uint_as_float(p[1]));
+    const u32x2 q = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return __uint_as_float(q[0]) + __uint_as_float(q[1]);
+}
+__device__ __forceinline__ unsigned quarter_max(unsigned v) {
+    const u32x2 p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    const unsigned c = max_u32(p[0], p[1]);
+    const u32x2 q = __builtin_amdgcn_permlane32_swap(c, c, false, false);
+    return max_u32(q[0], q[1]);
+}
+__device__ __forceinline__ u32x4 to_bf16(const float (&v)[8]) {
+    const f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+    return __builtin_bit_cast(u32x4, __builtin_convertvector(f, bf16x8));      // to nearest, ties to even
+}
+
+// Running sums over the experts, four of them a lane (E <= 256): lane l holds the sums up to and with experts 4 l .. 4 l + 3.
+struct Sums {
+    int s[4];
+    __device__ __forceinline__ int total() const { return __builtin_amdgcn_readlane(s[3], 63); }
+    // up to, and without, expert e
+    __device__ __forceinline__ int before(int e) const {
+        if (e == 0) return 0;
+        const int l = (e - 1) >> 2, j = (e - 1) & 3;
+        const int a = __builtin_amdgcn_readlane(s[0], l), b = __builtin_amdgcn_readlane(s[1], l);
+        const int c = __builtin_amdgcn_readlane(s[2], l), d = __builtin_amdgcn_readlane(s[3], l);
+        return j == 0 ? a : j == 1 ? b : j == 2 ? c : d;
+    }
+    // the expert in whose share `at` lies
+    __device__ __forceinline__ int find(int at) const {
+        return __popcll(__ballot(s[0] <= at)) + __popcll(__ballot(s[1] <= at)) + __popcll(__ballot(s[2] <= at)) + __popcll(__ballot(s[3] <= at));
+    }
+};
+template <typename F> __device__ __forceinline__ Sums sums_over_experts(const int32_t* offsets, int E, int lane, F share) {
+    Sums r;
+    int at[5];
+#pragma unroll
+    for (int j = 0; j < 5; ++j) at[j] = offsets[4 * lane + j < E ? 4 * lane + j : E];
+    int sum = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        sum += 4 * lane + j < E ? share(at[j + 1] - at[j]) : 0;
+        r.s[j] = sum;
+    }
+    const int before = (int)moe_wave_scan_u32((unsigned)sum) - sum;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.s[j] += before;
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------ products over an expert's rows
+// D[feature][row] = sum over terms of W[feature][term] R[row][term]: the features are the matrix instruction's rows, so that a lane has eight
+// neighbouring features of one row and can load and store them in whole pieces.
+enum { KEEP_RELU = 0, KEEP_SWIGLU = 1, HID_RELU = 2, HID_SWIGLU = 3, DX = 4 };
+
+struct NtArgs {
+    const uint16_t* rows;          // x, dy [T,K] (gathered) or dz [A, ld_rows]
+    const int32_t *offsets, *perm;
+    const void* const* w_ptrs;     // KEEP: packed [N,K] matrices
+    const uint16_t *w0, *w1;       // else: [E] matrices of N rows of ld_w values; w1 continues w0's contraction (DX, SwiGLU)
+    size_t w_stride;
+    int T, k, E, N, KT, KT0;       // stages, of them with w0
+    int ld_rows, ld_w, F, Z, parts;
+    const int8_t* q_in;
+    const float *scale_in, *gate_w;
+    int8_t* q_out;
+    float *scale_out, *dx_perm, *dgate_part;
+    uint16_t *h, *dz, *wh;
+};
+
+template <int TR> struct Nt {
+    static constexpr int NI = TR / 64;                     // 32-row blocks of a wavefront (two wavefronts share the rows, block by block)
+    static constexpr int F_BYTES = 256 * 128, R_BYTES = TR * 128, STAGE = F_BYTES + R_BYTES;
+    static constexpr int NFL = 8, NRL = TR / 32, LPS = NFL + NRL;      // loads per thread and stage
+    static constexpr size_t SMEM = 2 * STAGE + 2 * 256 * 4;
+};
+template <int TR> using NtAcc = f32x4[Nt<TR>::NI][2][4][2];            // [32-row block][its half][32-feature block][its half]
+template <int TR> struct NtFrags { bf16x8 f[4][2], r[Nt<TR>::NI][2]; };
+
+struct NtItem { int e, row0, rc, n0; };
+
+template <int TR> __device__ __forceinline__ NtItem nt_locate(const NtArgs& a, const Sums& tiles, int ncb, int item) {
+    NtItem it;
+    const int tile_at = item / ncb;
+    it.e = sgpr(tiles.find(tile_at));
+    const int first = tiles.before(it.e);
+    const int begin = a.offsets[it.e], n = a.offsets[it.e + 1] - begin;
+    const int R = (n + TR - 1) / TR;
+    const int local = item - first * ncb;
+    const int grp = local / (GROUP_ROWS * ncb), rem = local - grp * GROUP_ROWS * ncb;
+    const int gs = R - grp * GROUP_ROWS < GROUP_ROWS ? R - grp * GROUP_ROWS : GROUP_ROWS;
+    const int cb = rem / gs, tile = grp * GROUP_ROWS + rem - cb * gs;
+    it.row0 = sgpr(begin + tile * TR);
+    it.rc = sgpr(n - tile * TR < TR ? n - tile * TR : TR);
+    it.n0 = sgpr(cb * 256);
+    return it;
+}
+
+struct NtLoader {
+    __amdgpu_buffer_rsrc_t rr, rf0, rf1;
+    unsigned vr[8], vf;            // byte offsets: of this thread's rows, of its first feature
+};
+
+template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs& a, const NtItem& it, const int* rinfo, int ld_row, unsigned piece, NtLoader& L) {
+    const int nr = a.N - it.n0 < 256 ? a.N - it.n0 : 256;
+    const unsigned bytes = (unsigned)nr * (unsigned)a.ld_w * 2u;
+    if constexpr (KIND <= KEEP_SWIGLU) {
+        L.rf0 = make_rsrc((const uint16_t*)a.w_ptrs[it.e] + (size_t)it.n0 * a.ld_w, bytes);
+        L.vf = (unsigned)ld_row * (unsigned)a.ld_w * 2u + piece;
+    } else {
+        const size_t at = (size_t)it.e * a.w_stride + (size_t)it.n0 * a.ld_w;
+        L.rf0 = make_rsrc(a.w0 + at, bytes);
+        if constexpr (KIND == DX) L.rf1 = make_rsrc((a.w1 ? a.w1 : a.w0) + at, bytes);
+        // slot 16 h + j of a block of 32 holds feature 8 (j / 4) + 4 h + j % 4: the two halves give a lane eight neighbours
+        const int f = ((ld_row & 12) << 1) + ((ld_row & 16) >> 2) + (ld_row & 3);
+        L.vf = (unsigned)f * (unsigned)a.ld_w * 2u + piece;
+    }
+    if constexpr (KIND == DX) {
+        L.rr = make_rsrc(a.rows + (size_t)it.row0 * a.ld_rows, (unsigned)it.rc * (unsigned)a.ld_rows * 2u);
+#pragma unroll
+        for (int q = 0; q < Nt<TR>::NRL; ++q) L.vr[q] = (unsigned)(q * 32 + ld_row) * (unsigned)a.ld_rows * 2u + piece;
+    } else {
+        L.rr = make_rsrc(a.rows, (unsigned)a.T * (unsigned)a.ld_rows * 2u);
+#pragma unroll
+        for (int q = 0; q < Nt<TR>::NRL; ++q) {
+            const int row = q * 32 + ld_row;
+            unsigned src = (unsigned)rinfo[row];
+            if (a.k != 1) src /= (unsigned)a.k;
+            // (a row past the tile's end gets an offset beyond the matrix: the range check reads zeros)
+            L.vr[q] = row < it.rc ? src * (unsigned)a.ld_rows * 2u + piece : 0xFFFFFFF0u;
+        }
+    }
+}
+
+// load q of stage kt (the features first)
+template <int KIND, int TR> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtLoader& L, unsigned char* ring, int wave, int kt, int q) {
+    unsigned char* to = ring + (kt & 1) * Nt<TR>::STAGE + wave * 1024;
+    if (q < Nt<TR>::NFL) {
+        const unsigned at = L.vf + (unsigned)(q * 32) * (unsigned)a.ld_w * 2u;
+        if (KIND == DX && kt >= a.KT0) __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rf1, (lds_void_t*)(to + q * 4096), 16, at, (unsigned)(kt - a.KT0) * 128u, 0, 0);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rf0, (lds_void_t*)(to + q * 4096), 16, at, (unsigned)kt * 128u, 0, 0);
+    } else {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rr, (lds_void_t*)(to + Nt<TR>::F_BYTES + (q - Nt<TR>::NFL) * 4096), 16,
+                                                 L.vr[q < Nt<TR>::NFL ? 0 : q - Nt<TR>::NFL], (unsigned)kt * 128u, 0, 0);
+    }
+}
+
+struct NtLane { int wave, lane, f_rd, r_rd; };             // f_rd, r_rd: first half's fragment of the first block
+
+// fragment read j of a half (32 terms): features first
+template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const unsigned char* ring, int j, int at_f, int at_r) {
+    if (j < 8) fr.f[j >> 1][j & 1] = *(const bf16x8*)(ring + at_f + (j >> 1) * 4096 + (j & 1) * 2048);
+    else fr.r[(j - 8) >> 1][j & 1] = *(const bf16x8*)(ring + at_r + ((j - 8) >> 1) * 8192 + (j & 1) * 2048);
+}
+
+// Half S of stage kt: multiplies set S, reads the other.  LOAD: stage kt + 2 goes on its way (half 1: the buffer is free).
+template <int KIND, int TR, int S, bool LOAD, bool FULL>
+__device__ __forceinline__ void nt_half(const NtArgs& a, const NtLoader& L, const NtLane& ln, unsigned char* ring, int kt, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int ni_on) {
+    constexpr int NI = Nt<TR>::NI, G = NI * 4, READS = 8 + 2 * NI, SPREAD = G >= 16 ? 12 : G;
+    const int buf = ((S == 0 ? kt : kt + 1) & 1) * Nt<TR>::STAGE;
+    const int at_f = buf + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf + (ln.r_rd ^ (S == 0 ? 64 : 0));
+#pragma unroll
+    for (int t = 0; t < G; ++t) {
+        const int ni = t >> 2, n16 = (t >> 1) & 1, b0 = (t & 1) * 2;
+        if (FULL || ni < ni_on) {
+#pragma unroll
+            for (int b = b0; b < b0 + 2; ++b)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    acc[ni][n16][b][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fr[S].f[b][h], fr[S].r[ni][n16], acc[ni][n16][b][h], 0, 0, 0);
+        }
+        if (t < SPREAD) {
+#pragma unroll
+            for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) nt_read<TR>(fr[S ^ 1], ring, j, at_f, at_r);
+        }
+        if (S == 1 && LOAD) {
+#pragma unroll
+            for (int q = t * Nt<TR>::LPS / G; q < (t + 1) * Nt<TR>::LPS / G; ++q) nt_load<KIND, TR>(a, L, ring, ln.wave, kt + 2, q);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (S == 0) {
+        // everybody has read all of stage kt, and stage kt + 1 is there
+        MOE_WAIT_LGKMCNT(0);
+        MOE_WAIT_VMCNT(0);
+        wg_barrier();
+    }
+}
+
+template <int KIND, int TR, bool FULL>
+__device__ __forceinline__ void nt_contract(const NtArgs& a, const NtLoader& L, const NtLane& ln, unsigned char* ring, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int ni_on) {
+    int kt = 0;
+#pragma clang loop unroll(disable)
+    for (; kt + 2 < a.KT; ++kt) {
+        nt_half<KIND, TR, 0, true, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
+        nt_half<KIND, TR, 1, true, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
+    }
+#pragma clang loop unroll(disable)
+    for (; kt < a.KT; ++kt) {
+        nt_half<KIND, TR, 0, false, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
+        nt_half<KIND, TR, 1, false, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
+    }
+}
+
+// A lane's features of block b in a row: natural order (slots arranged by nt_turn), or packed rows (packed row 16 h + j = output 2 j + h).
+template <bool PACKED> __device__ __forceinline__ void lane_values(const f32x4 (&acc)[2], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = PACKED ? acc[i & 1][i >> 1] : acc[i >> 2][i & 3];
+}
+
+template <int KIND, int TR>
+__device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, const int* rinfo, const NtAcc<TR>& acc, int wm, int wn, int lane, int ni_on) {
+    const int l16 = lane & 15, lq = lane >> 4;
+    const int f0 = it.n0 + wm * 128;                       // this wavefront's first feature
+    if (f0 >= a.N) return;
+    const size_t row0 = (size_t)it.row0;
+    const unsigned rc = (unsigned)it.rc;
+    if constexpr (KIND == DX) {
+        const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.dx_perm + row0 * a.N, rc * (unsigned)a.N * 4u);
+#pragma unroll
+        for (int ni = 0; ni < Nt<TR>::NI; ++ni) {
+            if (ni >= ni_on) continue;
+#pragma unroll
+            for (int n16 = 0; n16 < 2; ++n16) {
+                const unsigned at = (unsigned)((ni * 2 + wn) * 32 + n16 * 16 + l16) * (unsigned)a.N * 4u + (unsigned)lq * 32u;
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+                    if (f0 + b * 32 < a.N) {
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][0]), ro, at, (unsigned)(f0 + b * 32) * 4u, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][1]), ro, at + 16u, (unsigned)(f0 + b * 32) * 4u, 0);
+                    }
+            }
+        }
+    } else if constexpr (KIND <= KEEP_SWIGLU) {
+        const unsigned F = (unsigned)a.F, Z = (unsigned)a.Z;
+        const __amdgpu_buffer_rsrc_t rh = make_rsrc(a.h + row0 * F, rc * F * 2u);
+        const __amdgpu_buffer_rsrc_t rq = make_rsrc(a.q_out + row0 * Z, rc * Z);
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.scale_out + row0 * (Z / 64), rc * (Z / 64) * 4u);
+#pragma unroll
+        for (int ni = 0; ni < Nt<TR>::NI; ++ni) {
+            if (ni >= ni_on) continue;
+#pragma unroll
+            for (int n16 = 0; n16 < 2; ++n16) {
+                const unsigned row = (unsigned)((ni * 2 + wn) * 32 + n16 * 16 + l16);
+                // two blocks of 64 kept columns: neighbouring features (ReLU), or the gates and the ups of the same 64 outputs
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    constexpr bool SW = KIND == KEEP_SWIGLU;
+                    const int b0 = SW ? p : 2 * p, db = SW ? 2 : 1;
+                    const int zc = SW ? f0 / 2 + p * a.F : f0 + p * 64;            // column of z
+                    if (!SW && zc >= a.F) continue;
+                    float v[2][8];
+                    unsigned most = 0;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        lane_values<true>(acc[ni][n16][b0 + i * db], v[i]);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) {
+                            if (!SW) v[i][c] = relu_f(v[i][c]);
+                            most = max_u32(most, magnitude(v[i][c]));
+                        }
+                    }
+                    const KeepScale ks = keep_scale(quarter_max(most));
+                    if (lq == 0) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(ks.scale), rs, row * (Z / 64) * 4u, (unsigned)(zc / 64) * 4u, 0);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const u32x2 w = {keep_four<!SW>(v[i][0], v[i][1], v[i][2], v[i][3], ks.to_q), keep_four<!SW>(v[i][4], v[i][5], v[i][6], v[i][7], ks.to_q)};
+                        __builtin_amdgcn_raw_buffer_store_b64(w, rq, row * Z + (unsigned)lq * 8u, (unsigned)(zc + i * 32), 0);
+                    }
+                    if (!SW || p == 1) {
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            if (SW) {                      // (v holds the ups)
+                                float g[8];
+                                lane_values<true>(acc[ni][n16][2 * i], g);
+#pragma unroll
+                                for (int c = 0; c < 8; ++c) v[i][c] *= silu_f(g[c]);
+                            }
+                            const u32x4 w = {half_bits(v[i][0], v[i][1]), half_bits(v[i][2], v[i][3]), half_bits(v[i][4], v[i][5]), half_bits(v[i][6], v[i][7])};
+                            __builtin_amdgcn_raw_buffer_store_b128(w, rh, row * F * 2u + (unsigned)lq * 16u, (unsigned)((SW ? f0 / 2 : zc) + i * 32) * 2u, 0);
+                        }
+                    }
+                }
+            }
+        }
+    } else {
+        constexpr bool SW = KIND == HID_SWIGLU;
+        const unsigned F = (unsigned)a.F, Z = (unsigned)a.Z;
+        const __amdgpu_buffer_rsrc_t rq = make_rsrc(a.q_in + row0 * Z, rc * Z);
+        const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.scale_in + row0 * (Z / 64), rc * (Z / 64) * 4u);
+        const __amdgpu_buffer_rsrc_t rz = make_rsrc(a.dz + row0 * Z, rc * Z * 2u);
+        const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wh + row0 * F, rc * F * 2u);
+        const int on = a.N - f0 < 128 ? a.N - f0 : 128;    // features of this wavefront: 64 or 128
+#pragma unroll
+        for (int ni = 0; ni < Nt<TR>::NI; ++ni) {
+            if (ni >= ni_on) continue;
+#pragma unroll
+            for (int n16 = 0; n16 < 2; ++n16) {
+                const unsigned row = (unsigned)((ni * 2 + wn) * 32 + n16 * 16 + l16);
+                const float gate = row < rc ? (a.gate_w ? a.gate_w[rinfo[row]] : 1.f) : 0.f;
+                u32x2 q[2][4];
+                float sc[2][2];
+#pragma unroll
+                for (int m = 0; m < (SW ? 2 : 1); ++m) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b)
+                        if (b * 32 < on) q[m][b] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, row * Z + (unsigned)lq * 8u, (unsigned)(f0 + b * 32 + m * a.F), 0));
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+                        if (j * 64 < on) sc[m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, row * (Z / 64) * 4u, (unsigned)((f0 + j * 64 + m * a.F) / 64) * 4u, 0));
+                }
+                float dgate = 0.f;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    if (b * 32 >= on) continue;
+                    float s[8], wh[8], dz0[8], dz1[8];
+                    lane_values<false>(acc[ni][n16][b], s);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float z = (float)((int)(q[0][b][c >> 2] << (24 - 8 * (c & 3))) >> 24) * sc[0][b >> 1];
+                        const float dh = gate * s[c];
+                        float h;
+                        if (SW) {
+                            const float u = (float)((int)(q[1][b][c >> 2] << (24 - 8 * (c & 3))) >> 24) * sc[1][b >> 1];
+                            const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-z)), silu = z * sig;
+                            h = silu * u;
+                            dz0[c] = dh * u * (sig + silu * (1.f - sig));
+                            dz1[c] = dh * silu;
+                        } else {
+                            h = z;
+                            dz0[c] = z > 0.f ? dh : z;     // (z is 0 else, or no number)
+                        }
+                        dgate = fmaf(h, s[c], dgate);
+                        wh[c] = gate * h;
+                    }
+                    const unsigned col = (unsigned)(f0 + b * 32) * 2u;
+                    __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, row * F * 2u + (unsigned)lq * 16u, col, 0);
+                    __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, row * Z * 2u + (unsigned)lq * 16u, col, 0);
+                    if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, row * Z * 2u + (unsigned)lq * 16u, col + F * 2u, 0);
+                }
+                dgate = quarter_sum(dgate);
+                if (lq == 0 && row < rc) a.dgate_part[(row0 + row) * (size_t)a.parts + (unsigned)(f0 / 128)] = dgate;
+            }
+        }
+    }
+}
+
+template <int KIND, int TR>
+__global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass makes the stub only: it has no buffer descriptors)
+    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+    int* rinfo = (int*)(ring + 2 * Nt<TR>::STAGE);         // (gather) assignments of an item's rows, two items in turn
+    const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
+    const int wm = wave & 1, wn = wave >> 1;
+    const int l16 = lane & 15, lq = lane >> 4;
+    const Sums tiles = sums_over_experts(a.offsets, a.E, lane, [](int n) { return (n + TR - 1) / TR; });
+    const int ncb = (a.N + 255) / 256;
+    // the XCDs take neighbouring runs of the items, so that an expert's matrix stays in few L2s
+    const long long all = (long long)tiles.total() * ncb;
+    const int xcd = (int)blockIdx.x % XCD, stride = (int)gridDim.x / XCD;
+    const int end = sgpr((int)(all * (xcd + 1) / XCD));
+    int item = sgpr((int)(all * xcd / XCD) + (int)blockIdx.x / XCD);
+    if (item >= end) return;
+
+    const int ld_row = tid >> 3;
+    const unsigned piece = (unsigned)((tid & 7) ^ ((ld_row >> 1) & 7)) << 4;
+    NtLane ln;
+    ln.wave = wave;
+    ln.lane = lane;
+    const int frag = l16 * 128 + ((lq ^ (l16 >> 1)) << 4);
+    ln.f_rd = wm * (128 * 128) + frag;
+    ln.r_rd = Nt<TR>::F_BYTES + wn * (32 * 128) + frag;
+    auto fetch_rows = [&](const NtItem& it, int par) {
+        if (KIND != DX && wave * 64 < TR)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(a.perm + it.row0, (unsigned)it.rc * 4u), (lds_void_t*)(rinfo + par * 256 + wave * 64), 4,
+                                                     (unsigned)(wave * 64 + lane) * 4u, 0, 0, 0);
+    };
+    auto start = [&](const NtLoader& L) {                  // an item's first two stages
+#pragma unroll
+        for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, L, ring, wave, 0, q);
+        if (a.KT > 1) {
+#pragma unroll
+            for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, L, ring, wave, 1, q);
+        }
+    };
+
+    NtLoader L;
+    NtItem it = nt_locate<TR>(a, tiles, ncb, item);
+    fetch_rows(it, 0);
+    MOE_WAIT_VMCNT(0);
+    __syncthreads();
+    nt_turn<KIND, TR>(a, it, rinfo, ld_row, piece, L);
+    start(L);
+    NtAcc<TR> acc;
+    NtFrags<TR> fr[2];
+    for (int par = 0;; par ^= 1) {
+        // stage 0 is there once no more than stage 1's loads are under way
+        if (a.KT > 1) MOE_WAIT_VMCNT(Nt<TR>::LPS);
+        else MOE_WAIT_VMCNT(0);
+        wg_barrier();
+        const int next = item + stride;
+        NtItem nx = it;
+        if (next < end) {
+            nx = nt_locate<TR>(a, tiles, ncb, next);
+            fetch_rows(nx, par ^ 1);
+        }
+#pragma unroll
+        for (int ni = 0; ni < Nt<TR>::NI; ++ni)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) acc[ni][j >> 3][(j >> 1) & 3][j & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < 8 + 2 * Nt<TR>::NI; ++j) nt_read<TR>(fr[0], ring, j, ln.f_rd, ln.r_rd);
+        int ni_on = ((it.rc + 31) / 32 - wn + 1) / 2;      // 32-row blocks of this wavefront that hold rows
+        ni_on = ni_on > Nt<TR>::NI ? Nt<TR>::NI : ni_on;
+        if (ni_on == Nt<TR>::NI) nt_contract<KIND, TR, true>(a, L, ln, ring, acc, fr, ni_on);
+        else nt_contract<KIND, TR, false>(a, L, ln, ring, acc, fr, ni_on);
+        // (since the last barrier nobody needs what is in the ring: the reads of the last half were of a stage that is not there)
+        if (next < end) {
+            nt_turn<KIND, TR>(a, nx, rinfo + (par ^ 1) * 256, ld_row, piece, L);
+            start(L);
+        }
+        nt_finish<KIND, TR>(a, it, rinfo + par * 256, acc, wm, wn, lane, ni_on);
+        if (next >= end) break;
+        item = next;
+        it = nx;
+    }
+#endif
+}
+
+// ------------------------------------------------------------------------------------------ products over the rows
+// dW[m][n] = sum over an expert's rows r of M[r][m] N[r][n].  Both operands lie with the contraction outermost: LDS holds 64 rows of 256
+// columns of each, and the reads that transpose (ds_read_b64_tr_b16: lane i of sixteen gets column i of four rows) bring the terms of a column together.
+// One operand is gathered (x for dW_in, dy for dW_out), the other lies in the experts' order (dz, w h).
+struct TnArgs {
+    const uint16_t *x, *dy, *dz, *wh;
+    const int32_t *offsets, *perm;
+    int T, k, E, d, F, Z, mats;
+    void *dwa, *dwb, *dwo;
+};
+
+constexpr int TN_OP = 64 * 512, TN_STAGE = 2 * TN_OP;      // LDS: an operand's 64 rows of 256 columns
+constexpr int TN_IDS = 64;
+constexpr size_t TN_SMEM = 2 * TN_STAGE + 4 * TN_IDS * 4;
+
+struct TnItem {
+    int e, row0, n, m0, n0, M, N;
+    bool out;                      // dW_out (M: w h, N: dy gathered); else dW_in (M: x gathered, N: dz from column zc)
+    int zc;
+    void* dw;
+};
+
+struct TnShape { int ta, tb, per_mat, per_expert; };       // tiles along d and F
+
+template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, const TnShape& sh, int item) {
+    TnItem it;
+    it.e = sgpr(item / sh.per_expert);
+    const int local = item - it.e * sh.per_expert, mat = local / sh.per_mat, at = local - mat * sh.per_mat;
+    it.out = mat == a.mats - 1;
+    it.M = it.out ? a.F : a.d;
+    it.N = it.out ? a.d : a.F;
+    const int tm = it.out ? sh.tb : sh.ta, tn = it.out ? sh.ta : sh.tb;
+    const int grp = at / (GROUP_ROWS * tn), rem = at - grp * GROUP_ROWS * tn;
+    const int gs = tm - grp * GROUP_ROWS < GROUP_ROWS ? tm - grp * GROUP_ROWS : GROUP_ROWS;
+    const int cb = rem / gs;
+    it.n0 = sgpr(cb * 256);
+    it.m0 = sgpr((grp * GROUP_ROWS + rem - cb * gs) * 256);
+    it.row0 = sgpr(a.offsets[it.e]);
+    it.n = sgpr(a.offsets[it.e + 1]) - it.row0;
+    it.zc = mat == 1 ? a.F : 0;
+    it.dw = (unsigned char*)(it.out ? a.dwo : mat == 1 ? a.dwb : a.dwa) + (size_t)it.e * a.d * a.F * ES;
+    return it;
+}
+
+// The loads of stage kt of an item; ids: the stage's assignments in LDS.
+struct TnLoads {
+    __amdgpu_buffer_rsrc_t rd, rg;
+    unsigned vd, vg[8], ld_d;
+    int to_d, to_g;
+};
+__device__ __forceinline__ void tn_stage(const TnArgs& a, const TnItem& it, const int* ids, int kt, int tid, unsigned piece, TnLoads& L) {
+    const int left = it.n - kt * 64, term = (tid >> 5) * 8;
+    const int ld = it.out ? a.F : a.Z;
+    const uint16_t* dir = (it.out ? a.wh : a.dz) + (size_t)(it.row0 + kt * 64) * ld;
+    L.ld_d = (unsigned)ld * 2u;
+    L.rd = make_rsrc(dir, (unsigned)(left < 64 ? left : 64) * L.ld_d);
+    L.rg = make_rsrc(it.out ? a.dy : a.x, (unsigned)a.T * (unsigned)a.d * 2u);
+    L.vd = (unsigned)term * L.ld_d + (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u + piece;
+    const unsigned cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u + piece;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+        unsigned src = (unsigned)ids[term + q];
+        if (a.k != 1) src /= (unsigned)a.k;
+        L.vg[q] = term + q < left ? src * (unsigned)a.d * 2u + cg : 0xFFFFFFF0u;
+    }
+    // LDS: the N operand's rows first
+    L.to_d = (kt & 1) * TN_STAGE + (it.out ? TN_OP : 0);
+    L.to_g = (kt & 1) * TN_STAGE + (it.out ? 0 : TN_OP);
+}
+__device__ __forceinline__ void tn_load(const TnLoads& L, unsigned char* ring, int wave, int q) {
+    if (q < 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rd, (lds_void_t*)(ring + L.to_d + q * 4096 + wave * 1024), 16, L.vd + (unsigned)q * L.ld_d, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rg, (lds_void_t*)(ring + L.to_g + (q - 8) * 4096 + wave * 1024), 16, L.vg[q < 8 ? 0 : q - 8], 0, 0, 0);
+}
+
+typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
+struct TnFrags { s16x4 n[8][2], m[8][2]; };
+
+// Read j (0..31) of a half: four terms of a column of a 16-column block.  at: this lane's row and 8 bytes in LDS, sw: its swizzle.
+__device__ __forceinline__ void tn_read(TnFrags& fr, unsigned char* ring, int j, int at_n, int at_m, int sw) {
+    const int c = (j & 15) >> 1, i = j & 1;
+    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(ring + at_n + i * 8192 + ((c * 32) ^ sw)));
+    else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(ring + at_m + i * 8192 + ((c * 32) ^ sw)));
+}
+__device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
+    typedef __attribute__((ext_vector_type(8))) short s16x8;
+    const s16x8 v = __builtin_shufflevector(f[0], f[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, v);
+}
+
+struct TnLane { int wave, at_n, at_m, sw; };
+
+template <int S, bool LOAD>
+__device__ __forceinline__ void tn_half(const TnLoads& L, const TnLane& ln, unsigned char* ring, int kt, TnAcc& acc, TnFrags (&fr)[2]) {
+    const int buf = ((S == 0 ? kt : kt + 1) & 1) * TN_STAGE + (S == 0 ? 16384 : 0);
+#pragma unroll
+    for (int t = 0; t < 16; ++t) {
+        const int m = t >> 1, n4 = (t & 1) * 4;
+#pragma unroll
+        for (int n = n4; n < n4 + 4; ++n)
+            acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
+        if (t < 12) {
+#pragma unroll
+            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ring, j, buf + ln.at_n, buf + ln.at_m, ln.sw);
+        }
+        if (S == 1 && LOAD) tn_load(L, ring, ln.wave, t);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    if (S == 0) {
+        MOE_WAIT_LGKMCNT(0);
+        MOE_WAIT_VMCNT(0);
+        wg_barrier();
+    }
+}
+
+template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const TnItem& it, TnAcc& acc, int wm, int wn, int lane) {
+    constexpr unsigned ES = sizeof(O);
+    const int l16 = lane & 15, lq = lane >> 4;
+    const int c0 = it.n0 + wm * 128;
+    if (c0 >= it.N) return;
+    const unsigned ld = (unsigned)it.N * ES;
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc((unsigned char*)it.dw + (size_t)it.m0 * ld, (unsigned)(it.M - it.m0 < 256 ? it.M - it.m0 : 256) * ld);
+#pragma unroll
+    for (int m = 0; m < 8; ++m) {
+        const unsigned row = (unsigned)(wn * 128 + m * 16 + l16) * ld;
+#pragma unroll
+        for (int n = 0; n < 8; n += 2) {
+            if (c0 + n * 16 >= it.N) continue;
+            const unsigned col = (unsigned)(c0 + n * 16) * ES;
+            if constexpr (ES == 4) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    f32x4 v = acc[m][n + i];
+                    if (ADD) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0));
+                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0);
+                }
+            } else {
+                // a lane has columns 4 lq + r of two blocks of 16; lanes 16 apart exchange them, so that each has eight neighbours:
+                // columns 0, 16, 8, 24 .. + 7 for lq = 0 .. 3
+                float v[8];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const u32x2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[m][n][r]), __float_as_uint(acc[m][n + 1][r]), false, false);
+                    v[r] = __uint_as_float(p[0]);
+                    v[4 + r] = __uint_as_float(p[1]);
+                }
+                const unsigned at = row + (unsigned)((lq & 1) * 16 + (lq >> 1) * 8) * 2u;
+                if (ADD) {
+                    const u32x4 old = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, at, col, 0));
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(i & 1 ? old[i >> 1] & 0xffff0000u : old[i >> 1] << 16);
+                }
+                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(v), ro, at, col, 0);
+            }
+        }
+    }
+}
+
+template <typename O, bool ADD>
+__global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
+#ifdef __HIP_DEVICE_COMPILE__
+    extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
+    int* ids = (int*)(ring + 2 * TN_STAGE);                // assignments of stages: kt & 1 of the item, and the next item's first two
+    const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
+    const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
+    TnShape sh;
+    sh.ta = (a.d + 255) / 256;
+    sh.tb = (a.F + 255) / 256;
+    sh.per_mat = sh.ta * sh.tb;
+    sh.per_expert = sh.per_mat * a.mats;
+    // An item costs its stages and the store of its tile (about six stages' time).  The XCDs take neighbouring runs of equal cost.
+    const Sums cost = sums_over_experts(a.offsets, a.E, lane, [](int n) { return 6 + (n + 63) / 64; });
+    const int xcd = (int)blockIdx.x % XCD, stride = (int)gridDim.x / XCD;
+    auto bound = [&](int x) {
+        const long long at = (long long)cost.total() * sh.per_expert * x / XCD;
+        if (x == XCD) return a.E * sh.per_expert;
+        const int e = cost.find((int)(at / sh.per_expert));
+        const long long in = at - (long long)cost.before(e) * sh.per_expert;
+        return sgpr(e * sh.per_expert + (int)(in / (cost.before(e + 1) - cost.before(e))));
+    };
+    const int end = bound(xcd + 1);
+    int item = bound(xcd) + (int)blockIdx.x / XCD;
+    if (item >= end) return;
+
+    TnLane ln;
+    ln.wave = wave;
+    // slot s of a stage: row (s % 8) 8 + s / 8 of its 64 (either operand's); lane (l16, lq) reads slots 4 lq + l16 / 4 of sixteen
+    const int slot = lq * 4 + (l16 >> 2);
+    ln.sw = (slot & 7) * 32;
+    ln.at_n = slot * 512 + (l16 & 3) * 8 + wm * 256;
+    ln.at_m = TN_OP + slot * 512 + (l16 & 3) * 8 + wn * 256;
+    const unsigned piece = (unsigned)((tid & 31) ^ (2 * (tid >> 5))) << 4;
+    auto fetch_ids = [&](const TnItem& it, int kt, int to) {
+        if (wave == 0)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(a.perm + it.row0, (unsigned)it.n * 4u), (lds_void_t*)(ids + to * TN_IDS), 4,
+                                                     (unsigned)(kt * 64 + lane) * 4u, 0, 0, 0);
+    };
+    TnLoads L;
+    // (stage 2's assignments go on their way first: they are there when stage 0 is)
+    auto start = [&](const TnItem& it, int KT, int at) {
+        if (KT > 2) fetch_ids(it, 2, at);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+            if (s < KT) {
+                tn_stage(a, it, ids + (2 + s) * TN_IDS, s, tid, piece, L);
+#pragma unroll
+                for (int q = 0; q < 16; ++q) tn_load(L, ring, wave, q);
+            }
+    };
+    TnItem it = tn_locate<sizeof(O)>(a, sh, item);
+    fetch_ids(it, 0, 2);
+    fetch_ids(it, 1, 3);
+    MOE_WAIT_VMCNT(0);
+    __syncthreads();
+    start(it, (it.n + 63) / 64, 0);
+    TnAcc acc;
+    TnFrags fr[2];
+    for (;;) {
+        const int KT = (it.n + 63) / 64;
+        const int next = item + stride;
+        TnItem nx = it;
+        if (KT > 1) MOE_WAIT_VMCNT(16);
+        else MOE_WAIT_VMCNT(0);
+        wg_barrier();
+        if (next < end) {
+            nx = tn_locate<sizeof(O)>(a, sh, next);
+            fetch_ids(nx, 0, 2);
+            fetch_ids(nx, 1, 3);
+        }
+#pragma unroll
+        for (int m = 0; m < 8; ++m)
+#pragma unroll
+            for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (KT > 0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) tn_read(fr[0], ring, j, ln.at_n, ln.at_m, ln.sw);
+        }
+        int kt = 0;
+#pragma clang loop unroll(disable)
+        for (; kt + 2 < KT; ++kt) {
+            tn_half<0, true>(L, ln, ring, kt, acc, fr);
+            tn_stage(a, it, ids + (kt & 1) * TN_IDS, kt + 2, tid, piece, L);
+            if (kt + 3 < KT) fetch_ids(it, kt + 3, (kt + 1) & 1);
+            tn_half<1, true>(L, ln, ring, kt, acc, fr);
+        }
+#pragma clang loop unroll(disable)
+        for (; kt < KT; ++kt) {
+            tn_half<0, false>(L, ln, ring, kt, acc, fr);
+            tn_half<1, false>(L, ln, ring, kt, acc, fr);
+        }
+        if (next < end) {
+            if (KT == 0) {                                 // (no stage has waited for the next item's assignments)
+                MOE_WAIT_VMCNT(0);
+                wg_barrier();
+            }
+            start(nx, (nx.n + 63) / 64, 0);
+        }
+        if (!ADD || KT > 0) tn_finish<O, ADD>(it, acc, wm, wn, lane);
+        if (next >= end) break;
+        item = next;
+        it = nx;
+    }
+#endif
+}
+
+// dgate_w[a] = the sum of its row's parts, in their order (an assignment without a row: 0)
+__global__ __launch_bounds__(256) void dgate_kernel(const float* __restrict__ part, const int32_t* __restrict__ inv_perm, int A, int parts, float* __restrict__ dgate_w) {
+    const int a = (int)(blockIdx.x * 256 + threadIdx.x);
+    if (a >= A) return;
+    const int r = inv_perm[a];
+    float s = 0.f;
+    if (r >= 0)
+        for (int j = 0; j < parts; ++j) s += part[(size_t)r * parts + j];
+    dgate_w[a] = s;
+}
+
+// dy in fp32, rounded once to the matrix instruction's type
+__global__ __launch_bounds__(256) void narrow_kernel(const f32x4* __restrict__ from, u32x4* __restrict__ to, size_t n) {
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= n) return;
+    const f32x4 a = from[2 * i], b = from[2 * i + 1];
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    to[i] = to_bf16(v);
+}
+
+template <typename K> int set_smem(K kern, size_t bytes) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != hipSuccess) return moe_fail(MOE_ERR_HIP, "moe_grouped_ffn (training): shared memory attribute: %s", hipGetErrorString(e));
+    return MOE_OK;
+}
+template <int KIND, int TR> int launch_nt(const NtArgs& a, hipStream_t st) {
+    auto kern = gemm_nt_kernel<KIND, TR>;
+    const int ok = set_smem(kern, Nt<TR>::SMEM);
+    if (ok != MOE_OK) return ok;
+    hipLaunchKernelGGL(kern, dim3(MOE_GEMM_GRID), dim3(NTH), Nt<TR>::SMEM, st, a);
+    MOE_CHECK_LAUNCH("moe_grouped_ffn (training, over rows)");
+    return MOE_OK;
+}
+// Rows per tile by the mean rows of an expert.
+template <int KIND> int launch_nt_rows(const NtArgs& a, int A, hipStream_t st) {
+    const long long mean = (A + a.E - 1) / a.E;
+    if (mean <= 64) return launch_nt<KIND, 64>(a, st);
+    if (mean < 512) return launch_nt<KIND, 128>(a, st);
+    return launch_nt<KIND, 256>(a, st);
+}
+template <typename O, bool ADD> int launch_tn(const TnArgs& a, hipStream_t st) {
+    auto kern = gemm_tn_kernel<O, ADD>;
+    const int ok = set_smem(kern, TN_SMEM);
+    if (ok != MOE_OK) return ok;
+    hipLaunchKernelGGL(kern, dim3(MOE_GEMM_GRID), dim3(NTH), TN_SMEM, st, a);
+    MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (over the rows)");
+    return MOE_OK;
+}
+
+int check_shape(const char* what, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt) {
+    MOE_REQUIRE(T >= 0 && d >= 1 && F >= 1 && E >= 1 && k >= 1, MOE_ERR_ARG, "%s: T=%d d=%d F=%d E=%d k=%d", what, T, d, F, E, k);
+    MOE_REQUIRE(act == MOE_RELU || act == MOE_SWIGLU, MOE_ERR_UNSUPPORTED, "%s: activation %d", what, (int)act);
+    MOE_REQUIRE(dt == MOE_BF16, MOE_ERR_UNSUPPORTED, "%s: dtype %d (MOE_BF16 only)", what, (int)dt);
+    MOE_REQUIRE(E <= MOE_MAX_EXPERTS, MOE_ERR_UNSUPPORTED, "%s: E=%d", what, E);
+    MOE_REQUIRE(d % 64 == 0 && F % 64 == 0, MOE_ERR_UNSUPPORTED, "%s: d=%d, F=%d have to be multiples of 64", what, d, F);
+    const long long limit = (1ll << 32) - (1 << 16);       // bytes that a 32-bit offset reaches, with the columns of a tile beside it
+    MOE_REQUIRE((long long)T * d * 2 < limit && 256ll * d * 4 < limit && 256ll * F * 4 < limit, MOE_ERR_UNSUPPORTED, "%s: T=%d rows of d=%d, F=%d pass 4 GiB", what, T, d, F);
+    MOE_REQUIRE((long long)T * k < (1ll << 30), MOE_ERR_UNSUPPORTED, "%s: T=%d k=%d", what, T, k);
+    MOE_REQUIRE(((long long)T * k / 64 + E) * ((F + 63) / 64) * 2 < (1ll << 30) && ((long long)T * k / 64 + E) * ((d + 63) / 64) < (1ll << 30) &&
+                    (long long)E * ((d + 255) / 256) * ((F + 255) / 256) * 3 < (1ll << 30),
+                MOE_ERR_UNSUPPORTED, "%s: T=%d k=%d E=%d d=%d F=%d make too many tiles", what, T, k, E, d, F);
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" int moe_grouped_ffn_keep(const void* x, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt, const void* const* w_in, const int32_t* offsets,
+                                    const int32_t* perm, void* h_scratch, int8_t* z_q, float* z_scale, void* stream) {
+    int ok = check_shape("moe_grouped_ffn_keep", T, d, F, E, k, act, dt);
+    if (ok != MOE_OK) return ok;
+    if (T == 0) return MOE_OK;
+    MOE_REQUIRE(x && w_in && offsets && perm && h_scratch && z_q && z_scale, MOE_ERR_ARG, "moe_grouped_ffn_keep: null pointer");
+    MOE_REQUIRE((((uintptr_t)x | (uintptr_t)h_scratch | (uintptr_t)z_q) & 15) == 0 && (((uintptr_t)z_scale | (uintptr_t)offsets | (uintptr_t)perm) & 3) == 0,
+                MOE_ERR_UNSUPPORTED, "moe_grouped_ffn_keep: x, h_scratch and z_q have to be aligned to 16 bytes");
+    ok = moe_check_gemm_device();
+    if (ok != MOE_OK) return ok;
+    NtArgs a = {};
+    a.rows = (const uint16_t*)x;
+    a.offsets = offsets;
+    a.perm = perm;
+    a.w_ptrs = w_in;
+    a.T = T;
+    a.k = k;
+    a.E = E;
+    a.F = F;
+    a.Z = act == MOE_SWIGLU ? 2 * F : F;
+    a.N = a.Z;
+    a.KT = a.KT0 = d / 64;
+    a.ld_rows = a.ld_w = d;
+    a.h = (uint16_t*)h_scratch;
+    a.q_out = z_q;
+    a.scale_out = z_scale;
+    return act == MOE_SWIGLU ? launch_nt_rows<KEEP_SWIGLU>(a, T * k, (hipStream_t)stream) : launch_nt_rows<KEEP_RELU>(a, T * k, (hipStream_t)stream);
+}
+
+// Workspace: dz [A,Z] and w h [A,F] in bf16, the parts of dgate_w [A, ceil(F / 128)] in fp32, dy [T,d] in bf16 where it comes in fp32, each
+// rounded up to 256 bytes.
+static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+size_t moe_ffn_back_bytes(int T, int d, int F, int k) {
+    if (T < 0 || d < 1 || F < 1 || k < 1) return 0;
+    const size_t A = (size_t)T * k;
+    return up256(A * 2 * F * 2) + up256(A * F * 2) + up256(A * ((F + 127) / 128) * 4) + up256((size_t)T * d * 2);
+}
+
+extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const void* x, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt,
+                                        const void* w_a, const void* w_b, const void* w_o, const int32_t* offsets, const int32_t* perm,
+                                        const int32_t* inv_perm, const float* gate_w, const int8_t* z_q, const float* z_scale, float* dx_perm,
+                                        float* dgate_w, void* dw_a, void* dw_b, void* dw_o, moe_dtype dw_dt, int accumulate, void* ws, size_t ws_bytes,
+                                        void* stream) {
+    int ok = check_shape("moe_grouped_ffn_backward", T, d, F, E, k, act, dt);
+    if (ok != MOE_OK) return ok;
+    const bool sw = act == MOE_SWIGLU;
+    MOE_REQUIRE(moe_dtype_ok(dy_dt) && moe_dtype_ok(dw_dt), MOE_ERR_UNSUPPORTED, "moe_grouped_ffn_backward: dy of dtype %d, gradients of dtype %d", (int)dy_dt, (int)dw_dt);
+    const bool dw = dw_a || dw_b || dw_o;
+    MOE_REQUIRE(!dw || (dw_a && dw_o && (dw_b != nullptr) == sw), MOE_ERR_ARG, "moe_grouped_ffn_backward: the matrices' gradients are wanted all or none");
+    MOE_REQUIRE(offsets, MOE_ERR_ARG, "moe_grouped_ffn_backward: null pointer");
+    if (T > 0)
+        MOE_REQUIRE(dy && (x || !dw) && w_o && perm && z_q && z_scale && (inv_perm || !dgate_w) && (!dx_perm || (w_a && (w_b != nullptr) == sw)), MOE_ERR_ARG,
+                    "moe_grouped_ffn_backward: null pointer, or w_b with MOE_RELU");
+    const size_t A = (size_t)T * k, Z = sw ? 2 * (size_t)F : F;
+    const int parts = (F + 127) / 128;
+    const size_t n_dz = up256(A * Z * 2), n_wh = up256(A * F * 2), n_parts = up256(A * parts * 4);
+    const size_t need = n_dz + n_wh + n_parts + (dy_dt == MOE_F32 ? up256((size_t)T * d * 2) : 0);
+    MOE_REQUIRE(T == 0 || (ws && ws_bytes >= need), MOE_ERR_WORKSPACE, "moe_grouped_ffn_backward: workspace of %zu bytes, %zu needed", ws_bytes, need);
+    MOE_REQUIRE((((uintptr_t)dy | (uintptr_t)x | (uintptr_t)w_a | (uintptr_t)w_b | (uintptr_t)w_o | (uintptr_t)z_q | (uintptr_t)dx_perm | (uintptr_t)dw_a |
+                  (uintptr_t)dw_b | (uintptr_t)dw_o | (uintptr_t)ws) & 15) == 0, MOE_ERR_UNSUPPORTED, "moe_grouped_ffn_backward: pointers have to be aligned to 16 bytes");
+    ok = moe_check_gemm_device();
+    if (ok != MOE_OK) return ok;
+    const hipStream_t st = (hipStream_t)stream;
+    if (dy_dt == MOE_F32 && T > 0) {
+        u32x4* to = (u32x4*)((unsigned char*)ws + n_dz + n_wh + n_parts);
+        const size_t n = (size_t)T * d / 8;
+        hipLaunchKernelGGL(narrow_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const f32x4*)dy, to, n);
+        MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (dy)");
+        dy = to;
+    }
+    if (T > 0) {
+        NtArgs a = {};
+        a.rows = (const uint16_t*)dy;
+        a.offsets = offsets;
+        a.perm = perm;
+        a.w0 = (const uint16_t*)w_o;
+        a.w_stride = (size_t)d * F;
+        a.T = T;
+        a.k = k;
+        a.E = E;
+        a.F = a.N = F;
+        a.Z = (int)Z;
+        a.KT = a.KT0 = d / 64;
+        a.ld_rows = a.ld_w = d;
+        a.parts = parts;
+        a.q_in = z_q;
+        a.scale_in = z_scale;
+        a.gate_w = gate_w;
+        a.dz = (uint16_t*)ws;
+        a.wh = (uint16_t*)((unsigned char*)ws + n_dz);
+        a.dgate_part = (float*)((unsigned char*)ws + n_dz + n_wh);
+        ok = sw ? launch_nt_rows<HID_SWIGLU>(a, (int)A, st) : launch_nt_rows<HID_RELU>(a, (int)A, st);
+        if (ok != MOE_OK) return ok;
+        if (dgate_w) {
+            hipLaunchKernelGGL(dgate_kernel, dim3((unsigned)((A + 255) / 256)), dim3(256), 0, st, a.dgate_part, inv_perm, (int)A, parts, dgate_w);
+            MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (gate values)");
+        }
+        if (dx_perm) {
+            NtArgs b = a;
+            b.rows = a.dz;
+            b.w0 = (const uint16_t*)w_a;
+            b.w1 = (const uint16_t*)w_b;
+            b.N = d;
+            b.KT0 = F / 64;
+            b.KT = (int)Z / 64;
+            b.ld_rows = (int)Z;
+            b.ld_w = F;
+            b.dx_perm = dx_perm;
+            ok = launch_nt_rows<DX>(b, (int)A, st);
+            if (ok != MOE_OK) return ok;
+        }
+    }
+    if (dw) {
+        TnArgs t = {};
+        t.x = (const uint16_t*)x;
+        t.dy = (const uint16_t*)dy;
+        t.dz = (const uint16_t*)ws;
+        t.wh = (const uint16_t*)((unsigned char*)ws + n_dz);
+        t.offsets = offsets;
+        t.perm = perm;
+        t.T = T;
+        t.k = k;
+        t.E = E;
+        t.d = d;
+        t.F = F;
+        t.Z = (int)Z;
+        t.mats = sw ? 3 : 2;
+        t.dwa = dw_a;
+        t.dwb = dw_b;
+        t.dwo = dw_o;
+        if (dw_dt == MOE_F32) ok = accumulate ? launch_tn<float, true>(t, st) : launch_tn<float, false>(t, st);
+        else ok = accumulate ? launch_tn<uint16_t, true>(t, st) : launch_tn<uint16_t, false>(t, st);
+        if (ok != MOE_OK) return ok;
+    }
+    return MOE_OK;
+}

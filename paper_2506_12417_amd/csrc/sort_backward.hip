@@ -1,0 +1,211 @@
+// The gradients of the token sort and of the weighted combine (moe_permute, moe_unpermute_combine):
+//
+//   moe_unpermute_combine_backward   dy_perm[r] = gate_w[a] dy[t]     dgate_w[a] = sum_c dy[t,c] y_perm[r,c]      r = inv_perm[a], a = t k + j
+//   moe_permute_backward             dx[t] = dx_add[t] + sum_j dx_perm[inv_perm[t k + j]]
+//
+// HBM bound: every row is read once and written once.  An assignment without a row (inv_perm negative) has dgate_w 0 and adds nothing.
+#include "common.h"
+#include "gemm_util.h"
+#include "lanes.h"
+
+namespace {
+
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+constexpr int NTH = 256;
+constexpr int GROUP = 4;                                   // rows of a token whose loads are under way together
+
+// a lane's values of a piece of 512 columns: eight neighbours (VEC), else every 64th
+template <bool VEC> __device__ __forceinline__ int col_of(int piece, int lane, int i) { return piece * 512 + (VEC ? lane * 8 + i : i * 64 + lane); }
+
+template <bool VEC> __device__ __forceinline__ void fetch(const float* row, int d, int piece, int lane, bool on, float (&v)[8]) {
+    if constexpr (VEC) {
+        const int c = col_of<true>(piece, lane, 0);
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        if (on && c < d) {
+            a = __builtin_nontemporal_load((const f32x4*)(row + c));
+            b = __builtin_nontemporal_load((const f32x4*)(row + c) + 1);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = col_of<false>(piece, lane, i);
+            v[i] = on && c < d ? row[c] : 0.f;
+        }
+    }
+}
+template <bool VEC> __device__ __forceinline__ void fetch(const uint16_t* row, int d, int piece, int lane, bool on, float (&v)[8]) {
+    if constexpr (VEC) {
+        const int c = col_of<true>(piece, lane, 0);
+        u32x4 a = {0u, 0u, 0u, 0u};
+        if (on && c < d) a = __builtin_nontemporal_load((const u32x4*)(row + c));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i & 1 ? a[i >> 1] & 0xffff0000u : a[i >> 1] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = col_of<false>(piece, lane, i);
+            v[i] = on && c < d ? bf16_to_f32(row[c]) : 0.f;
+        }
+    }
+}
+template <bool VEC> __device__ __forceinline__ void put(float* row, int d, int piece, int lane, const float (&v)[8]) {
+    if constexpr (VEC) {
+        const int c = col_of<true>(piece, lane, 0);
+        if (c >= d) return;
+        __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, (f32x4*)(row + c));
+        __builtin_nontemporal_store(f32x4{v[4], v[5], v[6], v[7]}, (f32x4*)(row + c) + 1);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col_of<false>(piece, lane, i) < d) row[col_of<false>(piece, lane, i)] = v[i];
+    }
+}
+template <bool VEC> __device__ __forceinline__ void put(uint16_t* row, int d, int piece, int lane, const float (&v)[8]) {
+    if constexpr (VEC) {
+        const int c = col_of<true>(piece, lane, 0);
+        if (c >= d) return;
+        const f32x8 f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, __builtin_convertvector(f, bf16x8)), (u32x4*)(row + c));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (col_of<false>(piece, lane, i) < d) row[col_of<false>(piece, lane, i)] = __builtin_bit_cast(uint16_t, (__bf16)v[i]);
+    }
+}
+
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp_xchg<0>(v);
+    v += dpp_xchg<1>(v);
+    v += dpp_xchg<2>(v);
+    v += dpp_xchg<3>(v);
+    const int b = __float_as_int(v);
+    return (__int_as_float(__builtin_amdgcn_readlane(b, 0)) + __int_as_float(__builtin_amdgcn_readlane(b, 16))) +
+           (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
+}
+
+// A wavefront has a token; its rows go GROUP at a time, so that dy is fetched once for up to four of them.
+template <typename D, typename P, bool VEC>
+__global__ __launch_bounds__(NTH) void combine_backward_kernel(const D* __restrict__ dy, const float* __restrict__ y_perm, const int32_t* __restrict__ inv_perm,
+                                                               const float* __restrict__ gate_w, int T, int d, int k, P* __restrict__ dy_perm,
+                                                               float* __restrict__ dgate_w) {
+    const int t = sgpr((int)(blockIdx.x * (NTH / 64) + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
+    if (t >= T) return;
+    const D* from = dy + (size_t)t * d;
+    for (int j0 = 0; j0 < k; j0 += GROUP) {
+        int row[GROUP];
+        float w[GROUP], sum[GROUP];
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) {
+            const size_t a = (size_t)t * k + j0 + j;
+            const bool on = j0 + j < k;
+            row[j] = on ? inv_perm[a] : -1;
+            w[j] = on && gate_w ? gate_w[a] : 1.f;
+            sum[j] = 0.f;
+        }
+        for (int piece = 0; piece * 512 < d; ++piece) {
+            float g[8], y[GROUP][8];
+            fetch<VEC>(from, d, piece, lane, true, g);
+            if (dgate_w) {
+#pragma unroll
+                for (int j = 0; j < GROUP; ++j) fetch<VEC>(y_perm + (size_t)(row[j] < 0 ? 0 : row[j]) * d, d, piece, lane, row[j] >= 0, y[j]);
+#pragma unroll
+                for (int j = 0; j < GROUP; ++j)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum[j] = fmaf(g[i], y[j][i], sum[j]);
+            }
+            if (dy_perm) {
+#pragma unroll
+                for (int j = 0; j < GROUP; ++j) {
+                    if (row[j] < 0) continue;
+                    float v[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] = w[j] * g[i];
+                    put<VEC>(dy_perm + (size_t)row[j] * d, d, piece, lane, v);
+                }
+            }
+        }
+        if (dgate_w) {
+#pragma unroll
+            for (int j = 0; j < GROUP; ++j) {
+                const float s = wave_sum(sum[j]);
+                if (j0 + j < k && lane == 0) dgate_w[(size_t)t * k + j0 + j] = row[j] < 0 ? 0.f : s;
+            }
+        }
+    }
+}
+
+template <typename P, bool VEC>
+__global__ __launch_bounds__(NTH) void permute_backward_kernel(const float* __restrict__ dx_perm, const int32_t* __restrict__ inv_perm, int T, int d, int k,
+                                                               const float* __restrict__ dx_add, P* __restrict__ dx, int pieces) {
+    const size_t id = (size_t)blockIdx.x * (NTH / 64) + (threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int t = sgpr((int)(id / (unsigned)pieces)), piece = sgpr((int)(id % (unsigned)pieces));
+    if (t >= T) return;
+    float acc[8];
+    fetch<VEC>(dx_add + (size_t)t * d, d, piece, lane, dx_add != nullptr, acc);
+    for (int j0 = 0; j0 < k; j0 += GROUP) {
+        float y[GROUP][8];
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j) {
+            const int r = j0 + j < k ? inv_perm[(size_t)t * k + j0 + j] : -1;
+            fetch<VEC>(dx_perm + (size_t)(r < 0 ? 0 : r) * d, d, piece, lane, r >= 0, y[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < GROUP; ++j)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[i] += y[j][i];
+    }
+    put<VEC>(dx + (size_t)t * d, d, piece, lane, acc);
+}
+
+bool whole_pieces(int d, std::initializer_list<const void*> ps) {
+    uintptr_t all = 0;
+    for (const void* p : ps) all |= (uintptr_t)p;
+    return d % 8 == 0 && (all & 15) == 0;
+}
+
+}  // namespace
+
+extern "C" int moe_unpermute_combine_backward(const void* dy, moe_dtype dy_dt, const float* y_perm, const int32_t* inv_perm, const float* gate_w, int T, int d,
+                                              int k, void* dy_perm, moe_dtype perm_dt, float* dgate_w, void* stream) {
+    MOE_REQUIRE(T >= 0 && d >= 1 && k >= 1, MOE_ERR_ARG, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
+    MOE_REQUIRE(moe_dtype_ok(dy_dt) && moe_dtype_ok(perm_dt), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: dtypes %d, %d", (int)dy_dt, (int)perm_dt);
+    MOE_REQUIRE((long long)T * k < (1ll << 31) && T < (1 << 30), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: T=%d k=%d", T, k);
+    if (T == 0) return MOE_OK;
+    MOE_REQUIRE(dy && inv_perm && (dy_perm || dgate_w) && (y_perm || !dgate_w), MOE_ERR_ARG, "moe_unpermute_combine_backward: null pointer");
+    const bool vec = whole_pieces(d, {dy, y_perm, dy_perm});
+    auto go = [&](auto kern, auto* from, auto* to) {
+        hipLaunchKernelGGL(kern, dim3((T + NTH / 64 - 1) / (NTH / 64)), dim3(NTH), 0, (hipStream_t)stream, from, y_perm, inv_perm, gate_w, T, d, k, to, dgate_w);
+    };
+    auto types = [&](auto* from, auto* to) {
+        using D = std::remove_const_t<std::remove_pointer_t<decltype(from)>>;
+        using P = std::remove_pointer_t<decltype(to)>;
+        vec ? go(combine_backward_kernel<D, P, true>, from, to) : go(combine_backward_kernel<D, P, false>, from, to);
+    };
+    if (dy_dt == MOE_F32) perm_dt == MOE_F32 ? types((const float*)dy, (float*)dy_perm) : types((const float*)dy, (uint16_t*)dy_perm);
+    else perm_dt == MOE_F32 ? types((const uint16_t*)dy, (float*)dy_perm) : types((const uint16_t*)dy, (uint16_t*)dy_perm);
+    MOE_CHECK_LAUNCH("moe_unpermute_combine_backward");
+    return MOE_OK;
+}
+
+extern "C" int moe_permute_backward(const float* dx_perm, const int32_t* inv_perm, int T, int d, int k, const float* dx_add, void* dx, moe_dtype dx_dt,
+                                    void* stream) {
+    MOE_REQUIRE(T >= 0 && d >= 1 && k >= 1, MOE_ERR_ARG, "moe_permute_backward: T=%d d=%d k=%d", T, d, k);
+    MOE_REQUIRE(moe_dtype_ok(dx_dt), MOE_ERR_UNSUPPORTED, "moe_permute_backward: dtype %d", (int)dx_dt);
+    const int pieces = (int)(((long long)d + 511) / 512);
+    MOE_REQUIRE((long long)T * k < (1ll << 31) && (long long)T * pieces < (1ll << 32), MOE_ERR_UNSUPPORTED, "moe_permute_backward: T=%d d=%d k=%d", T, d, k);
+    if (T == 0) return MOE_OK;
+    MOE_REQUIRE(dx_perm && inv_perm && dx, MOE_ERR_ARG, "moe_permute_backward: null pointer");
+    const bool vec = whole_pieces(d, {dx_perm, dx_add, dx});
+    const unsigned grid = (unsigned)(((long long)T * pieces + NTH / 64 - 1) / (NTH / 64));
+    auto go = [&](auto kern, auto* to) {
+        hipLaunchKernelGGL(kern, dim3(grid), dim3(NTH), 0, (hipStream_t)stream, dx_perm, inv_perm, T, d, k, dx_add, to, pieces);
+    };
+    if (dx_dt == MOE_F32) vec ? go(permute_backward_kernel<float, true>, (float*)dx) : go(permute_backward_kernel<float, false>, (float*)dx);
+    else vec ? go(permute_backward_kernel<uint16_t, true>, (uint16_t*)dx) : go(permute_backward_kernel<uint16_t, false>, (uint16_t*)dx);
+    MOE_CHECK_LAUNCH("moe_permute_backward");
+    return MOE_OK;
+}

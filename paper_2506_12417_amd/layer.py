@@ -70,8 +70,10 @@ class MoELayer:
     def __init__(self, T: int, d: int, F: int, E: int, k: int, act: str, dtype: str, renorm: int,
                  shared_F: int = 0, n_bins: int = XCDS, q_tokens: Optional[int] = None,
                  policy: int = B.MOE_PLAN_HARMOENY, tile_m: Optional[int] = None, device="cuda:0",
-                 fuse_gather: Optional[bool] = None):
+                 fuse_gather: Optional[bool] = None, train: bool = False):
         self.T, self.d, self.F, self.E, self.k, self.renorm = T, d, F, E, k, renorm
+        assert not train or dtype == "bf16", "the experts' gradients are there for bf16 layers"
+        self.train = train
         self.A = T * k
         self.act = B.MOE_SWIGLU if act == "swiglu" else B.MOE_RELU
         self.dt = B.MOE_BF16 if dtype == "bf16" else B.MOE_F32
@@ -139,6 +141,30 @@ class MoELayer:
             self.s_y = torch.empty((T, d), dtype=f32, device=dev)
             B.moe_plan_tiles(self.s_counts, self.s_offsets, 1, T, self.s_tile_m, n_bins, self.q_tokens,
                              B.MOE_PLAN_HARMOENY, self.s_tiles, self.s_capacity, self.s_hdr, None)
+        if train:
+            self._make_training_buffers()
+
+    def _make_training_buffers(self):
+        """What a training step keeps: the matrices as given (`weight`), their gradients and the router's (`grad`), the hidden pre-activations in
+        8 bits, and what the backward calls write."""
+        T, d, E, k, A, dev = self.T, self.d, self.E, self.k, self.A, self.device
+        f32, new = torch.float32, lambda shape, t: torch.empty(shape, dtype=t, device=dev)     # noqa: E731
+        self.weight: Dict[str, Optional[torch.Tensor]] = {}
+        shapes = [("", E, A, self.F, self.act)] + ([("s", 1, T, self.shared_F, B.MOE_SWIGLU)] if self.shared_F else [])
+        self.kept = {}
+        need = B.moe_workspace_bytes(B.MOE_OP_ROUTE_BACKWARD, T, d, 0, E, 0, self.dt)
+        for s, n, rows, F, act in shapes:
+            Z = 2 * F if act == B.MOE_SWIGLU else F
+            self.weight.update({s + "a": new((n, d, F), self.tdt), s + "b": new((n, d, F), self.tdt) if Z > F else None, s + "o": new((n, F, d), self.tdt)})
+            self.kept[s] = (new((rows, Z), torch.int8), new((rows, Z // 64), f32))
+            need = max(need, B.moe_workspace_bytes(B.MOE_OP_FFN_BACKWARD, T, d, F, n, rows // max(T, 1), self.dt))
+        self.grad = {n: None if w is None else torch.empty_like(w) for n, w in self.weight.items()}
+        self.grad["W_g"], self.grad["bias"] = new((d, E), f32), new((E,), f32)
+        self.logits, self.dlogits, self.dgate_w = new((T, E), f32), new((T, E), f32), new((T, k), f32)
+        self.dx_perm, self.dx_sum, self.dx = new((A, d), f32), new((T, d), f32), new((T, d), self.tdt)
+        self.back_ws = new((max(need, 16),), torch.uint8)
+        if self.shared_F:
+            self.s_perm = torch.arange(T, dtype=torch.int32, device=dev)
 
     # ------------------------------------------------------------------ parameters
     def load_router(self, W_g: np.ndarray, b: Optional[np.ndarray], packed: Optional[bool] = None):
@@ -156,11 +182,36 @@ class MoELayer:
 
     def load_experts(self, weights: Dict[str, np.ndarray]):
         """weights: stacked [E, ...] arrays in the paper's orientation."""
+        if self.train:
+            names = ("Wg", "Wu", "Wd") if self.act == B.MOE_SWIGLU else ("W1", None, "W2")
+            for n, a in zip("abo", names):
+                if a is not None:
+                    self.weight[n].copy_(to_device(np.asarray(weights[a]), self.device))
+            self._pack(self.experts, "")
+            return
         for e in range(self.E):
             self.experts.load_expert(e, {n: a[e] for n, a in weights.items() if not n.startswith("s")})
 
     def load_shared(self, w: Dict[str, np.ndarray]):
+        if self.train:
+            for n, a in zip(("sa", "sb", "so"), ("Wg", "Wu", "Wd")):
+                self.weight[n][0].copy_(to_device(np.asarray(w[a]), self.device))
+            self._pack(self.shared, "s")
+            return
         self.shared.load_expert(0, w)
+
+    def _pack(self, g: ExpertGroup, s: str, stream=None):
+        w = self.weight
+        B.moe_pack_weights(w[s + "a"], w[s + "b"], g.E, g.d, g.F, g.dt, g.w_in, stream)
+        B.moe_pack_w_out(w[s + "o"], g.E, g.F, g.d, g.dt, g.w_out, stream)
+
+    def pack(self, stream=None):
+        """After a change of `weight` or of W_g (an optimizer's step): the layouts that the forward products and the router read."""
+        self._pack(self.experts, "", stream)
+        if self.shared_F:
+            self._pack(self.shared, "s", stream)
+        if self.packed_router:
+            B.moe_pack_router(self.W_g, self.d, self.E, self.dt, self.W_gt, self.w_norm2, stream)
 
     # ------------------------------------------------------------------ the path, step by step
     def route(self, x, logits_out=None, stream=None):
@@ -271,6 +322,9 @@ class MoELayer:
         if y is not None:
             B.check_rows("y", y, self.T, self.d, (torch.float32,), self.own_y.device)
         self.y = self.own_y if y is None else y
+        if self.train:
+            assert marks is None and stages is None and not rows, "a training layer runs whole"
+            return self._forward_train(x, routed, stream)
         mark = None
         if stages is not None:
             stream = None
@@ -321,6 +375,55 @@ class MoELayer:
         if mark:
             mark("combine")
         return self.y
+
+    def _forward_train(self, x: torch.Tensor, routed: bool, stream) -> torch.Tensor:
+        g, shape, kinds = self.experts, (self.T, self.d, self.F, self.E), (self.act, self.dt)
+        B.check_rows("x", x, self.T, self.d, (self.tdt,), self.own_y.device)
+        self.was_routed = routed             # by the caller: the gate values are not the router's, which gets no gradient
+        if not routed:
+            self.route(x, self.logits, stream)
+        self.permute_plan(stream)
+        B.moe_grouped_ffn_keep(x, *shape, self.k, *kinds, g.in_ptrs, self.offsets, self.perm, self.h, *self.kept[""], stream)
+        table = (g.in_ptrs, g.out_ptrs, self.tiles, self.plan_hdr, self.ffn_tile_m, self.h)
+        if self.fold_combine:
+            B.moe_grouped_ffn_top1_phase(2, None, *shape, *kinds, *table, self.perm, self.gate_w, self.y, stream)
+            return self.y
+        B.moe_grouped_ffn_phase(2, None, self.A, *shape[1:], *kinds, *table, self.y_perm, stream)
+        if self.shared_F:
+            s, one = self.shared, (self.T, self.d, self.shared_F, 1)
+            B.moe_grouped_ffn_keep(x, *one, 1, B.MOE_SWIGLU, self.dt, s.in_ptrs, self.s_offsets, self.s_perm, self.s_h, *self.kept["s"], stream)
+            B.moe_grouped_ffn_phase(2, None, *one, B.MOE_SWIGLU, self.dt, s.in_ptrs, s.out_ptrs, self.s_tiles, self.s_hdr, self.s_ffn_tile_m, self.s_h,
+                                    self.s_y, stream)
+        self.combine(True, stream)
+        return self.y
+
+    def backward(self, dy: torch.Tensor, x: torch.Tensor, dlogits_add: Optional[torch.Tensor] = None, accumulate: bool = False,
+                 stream=None) -> torch.Tensor:
+        """The gradients of the last forward() of a training layer (train=True), whose x this is: returns that of x ([T,d], the layer's type);
+        those of the matrices and the router go to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).
+        dy: [T,d] fp32 or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the experts'
+        gradients are added to what `grad` holds (the router's are not: they are set)."""
+        assert self.train, "MoELayer(train=True) keeps what the gradients are made of"
+        T, d, E, k, dev = self.T, self.d, self.E, self.k, self.own_y.device
+        B.check_rows("dy", dy, T, d, (torch.float32, self.tdt), dev)
+        B.check_rows("x", x, T, d, (self.tdt,), dev)
+        if dlogits_add is not None:
+            B.check_rows("dlogits_add", dlogits_add, T, E, (torch.float32,), dev)
+        w, g, n = self.weight, self.grad, self.back_ws.numel()
+        dy_dt, add, acc = B.dtype_code(dy), None, int(accumulate)
+        if self.shared_F:
+            B.moe_grouped_ffn_backward(dy, dy_dt, x, T, d, self.shared_F, 1, 1, B.MOE_SWIGLU, self.dt, w["sa"], w["sb"], w["so"], self.s_offsets,
+                                       self.s_perm, None, None, *self.kept["s"], self.dx_sum, None, g["sa"], g["sb"], g["so"], self.dt, acc,
+                                       self.back_ws, n, stream)
+            add = self.dx_sum
+        B.moe_grouped_ffn_backward(dy, dy_dt, x, T, d, self.F, E, k, self.act, self.dt, w["a"], w["b"], w["o"], self.offsets, self.perm, self.inv_perm,
+                                   self.gate_w, *self.kept[""], self.dx_perm, self.dgate_w, g["a"], g["b"], g["o"], self.dt, acc, self.back_ws, n, stream)
+        if not self.was_routed:
+            B.moe_route_topk_backward(self.dgate_w, self.gate_w, self.expert_idx, self.logits, dlogits_add, x, self.W_g, T, d, E, k, self.renorm, self.dt,
+                                      self.dlogits, add, self.dx_sum, g["W_g"], g["bias"], self.back_ws, n, stream)
+            add = self.dx_sum
+        B.moe_permute_backward(self.dx_perm, self.inv_perm, T, d, k, add, self.dx, self.dt, stream)
+        return self.dx
 
 
 class ExpertCache:
