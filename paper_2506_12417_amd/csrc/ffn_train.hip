@@ -41,6 +41,36 @@ __device__ __forceinline__ void wg_barrier() {
     asm volatile("" ::: "memory");
 }
 
+// A buffer descriptor as four registers, for loads written as assembly: the compiler counts a global -> LDS load that it knows of as a store
+// that any LDS read may depend on, and waits for all of them before reads that it cannot tell apart from their targets (the transposing
+// ones, row tables): the loads here have no register that is written, and the kernels wait for them by themselves.
+__device__ __forceinline__ u32x4 descriptor(const void* p, unsigned bytes) {
+    const uint64_t u = (uint64_t)p;
+    return u32x4{(unsigned)sgpr((int)(unsigned)u), (unsigned)sgpr((int)(unsigned)(u >> 32)) & 0xffffu, (unsigned)sgpr((int)bytes), 0x00020000u};
+}
+// 16 (4) bytes a lane to LDS at `to` (bytes, wave-uniform) + 16 (4) lane; only voff is range-checked
+__device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned to, unsigned voff, unsigned soff) {
+    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(to), "v"(voff), "s"(d), "s"(soff) : "memory");
+}
+__device__ __forceinline__ void load_to_lds4(const u32x4& d, unsigned to, unsigned voff) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
+}
+
+// What was issued before an item's stores is there once only those (at least `stores` of them) are under way.
+__device__ __forceinline__ void wait_landed(int stores) {
+    if (stores >= 63) MOE_WAIT_VMCNT(63);
+    else if (stores >= 32) MOE_WAIT_VMCNT(32);
+    else if (stores >= 16) MOE_WAIT_VMCNT(16);
+    else MOE_WAIT_VMCNT(0);
+}
+
+// a / k for a < 2^30, m = (2^32 - 1) / k: the product is one too small at most (k = 1 too)
+__device__ __forceinline__ unsigned divided(unsigned a, unsigned k, unsigned m) {
+    const unsigned q = __umulhi(a, m);
+    return a - q * k >= k ? q + 1 : q;
+}
+
 // Sum and largest over the four lanes l16, l16 + 16, l16 + 32, l16 + 48; all four get it.
 __device__ __forceinline__ float quarter_sum(float v) {
     const unsigned b = __float_as_uint(v);
@@ -118,7 +148,7 @@ template <int TR> struct Nt {
     static constexpr int NI = TR / 64;                     // 32-row blocks of a wavefront (two wavefronts share the rows, block by block)
     static constexpr int F_BYTES = 256 * 128, R_BYTES = TR * 128, STAGE = F_BYTES + R_BYTES;
     static constexpr int NFL = 8, NRL = TR / 32, LPS = NFL + NRL;      // loads per thread and stage
-    static constexpr size_t SMEM = 2 * STAGE + 2 * 256 * 4;
+    static constexpr size_t SMEM = 2 * STAGE + 4 * TR * 4;
 };
 template <int TR> using NtAcc = f32x4[Nt<TR>::NI][2][4][2];            // [32-row block][its half][32-feature block][its half]
 template <int TR> struct NtFrags { bf16x8 f[4][2], r[Nt<TR>::NI][2]; };
@@ -142,56 +172,79 @@ template <int TR> __device__ __forceinline__ NtItem nt_locate(const NtArgs& a, c
     return it;
 }
 
-struct NtLoader {
-    __amdgpu_buffer_rsrc_t rr, rf0, rf1;
-    unsigned vr[8], vf;            // byte offsets: of this thread's rows, of its first feature
+// The loader's place in the stream of stages: it runs two of them ahead of the multiplications, across the items' borders.
+template <int TR> struct NtLoader {
+    u32x4 rr, rf;
+    unsigned vr[Nt<TR>::NRL], vf;  // byte offsets: of this thread's rows, of its first feature
+    int item, kt, buf, seq;
+};
+struct NtWork {
+    int ncb, end, stride;
+    unsigned ring, rinfo, div;     // LDS addresses; for the division by k
+    int wave, lane, ld_row;
+    unsigned piece;
 };
 
-template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs& a, const NtItem& it, const int* rinfo, int ld_row, unsigned piece, NtLoader& L) {
+// (gather) the assignments of an item's rows: four items' tables in turn
+template <int TR> __device__ __forceinline__ void nt_fetch_rows(const NtArgs& a, const NtWork& w, const NtItem& it, int seq) {
+    if (w.wave * 64 < TR)
+        load_to_lds4(descriptor(a.perm + it.row0, (unsigned)it.rc * 4u), w.rinfo + (unsigned)((seq & 3) * TR + w.wave * 64) * 4u, (unsigned)(w.wave * 64 + w.lane) * 4u);
+}
+
+template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L) {
+    if (L.item >= w.end) {                                 // past the last item: nothing is fetched, the schedule stays
+        L.rr = L.rf = descriptor(a.rows, 0u);
+        return;
+    }
+    const NtItem it = nt_locate<TR>(a, tiles, w.ncb, L.item);
     const int nr = a.N - it.n0 < 256 ? a.N - it.n0 : 256;
     const unsigned bytes = (unsigned)nr * (unsigned)a.ld_w * 2u;
     if constexpr (KIND <= KEEP_SWIGLU) {
-        L.rf0 = make_rsrc((const uint16_t*)a.w_ptrs[it.e] + (size_t)it.n0 * a.ld_w, bytes);
-        L.vf = (unsigned)ld_row * (unsigned)a.ld_w * 2u + piece;
+        L.rf = descriptor((const uint16_t*)a.w_ptrs[it.e] + (size_t)it.n0 * a.ld_w, bytes);
     } else {
         const size_t at = (size_t)it.e * a.w_stride + (size_t)it.n0 * a.ld_w;
-        L.rf0 = make_rsrc(a.w0 + at, bytes);
-        if constexpr (KIND == DX) L.rf1 = make_rsrc((a.w1 ? a.w1 : a.w0) + at, bytes);
-        // slot 16 h + j of a block of 32 holds feature 8 (j / 4) + 4 h + j % 4: the two halves give a lane eight neighbours
-        const int f = ((ld_row & 12) << 1) + ((ld_row & 16) >> 2) + (ld_row & 3);
-        L.vf = (unsigned)f * (unsigned)a.ld_w * 2u + piece;
+        L.rf = descriptor(a.w0 + at, bytes);
     }
     if constexpr (KIND == DX) {
-        L.rr = make_rsrc(a.rows + (size_t)it.row0 * a.ld_rows, (unsigned)it.rc * (unsigned)a.ld_rows * 2u);
-#pragma unroll
-        for (int q = 0; q < Nt<TR>::NRL; ++q) L.vr[q] = (unsigned)(q * 32 + ld_row) * (unsigned)a.ld_rows * 2u + piece;
+        L.rr = descriptor(a.rows + (size_t)it.row0 * a.ld_rows, (unsigned)it.rc * (unsigned)a.ld_rows * 2u);
     } else {
-        L.rr = make_rsrc(a.rows, (unsigned)a.T * (unsigned)a.ld_rows * 2u);
+        L.rr = descriptor(a.rows, (unsigned)a.T * (unsigned)a.ld_rows * 2u);
 #pragma unroll
         for (int q = 0; q < Nt<TR>::NRL; ++q) {
-            const int row = q * 32 + ld_row;
-            unsigned src = (unsigned)rinfo[row];
-            if (a.k != 1) src /= (unsigned)a.k;
+            const int row = q * 32 + w.ld_row;
+            unsigned src = (unsigned)rinfo[(L.seq & 3) * TR + row];
+            src = divided(src, (unsigned)a.k, w.div);
             // (a row past the tile's end gets an offset beyond the matrix: the range check reads zeros)
-            L.vr[q] = row < it.rc ? src * (unsigned)a.ld_rows * 2u + piece : 0xFFFFFFF0u;
+            L.vr[q] = row < it.rc ? src * (unsigned)a.ld_rows * 2u + w.piece : 0xFFFFFFF0u;
         }
+        if (L.item + w.stride < w.end) nt_fetch_rows<TR>(a, w, nt_locate<TR>(a, tiles, w.ncb, L.item + w.stride), L.seq + 1);
+        ++L.seq;
     }
 }
 
-// load q of stage kt (the features first)
-template <int KIND, int TR> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtLoader& L, unsigned char* ring, int wave, int kt, int q) {
-    unsigned char* to = ring + (kt & 1) * Nt<TR>::STAGE + wave * 1024;
+// load q of the loader's stage (the features first)
+template <int KIND, int TR> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, int q) {
+    const unsigned to = w.ring + (unsigned)(L.buf * Nt<TR>::STAGE + w.wave * 1024);
     if (q < Nt<TR>::NFL) {
-        const unsigned at = L.vf + (unsigned)(q * 32) * (unsigned)a.ld_w * 2u;
-        if (KIND == DX && kt >= a.KT0) __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rf1, (lds_void_t*)(to + q * 4096), 16, at, (unsigned)(kt - a.KT0) * 128u, 0, 0);
-        else __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rf0, (lds_void_t*)(to + q * 4096), 16, at, (unsigned)kt * 128u, 0, 0);
+        load_to_lds(L.rf, to + (unsigned)q * 4096u, L.vf + (unsigned)(q * 32) * (unsigned)a.ld_w * 2u, (unsigned)(KIND == DX && L.kt >= a.KT0 ? L.kt - a.KT0 : L.kt) * 128u);
     } else {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rr, (lds_void_t*)(to + Nt<TR>::F_BYTES + (q - Nt<TR>::NFL) * 4096), 16,
-                                                 L.vr[q < Nt<TR>::NFL ? 0 : q - Nt<TR>::NFL], (unsigned)kt * 128u, 0, 0);
+        load_to_lds(L.rr, to + (unsigned)(Nt<TR>::F_BYTES + (q - Nt<TR>::NFL) * 4096), L.vr[q < Nt<TR>::NFL ? 0 : q - Nt<TR>::NFL], (unsigned)L.kt * 128u);
+    }
+}
+// after the last load of a stage
+template <int KIND, int TR> __device__ __forceinline__ void nt_advance(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L) {
+    L.buf ^= 1;
+    ++L.kt;
+    if (KIND == DX && L.kt == a.KT0 && L.kt < a.KT)        // the second matrix: its place in the first one's stead
+        L.rf = descriptor((const void*)(((uint64_t)L.rf[1] << 32 | L.rf[0]) + ((uint64_t)a.w1 - (uint64_t)a.w0)), L.rf[2]);
+    if (L.kt == a.KT) {
+        L.kt = 0;
+        if (L.item < w.end) L.item += w.stride;
+        nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
     }
 }
 
-struct NtLane { int wave, lane, f_rd, r_rd; };             // f_rd, r_rd: first half's fragment of the first block
+struct NtLane { int f_rd, r_rd; };              // first half's fragment of the first block
 
 // fragment read j of a half (32 terms): features first
 template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const unsigned char* ring, int j, int at_f, int at_r) {
@@ -199,12 +252,14 @@ template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const
     else fr.r[(j - 8) >> 1][j & 1] = *(const bf16x8*)(ring + at_r + ((j - 8) >> 1) * 8192 + (j & 1) * 2048);
 }
 
-// Half S of stage kt: multiplies set S, reads the other.  LOAD: stage kt + 2 goes on its way (half 1: the buffer is free).
-template <int KIND, int TR, int S, bool LOAD, bool FULL>
-__device__ __forceinline__ void nt_half(const NtArgs& a, const NtLoader& L, const NtLane& ln, unsigned char* ring, int kt, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int ni_on) {
+// Half S of the stage in buffer `buf`: multiplies set S, reads the other.  Half 1 issues the loads of the stage after the next into the buffer that
+// this one has left.  FIRST: of an item, whose predecessor's stores (at least `stores`) may be under way.
+template <int KIND, int TR, int S, bool FIRST, bool FULL>
+__device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L, const NtLane& ln, const unsigned char* ring, int& buf,
+                                        NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
     constexpr int NI = Nt<TR>::NI, G = NI * 4, READS = 8 + 2 * NI, SPREAD = G >= 16 ? 12 : G;
-    const int buf = ((S == 0 ? kt : kt + 1) & 1) * Nt<TR>::STAGE;
-    const int at_f = buf + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf + (ln.r_rd ^ (S == 0 ? 64 : 0));
+    if (S == 1) buf ^= 1;
+    const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
 #pragma unroll
     for (int t = 0; t < G; ++t) {
         const int ni = t >> 2, n16 = (t >> 1) & 1, b0 = (t & 1) * 2;
@@ -219,32 +274,31 @@ __device__ __forceinline__ void nt_half(const NtArgs& a, const NtLoader& L, cons
 #pragma unroll
             for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) nt_read<TR>(fr[S ^ 1], ring, j, at_f, at_r);
         }
-        if (S == 1 && LOAD) {
+        if (S == 1) {
 #pragma unroll
-            for (int q = t * Nt<TR>::LPS / G; q < (t + 1) * Nt<TR>::LPS / G; ++q) nt_load<KIND, TR>(a, L, ring, ln.wave, kt + 2, q);
+            for (int q = t * Nt<TR>::LPS / G; q < (t + 1) * Nt<TR>::LPS / G; ++q) nt_load<KIND, TR>(a, w, L, q);
         }
         __builtin_amdgcn_sched_barrier(0);
     }
     if (S == 0) {
-        // everybody has read all of stage kt, and stage kt + 1 is there
+        // everybody has read all of this stage, and the next one is there
         MOE_WAIT_LGKMCNT(0);
-        MOE_WAIT_VMCNT(0);
+        if (FIRST) wait_landed(stores);
+        else MOE_WAIT_VMCNT(0);
         wg_barrier();
+        nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
     }
 }
 
 template <int KIND, int TR, bool FULL>
-__device__ __forceinline__ void nt_contract(const NtArgs& a, const NtLoader& L, const NtLane& ln, unsigned char* ring, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int ni_on) {
-    int kt = 0;
+__device__ __forceinline__ void nt_contract(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L, const NtLane& ln, const unsigned char* ring,
+                                            int& buf, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
+    nt_half<KIND, TR, 0, true, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
+    nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
 #pragma clang loop unroll(disable)
-    for (; kt + 2 < a.KT; ++kt) {
-        nt_half<KIND, TR, 0, true, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
-        nt_half<KIND, TR, 1, true, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
-    }
-#pragma clang loop unroll(disable)
-    for (; kt < a.KT; ++kt) {
-        nt_half<KIND, TR, 0, false, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
-        nt_half<KIND, TR, 1, false, FULL>(a, L, ln, ring, kt, acc, fr, ni_on);
+    for (int kt = 1; kt < a.KT; ++kt) {
+        nt_half<KIND, TR, 0, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
+        nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
     }
 }
 
@@ -395,81 +449,80 @@ template <int KIND, int TR>
 __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass makes the stub only: it has no buffer descriptors)
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
-    int* rinfo = (int*)(ring + 2 * Nt<TR>::STAGE);         // (gather) assignments of an item's rows, two items in turn
+    const int* rinfo = (const int*)(ring + 2 * Nt<TR>::STAGE);
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const int l16 = lane & 15, lq = lane >> 4;
     const Sums tiles = sums_over_experts(a.offsets, a.E, lane, [](int n) { return (n + TR - 1) / TR; });
-    const int ncb = (a.N + 255) / 256;
+    NtWork w;
+    w.ncb = (a.N + 255) / 256;
     // the XCDs take neighbouring runs of the items, so that an expert's matrix stays in few L2s
-    const long long all = (long long)tiles.total() * ncb;
-    const int xcd = (int)blockIdx.x % XCD, stride = (int)gridDim.x / XCD;
-    const int end = sgpr((int)(all * (xcd + 1) / XCD));
-    int item = sgpr((int)(all * xcd / XCD) + (int)blockIdx.x / XCD);
-    if (item >= end) return;
-
-    const int ld_row = tid >> 3;
-    const unsigned piece = (unsigned)((tid & 7) ^ ((ld_row >> 1) & 7)) << 4;
+    const long long all = (long long)tiles.total() * w.ncb;
+    const int xcd = (int)blockIdx.x % XCD;
+    w.stride = (int)gridDim.x / XCD;
+    w.end = sgpr((int)(all * (xcd + 1) / XCD));
+    const int first = sgpr((int)(all * xcd / XCD) + (int)blockIdx.x / XCD);
+    if (first >= w.end) return;
+    w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
+    w.rinfo = w.ring + 2 * Nt<TR>::STAGE;
+    w.div = 0xFFFFFFFFu / (unsigned)a.k;
+    w.wave = wave;
+    w.lane = lane;
+    w.ld_row = tid >> 3;
+    w.piece = (unsigned)((tid & 7) ^ ((w.ld_row >> 1) & 7)) << 4;
     NtLane ln;
-    ln.wave = wave;
-    ln.lane = lane;
     const int frag = l16 * 128 + ((lq ^ (l16 >> 1)) << 4);
     ln.f_rd = wm * (128 * 128) + frag;
     ln.r_rd = Nt<TR>::F_BYTES + wn * (32 * 128) + frag;
-    auto fetch_rows = [&](const NtItem& it, int par) {
-        if (KIND != DX && wave * 64 < TR)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(a.perm + it.row0, (unsigned)it.rc * 4u), (lds_void_t*)(rinfo + par * 256 + wave * 64), 4,
-                                                     (unsigned)(wave * 64 + lane) * 4u, 0, 0, 0);
-    };
-    auto start = [&](const NtLoader& L) {                  // an item's first two stages
-#pragma unroll
-        for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, L, ring, wave, 0, q);
-        if (a.KT > 1) {
-#pragma unroll
-            for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, L, ring, wave, 1, q);
-        }
-    };
 
-    NtLoader L;
-    NtItem it = nt_locate<TR>(a, tiles, ncb, item);
-    fetch_rows(it, 0);
-    MOE_WAIT_VMCNT(0);
-    __syncthreads();
-    nt_turn<KIND, TR>(a, it, rinfo, ld_row, piece, L);
-    start(L);
+    NtLoader<TR> L;
+    // packed matrices: rows as they lie; else slot 16 h + j of a block of 32 holds feature 8 (j / 4) + 4 h + j % 4: the two halves give a lane
+    // eight neighbours
+    const int f = KIND <= KEEP_SWIGLU ? w.ld_row : ((w.ld_row & 12) << 1) + ((w.ld_row & 16) >> 2) + (w.ld_row & 3);
+    L.vf = (unsigned)f * (unsigned)a.ld_w * 2u + w.piece;
+#pragma unroll
+    for (int q = 0; q < Nt<TR>::NRL; ++q) L.vr[q] = (unsigned)(q * 32 + w.ld_row) * (unsigned)a.ld_rows * 2u + w.piece;      // (DX)
+    L.item = first;
+    L.kt = L.buf = L.seq = 0;
+    if constexpr (KIND != DX) {
+        nt_fetch_rows<TR>(a, w, nt_locate<TR>(a, tiles, w.ncb, first), 0);
+        MOE_WAIT_VMCNT(0);
+        wg_barrier();
+    }
+    nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
+#pragma unroll
+    for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, w, L, q);
+    if (KIND != DX && a.KT == 1) {                         // (the next item's rows are wanted now)
+        MOE_WAIT_VMCNT(0);
+        wg_barrier();
+    }
+    nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
+#pragma unroll
+    for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, w, L, q);
+    MOE_WAIT_VMCNT(Nt<TR>::LPS);
+    wg_barrier();
     NtAcc<TR> acc;
     NtFrags<TR> fr[2];
-    for (int par = 0;; par ^= 1) {
-        // stage 0 is there once no more than stage 1's loads are under way
-        if (a.KT > 1) MOE_WAIT_VMCNT(Nt<TR>::LPS);
-        else MOE_WAIT_VMCNT(0);
-        wg_barrier();
-        const int next = item + stride;
-        NtItem nx = it;
-        if (next < end) {
-            nx = nt_locate<TR>(a, tiles, ncb, next);
-            fetch_rows(nx, par ^ 1);
-        }
+#pragma unroll
+    for (int j = 0; j < 8 + 2 * Nt<TR>::NI; ++j) nt_read<TR>(fr[0], ring, j, ln.f_rd, ln.r_rd);
+    int buf = 0, stores = 0, seq = 0;
+    for (int item = first; item < w.end; item += w.stride, ++seq) {
+        const NtItem it = nt_locate<TR>(a, tiles, w.ncb, item);
 #pragma unroll
         for (int ni = 0; ni < Nt<TR>::NI; ++ni)
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[ni][j >> 3][(j >> 1) & 3][j & 1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < 8 + 2 * Nt<TR>::NI; ++j) nt_read<TR>(fr[0], ring, j, ln.f_rd, ln.r_rd);
         int ni_on = ((it.rc + 31) / 32 - wn + 1) / 2;      // 32-row blocks of this wavefront that hold rows
         ni_on = ni_on > Nt<TR>::NI ? Nt<TR>::NI : ni_on;
-        if (ni_on == Nt<TR>::NI) nt_contract<KIND, TR, true>(a, L, ln, ring, acc, fr, ni_on);
-        else nt_contract<KIND, TR, false>(a, L, ln, ring, acc, fr, ni_on);
-        // (since the last barrier nobody needs what is in the ring: the reads of the last half were of a stage that is not there)
-        if (next < end) {
-            nt_turn<KIND, TR>(a, nx, rinfo + (par ^ 1) * 256, ld_row, piece, L);
-            start(L);
-        }
-        nt_finish<KIND, TR>(a, it, rinfo + par * 256, acc, wm, wn, lane, ni_on);
-        if (next >= end) break;
-        item = next;
-        it = nx;
+        if (ni_on == Nt<TR>::NI) nt_contract<KIND, TR, true>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
+        else nt_contract<KIND, TR, false>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
+        nt_finish<KIND, TR>(a, it, rinfo + (seq & 3) * TR, acc, wm, wn, lane, ni_on);
+        // store instructions just issued, at least: two for every 32 rows x 32 features (SwiGLU: gates and ups make one block of outputs)
+        int cols = (a.N - it.n0 - wm * 128 + 31) / 32;
+        cols = cols < 0 ? 0 : cols > 4 ? 4 : cols;
+        stores = ni_on * 2 * cols * (KIND == KEEP_SWIGLU ? 1 : 2);
     }
+    MOE_WAIT_VMCNT(0);                                      // (the trailing empty loads still target this LDS)
 #endif
 }
 
@@ -485,8 +538,7 @@ struct TnArgs {
 };
 
 constexpr int TN_OP = 64 * 512, TN_STAGE = 2 * TN_OP;      // LDS: an operand's 64 rows of 256 columns
-constexpr int TN_IDS = 64;
-constexpr size_t TN_SMEM = 2 * TN_STAGE + 4 * TN_IDS * 4;
+constexpr size_t TN_SMEM = 2 * TN_STAGE + 2 * 64 * 4;
 
 struct TnItem {
     int e, row0, n, m0, n0, M, N;
@@ -517,34 +569,70 @@ template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, c
     return it;
 }
 
-// The loads of stage kt of an item; ids: the stage's assignments in LDS.
-struct TnLoads {
-    __amdgpu_buffer_rsrc_t rd, rg;
-    unsigned vd, vg[8], ld_d;
-    int to_d, to_g;
+struct TnWork {
+    TnShape sh;
+    int end, stride;
+    unsigned ring, ids, div;       // LDS addresses; for the division by k
+    int wave, lane, term;          // term: this thread's rows of a stage are term .. term + 3 and 32 + those
+    unsigned piece;
 };
-__device__ __forceinline__ void tn_stage(const TnArgs& a, const TnItem& it, const int* ids, int kt, int tid, unsigned piece, TnLoads& L) {
-    const int left = it.n - kt * 64, term = (tid >> 5) * 8;
-    const int ld = it.out ? a.F : a.Z;
-    const uint16_t* dir = (it.out ? a.wh : a.dz) + (size_t)(it.row0 + kt * 64) * ld;
-    L.ld_d = (unsigned)ld * 2u;
-    L.rd = make_rsrc(dir, (unsigned)(left < 64 ? left : 64) * L.ld_d);
-    L.rg = make_rsrc(it.out ? a.dy : a.x, (unsigned)a.T * (unsigned)a.d * 2u);
-    L.vd = (unsigned)term * L.ld_d + (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u + piece;
-    const unsigned cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u + piece;
-#pragma unroll
-    for (int q = 0; q < 8; ++q) {
-        unsigned src = (unsigned)ids[term + q];
-        if (a.k != 1) src /= (unsigned)a.k;
-        L.vg[q] = term + q < left ? src * (unsigned)a.d * 2u + cg : 0xFFFFFFF0u;
+
+// A place in the stream of stages (items without rows have none).
+struct TnPlace {
+    int item, kt, KT;
+    TnItem it;
+};
+template <int ES> __device__ __forceinline__ void tn_settle(const TnArgs& a, const TnWork& w, TnPlace& p) {
+    p.kt = p.KT = 0;
+    for (; p.item < w.end; p.item += w.stride) {
+        p.it = tn_locate<ES>(a, w.sh, p.item);
+        p.KT = (p.it.n + 63) / 64;
+        if (p.KT > 0) return;
     }
-    // LDS: the N operand's rows first
-    L.to_d = (kt & 1) * TN_STAGE + (it.out ? TN_OP : 0);
-    L.to_g = (kt & 1) * TN_STAGE + (it.out ? 0 : TN_OP);
 }
-__device__ __forceinline__ void tn_load(const TnLoads& L, unsigned char* ring, int wave, int q) {
-    if (q < 8) __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rd, (lds_void_t*)(ring + L.to_d + q * 4096 + wave * 1024), 16, L.vd + (unsigned)q * L.ld_d, 0, 0, 0);
-    else __builtin_amdgcn_raw_ptr_buffer_load_lds(L.rg, (lds_void_t*)(ring + L.to_g + (q - 8) * 4096 + wave * 1024), 16, L.vg[q < 8 ? 0 : q - 8], 0, 0, 0);
+template <int ES> __device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnPlace& p) {
+    if (++p.kt < p.KT) return;
+    if (p.item < w.end) p.item += w.stride;
+    tn_settle<ES>(a, w, p);
+}
+// the assignments of a stage's rows, into one of two tables
+__device__ __forceinline__ void tn_fetch_ids(const TnArgs& a, const TnWork& w, const TnPlace& p, int slot) {
+    if (w.wave == 0 && p.item < w.end)
+        load_to_lds4(descriptor(a.perm + p.it.row0 + p.kt * 64, (unsigned)(p.it.n - p.kt * 64) * 4u), w.ids + (unsigned)slot * 256u, (unsigned)w.lane * 4u);
+}
+
+// The loads of a stage.  Slot s = 8 q + j of an operand's 64 in LDS (q: a thread's load, j = thread / 32) holds row 4 j + q, or 28 + 4 j + q for q >= 4: a
+// thread's assignments are two runs of four.
+struct TnLoads {
+    u32x4 rd, rg;
+    unsigned vd, cg, ld_d, to_d, to_g;
+    int left;
+};
+__device__ __forceinline__ void tn_stage(const TnArgs& a, const TnWork& w, const TnPlace& p, int buf, TnLoads& L) {
+    const TnItem& it = p.it;
+    const bool on = p.item < w.end;
+    const int left = on ? it.n - p.kt * 64 : 0;
+    L.left = left;
+    const int ld = it.out ? a.F : a.Z;
+    L.ld_d = (unsigned)ld * 2u;
+    L.rd = descriptor((it.out ? a.wh : a.dz) + (on ? (size_t)(it.row0 + p.kt * 64) * ld : 0), (unsigned)(left < 64 ? left : 64) * L.ld_d);
+    L.rg = descriptor(it.out ? a.dy : a.x, on ? (unsigned)a.T * (unsigned)a.d * 2u : 0u);
+    L.vd = (unsigned)w.term * L.ld_d + (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u + w.piece;
+    L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u + w.piece;
+    // LDS: the N operand's rows first
+    const unsigned to = w.ring + (unsigned)(buf * TN_STAGE + w.wave * 1024);
+    L.to_d = to + (it.out ? TN_OP : 0);
+    L.to_g = to + (it.out ? 0 : TN_OP);
+}
+// load q: the direct operand's first
+__device__ __forceinline__ void tn_load(const TnArgs& a, const TnWork& w, const TnLoads& L, const u32x4 (&id)[2], int q) {
+    const int at = (q & 3) + ((q >> 2) & 1) * 32;
+    if (q < 8) {
+        load_to_lds(L.rd, L.to_d + (unsigned)q * 4096u, L.vd + (unsigned)at * L.ld_d, 0u);
+    } else {
+        const unsigned src = divided(id[(q >> 2) & 1][q & 3], (unsigned)a.k, w.div);
+        load_to_lds(L.rg, L.to_g + (unsigned)(q - 8) * 4096u, w.term + at < L.left ? src * (unsigned)a.d * 2u + L.cg : 0xFFFFFFF0u, 0u);
+    }
 }
 
 typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
@@ -562,28 +650,55 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-struct TnLane { int wave, at_n, at_m, sw; };
+struct TnLane { int at_n, at_m, sw; };
 
-template <int S, bool LOAD>
-__device__ __forceinline__ void tn_half(const TnLoads& L, const TnLane& ln, unsigned char* ring, int kt, TnAcc& acc, TnFrags (&fr)[2]) {
-    const int buf = ((S == 0 ? kt : kt + 1) & 1) * TN_STAGE + (S == 0 ? 16384 : 0);
+// Half S of the stage in buffer `buf`, as in the kernel over rows.
+template <int ES, int S, bool FIRST>
+__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, const TnLane& ln, unsigned char* ring, const u32x4* ids, int& buf,
+                                        TnAcc& acc, TnFrags (&fr)[2], int stores) {
+    const int at = (S == 0 ? buf : buf ^ 1) * TN_STAGE + (S == 0 ? 16384 : 0);
+    u32x4 id[2];
 #pragma unroll
     for (int t = 0; t < 16; ++t) {
         const int m = t >> 1, n4 = (t & 1) * 4;
+        if (S == 1 && t == 0) {
+            id[0] = ids[buf * 16 + (w.term >> 2)];
+            id[1] = ids[buf * 16 + 8 + (w.term >> 2)];
+        }
 #pragma unroll
         for (int n = n4; n < n4 + 4; ++n)
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
         if (t < 12) {
 #pragma unroll
-            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ring, j, buf + ln.at_n, buf + ln.at_m, ln.sw);
+            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ring, j, at + ln.at_n, at + ln.at_m, ln.sw);
         }
-        if (S == 1 && LOAD) tn_load(L, ring, ln.wave, t);
+        if (S == 1) tn_load(a, w, L, id, t);
         __builtin_amdgcn_sched_barrier(0);
     }
     if (S == 0) {
+        // everybody has read all of this stage; the next one is there, and the assignments of the one behind it
         MOE_WAIT_LGKMCNT(0);
-        MOE_WAIT_VMCNT(0);
+        if (FIRST) wait_landed(stores);
+        else MOE_WAIT_VMCNT(0);
         wg_barrier();
+        tn_next<ES>(a, w, load);
+        tn_stage(a, w, load, buf, L);
+        tn_next<ES>(a, w, ahead);
+        tn_fetch_ids(a, w, ahead, buf ^ 1);
+    } else {
+        buf ^= 1;
+    }
+}
+
+template <int ES>
+__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, const TnLane& ln, unsigned char* ring, const u32x4* ids,
+                                            int KT, int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
+    tn_half<ES, 0, true>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, stores);
+    tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
+#pragma clang loop unroll(disable)
+    for (int kt = 1; kt < KT; ++kt) {
+        tn_half<ES, 0, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
+        tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
     }
 }
 
@@ -634,106 +749,89 @@ template <typename O, bool ADD>
 __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
-    int* ids = (int*)(ring + 2 * TN_STAGE);                // assignments of stages: kt & 1 of the item, and the next item's first two
+    constexpr int ES = sizeof(O);
+    const u32x4* ids = (const u32x4*)(ring + 2 * TN_STAGE);      // assignments of two stages' rows
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
-    TnShape sh;
-    sh.ta = (a.d + 255) / 256;
-    sh.tb = (a.F + 255) / 256;
-    sh.per_mat = sh.ta * sh.tb;
-    sh.per_expert = sh.per_mat * a.mats;
+    TnWork w;
+    w.sh.ta = (a.d + 255) / 256;
+    w.sh.tb = (a.F + 255) / 256;
+    w.sh.per_mat = w.sh.ta * w.sh.tb;
+    w.sh.per_expert = w.sh.per_mat * a.mats;
     // An item costs its stages and the store of its tile (about six stages' time).  The XCDs take neighbouring runs of equal cost.
     const Sums cost = sums_over_experts(a.offsets, a.E, lane, [](int n) { return 6 + (n + 63) / 64; });
-    const int xcd = (int)blockIdx.x % XCD, stride = (int)gridDim.x / XCD;
+    const int xcd = (int)blockIdx.x % XCD;
     auto bound = [&](int x) {
-        const long long at = (long long)cost.total() * sh.per_expert * x / XCD;
-        if (x == XCD) return a.E * sh.per_expert;
-        const int e = cost.find((int)(at / sh.per_expert));
-        const long long in = at - (long long)cost.before(e) * sh.per_expert;
-        return sgpr(e * sh.per_expert + (int)(in / (cost.before(e + 1) - cost.before(e))));
+        const long long at = (long long)cost.total() * w.sh.per_expert * x / XCD;
+        if (x == XCD) return a.E * w.sh.per_expert;
+        const int e = cost.find((int)(at / w.sh.per_expert));
+        const long long in = at - (long long)cost.before(e) * w.sh.per_expert;
+        return sgpr(e * w.sh.per_expert + (int)(in / (cost.before(e + 1) - cost.before(e))));
     };
-    const int end = bound(xcd + 1);
-    int item = bound(xcd) + (int)blockIdx.x / XCD;
-    if (item >= end) return;
-
+    w.stride = (int)gridDim.x / XCD;
+    w.end = bound(xcd + 1);
+    const int first = bound(xcd) + (int)blockIdx.x / XCD;
+    if (first >= w.end) return;
+    w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
+    w.ids = w.ring + 2 * TN_STAGE;
+    w.div = 0xFFFFFFFFu / (unsigned)a.k;
+    w.wave = wave;
+    w.lane = lane;
+    w.term = (tid >> 5) * 4;
+    // row r of an operand's 64: 512 bytes, piece p (16 bytes) at p ^ 2 (slot % 8): the transposing reads of 32 lanes then touch all 64 banks once
+    w.piece = (unsigned)((tid & 31) ^ (2 * (tid >> 5))) << 4;
     TnLane ln;
-    ln.wave = wave;
-    // slot s of a stage: row (s % 8) 8 + s / 8 of its 64 (either operand's); lane (l16, lq) reads slots 4 lq + l16 / 4 of sixteen
-    const int slot = lq * 4 + (l16 >> 2);
+    const int slot = lq * 4 + (l16 >> 2);                  // lane (l16, lq) reads from slots 4 lq + l16 / 4 of sixteen
     ln.sw = (slot & 7) * 32;
     ln.at_n = slot * 512 + (l16 & 3) * 8 + wm * 256;
     ln.at_m = TN_OP + slot * 512 + (l16 & 3) * 8 + wn * 256;
-    const unsigned piece = (unsigned)((tid & 31) ^ (2 * (tid >> 5))) << 4;
-    auto fetch_ids = [&](const TnItem& it, int kt, int to) {
-        if (wave == 0)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(a.perm + it.row0, (unsigned)it.n * 4u), (lds_void_t*)(ids + to * TN_IDS), 4,
-                                                     (unsigned)(kt * 64 + lane) * 4u, 0, 0, 0);
-    };
+
+    // two stages on their way, the assignments of the third behind them
+    TnPlace load, ahead;
+    load.item = first;
+    tn_settle<ES>(a, w, load);
+    ahead = load;
     TnLoads L;
-    // (stage 2's assignments go on their way first: they are there when stage 0 is)
-    auto start = [&](const TnItem& it, int KT, int at) {
-        if (KT > 2) fetch_ids(it, 2, at);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-            if (s < KT) {
-                tn_stage(a, it, ids + (2 + s) * TN_IDS, s, tid, piece, L);
-#pragma unroll
-                for (int q = 0; q < 16; ++q) tn_load(L, ring, wave, q);
-            }
-    };
-    TnItem it = tn_locate<sizeof(O)>(a, sh, item);
-    fetch_ids(it, 0, 2);
-    fetch_ids(it, 1, 3);
+    tn_fetch_ids(a, w, ahead, 0);
+    tn_next<ES>(a, w, ahead);
+    tn_fetch_ids(a, w, ahead, 1);
+    tn_next<ES>(a, w, ahead);
     MOE_WAIT_VMCNT(0);
-    __syncthreads();
-    start(it, (it.n + 63) / 64, 0);
+    wg_barrier();
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        if (st == 1) tn_next<ES>(a, w, load);
+        tn_stage(a, w, load, st, L);
+        const u32x4 id[2] = {ids[st * 16 + (w.term >> 2)], ids[st * 16 + 8 + (w.term >> 2)]};
+#pragma unroll
+        for (int q = 0; q < 16; ++q) tn_load(a, w, L, id, q);
+    }
+    MOE_WAIT_VMCNT(16);
+    wg_barrier();
+    tn_fetch_ids(a, w, ahead, 0);
     TnAcc acc;
     TnFrags fr[2];
-    for (;;) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) tn_read(fr[0], ring, j, ln.at_n, ln.at_m, ln.sw);
+    int buf = 0, stores = 0;
+    for (int item = first; item < w.end; item += w.stride) {
+        const TnItem it = tn_locate<ES>(a, w.sh, item);
         const int KT = (it.n + 63) / 64;
-        const int next = item + stride;
-        TnItem nx = it;
-        if (KT > 1) MOE_WAIT_VMCNT(16);
-        else MOE_WAIT_VMCNT(0);
-        wg_barrier();
-        if (next < end) {
-            nx = tn_locate<sizeof(O)>(a, sh, next);
-            fetch_ids(nx, 0, 2);
-            fetch_ids(nx, 1, 3);
-        }
+        if (ADD && KT == 0) continue;
+        int n_on = (it.N - it.n0 - wm * 128) / 16;         // 16-column blocks of this wavefront inside the matrix
+        n_on = n_on < 0 ? 0 : n_on > 8 ? 8 : n_on;
 #pragma unroll
         for (int m = 0; m < 8; ++m)
 #pragma unroll
             for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (KT > 0) {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) tn_read(fr[0], ring, j, ln.at_n, ln.at_m, ln.sw);
+            tn_contract<ES>(a, w, load, ahead, L, ln, ring, ids, KT, buf, acc, fr, stores);
+            stores = 0;
         }
-        int kt = 0;
-#pragma clang loop unroll(disable)
-        for (; kt + 2 < KT; ++kt) {
-            tn_half<0, true>(L, ln, ring, kt, acc, fr);
-            tn_stage(a, it, ids + (kt & 1) * TN_IDS, kt + 2, tid, piece, L);
-            if (kt + 3 < KT) fetch_ids(it, kt + 3, (kt + 1) & 1);
-            tn_half<1, true>(L, ln, ring, kt, acc, fr);
-        }
-#pragma clang loop unroll(disable)
-        for (; kt < KT; ++kt) {
-            tn_half<0, false>(L, ln, ring, kt, acc, fr);
-            tn_half<1, false>(L, ln, ring, kt, acc, fr);
-        }
-        if (next < end) {
-            if (KT == 0) {                                 // (no stage has waited for the next item's assignments)
-                MOE_WAIT_VMCNT(0);
-                wg_barrier();
-            }
-            start(nx, (nx.n + 63) / 64, 0);
-        }
-        if (!ADD || KT > 0) tn_finish<O, ADD>(it, acc, wm, wn, lane);
-        if (next >= end) break;
-        item = next;
-        it = nx;
+        tn_finish<O, ADD>(it, acc, wm, wn, lane);
+        stores += 4 * n_on * (ES / 2);                     // store instructions just issued
     }
+    MOE_WAIT_VMCNT(0);                                      // (the trailing empty loads still target this LDS)
 #endif
 }
 
