@@ -48,11 +48,22 @@ __device__ __forceinline__ u32x4 descriptor(const void* p, unsigned bytes) {
     const uint64_t u = (uint64_t)p;
     return u32x4{(unsigned)sgpr((int)(unsigned)u), (unsigned)sgpr((int)(unsigned)(u >> 32)) & 0xffffu, (unsigned)sgpr((int)bytes), 0x00020000u};
 }
-// 16 (4) bytes a lane to LDS at `to` (bytes, wave-uniform) + 16 (4) lane; only voff is range-checked
-__device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned to, unsigned voff, unsigned soff) {
+// 16 bytes a lane to LDS at base + at (bytes, wave-uniform) + 16 lane, from voff + add (the sum saturates: an offset beyond everything stays that);
+// only this one is range-checked, soff is not.  (M0 may not be used in the instruction behind the one that sets it: the sum stands between.)
+__device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned base, unsigned at, unsigned voff, unsigned add, unsigned soff) {
     const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(to), "v"(voff), "s"(d), "s"(soff) : "memory");
+    unsigned sum;
+    asm volatile("s_add_u32 m0, %1, %2\n\tv_add_u32_e64 %0, %3, %4 clamp\n\tbuffer_load_dwordx4 %0, %5, %6 offen lds"
+                 : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "s"(add), "s"(d), "s"(soff) : "memory", "scc");
 }
+// the same with a sum that differs from lane to lane
+__device__ __forceinline__ void load_to_lds_v(const u32x4& r, unsigned base, unsigned at, unsigned voff, unsigned add) {
+    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
+    unsigned sum;
+    asm volatile("s_add_u32 m0, %1, %2\n\tv_add_u32_e64 %0, %3, %4 clamp\n\tbuffer_load_dwordx4 %0, %5, 0 offen lds"
+                 : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "v"(add), "s"(d) : "memory", "scc");
+}
+// 4 bytes a lane
 __device__ __forceinline__ void load_to_lds4(const u32x4& d, unsigned to, unsigned voff) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
 }
@@ -222,13 +233,18 @@ template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs
     }
 }
 
-// load q of the loader's stage (the features first)
-template <int KIND, int TR> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, int q) {
+// load Q of the loader's stage (the features first)
+template <int KIND, int TR, int Q> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L) {
     const unsigned to = w.ring + (unsigned)(L.buf * Nt<TR>::STAGE + w.wave * 1024);
-    if (q < Nt<TR>::NFL) {
-        load_to_lds(L.rf, to + (unsigned)q * 4096u, L.vf + (unsigned)(q * 32) * (unsigned)a.ld_w * 2u, (unsigned)(KIND == DX && L.kt >= a.KT0 ? L.kt - a.KT0 : L.kt) * 128u);
-    } else {
-        load_to_lds(L.rr, to + (unsigned)(Nt<TR>::F_BYTES + (q - Nt<TR>::NFL) * 4096), L.vr[q < Nt<TR>::NFL ? 0 : q - Nt<TR>::NFL], (unsigned)L.kt * 128u);
+    if constexpr (Q < Nt<TR>::NFL)
+        load_to_lds(L.rf, to, Q * 4096, L.vf, (unsigned)(Q * 32) * (unsigned)a.ld_w * 2u, (unsigned)(KIND == DX && L.kt >= a.KT0 ? L.kt - a.KT0 : L.kt) * 128u);
+    else
+        load_to_lds(L.rr, to, Nt<TR>::F_BYTES + (Q - Nt<TR>::NFL) * 4096, L.vr[Q - Nt<TR>::NFL], 0u, (unsigned)L.kt * 128u);
+}
+template <int KIND, int TR, int FROM, int TO> __device__ __forceinline__ void nt_loads(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L) {
+    if constexpr (FROM < TO) {
+        nt_load<KIND, TR, FROM>(a, w, L);
+        nt_loads<KIND, TR, FROM + 1, TO>(a, w, L);
     }
 }
 // after the last load of a stage
@@ -254,15 +270,12 @@ template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const
 
 // Half S of the stage in buffer `buf`: multiplies set S, reads the other.  Half 1 issues the loads of the stage after the next into the buffer that
 // this one has left.  FIRST: of an item, whose predecessor's stores (at least `stores`) may be under way.
-template <int KIND, int TR, int S, bool FIRST, bool FULL>
-__device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L, const NtLane& ln, const unsigned char* ring, int& buf,
-                                        NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
-    constexpr int NI = Nt<TR>::NI, G = NI * 4, READS = 8 + 2 * NI, SPREAD = G >= 16 ? 12 : G;
-    if (S == 1) buf ^= 1;
-    const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
-#pragma unroll
-    for (int t = 0; t < G; ++t) {
-        const int ni = t >> 2, n16 = (t >> 1) & 1, b0 = (t & 1) * 2;
+template <int KIND, int TR, int S, bool FULL, int t>
+__device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const unsigned char* ring, int at_f, int at_r, NtAcc<TR>& acc,
+                                          NtFrags<TR> (&fr)[2], int ni_on) {
+    constexpr int G = Nt<TR>::NI * 4, READS = 8 + 2 * Nt<TR>::NI, SPREAD = G >= 16 ? 12 : G, LPS = Nt<TR>::LPS;
+    if constexpr (t < G) {
+        constexpr int ni = t >> 2, n16 = (t >> 1) & 1, b0 = (t & 1) * 2;
         if (FULL || ni < ni_on) {
 #pragma unroll
             for (int b = b0; b < b0 + 2; ++b)
@@ -274,12 +287,17 @@ __device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const 
 #pragma unroll
             for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) nt_read<TR>(fr[S ^ 1], ring, j, at_f, at_r);
         }
-        if (S == 1) {
-#pragma unroll
-            for (int q = t * Nt<TR>::LPS / G; q < (t + 1) * Nt<TR>::LPS / G; ++q) nt_load<KIND, TR>(a, w, L, q);
-        }
+        if constexpr (S == 1) nt_loads<KIND, TR, t * LPS / G, (t + 1) * LPS / G>(a, w, L);
         __builtin_amdgcn_sched_barrier(0);
+        nt_groups<KIND, TR, S, FULL, t + 1>(a, w, L, ring, at_f, at_r, acc, fr, ni_on);
     }
+}
+template <int KIND, int TR, int S, bool FIRST, bool FULL>
+__device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L, const NtLane& ln, const unsigned char* ring, int& buf,
+                                        NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
+    if (S == 1) buf ^= 1;
+    const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
+    nt_groups<KIND, TR, S, FULL, 0>(a, w, L, ring, at_f, at_r, acc, fr, ni_on);
     if (S == 0) {
         // everybody has read all of this stage, and the next one is there
         MOE_WAIT_LGKMCNT(0);
@@ -301,6 +319,9 @@ __device__ __forceinline__ void nt_contract(const NtArgs& a, const NtWork& w, co
         nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
     }
 }
+
+// (v_rcp_f32 is off by one unit in the last place at most)
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
 // A lane's features of block b in a row: natural order (slots arranged by nt_turn), or packed rows (packed row 16 h + j = output 2 j + h).
 template <bool PACKED> __device__ __forceinline__ void lane_values(const f32x4 (&acc)[2], float (&v)[8]) {
@@ -361,6 +382,7 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                         }
                     }
                     const KeepScale ks = keep_scale(quarter_max(most));
+                    __builtin_amdgcn_sched_barrier(0);     // (one block's values at a time: there are no registers for more)
                     if (lq == 0) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(ks.scale), rs, row * (Z / 64) * 4u, (unsigned)(zc / 64) * 4u, 0);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -374,7 +396,7 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                                 float g[8];
                                 lane_values<true>(acc[ni][n16][2 * i], g);
 #pragma unroll
-                                for (int c = 0; c < 8; ++c) v[i][c] *= silu_f(g[c]);
+                                for (int c = 0; c < 8; ++c) v[i][c] *= g[c] * sigmoid(g[c]);
                             }
                             const u32x4 w = {half_bits(v[i][0], v[i][1]), half_bits(v[i][2], v[i][3]), half_bits(v[i][4], v[i][5]), half_bits(v[i][6], v[i][7])};
                             __builtin_amdgcn_raw_buffer_store_b128(w, rh, row * F * 2u + (unsigned)lq * 16u, (unsigned)((SW ? f0 / 2 : zc) + i * 32) * 2u, 0);
@@ -385,62 +407,81 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
         }
     } else {
         constexpr bool SW = KIND == HID_SWIGLU;
+        constexpr int MATS = SW ? 2 : 1, NG = Nt<TR>::NI * 2;
         const unsigned F = (unsigned)a.F, Z = (unsigned)a.Z;
         const __amdgpu_buffer_rsrc_t rq = make_rsrc(a.q_in + row0 * Z, rc * Z);
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(a.scale_in + row0 * (Z / 64), rc * (Z / 64) * 4u);
         const __amdgpu_buffer_rsrc_t rz = make_rsrc(a.dz + row0 * Z, rc * Z * 2u);
         const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wh + row0 * F, rc * F * 2u);
         const int on = a.N - f0 < 128 ? a.N - f0 : 128;    // features of this wavefront: 64 or 128
+        const unsigned last = (unsigned)((on - 64) / 64);  // (where there are 64, the second 64 read the first's once more)
+        auto row_of = [&](int g) { return (unsigned)(((g >> 1) * 2 + wn) * 32 + (g & 1) * 16 + l16); };
+        float gate[NG];
 #pragma unroll
-        for (int ni = 0; ni < Nt<TR>::NI; ++ni) {
-            if (ni >= ni_on) continue;
+        for (int g = 0; g < NG; ++g) {
+            const unsigned row = row_of(g);
+            gate[g] = a.gate_w && row < rc ? a.gate_w[rinfo[row]] : 1.f;
+        }
+        // what is kept of 16 rows is fetched while the 16 before are worked on
+        u32x2 q[2][2][4];
+        float sc[2][2][2];
+        auto fetch = [&](int g, int to) {
+            const unsigned row = row_of(g);
 #pragma unroll
-            for (int n16 = 0; n16 < 2; ++n16) {
-                const unsigned row = (unsigned)((ni * 2 + wn) * 32 + n16 * 16 + l16);
-                const float gate = row < rc ? (a.gate_w ? a.gate_w[rinfo[row]] : 1.f) : 0.f;
-                u32x2 q[2][4];
-                float sc[2][2];
+            for (int m = 0; m < MATS; ++m) {
 #pragma unroll
-                for (int m = 0; m < (SW ? 2 : 1); ++m) {
+                for (int b = 0; b < 4; ++b)
+                    q[to][m][b] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, row * Z + (unsigned)lq * 8u,
+                                                                                                 (unsigned)(f0 + m * a.F) + (b < 2 ? 0u : last * 64u) + (unsigned)(b & 1) * 32u, 0));
 #pragma unroll
-                    for (int b = 0; b < 4; ++b)
-                        if (b * 32 < on) q[m][b] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, row * Z + (unsigned)lq * 8u, (unsigned)(f0 + b * 32 + m * a.F), 0));
-#pragma unroll
-                    for (int j = 0; j < 2; ++j)
-                        if (j * 64 < on) sc[m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, row * (Z / 64) * 4u, (unsigned)((f0 + j * 64 + m * a.F) / 64) * 4u, 0));
-                }
-                float dgate = 0.f;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    if (b * 32 >= on) continue;
-                    float s[8], wh[8], dz0[8], dz1[8];
-                    lane_values<false>(acc[ni][n16][b], s);
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float z = (float)((int)(q[0][b][c >> 2] << (24 - 8 * (c & 3))) >> 24) * sc[0][b >> 1];
-                        const float dh = gate * s[c];
-                        float h;
-                        if (SW) {
-                            const float u = (float)((int)(q[1][b][c >> 2] << (24 - 8 * (c & 3))) >> 24) * sc[1][b >> 1];
-                            const float sig = __builtin_amdgcn_rcpf(1.f + __expf(-z)), silu = z * sig;
-                            h = silu * u;
-                            dz0[c] = dh * u * (sig + silu * (1.f - sig));
-                            dz1[c] = dh * silu;
-                        } else {
-                            h = z;
-                            dz0[c] = z > 0.f ? dh : z;     // (z is 0 else, or no number)
-                        }
-                        dgate = fmaf(h, s[c], dgate);
-                        wh[c] = gate * h;
-                    }
-                    const unsigned col = (unsigned)(f0 + b * 32) * 2u;
-                    __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, row * F * 2u + (unsigned)lq * 16u, col, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, row * Z * 2u + (unsigned)lq * 16u, col, 0);
-                    if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, row * Z * 2u + (unsigned)lq * 16u, col + F * 2u, 0);
-                }
-                dgate = quarter_sum(dgate);
-                if (lq == 0 && row < rc) a.dgate_part[(row0 + row) * (size_t)a.parts + (unsigned)(f0 / 128)] = dgate;
+                for (int j = 0; j < 2; ++j)
+                    sc[to][m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, row * (Z / 64) * 4u, ((unsigned)(f0 + m * a.F) / 64u + (j ? last : 0u)) * 4u, 0));
             }
+        };
+        fetch(0, 0);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+            const int ni = g >> 1, n16 = g & 1, at = g & 1;
+            if (g + 1 < NG) fetch(g + 1, at ^ 1);
+            __builtin_amdgcn_sched_barrier(0);
+            if (ni >= ni_on) continue;
+            const unsigned row = row_of(g);
+            float dgate = 0.f;
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                if (b * 32 >= on) continue;
+                float s[8], wh[8], dz0[8], dz1[8];
+                lane_values<false>(acc[ni][n16][b], s);
+                // a byte with its top bit turned is the value + 128
+                const unsigned zw[2] = {q[at][0][b][0] ^ 0x80808080u, q[at][0][b][1] ^ 0x80808080u};
+                const unsigned uw[2] = {q[at][MATS - 1][b][0] ^ 0x80808080u, q[at][MATS - 1][b][1] ^ 0x80808080u};
+                const float zs = sc[at][0][b >> 1], us = sc[at][MATS - 1][b >> 1], z0 = -128.f * zs, u0 = -128.f * us;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {
+                    const float z = fmaf((float)(zw[c >> 2] >> (8 * (c & 3)) & 255u), zs, z0);
+                    const float dh = gate[g] * s[c];
+                    float h;
+                    if (SW) {
+                        const float u = fmaf((float)(uw[c >> 2] >> (8 * (c & 3)) & 255u), us, u0);
+                        const float sig = sigmoid(z), silu = z * sig;
+                        h = silu * u;
+                        dz0[c] = dh * u * fmaf(silu, 1.f - sig, sig);
+                        dz1[c] = dh * silu;
+                    } else {
+                        h = z;
+                        dz0[c] = z > 0.f ? dh : z;         // (z is 0 else, or no number)
+                    }
+                    dgate = fmaf(h, s[c], dgate);
+                    wh[c] = gate[g] * h;
+                }
+                const unsigned col = (unsigned)(f0 + b * 32) * 2u;
+                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, row * F * 2u + (unsigned)lq * 16u, col, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, row * Z * 2u + (unsigned)lq * 16u, col, 0);
+                if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, row * Z * 2u + (unsigned)lq * 16u, col + F * 2u, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            dgate = quarter_sum(dgate);
+            if (lq == 0 && row < rc) a.dgate_part[(row0 + row) * (size_t)a.parts + (unsigned)(f0 / 128)] = dgate;
         }
     }
 }
@@ -490,15 +531,13 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
         wg_barrier();
     }
     nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
-#pragma unroll
-    for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, w, L, q);
+    nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
     if (KIND != DX && a.KT == 1) {                         // (the next item's rows are wanted now)
         MOE_WAIT_VMCNT(0);
         wg_barrier();
     }
     nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
-#pragma unroll
-    for (int q = 0; q < Nt<TR>::LPS; ++q) nt_load<KIND, TR>(a, w, L, q);
+    nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
     MOE_WAIT_VMCNT(Nt<TR>::LPS);
     wg_barrier();
     NtAcc<TR> acc;
@@ -532,13 +571,14 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
 // One operand is gathered (x for dW_in, dy for dW_out), the other lies in the experts' order (dz, w h).
 struct TnArgs {
     const uint16_t *x, *dy, *dz, *wh;
-    const int32_t *offsets, *perm;
-    int T, k, E, d, F, Z, mats;
+    const int32_t* offsets;
+    const uint32_t* src;           // of each row in the experts' order, the bits of its token's byte offset in x and dy inverted
+    int T, E, d, F, Z, mats;
     void *dwa, *dwb, *dwo;
 };
 
-constexpr int TN_OP = 64 * 512, TN_STAGE = 2 * TN_OP;      // LDS: an operand's 64 rows of 256 columns
-constexpr size_t TN_SMEM = 2 * TN_STAGE + 2 * 64 * 4;
+constexpr int TN_OP = 64 * 512;    // LDS: an operand's 64 rows of 256 columns; both buffers of the N operand, then both of the M operand
+constexpr size_t TN_SMEM = 4 * TN_OP + 2 * 64 * 4;
 
 struct TnItem {
     int e, row0, n, m0, n0, M, N;
@@ -572,7 +612,7 @@ template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, c
 struct TnWork {
     TnShape sh;
     int end, stride;
-    unsigned ring, ids, div;       // LDS addresses; for the division by k
+    unsigned ring, ids;            // LDS addresses
     int wave, lane, term;          // term: this thread's rows of a stage are term .. term + 3 and 32 + those
     unsigned piece;
 };
@@ -595,10 +635,10 @@ template <int ES> __device__ __forceinline__ void tn_next(const TnArgs& a, const
     if (p.item < w.end) p.item += w.stride;
     tn_settle<ES>(a, w, p);
 }
-// the assignments of a stage's rows, into one of two tables
+// the source rows of a stage, into one of two tables (behind the expert's last row: zeros)
 __device__ __forceinline__ void tn_fetch_ids(const TnArgs& a, const TnWork& w, const TnPlace& p, int slot) {
     if (w.wave == 0 && p.item < w.end)
-        load_to_lds4(descriptor(a.perm + p.it.row0 + p.kt * 64, (unsigned)(p.it.n - p.kt * 64) * 4u), w.ids + (unsigned)slot * 256u, (unsigned)w.lane * 4u);
+        load_to_lds4(descriptor(a.src + p.it.row0 + p.kt * 64, (unsigned)(p.it.n - p.kt * 64) * 4u), w.ids + (unsigned)slot * 256u, (unsigned)w.lane * 4u);
 }
 
 // The loads of a stage.  Slot s = 8 q + j of an operand's 64 in LDS (q: a thread's load, j = thread / 32) holds row 4 j + q, or 28 + 4 j + q for q >= 4: a
@@ -606,43 +646,43 @@ __device__ __forceinline__ void tn_fetch_ids(const TnArgs& a, const TnWork& w, c
 struct TnLoads {
     u32x4 rd, rg;
     unsigned vd, cg, ld_d, to_d, to_g;
-    int left;
 };
 __device__ __forceinline__ void tn_stage(const TnArgs& a, const TnWork& w, const TnPlace& p, int buf, TnLoads& L) {
     const TnItem& it = p.it;
     const bool on = p.item < w.end;
     const int left = on ? it.n - p.kt * 64 : 0;
-    L.left = left;
     const int ld = it.out ? a.F : a.Z;
     L.ld_d = (unsigned)ld * 2u;
     L.rd = descriptor((it.out ? a.wh : a.dz) + (on ? (size_t)(it.row0 + p.kt * 64) * ld : 0), (unsigned)(left < 64 ? left : 64) * L.ld_d);
     L.rg = descriptor(it.out ? a.dy : a.x, on ? (unsigned)a.T * (unsigned)a.d * 2u : 0u);
     L.vd = (unsigned)w.term * L.ld_d + (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u + w.piece;
     L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u + w.piece;
-    // LDS: the N operand's rows first
-    const unsigned to = w.ring + (unsigned)(buf * TN_STAGE + w.wave * 1024);
-    L.to_d = to + (it.out ? TN_OP : 0);
-    L.to_g = to + (it.out ? 0 : TN_OP);
+    const unsigned to = w.ring + (unsigned)(buf * TN_OP + w.wave * 1024);
+    L.to_d = to + (it.out ? 2 * TN_OP : 0);
+    L.to_g = to + (it.out ? 0 : 2 * TN_OP);
 }
-// load q: the direct operand's first
-__device__ __forceinline__ void tn_load(const TnArgs& a, const TnWork& w, const TnLoads& L, const u32x4 (&id)[2], int q) {
-    const int at = (q & 3) + ((q >> 2) & 1) * 32;
-    if (q < 8) {
-        load_to_lds(L.rd, L.to_d + (unsigned)q * 4096u, L.vd + (unsigned)at * L.ld_d, 0u);
-    } else {
-        const unsigned src = divided(id[(q >> 2) & 1][q & 3], (unsigned)a.k, w.div);
-        load_to_lds(L.rg, L.to_g + (unsigned)(q - 8) * 4096u, w.term + at < L.left ? src * (unsigned)a.d * 2u + L.cg : 0xFFFFFFF0u, 0u);
+// load Q: the direct operand's first.  (A row that is not there has the largest offset, and keeps it: the range check reads zeros.)
+template <int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, const u32x4 (&id)[2]) {
+    if constexpr (Q < 8) load_to_lds(L.rd, L.to_d, Q * 4096, L.vd, (unsigned)((Q & 3) + (Q >> 2) * 32) * L.ld_d, 0u);
+    else load_to_lds_v(L.rg, L.to_g, (Q - 8) * 4096, ~id[(Q >> 2) & 1][Q & 3], L.cg);
+}
+template <int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, const u32x4 (&id)[2]) {
+    if constexpr (Q < 16) {
+        tn_load<Q>(L, id);
+        tn_loads<Q + 1>(L, id);
     }
 }
 
 typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
 struct TnFrags { s16x4 n[8][2], m[8][2]; };
 
-// Read j (0..31) of a half: four terms of a column of a 16-column block.  at: this lane's row and 8 bytes in LDS, sw: its swizzle.
-__device__ __forceinline__ void tn_read(TnFrags& fr, unsigned char* ring, int j, int at_n, int at_m, int sw) {
+// Read j (0..31) of half S: four terms of a column of a 16-column block.  at: this lane's place in the first rows of each block (buffer included).
+struct TnLane { unsigned n[8], m[8]; };
+__device__ __forceinline__ void tn_read(TnFrags& fr, const TnLane& at, int half, int j) {
     const int c = (j & 15) >> 1, i = j & 1;
-    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(ring + at_n + i * 8192 + ((c * 32) ^ sw)));
-    else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(ring + at_m + i * 8192 + ((c * 32) ^ sw)));
+    typedef __attribute__((address_space(3))) unsigned char lds_byte;
+    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c] + half * 16384 + i * 8192));
+    else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.m[c] + half * 16384 + i * 8192));
 }
 __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -650,17 +690,10 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-struct TnLane { int at_n, at_m, sw; };
-
 // Half S of the stage in buffer `buf`, as in the kernel over rows.
-template <int ES, int S, bool FIRST>
-__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, const TnLane& ln, unsigned char* ring, const u32x4* ids, int& buf,
-                                        TnAcc& acc, TnFrags (&fr)[2], int stores) {
-    const int at = (S == 0 ? buf : buf ^ 1) * TN_STAGE + (S == 0 ? 16384 : 0);
-    u32x4 id[2];
-#pragma unroll
-    for (int t = 0; t < 16; ++t) {
-        const int m = t >> 1, n4 = (t & 1) * 4;
+template <int S, int t> __device__ __forceinline__ void tn_groups(const TnWork& w, const TnLoads& L, const TnLane& ln, const u32x4* ids, int buf, u32x4 (&id)[2], TnAcc& acc, TnFrags (&fr)[2]) {
+    if constexpr (t < 16) {
+        constexpr int m = t >> 1, n4 = (t & 1) * 4;
         if (S == 1 && t == 0) {
             id[0] = ids[buf * 16 + (w.term >> 2)];
             id[1] = ids[buf * 16 + 8 + (w.term >> 2)];
@@ -670,13 +703,27 @@ __device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlac
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
         if (t < 12) {
 #pragma unroll
-            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ring, j, at + ln.at_n, at + ln.at_m, ln.sw);
+            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ln, S ^ 1, j);
         }
-        if (S == 1) tn_load(a, w, L, id, t);
+        if constexpr (S == 1) tn_load<t>(L, id);
         __builtin_amdgcn_sched_barrier(0);
+        tn_groups<S, t + 1>(w, L, ln, ids, buf, id, acc, fr);
     }
+}
+template <int ES, int S, bool FIRST>
+__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, TnLane& ln, const u32x4* ids, int& buf, TnAcc& acc, TnFrags (&fr)[2],
+                                        int stores) {
+    if (S == 1) {
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            ln.n[c] ^= TN_OP;
+            ln.m[c] ^= TN_OP;
+        }
+    }
+    u32x4 id[2];
+    tn_groups<S, 0>(w, L, ln, ids, buf, id, acc, fr);
     if (S == 0) {
-        // everybody has read all of this stage; the next one is there, and the assignments of the one behind it
+        // everybody has read all of this stage; the next one is there, and the source rows of the one behind it
         MOE_WAIT_LGKMCNT(0);
         if (FIRST) wait_landed(stores);
         else MOE_WAIT_VMCNT(0);
@@ -691,14 +738,14 @@ __device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlac
 }
 
 template <int ES>
-__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, const TnLane& ln, unsigned char* ring, const u32x4* ids,
-                                            int KT, int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
-    tn_half<ES, 0, true>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, stores);
-    tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
+__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, TnLane& ln, const u32x4* ids, int KT,
+                                            int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
+    tn_half<ES, 0, true>(a, w, load, ahead, L, ln, ids, buf, acc, fr, stores);
+    tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
 #pragma clang loop unroll(disable)
     for (int kt = 1; kt < KT; ++kt) {
-        tn_half<ES, 0, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
-        tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ring, ids, buf, acc, fr, 0);
+        tn_half<ES, 0, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
+        tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
     }
 }
 
@@ -750,7 +797,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
     constexpr int ES = sizeof(O);
-    const u32x4* ids = (const u32x4*)(ring + 2 * TN_STAGE);      // assignments of two stages' rows
+    const u32x4* ids = (const u32x4*)(ring + 4 * TN_OP);      // source rows of two stages
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
     TnWork w;
@@ -773,8 +820,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     const int first = bound(xcd) + (int)blockIdx.x / XCD;
     if (first >= w.end) return;
     w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
-    w.ids = w.ring + 2 * TN_STAGE;
-    w.div = 0xFFFFFFFFu / (unsigned)a.k;
+    w.ids = w.ring + 4 * TN_OP;
     w.wave = wave;
     w.lane = lane;
     w.term = (tid >> 5) * 4;
@@ -782,11 +828,14 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     w.piece = (unsigned)((tid & 31) ^ (2 * (tid >> 5))) << 4;
     TnLane ln;
     const int slot = lq * 4 + (l16 >> 2);                  // lane (l16, lq) reads from slots 4 lq + l16 / 4 of sixteen
-    ln.sw = (slot & 7) * 32;
-    ln.at_n = slot * 512 + (l16 & 3) * 8 + wm * 256;
-    ln.at_m = TN_OP + slot * 512 + (l16 & 3) * 8 + wn * 256;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const unsigned at = w.ring + (unsigned)(slot * 512 + (l16 & 3) * 8) + (unsigned)((c * 32) ^ ((slot & 7) * 32));
+        ln.n[c] = at + (unsigned)wm * 256u;
+        ln.m[c] = at + (unsigned)(2 * TN_OP + wn * 256);
+    }
 
-    // two stages on their way, the assignments of the third behind them
+    // two stages on their way, the source rows of the third behind them
     TnPlace load, ahead;
     load.item = first;
     tn_settle<ES>(a, w, load);
@@ -803,8 +852,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
         if (st == 1) tn_next<ES>(a, w, load);
         tn_stage(a, w, load, st, L);
         const u32x4 id[2] = {ids[st * 16 + (w.term >> 2)], ids[st * 16 + 8 + (w.term >> 2)]};
-#pragma unroll
-        for (int q = 0; q < 16; ++q) tn_load(a, w, L, id, q);
+        tn_loads<0>(L, id);
     }
     MOE_WAIT_VMCNT(16);
     wg_barrier();
@@ -812,7 +860,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     TnAcc acc;
     TnFrags fr[2];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) tn_read(fr[0], ring, j, ln.at_n, ln.at_m, ln.sw);
+    for (int j = 0; j < 32; ++j) tn_read(fr[0], ln, 0, j);
     int buf = 0, stores = 0;
     for (int item = first; item < w.end; item += w.stride) {
         const TnItem it = tn_locate<ES>(a, w.sh, item);
@@ -825,7 +873,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #pragma unroll
             for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (KT > 0) {
-            tn_contract<ES>(a, w, load, ahead, L, ln, ring, ids, KT, buf, acc, fr, stores);
+            tn_contract<ES>(a, w, load, ahead, L, ln, ids, KT, buf, acc, fr, stores);
             stores = 0;
         }
         tn_finish<O, ADD>(it, acc, wm, wn, lane);
@@ -835,10 +883,15 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #endif
 }
 
-// dgate_w[a] = the sum of its row's parts, in their order (an assignment without a row: 0)
-__global__ __launch_bounds__(256) void dgate_kernel(const float* __restrict__ part, const int32_t* __restrict__ inv_perm, int A, int parts, float* __restrict__ dgate_w) {
+// dgate_w[a] = the sum of its row's parts, in their order (an assignment without a row: 0), and for the kernel over the rows where each row comes
+// from: the byte offset of its token, inverted.
+__global__ __launch_bounds__(256) void dgate_kernel(const float* __restrict__ part, const int32_t* __restrict__ offsets, const int32_t* __restrict__ perm,
+                                                    const int32_t* __restrict__ inv_perm, int A, int E, int k, unsigned row_bytes, int parts, float* __restrict__ dgate_w,
+                                                    uint32_t* __restrict__ src) {
     const int a = (int)(blockIdx.x * 256 + threadIdx.x);
     if (a >= A) return;
+    if (src && a < offsets[E]) src[a] = ~((unsigned)perm[a] / (unsigned)k * row_bytes);
+    if (!dgate_w) return;
     const int r = inv_perm[a];
     float s = 0.f;
     if (r >= 0)
@@ -930,13 +983,13 @@ extern "C" int moe_grouped_ffn_keep(const void* x, int T, int d, int F, int E, i
     return act == MOE_SWIGLU ? launch_nt_rows<KEEP_SWIGLU>(a, T * k, (hipStream_t)stream) : launch_nt_rows<KEEP_RELU>(a, T * k, (hipStream_t)stream);
 }
 
-// Workspace: dz [A,Z] and w h [A,F] in bf16, the parts of dgate_w [A, ceil(F / 128)] in fp32, dy [T,d] in bf16 where it comes in fp32, each
-// rounded up to 256 bytes.
+// Workspace: dz [A,Z] and w h [A,F] in bf16, the parts of dgate_w [A, ceil(F / 128)] in fp32, the rows' sources [A], dy [T,d] in bf16 where it
+// comes in fp32, each rounded up to 256 bytes.
 static size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
 size_t moe_ffn_back_bytes(int T, int d, int F, int k) {
     if (T < 0 || d < 1 || F < 1 || k < 1) return 0;
     const size_t A = (size_t)T * k;
-    return up256(A * 2 * F * 2) + up256(A * F * 2) + up256(A * ((F + 127) / 128) * 4) + up256((size_t)T * d * 2);
+    return up256(A * 2 * F * 2) + up256(A * F * 2) + up256(A * ((F + 127) / 128) * 4) + up256(A * 4) + up256((size_t)T * d * 2);
 }
 
 extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const void* x, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt,
@@ -957,15 +1010,16 @@ extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const v
     const size_t A = (size_t)T * k, Z = sw ? 2 * (size_t)F : F;
     const int parts = (F + 127) / 128;
     const size_t n_dz = up256(A * Z * 2), n_wh = up256(A * F * 2), n_parts = up256(A * parts * 4);
-    const size_t need = n_dz + n_wh + n_parts + (dy_dt == MOE_F32 ? up256((size_t)T * d * 2) : 0);
+    const size_t n_src = up256(A * 4), need = n_dz + n_wh + n_parts + n_src + (dy_dt == MOE_F32 ? up256((size_t)T * d * 2) : 0);
     MOE_REQUIRE(T == 0 || (ws && ws_bytes >= need), MOE_ERR_WORKSPACE, "moe_grouped_ffn_backward: workspace of %zu bytes, %zu needed", ws_bytes, need);
     MOE_REQUIRE((((uintptr_t)dy | (uintptr_t)x | (uintptr_t)w_a | (uintptr_t)w_b | (uintptr_t)w_o | (uintptr_t)z_q | (uintptr_t)dx_perm | (uintptr_t)dw_a |
                   (uintptr_t)dw_b | (uintptr_t)dw_o | (uintptr_t)ws) & 15) == 0, MOE_ERR_UNSUPPORTED, "moe_grouped_ffn_backward: pointers have to be aligned to 16 bytes");
     ok = moe_check_gemm_device();
     if (ok != MOE_OK) return ok;
     const hipStream_t st = (hipStream_t)stream;
+    uint32_t* src = (uint32_t*)((unsigned char*)ws + n_dz + n_wh + n_parts);
     if (dy_dt == MOE_F32 && T > 0) {
-        u32x4* to = (u32x4*)((unsigned char*)ws + n_dz + n_wh + n_parts);
+        u32x4* to = (u32x4*)((unsigned char*)ws + n_dz + n_wh + n_parts + n_src);
         const size_t n = (size_t)T * d / 8;
         hipLaunchKernelGGL(narrow_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, st, (const f32x4*)dy, to, n);
         MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (dy)");
@@ -994,8 +1048,9 @@ extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const v
         a.dgate_part = (float*)((unsigned char*)ws + n_dz + n_wh);
         ok = sw ? launch_nt_rows<HID_SWIGLU>(a, (int)A, st) : launch_nt_rows<HID_RELU>(a, (int)A, st);
         if (ok != MOE_OK) return ok;
-        if (dgate_w) {
-            hipLaunchKernelGGL(dgate_kernel, dim3((unsigned)((A + 255) / 256)), dim3(256), 0, st, a.dgate_part, inv_perm, (int)A, parts, dgate_w);
+        if (dgate_w || dw) {
+            hipLaunchKernelGGL(dgate_kernel, dim3((unsigned)((A + 255) / 256)), dim3(256), 0, st, a.dgate_part, offsets, perm, inv_perm, (int)A, E, k, (unsigned)d * 2u, parts,
+                               dgate_w, dw ? src : nullptr);
             MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (gate values)");
         }
         if (dx_perm) {
@@ -1020,9 +1075,8 @@ extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const v
         t.dz = (const uint16_t*)ws;
         t.wh = (const uint16_t*)((unsigned char*)ws + n_dz);
         t.offsets = offsets;
-        t.perm = perm;
+        t.src = src;
         t.T = T;
-        t.k = k;
         t.E = E;
         t.d = d;
         t.F = F;
