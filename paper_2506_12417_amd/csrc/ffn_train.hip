@@ -56,16 +56,17 @@ __device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned base, unsig
     asm volatile("s_add_u32 m0, %1, %2\n\tv_add_u32_e64 %0, %3, %4 clamp\n\tbuffer_load_dwordx4 %0, %5, %6 offen lds"
                  : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "s"(add), "s"(d), "s"(soff) : "memory", "scc");
 }
-// the same with a sum that differs from lane to lane
-__device__ __forceinline__ void load_to_lds_v(const u32x4& r, unsigned base, unsigned at, unsigned voff, unsigned add) {
-    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
-    unsigned sum;
-    asm volatile("s_add_u32 m0, %1, %2\n\tv_add_u32_e64 %0, %3, %4 clamp\n\tbuffer_load_dwordx4 %0, %5, 0 offen lds"
-                 : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "v"(add), "s"(d) : "memory", "scc");
-}
 // 4 bytes a lane
 __device__ __forceinline__ void load_to_lds4(const u32x4& d, unsigned to, unsigned voff) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
+}
+
+// The lane's number, formed where it is used: held in a register over the loops it ends up in scratch memory, and the wait for its way back is one
+// for all loads under way.
+__device__ __forceinline__ int lane_now() {
+    int v;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(v));
+    return v;
 }
 
 // What was issued before an item's stores is there once only those (at least `stores` of them) are under way.
@@ -415,37 +416,47 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
         const __amdgpu_buffer_rsrc_t rw = make_rsrc(a.wh + row0 * F, rc * F * 2u);
         const int on = a.N - f0 < 128 ? a.N - f0 : 128;    // features of this wavefront: 64 or 128
         const unsigned last = (unsigned)((on - 64) / 64);  // (where there are 64, the second 64 read the first's once more)
-        auto row_of = [&](int g) { return (unsigned)(((g >> 1) * 2 + wn) * 32 + (g & 1) * 16 + l16); };
+        // (group g: 16 rows, first_row + rows_of(g); what is added to a lane's offset is wave-uniform)
+        const unsigned first_row = (unsigned)(wn * 32 + l16);
+        auto rows_of = [](int g) { return (unsigned)((g >> 1) * 64 + (g & 1) * 16); };
         float gate[NG];
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const unsigned row = row_of(g);
+            const unsigned row = first_row + rows_of(g);
             gate[g] = a.gate_w && row < rc ? a.gate_w[rinfo[row]] : 1.f;
         }
-        // what is kept of 16 rows is fetched while the 16 before are worked on
-        u32x2 q[2][2][4];
-        float sc[2][2][2];
-        auto fetch = [&](int g, int to) {
-            const unsigned row = row_of(g);
+        // What is kept is fetched AHEAD groups ahead: loads are counted together with the stores before them, so that a load issued
+        // behind a group's stores would wait for their way to memory.
+        constexpr int AHEAD = NG < 4 ? NG - 1 : 3;
+        u32x2 q[AHEAD + 1][MATS][4];
+        float sc[AHEAD + 1][MATS][2];
+        unsigned q_at = first_row * Z + (unsigned)lq * 8u, s_at = first_row * (Z / 64) * 4u;
+        auto fetch = [&](int g) {
+            const int to = g % (AHEAD + 1);
+            asm volatile("" : "+v"(q_at), "+v"(s_at));     // (keeps the groups' offsets from being formed, and held, up front)
+            const unsigned qo = q_at + rows_of(g) * Z, so = s_at + rows_of(g) * (Z / 64) * 4u;
 #pragma unroll
             for (int m = 0; m < MATS; ++m) {
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
-                    q[to][m][b] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, row * Z + (unsigned)lq * 8u,
-                                                                                                 (unsigned)(f0 + m * a.F) + (b < 2 ? 0u : last * 64u) + (unsigned)(b & 1) * 32u, 0));
+                    q[to][m][b] = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rq, qo, (unsigned)(f0 + m * a.F) + (b < 2 ? 0u : last * 64u) + (unsigned)(b & 1) * 32u, 0));
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
-                    sc[to][m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, row * (Z / 64) * 4u, ((unsigned)(f0 + m * a.F) / 64u + (j ? last : 0u)) * 4u, 0));
+                    sc[to][m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, so, ((unsigned)(f0 + m * a.F) / 64u + (j ? last : 0u)) * 4u, 0));
             }
         };
-        fetch(0, 0);
+        unsigned w_at = first_row * F * 2u + (unsigned)lq * 16u, z_at = first_row * Z * 2u + (unsigned)lq * 16u;
+#pragma unroll
+        for (int g = 0; g < AHEAD; ++g) fetch(g);
 #pragma unroll
         for (int g = 0; g < NG; ++g) {
-            const int ni = g >> 1, n16 = g & 1, at = g & 1;
-            if (g + 1 < NG) fetch(g + 1, at ^ 1);
+            const int ni = g >> 1, n16 = g & 1, at = g % (AHEAD + 1);
+            if (g + AHEAD < NG) fetch(g + AHEAD);
             __builtin_amdgcn_sched_barrier(0);
             if (ni >= ni_on) continue;
-            const unsigned row = row_of(g);
+            const unsigned row = first_row + rows_of(g);
+            asm volatile("" : "+v"(w_at), "+v"(z_at));
+            const unsigned wo = w_at + rows_of(g) * F * 2u, zo = z_at + rows_of(g) * Z * 2u;
             float dgate = 0.f;
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -475,9 +486,9 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                     wh[c] = gate[g] * h;
                 }
                 const unsigned col = (unsigned)(f0 + b * 32) * 2u;
-                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, row * F * 2u + (unsigned)lq * 16u, col, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, row * Z * 2u + (unsigned)lq * 16u, col, 0);
-                if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, row * Z * 2u + (unsigned)lq * 16u, col + F * 2u, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, wo, col, 0);
+                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, zo, col, 0);
+                if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, zo, col + F * 2u, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
             dgate = quarter_sum(dgate);
@@ -613,76 +624,116 @@ struct TnWork {
     TnShape sh;
     int end, stride;
     unsigned ring, ids;            // LDS addresses
-    int wave, lane, term;          // term: this thread's rows of a stage are term .. term + 3 and 32 + those
-    unsigned piece;
+    int wave;
 };
 
-// A place in the stream of stages (items without rows have none).
-struct TnPlace {
-    int item, kt, KT;
-    TnItem it;
+// The loader's place in the stream of stages (items without rows have none) and the loads of its stage.  An operand's 64 rows of 256 columns lie in LDS as
+// four panels of 64 columns, so that a load of a wavefront fetches whole 128-byte lines of eight rows: load Q is rows 32 (Q & 1) + 8 wave + lane / 8 of panel
+// Q / 2.  (Two rows of 512 bytes a load crowd the L2's channels: the loads alone took 1.9 us a stage.)
+struct TnLoads {
+    int item, left;                // rows of the item from this stage on
+    u32x4 rd, rg;                  // the direct operand's rows of this stage, the gathered one's matrix
+    unsigned ld_d, cd, cg, to_d, to_g;
+    unsigned vd;                   // this thread's first row in the direct operand
 };
-template <int ES> __device__ __forceinline__ void tn_settle(const TnArgs& a, const TnWork& w, TnPlace& p) {
-    p.kt = p.KT = 0;
-    for (; p.item < w.end; p.item += w.stride) {
-        p.it = tn_locate<ES>(a, w.sh, p.item);
-        p.KT = (p.it.n + 63) / 64;
-        if (p.KT > 0) return;
-    }
+// ahead of it, the fetch of source rows
+struct TnAhead {
+    int item, left;
+    u32x4 src;
+};
+// the piece of 16 bytes that a lane fetches of a panel's row: rows 2 r and 2 r + 1 fill 256 bytes, and the transposing reads of 32 lanes (32 bytes of
+// eight rows) touch all 64 banks once
+__device__ __forceinline__ unsigned tn_piece() {
+    const unsigned l = (unsigned)lane_now();
+    return ((l & 7u) ^ ((l >> 4 & 3u) << 1)) << 4;
 }
-template <int ES> __device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnPlace& p) {
-    if (++p.kt < p.KT) return;
+// Turns to the first item with rows from L.item on.
+template <int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnLoads& L) {
+    for (; L.item < w.end; L.item += w.stride) {
+        const TnItem it = tn_locate<ES>(a, w.sh, L.item);
+        if (it.n == 0) continue;
+        const int ld = it.out ? a.F : a.Z;
+        L.left = it.n;
+        L.ld_d = (unsigned)ld * 2u;
+        L.rd = descriptor((it.out ? a.wh : a.dz) + (size_t)it.row0 * ld, (unsigned)(it.n < 64 ? it.n : 64) * L.ld_d);
+        L.rg = descriptor(it.out ? a.dy : a.x, (unsigned)a.T * (unsigned)a.d * 2u);
+        L.vd = (unsigned)(w.wave * 8 + (lane_now() >> 3)) * L.ld_d + tn_piece();
+        L.cd = (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u;
+        L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u;
+        const unsigned to = w.ring + (unsigned)(w.wave * 1024);
+        L.to_d = to + (it.out ? 2 * TN_OP : 0);
+        L.to_g = to + (it.out ? 0 : 2 * TN_OP);
+        return;
+    }
+    L.left = 0;                                            // past the last item: nothing is fetched, the schedule stays
+    L.rd = L.rg = descriptor(a.dz, 0u);
+}
+template <int ES> __device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnLoads& L) {
+    if (L.left > 64) {
+        L.left -= 64;
+        const uint64_t at = ((uint64_t)L.rd[1] << 32 | L.rd[0]) + (uint64_t)L.ld_d * 64u;
+        L.rd = descriptor((const void*)at, (unsigned)(L.left < 64 ? L.left : 64) * L.ld_d);
+        return;
+    }
+    if (L.item < w.end) L.item += w.stride;
+    tn_turn<ES>(a, w, L);
+}
+__device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnAhead& p) {
+    for (; p.item < w.end; p.item += w.stride) {
+        const int e = sgpr(p.item / w.sh.per_expert), row0 = sgpr(a.offsets[e]);
+        p.left = sgpr(a.offsets[e + 1]) - row0;
+        p.src = descriptor(a.src + row0, (unsigned)p.left * 4u);
+        if (p.left > 0) return;
+    }
+    p.left = 0;
+    p.src = descriptor(a.src, 0u);
+}
+__device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnAhead& p) {
+    if (p.left > 64) {
+        p.left -= 64;
+        const uint64_t at = ((uint64_t)p.src[1] << 32 | p.src[0]) + 256u;
+        p.src = descriptor((const void*)at, (unsigned)p.left * 4u);
+        return;
+    }
     if (p.item < w.end) p.item += w.stride;
-    tn_settle<ES>(a, w, p);
+    tn_turn(a, w, p);
 }
 // the source rows of a stage, into one of two tables (behind the expert's last row: zeros)
-__device__ __forceinline__ void tn_fetch_ids(const TnArgs& a, const TnWork& w, const TnPlace& p, int slot) {
-    if (w.wave == 0 && p.item < w.end)
-        load_to_lds4(descriptor(a.src + p.it.row0 + p.kt * 64, (unsigned)(p.it.n - p.kt * 64) * 4u), w.ids + (unsigned)slot * 256u, (unsigned)w.lane * 4u);
+__device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnAhead& p, int slot) {
+    if (w.wave == 0) load_to_lds4(p.src, w.ids + (unsigned)slot * 256u, (unsigned)lane_now() * 4u);
 }
 
-// The loads of a stage.  Slot s = 8 q + j of an operand's 64 in LDS (q: a thread's load, j = thread / 32) holds row 4 j + q, or 28 + 4 j + q for q >= 4: a
-// thread's assignments are two runs of four.
-struct TnLoads {
-    u32x4 rd, rg;
-    unsigned vd, cg, ld_d, to_d, to_g;
-};
-__device__ __forceinline__ void tn_stage(const TnArgs& a, const TnWork& w, const TnPlace& p, int buf, TnLoads& L) {
-    const TnItem& it = p.it;
-    const bool on = p.item < w.end;
-    const int left = on ? it.n - p.kt * 64 : 0;
-    const int ld = it.out ? a.F : a.Z;
-    L.ld_d = (unsigned)ld * 2u;
-    L.rd = descriptor((it.out ? a.wh : a.dz) + (on ? (size_t)(it.row0 + p.kt * 64) * ld : 0), (unsigned)(left < 64 ? left : 64) * L.ld_d);
-    L.rg = descriptor(it.out ? a.dy : a.x, on ? (unsigned)a.T * (unsigned)a.d * 2u : 0u);
-    L.vd = (unsigned)w.term * L.ld_d + (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u + w.piece;
-    L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u + w.piece;
-    const unsigned to = w.ring + (unsigned)(buf * TN_OP + w.wave * 1024);
-    L.to_d = to + (it.out ? 2 * TN_OP : 0);
-    L.to_g = to + (it.out ? 0 : 2 * TN_OP);
+// The offsets of a thread's two source rows.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
+__device__ __forceinline__ void tn_rows(const TnWork& w, const unsigned* ids, int slot, unsigned (&row)[2]) {
+    const unsigned* at = ids + slot * 64 + w.wave * 8 + (lane_now() >> 3);
+    const unsigned piece = tn_piece();
+    row[0] = __builtin_elementwise_add_sat(~at[0], piece);
+    row[1] = __builtin_elementwise_add_sat(~at[32], piece);
 }
-// load Q: the direct operand's first.  (A row that is not there has the largest offset, and keeps it: the range check reads zeros.)
-template <int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, const u32x4 (&id)[2]) {
-    if constexpr (Q < 8) load_to_lds(L.rd, L.to_d, Q * 4096, L.vd, (unsigned)((Q & 3) + (Q >> 2) * 32) * L.ld_d, 0u);
-    else load_to_lds_v(L.rg, L.to_g, (Q - 8) * 4096, ~id[(Q >> 2) & 1][Q & 3], L.cg);
+// load Q: the direct operand's first
+template <int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, const unsigned (&row)[2]) {
+    constexpr int h = Q & 1, p = (Q >> 1) & 3, at = p * 8192 + h * 4096;
+    if constexpr (Q < 8) load_to_lds(L.rd, L.to_d + buf_at, at, L.vd, L.cd + (unsigned)(h * 32) * L.ld_d + (unsigned)p * 128u, 0u);
+    else load_to_lds(L.rg, L.to_g + buf_at, at, row[h], L.cg + (unsigned)p * 128u, 0u);
 }
-template <int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, const u32x4 (&id)[2]) {
+template <int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, const unsigned (&row)[2]) {
     if constexpr (Q < 16) {
-        tn_load<Q>(L, id);
-        tn_loads<Q + 1>(L, id);
+        tn_load<Q>(L, buf_at, row);
+        tn_loads<Q + 1>(L, buf_at, row);
     }
 }
 
 typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
 struct TnFrags { s16x4 n[8][2], m[8][2]; };
 
-// Read j (0..31) of half S: four terms of a column of a 16-column block.  at: this lane's place in the first rows of each block (buffer included).
-struct TnLane { unsigned n[8], m[8]; };
+// Read j (0..31) of half S: four terms of a column of a 16-column block.  n[c]: this lane's place in block c of the N operand's first panel (buffer
+// included); the M operand's lie a wave-uniform distance behind.
+struct TnLane { unsigned n[4], to_m; };
 __device__ __forceinline__ void tn_read(TnFrags& fr, const TnLane& at, int half, int j) {
-    const int c = (j & 15) >> 1, i = j & 1;
+    const int c = (j & 15) >> 1, i = j & 1, off = (c >> 2) * 8192 + half * 4096 + i * 2048;
     typedef __attribute__((address_space(3))) unsigned char lds_byte;
-    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c] + half * 16384 + i * 8192));
-    else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.m[c] + half * 16384 + i * 8192));
+    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c & 3] + off));
+    else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)(at.n[c & 3] + at.to_m) + off));
 }
 __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -691,13 +742,12 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
 }
 
 // Half S of the stage in buffer `buf`, as in the kernel over rows.
-template <int S, int t> __device__ __forceinline__ void tn_groups(const TnWork& w, const TnLoads& L, const TnLane& ln, const u32x4* ids, int buf, u32x4 (&id)[2], TnAcc& acc, TnFrags (&fr)[2]) {
+template <int ES, int S, int t>
+__device__ __forceinline__ void tn_groups(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, const TnLane& ln, const unsigned* ids, int buf, unsigned (&row)[2], TnAcc& acc,
+                                          TnFrags (&fr)[2]) {
     if constexpr (t < 16) {
         constexpr int m = t >> 1, n4 = (t & 1) * 4;
-        if (S == 1 && t == 0) {
-            id[0] = ids[buf * 16 + (w.term >> 2)];
-            id[1] = ids[buf * 16 + 8 + (w.term >> 2)];
-        }
+        if constexpr (S == 1 && t == 6) tn_rows(w, ids, buf, row);
 #pragma unroll
         for (int n = n4; n < n4 + 4; ++n)
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
@@ -705,53 +755,48 @@ template <int S, int t> __device__ __forceinline__ void tn_groups(const TnWork& 
 #pragma unroll
             for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ln, S ^ 1, j);
         }
-        if constexpr (S == 1) tn_load<t>(L, id);
+        if constexpr (S == 1) tn_load<t>(L, (unsigned)(buf * TN_OP), row);
         __builtin_amdgcn_sched_barrier(0);
-        tn_groups<S, t + 1>(w, L, ln, ids, buf, id, acc, fr);
+        tn_groups<ES, S, t + 1>(a, w, L, ahead, ln, ids, buf, row, acc, fr);
     }
 }
 template <int ES, int S, bool FIRST>
-__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, TnLane& ln, const u32x4* ids, int& buf, TnAcc& acc, TnFrags (&fr)[2],
-                                        int stores) {
+__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, TnLane& ln, const unsigned* ids, int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
     if (S == 1) {
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            ln.n[c] ^= TN_OP;
-            ln.m[c] ^= TN_OP;
-        }
+        for (int c = 0; c < 4; ++c) ln.n[c] ^= TN_OP;
     }
-    u32x4 id[2];
-    tn_groups<S, 0>(w, L, ln, ids, buf, id, acc, fr);
+    unsigned row[2];
+    tn_groups<ES, S, 0>(a, w, L, ahead, ln, ids, buf, row, acc, fr);
     if (S == 0) {
         // everybody has read all of this stage; the next one is there, and the source rows of the one behind it
         MOE_WAIT_LGKMCNT(0);
         if (FIRST) wait_landed(stores);
         else MOE_WAIT_VMCNT(0);
         wg_barrier();
-        tn_next<ES>(a, w, load);
-        tn_stage(a, w, load, buf, L);
-        tn_next<ES>(a, w, ahead);
-        tn_fetch_ids(a, w, ahead, buf ^ 1);
+        tn_next<ES>(a, w, L);
+        tn_next(a, w, ahead);
+        tn_fetch_ids(w, ahead, buf ^ 1);
     } else {
         buf ^= 1;
     }
 }
 
 template <int ES>
-__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnPlace& load, TnPlace& ahead, TnLoads& L, TnLane& ln, const u32x4* ids, int KT,
-                                            int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
-    tn_half<ES, 0, true>(a, w, load, ahead, L, ln, ids, buf, acc, fr, stores);
-    tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
+__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, TnLane& ln, const unsigned* ids, int KT, int& buf, TnAcc& acc, TnFrags (&fr)[2],
+                                            int stores) {
+    tn_half<ES, 0, true>(a, w, L, ahead, ln, ids, buf, acc, fr, stores);
+    tn_half<ES, 1, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
 #pragma clang loop unroll(disable)
     for (int kt = 1; kt < KT; ++kt) {
-        tn_half<ES, 0, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
-        tn_half<ES, 1, false>(a, w, load, ahead, L, ln, ids, buf, acc, fr, 0);
+        tn_half<ES, 0, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
+        tn_half<ES, 1, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
     }
 }
 
-template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const TnItem& it, TnAcc& acc, int wm, int wn, int lane) {
+template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const TnItem& it, TnAcc& acc, int wm, int wn) {
     constexpr unsigned ES = sizeof(O);
-    const int l16 = lane & 15, lq = lane >> 4;
+    const int lane = lane_now(), l16 = lane & 15, lq = lane >> 4;
     const int c0 = it.n0 + wm * 128;
     if (c0 >= it.N) return;
     const unsigned ld = (unsigned)it.N * ES;
@@ -759,6 +804,7 @@ template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const 
 #pragma unroll
     for (int m = 0; m < 8; ++m) {
         const unsigned row = (unsigned)(wn * 128 + m * 16 + l16) * ld;
+        __builtin_amdgcn_sched_barrier(0);                 // (16 rows at a time: there are no registers for more)
 #pragma unroll
         for (int n = 0; n < 8; n += 2) {
             if (c0 + n * 16 >= it.N) continue;
@@ -797,7 +843,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
     constexpr int ES = sizeof(O);
-    const u32x4* ids = (const u32x4*)(ring + 4 * TN_OP);      // source rows of two stages
+    const unsigned* ids = (const unsigned*)(ring + 4 * TN_OP);      // source rows of two stages
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
     TnWork w;
@@ -822,41 +868,36 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
     w.ids = w.ring + 4 * TN_OP;
     w.wave = wave;
-    w.lane = lane;
-    w.term = (tid >> 5) * 4;
-    // row r of an operand's 64: 512 bytes, piece p (16 bytes) at p ^ 2 (slot % 8): the transposing reads of 32 lanes then touch all 64 banks once
-    w.piece = (unsigned)((tid & 31) ^ (2 * (tid >> 5))) << 4;
     TnLane ln;
-    const int slot = lq * 4 + (l16 >> 2);                  // lane (l16, lq) reads from slots 4 lq + l16 / 4 of sixteen
+    const int row = lq * 4 + (l16 >> 2);                   // lane (l16, lq) reads from rows 4 lq + l16 / 4 of sixteen
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const unsigned at = w.ring + (unsigned)(slot * 512 + (l16 & 3) * 8) + (unsigned)((c * 32) ^ ((slot & 7) * 32));
-        ln.n[c] = at + (unsigned)wm * 256u;
-        ln.m[c] = at + (unsigned)(2 * TN_OP + wn * 256);
-    }
+    for (int c = 0; c < 4; ++c) ln.n[c] = w.ring + (unsigned)(wm * 16384 + row * 128 + (l16 & 3) * 8) + (unsigned)((c ^ (row >> 1 & 3)) * 32);
+    ln.to_m = (unsigned)sgpr(2 * TN_OP + (wn - wm) * 16384);
 
     // two stages on their way, the source rows of the third behind them
-    TnPlace load, ahead;
-    load.item = first;
-    tn_settle<ES>(a, w, load);
-    ahead = load;
     TnLoads L;
-    tn_fetch_ids(a, w, ahead, 0);
-    tn_next<ES>(a, w, ahead);
-    tn_fetch_ids(a, w, ahead, 1);
-    tn_next<ES>(a, w, ahead);
+    L.item = first;
+    L.vd = L.cd = L.cg = L.ld_d = L.to_d = L.to_g = 0u;
+    tn_turn<ES>(a, w, L);
+    TnAhead ahead;
+    ahead.item = first;
+    tn_turn(a, w, ahead);
+    tn_fetch_ids(w, ahead, 0);
+    tn_next(a, w, ahead);
+    tn_fetch_ids(w, ahead, 1);
+    tn_next(a, w, ahead);
     MOE_WAIT_VMCNT(0);
     wg_barrier();
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        if (st == 1) tn_next<ES>(a, w, load);
-        tn_stage(a, w, load, st, L);
-        const u32x4 id[2] = {ids[st * 16 + (w.term >> 2)], ids[st * 16 + 8 + (w.term >> 2)]};
-        tn_loads<0>(L, id);
+        if (st == 1) tn_next<ES>(a, w, L);
+        unsigned at[2];
+        tn_rows(w, ids, st, at);
+        tn_loads<0>(L, (unsigned)(st * TN_OP), at);
     }
     MOE_WAIT_VMCNT(16);
     wg_barrier();
-    tn_fetch_ids(a, w, ahead, 0);
+    tn_fetch_ids(w, ahead, 0);
     TnAcc acc;
     TnFrags fr[2];
 #pragma unroll
@@ -873,10 +914,10 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #pragma unroll
             for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (KT > 0) {
-            tn_contract<ES>(a, w, load, ahead, L, ln, ids, KT, buf, acc, fr, stores);
+            tn_contract<ES>(a, w, L, ahead, ln, ids, KT, buf, acc, fr, stores);
             stores = 0;
         }
-        tn_finish<O, ADD>(it, acc, wm, wn, lane);
+        tn_finish<O, ADD>(it, acc, wm, wn);
         stores += 4 * n_on * (ES / 2);                     // store instructions just issued
     }
     MOE_WAIT_VMCNT(0);                                      // (the trailing empty loads still target this LDS)
