@@ -57,7 +57,8 @@ __device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned base, unsig
                  : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "s"(add), "s"(d), "s"(soff) : "memory", "scc");
 }
 // 4 bytes a lane
-__device__ __forceinline__ void load_to_lds4(const u32x4& d, unsigned to, unsigned voff) {
+__device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsigned voff) {
+    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
 }
 
@@ -588,8 +589,9 @@ struct TnArgs {
     void *dwa, *dwb, *dwo;
 };
 
-constexpr int TN_OP = 64 * 512;    // LDS: an operand's 64 rows of 256 columns; both buffers of the N operand, then both of the M operand
-constexpr size_t TN_SMEM = 4 * TN_OP + 2 * 64 * 4;
+constexpr int TN_BUF = 32 * 512;   // LDS: an operand's 32 rows of 256 columns; the N operand's four buffers, then the M operand's
+constexpr int TN_IDS = 8 * TN_BUF; // behind them source rows: [8 halves][4 wavefronts][64 lanes]
+constexpr size_t TN_SMEM = TN_IDS + 8 * 4 * 256;
 
 struct TnItem {
     int e, row0, n, m0, n0, M, N;
@@ -623,60 +625,72 @@ template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, c
 struct TnWork {
     TnShape sh;
     int end, stride;
-    unsigned ring, ids;            // LDS addresses
+    unsigned ring;                 // LDS address
     int wave;
 };
+// A lane's row among a load's 32, times 4; its place in the tables of source rows; the piece of 16 bytes that it fetches of a panel's row (rows 2 r and
+// 2 r + 1 fill 256 bytes, and the transposing reads of 32 lanes, 32 bytes of eight rows, touch all 64 banks once).
+struct TnThread {
+    int wave;
+    unsigned tables;
+    __device__ __forceinline__ unsigned row4() const { return (unsigned)(wave * 8 + (lane_now() >> 3)) * 4u; }
+    __device__ __forceinline__ unsigned ids() const { return tables + (unsigned)lane_now() * 4u; }
+    __device__ __forceinline__ unsigned piece() const {
+        const unsigned l = (unsigned)lane_now();
+        return ((l & 7u) ^ ((l >> 4 & 3u) << 1)) << 4;
+    }
+};
 
-// The loader's place in the stream of stages (items without rows have none) and the loads of its stage.  An operand's 64 rows of 256 columns lie in LDS as
-// four panels of 64 columns, so that a load of a wavefront fetches whole 128-byte lines of eight rows: load Q is rows 32 (Q & 1) + 8 wave + lane / 8 of panel
-// Q / 2.  (Two rows of 512 bytes a load crowd the L2's channels: the loads alone took 1.9 us a stage.)
+// The contraction goes in stages of 64 rows, in halves of 32 through four buffers: the loads of a half are issued while the one four before is multiplied and
+// are due two steps later.  An operand's 32 rows of 256 columns lie in LDS as four panels of 64 columns: a load of a wavefront fetches whole
+// 128-byte lines of eight rows, load Q rows 8 wave + lane / 8 of panel Q.
+//
+// The loader's place in the stream of stages (items without rows have none).
 struct TnLoads {
     int item, left;                // rows of the item from this stage on
     u32x4 rd, rg;                  // the direct operand's rows of this stage, the gathered one's matrix
     unsigned ld_d, cd, cg, to_d, to_g;
-    unsigned vd;                   // this thread's first row in the direct operand
+    unsigned vd;                   // this thread's row in the direct operand
 };
-// ahead of it, the fetch of source rows
+// two stages ahead of it, the fetch of source rows
 struct TnAhead {
     int item, left;
     u32x4 src;
 };
-// the piece of 16 bytes that a lane fetches of a panel's row: rows 2 r and 2 r + 1 fill 256 bytes, and the transposing reads of 32 lanes (32 bytes of
-// eight rows) touch all 64 banks once
-__device__ __forceinline__ unsigned tn_piece() {
-    const unsigned l = (unsigned)lane_now();
-    return ((l & 7u) ^ ((l >> 4 & 3u) << 1)) << 4;
-}
+__device__ __forceinline__ unsigned rows_of_stage(int left) { return (unsigned)(left < 0 ? 0 : left < 64 ? left : 64); }
 // Turns to the first item with rows from L.item on.
-template <int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnLoads& L) {
+template <int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
     for (; L.item < w.end; L.item += w.stride) {
         const TnItem it = tn_locate<ES>(a, w.sh, L.item);
         if (it.n == 0) continue;
         const int ld = it.out ? a.F : a.Z;
         L.left = it.n;
         L.ld_d = (unsigned)ld * 2u;
-        L.rd = descriptor((it.out ? a.wh : a.dz) + (size_t)it.row0 * ld, (unsigned)(it.n < 64 ? it.n : 64) * L.ld_d);
+        L.rd = descriptor((it.out ? a.wh : a.dz) + (size_t)it.row0 * ld, rows_of_stage(it.n) * L.ld_d);
         L.rg = descriptor(it.out ? a.dy : a.x, (unsigned)a.T * (unsigned)a.d * 2u);
-        L.vd = (unsigned)(w.wave * 8 + (lane_now() >> 3)) * L.ld_d + tn_piece();
+        L.vd = (th.row4() >> 2) * L.ld_d + th.piece();
         L.cd = (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u;
         L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u;
         const unsigned to = w.ring + (unsigned)(w.wave * 1024);
-        L.to_d = to + (it.out ? 2 * TN_OP : 0);
-        L.to_g = to + (it.out ? 0 : 2 * TN_OP);
+        L.to_d = to + (it.out ? 4 * TN_BUF : 0);
+        L.to_g = to + (it.out ? 0 : 4 * TN_BUF);
         return;
     }
     L.left = 0;                                            // past the last item: nothing is fetched, the schedule stays
+    L.ld_d = 0u;
     L.rd = L.rg = descriptor(a.dz, 0u);
 }
-template <int ES> __device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnLoads& L) {
-    if (L.left > 64) {
-        L.left -= 64;
-        const uint64_t at = ((uint64_t)L.rd[1] << 32 | L.rd[0]) + (uint64_t)L.ld_d * 64u;
-        L.rd = descriptor((const void*)at, (unsigned)(L.left < 64 ? L.left : 64) * L.ld_d);
-        return;
-    }
+// To the next stage of the item; at its end, which the caller sees to (left <= 0), to something that is not used.
+__device__ __forceinline__ void tn_step_on(TnLoads& L) {
+    const uint64_t at = ((uint64_t)L.rd[1] << 32 | L.rd[0]) + (uint64_t)L.ld_d * 64u;
+    L.left -= 64;
+    L.rd[0] = (unsigned)at;
+    L.rd[1] = (unsigned)(at >> 32);
+    L.rd[2] = rows_of_stage(L.left) * L.ld_d;
+}
+template <int ES> __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
     if (L.item < w.end) L.item += w.stride;
-    tn_turn<ES>(a, w, L);
+    tn_turn<ES>(a, w, th, L);
 }
 __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnAhead& p) {
     for (; p.item < w.end; p.item += w.stride) {
@@ -688,49 +702,47 @@ __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnAhea
     p.left = 0;
     p.src = descriptor(a.src, 0u);
 }
-__device__ __forceinline__ void tn_next(const TnArgs& a, const TnWork& w, TnAhead& p) {
-    if (p.left > 64) {
-        p.left -= 64;
-        const uint64_t at = ((uint64_t)p.src[1] << 32 | p.src[0]) + 256u;
-        p.src = descriptor((const void*)at, (unsigned)p.left * 4u);
-        return;
-    }
+__device__ __forceinline__ void tn_step_on(TnAhead& p) {
+    const uint64_t at = ((uint64_t)p.src[1] << 32 | p.src[0]) + 256u;
+    p.left -= 64;
+    p.src[0] = (unsigned)at;
+    p.src[1] = (unsigned)(at >> 32);
+    p.src[2] = (unsigned)(p.left < 0 ? 0 : p.left) * 4u;
+}
+__device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, TnAhead& p) {
     if (p.item < w.end) p.item += w.stride;
     tn_turn(a, w, p);
 }
-// the source rows of a stage, into one of two tables (behind the expert's last row: zeros)
-__device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnAhead& p, int slot) {
-    if (w.wave == 0) load_to_lds4(p.src, w.ids + (unsigned)slot * 256u, (unsigned)lane_now() * 4u);
+// Every lane's source row of half h of a stage, into one of eight tables of its wavefront's (behind the expert's last row: zeros).
+__device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const TnAhead& p, int h, int slot) {
+    load_to_lds4(p.src, w.ring + (unsigned)(TN_IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
 }
-
-// The offsets of a thread's two source rows.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
-__device__ __forceinline__ void tn_rows(const TnWork& w, const unsigned* ids, int slot, unsigned (&row)[2]) {
-    const unsigned* at = ids + slot * 64 + w.wave * 8 + (lane_now() >> 3);
-    const unsigned piece = tn_piece();
-    row[0] = __builtin_elementwise_add_sat(~at[0], piece);
-    row[1] = __builtin_elementwise_add_sat(~at[32], piece);
+// Its offset.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
+__device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
+    typedef __attribute__((address_space(3))) unsigned lds_word;
+    return __builtin_elementwise_add_sat(~*(lds_word*)(uintptr_t)(th.ids() + (unsigned)slot * 1024u), th.piece());
 }
-// load Q: the direct operand's first
-template <int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, const unsigned (&row)[2]) {
-    constexpr int h = Q & 1, p = (Q >> 1) & 3, at = p * 8192 + h * 4096;
-    if constexpr (Q < 8) load_to_lds(L.rd, L.to_d + buf_at, at, L.vd, L.cd + (unsigned)(h * 32) * L.ld_d + (unsigned)p * 128u, 0u);
-    else load_to_lds(L.rg, L.to_g + buf_at, at, row[h], L.cg + (unsigned)p * 128u, 0u);
+// load Q of half H: the direct operand's first
+template <int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, unsigned row) {
+    constexpr int p = Q & 3;
+    if constexpr (Q < 4) load_to_lds(L.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
+    else load_to_lds(L.rg, L.to_g + buf_at, p * 4096, row, L.cg + (unsigned)p * 128u, 0u);
 }
-template <int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, const unsigned (&row)[2]) {
-    if constexpr (Q < 16) {
-        tn_load<Q>(L, buf_at, row);
-        tn_loads<Q + 1>(L, buf_at, row);
+template <int H, int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, unsigned row) {
+    if constexpr (Q < 8) {
+        tn_load<H, Q>(L, buf_at, row);
+        tn_loads<H, Q + 1>(L, buf_at, row);
     }
 }
 
 typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
 struct TnFrags { s16x4 n[8][2], m[8][2]; };
 
-// Read j (0..31) of half S: four terms of a column of a 16-column block.  n[c]: this lane's place in block c of the N operand's first panel (buffer
-// included); the M operand's lie a wave-uniform distance behind.
+// Read j (0..31) of the half in buffer `half` of two: four terms of a column of a 16-column block.  n[c]: this lane's place in block c of the N operand's
+// first panel (pair of buffers included); the M operand's lie a wave-uniform distance behind.
 struct TnLane { unsigned n[4], to_m; };
 __device__ __forceinline__ void tn_read(TnFrags& fr, const TnLane& at, int half, int j) {
-    const int c = (j & 15) >> 1, i = j & 1, off = (c >> 2) * 8192 + half * 4096 + i * 2048;
+    const int c = (j & 15) >> 1, i = j & 1, off = half * TN_BUF + (c >> 2) * 4096 + i * 2048;
     typedef __attribute__((address_space(3))) unsigned char lds_byte;
     if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c & 3] + off));
     else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)(at.n[c & 3] + at.to_m) + off));
@@ -741,13 +753,27 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// Half S of the stage in buffer `buf`, as in the kernel over rows.
-template <int ES, int S, int t>
-__device__ __forceinline__ void tn_groups(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, const TnLane& ln, const unsigned* ids, int buf, unsigned (&row)[2], TnAcc& acc,
+// Memory operations of a step that may be under way at its end: those of two steps (eight loads and the fetch of source rows each), and an item's stores
+// issued between.
+__device__ __forceinline__ void tn_wait(int stores) {
+    if (stores >= 45) MOE_WAIT_VMCNT(63);
+    else if (stores >= 32) MOE_WAIT_VMCNT(50);
+    else if (stores >= 16) MOE_WAIT_VMCNT(34);
+    else MOE_WAIT_VMCNT(18);
+}
+// Step S multiplies the half in buffer 2 pair + S (its fragments are in registers), reads the next one's fragments and issues the loads of the fourth one
+// behind it into the same buffer, which everybody has read.  What moves the places on stands between the multiplications: a wavefront has
+// its SIMD for itself, an instruction that none of them covers costs its whole time.
+template <int S, int t>
+__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, const TnLane& ln, int pair, int slot, unsigned& row, TnAcc& acc,
                                           TnFrags (&fr)[2]) {
     if constexpr (t < 16) {
         constexpr int m = t >> 1, n4 = (t & 1) * 4;
-        if constexpr (S == 1 && t == 6) tn_rows(w, ids, buf, row);
+        constexpr int Q = t < 12 && t % 3 != 2 ? t / 3 * 2 + t % 3 : -1;
+        if constexpr (t == 1) row = tn_row(th, (slot + 4) & 7);
+        if constexpr (t == 13) tn_fetch_ids(w, th, ahead, S, slot);
+        if constexpr (S == 1 && t == 14) tn_step_on(L);
+        if constexpr (S == 1 && t == 15) tn_step_on(ahead);
 #pragma unroll
         for (int n = n4; n < n4 + 4; ++n)
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
@@ -755,42 +781,41 @@ __device__ __forceinline__ void tn_groups(const TnArgs& a, const TnWork& w, TnLo
 #pragma unroll
             for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ln, S ^ 1, j);
         }
-        if constexpr (S == 1) tn_load<t>(L, (unsigned)(buf * TN_OP), row);
+        if constexpr (Q >= 0) tn_load<S, Q>(L, (unsigned)((pair * 2 + S) * TN_BUF), row);
         __builtin_amdgcn_sched_barrier(0);
-        tn_groups<ES, S, t + 1>(a, w, L, ahead, ln, ids, buf, row, acc, fr);
+        tn_groups<S, t + 1>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
     }
 }
-template <int ES, int S, bool FIRST>
-__device__ __forceinline__ void tn_half(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, TnLane& ln, const unsigned* ids, int& buf, TnAcc& acc, TnFrags (&fr)[2], int stores) {
+template <int ES, int S>
+__device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int& slot, TnAcc& acc, TnFrags (&fr)[2],
+                                        int stores) {
+    const int pair = (slot >> 1) & 1;
     if (S == 1) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) ln.n[c] ^= TN_OP;
+        for (int c = 0; c < 4; ++c) ln.n[c] ^= 2 * TN_BUF;
     }
-    unsigned row[2];
-    tn_groups<ES, S, 0>(a, w, L, ahead, ln, ids, buf, row, acc, fr);
-    if (S == 0) {
-        // everybody has read all of this stage; the next one is there, and the source rows of the one behind it
-        MOE_WAIT_LGKMCNT(0);
-        if (FIRST) wait_landed(stores);
-        else MOE_WAIT_VMCNT(0);
-        wg_barrier();
-        tn_next<ES>(a, w, L);
-        tn_next(a, w, ahead);
-        tn_fetch_ids(w, ahead, buf ^ 1);
-    } else {
-        buf ^= 1;
+    unsigned row;
+    tn_groups<S, 0>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
+    slot = (slot + 1) & 7;
+    // everybody has read the next half, and the one behind it is there
+    MOE_WAIT_LGKMCNT(0);
+    tn_wait(stores);
+    wg_barrier();
+    if (S == 1) {
+        if (L.left <= 0) tn_next_item<ES>(a, w, th, L);
+        if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
 }
 
 template <int ES>
-__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, TnLoads& L, TnAhead& ahead, TnLane& ln, const unsigned* ids, int KT, int& buf, TnAcc& acc, TnFrags (&fr)[2],
+__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int KT, int& slot, TnAcc& acc, TnFrags (&fr)[2],
                                             int stores) {
-    tn_half<ES, 0, true>(a, w, L, ahead, ln, ids, buf, acc, fr, stores);
-    tn_half<ES, 1, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
+    tn_step<ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
+    tn_step<ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
 #pragma clang loop unroll(disable)
     for (int kt = 1; kt < KT; ++kt) {
-        tn_half<ES, 0, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
-        tn_half<ES, 1, false>(a, w, L, ahead, ln, ids, buf, acc, fr, 0);
+        tn_step<ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
+        tn_step<ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
     }
 }
 
@@ -843,7 +868,6 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
     constexpr int ES = sizeof(O);
-    const unsigned* ids = (const unsigned*)(ring + 4 * TN_OP);      // source rows of two stages
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
     TnWork w;
@@ -866,43 +890,51 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     const int first = bound(xcd) + (int)blockIdx.x / XCD;
     if (first >= w.end) return;
     w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
-    w.ids = w.ring + 4 * TN_OP;
     w.wave = wave;
     TnLane ln;
     const int row = lq * 4 + (l16 >> 2);                   // lane (l16, lq) reads from rows 4 lq + l16 / 4 of sixteen
 #pragma unroll
-    for (int c = 0; c < 4; ++c) ln.n[c] = w.ring + (unsigned)(wm * 16384 + row * 128 + (l16 & 3) * 8) + (unsigned)((c ^ (row >> 1 & 3)) * 32);
-    ln.to_m = (unsigned)sgpr(2 * TN_OP + (wn - wm) * 16384);
+    for (int c = 0; c < 4; ++c) ln.n[c] = w.ring + (unsigned)(wm * 8192 + row * 128 + (l16 & 3) * 8) + (unsigned)((c ^ (row >> 1 & 3)) * 32);
+    ln.to_m = (unsigned)sgpr(4 * TN_BUF + (wn - wm) * 8192);
 
-    // two stages on their way, the source rows of the third behind them
+    TnThread th;
+    th.wave = wave;
+    th.tables = w.ring + (unsigned)(TN_IDS + wave * 256);
+
+    // two stages on their way, the source rows of the two behind them
     TnLoads L;
     L.item = first;
-    L.vd = L.cd = L.cg = L.ld_d = L.to_d = L.to_g = 0u;
-    tn_turn<ES>(a, w, L);
+    L.vd = L.cd = L.cg = L.to_d = L.to_g = 0u;
+    tn_turn<ES>(a, w, th, L);
     TnAhead ahead;
     ahead.item = first;
     tn_turn(a, w, ahead);
-    tn_fetch_ids(w, ahead, 0);
-    tn_next(a, w, ahead);
-    tn_fetch_ids(w, ahead, 1);
-    tn_next(a, w, ahead);
-    MOE_WAIT_VMCNT(0);
-    wg_barrier();
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        if (st == 1) tn_next<ES>(a, w, L);
-        unsigned at[2];
-        tn_rows(w, ids, st, at);
-        tn_loads<0>(L, (unsigned)(st * TN_OP), at);
+        tn_fetch_ids(w, th, ahead, 0, 2 * st);
+        tn_fetch_ids(w, th, ahead, 1, 2 * st + 1);
+        tn_step_on(ahead);
+        if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
-    MOE_WAIT_VMCNT(16);
+    MOE_WAIT_VMCNT(0);
+#pragma unroll
+    for (int st = 0; st < 2; ++st) {
+        tn_loads<0, 0>(L, (unsigned)(2 * st * TN_BUF), tn_row(th, 2 * st));
+        tn_fetch_ids(w, th, ahead, 0, 4 + 2 * st);
+        tn_loads<1, 0>(L, (unsigned)((2 * st + 1) * TN_BUF), tn_row(th, 2 * st + 1));
+        tn_fetch_ids(w, th, ahead, 1, 5 + 2 * st);
+        tn_step_on(L);
+        if (L.left <= 0) tn_next_item<ES>(a, w, th, L);
+        tn_step_on(ahead);
+        if (ahead.left <= 0) tn_next_item(a, w, ahead);
+    }
+    MOE_WAIT_VMCNT(18);
     wg_barrier();
-    tn_fetch_ids(w, ahead, 0);
     TnAcc acc;
     TnFrags fr[2];
 #pragma unroll
     for (int j = 0; j < 32; ++j) tn_read(fr[0], ln, 0, j);
-    int buf = 0, stores = 0;
+    int slot = 0, stores = 0;
     for (int item = first; item < w.end; item += w.stride) {
         const TnItem it = tn_locate<ES>(a, w.sh, item);
         const int KT = (it.n + 63) / 64;
@@ -914,7 +946,7 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
 #pragma unroll
             for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (KT > 0) {
-            tn_contract<ES>(a, w, L, ahead, ln, ids, KT, buf, acc, fr, stores);
+            tn_contract<ES>(a, w, th, L, ahead, ln, KT, slot, acc, fr, stores);
             stores = 0;
         }
         tn_finish<O, ADD>(it, acc, wm, wn);
