@@ -70,12 +70,13 @@ __device__ __forceinline__ int lane_now() {
     return v;
 }
 
-// What was issued before an item's stores is there once only those (at least `stores` of them) are under way.
-__device__ __forceinline__ void wait_landed(int stores) {
-    if (stores >= 63) MOE_WAIT_VMCNT(63);
-    else if (stores >= 32) MOE_WAIT_VMCNT(32);
-    else if (stores >= 16) MOE_WAIT_VMCNT(16);
-    else MOE_WAIT_VMCNT(0);
+// What was issued before `LOADS` loads and an item's stores is there once only those (at least `stores` of the latter) are under way.
+template <int LOADS> __device__ __forceinline__ void wait_landed(int stores) {
+    static_assert(LOADS <= 30, "vmcnt range");
+    if (stores >= 63 - LOADS) MOE_WAIT_VMCNT(63);
+    else if (stores >= 32) MOE_WAIT_VMCNT(LOADS + 32);
+    else if (stores >= 16) MOE_WAIT_VMCNT(LOADS + 16);
+    else MOE_WAIT_VMCNT(LOADS);
 }
 
 // a / k for a < 2^30, m = (2^32 - 1) / k: the product is one too small at most (k = 1 too)
@@ -161,7 +162,9 @@ template <int TR> struct Nt {
     static constexpr int NI = TR / 64;                     // 32-row blocks of a wavefront (two wavefronts share the rows, block by block)
     static constexpr int F_BYTES = 256 * 128, R_BYTES = TR * 128, STAGE = F_BYTES + R_BYTES;
     static constexpr int NFL = 8, NRL = TR / 32, LPS = NFL + NRL;      // loads per thread and stage
-    static constexpr size_t SMEM = 2 * STAGE + 4 * TR * 4;
+    // Stages in LDS: two of 256 rows (all that there is room for), three of fewer, whose time is the way of the matrices from HBM.
+    static constexpr int RING = TR == 256 ? 2 : 3, ROWS_AT = RING * STAGE;
+    static constexpr size_t SMEM = ROWS_AT + 8 * TR * 4;
 };
 template <int TR> using NtAcc = f32x4[Nt<TR>::NI][2][4][2];            // [32-row block][its half][32-feature block][its half]
 template <int TR> struct NtFrags { bf16x8 f[4][2], r[Nt<TR>::NI][2]; };
@@ -185,7 +188,7 @@ template <int TR> __device__ __forceinline__ NtItem nt_locate(const NtArgs& a, c
     return it;
 }
 
-// The loader's place in the stream of stages: it runs two of them ahead of the multiplications, across the items' borders.
+// The loader's place in the stream of stages: it runs RING of them ahead of the multiplications, across the items' borders.
 template <int TR> struct NtLoader {
     u32x4 rr, rf;
     unsigned vr[Nt<TR>::NRL], vf;  // byte offsets: of this thread's rows, of its first feature
@@ -198,10 +201,10 @@ struct NtWork {
     unsigned piece;
 };
 
-// (gather) the assignments of an item's rows: four items' tables in turn
+// (gather) the assignments of an item's rows: eight items' tables in turn
 template <int TR> __device__ __forceinline__ void nt_fetch_rows(const NtArgs& a, const NtWork& w, const NtItem& it, int seq) {
     if (w.wave * 64 < TR)
-        load_to_lds4(descriptor(a.perm + it.row0, (unsigned)it.rc * 4u), w.rinfo + (unsigned)((seq & 3) * TR + w.wave * 64) * 4u, (unsigned)(w.wave * 64 + w.lane) * 4u);
+        load_to_lds4(descriptor(a.perm + it.row0, (unsigned)it.rc * 4u), w.rinfo + (unsigned)((seq & 7) * TR + w.wave * 64) * 4u, (unsigned)(w.wave * 64 + w.lane) * 4u);
 }
 
 template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L) {
@@ -225,7 +228,7 @@ template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs
 #pragma unroll
         for (int q = 0; q < Nt<TR>::NRL; ++q) {
             const int row = q * 32 + w.ld_row;
-            unsigned src = (unsigned)rinfo[(L.seq & 3) * TR + row];
+            unsigned src = (unsigned)rinfo[(L.seq & 7) * TR + row];
             src = divided(src, (unsigned)a.k, w.div);
             // (a row past the tile's end gets an offset beyond the matrix: the range check reads zeros)
             L.vr[q] = row < it.rc ? src * (unsigned)a.ld_rows * 2u + w.piece : 0xFFFFFFF0u;
@@ -251,7 +254,7 @@ template <int KIND, int TR, int FROM, int TO> __device__ __forceinline__ void nt
 }
 // after the last load of a stage
 template <int KIND, int TR> __device__ __forceinline__ void nt_advance(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L) {
-    L.buf ^= 1;
+    L.buf = L.buf + 1 == Nt<TR>::RING ? 0 : L.buf + 1;
     ++L.kt;
     if (KIND == DX && L.kt == a.KT0 && L.kt < a.KT)        // the second matrix: its place in the first one's stead
         L.rf = descriptor((const void*)(((uint64_t)L.rf[1] << 32 | L.rf[0]) + ((uint64_t)a.w1 - (uint64_t)a.w0)), L.rf[2]);
@@ -271,7 +274,8 @@ template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const
 }
 
 // Half S of the stage in buffer `buf`: multiplies set S, reads the other.  Half 1 issues the loads of the stage after the next into the buffer that
-// this one has left.  FIRST: of an item, whose predecessor's stores (at least `stores`) may be under way.
+// this one has left.  FIRST: of an item's first RING - 1 stages,
+// behind whose loads the stores of the item before (at least `stores`) may be under way.
 template <int KIND, int TR, int S, bool FULL, int t>
 __device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const unsigned char* ring, int at_f, int at_r, NtAcc<TR>& acc,
                                           NtFrags<TR> (&fr)[2], int ni_on) {
@@ -297,14 +301,14 @@ __device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, cons
 template <int KIND, int TR, int S, bool FIRST, bool FULL>
 __device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L, const NtLane& ln, const unsigned char* ring, int& buf,
                                         NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
-    if (S == 1) buf ^= 1;
+    if (S == 1) buf = buf + 1 == Nt<TR>::RING ? 0 : buf + 1;
     const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
     nt_groups<KIND, TR, S, FULL, 0>(a, w, L, ring, at_f, at_r, acc, fr, ni_on);
     if (S == 0) {
         // everybody has read all of this stage, and the next one is there
         MOE_WAIT_LGKMCNT(0);
-        if (FIRST) wait_landed(stores);
-        else MOE_WAIT_VMCNT(0);
+        if (FIRST) wait_landed<(Nt<TR>::RING - 2) * Nt<TR>::LPS>(stores);
+        else MOE_WAIT_VMCNT((Nt<TR>::RING - 2) * Nt<TR>::LPS);
         wg_barrier();
         nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
     }
@@ -315,8 +319,14 @@ __device__ __forceinline__ void nt_contract(const NtArgs& a, const NtWork& w, co
                                             int& buf, NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
     nt_half<KIND, TR, 0, true, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
     nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
+    int kt = 1;
+    if (Nt<TR>::RING > 2 && kt < a.KT) {
+        nt_half<KIND, TR, 0, true, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
+        nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
+        ++kt;
+    }
 #pragma clang loop unroll(disable)
-    for (int kt = 1; kt < a.KT; ++kt) {
+    for (; kt < a.KT; ++kt) {
         nt_half<KIND, TR, 0, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
         nt_half<KIND, TR, 1, false, FULL>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, 0, ni_on);
     }
@@ -502,7 +512,7 @@ template <int KIND, int TR>
 __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass makes the stub only: it has no buffer descriptors)
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
-    const int* rinfo = (const int*)(ring + 2 * Nt<TR>::STAGE);
+    const int* rinfo = (const int*)(ring + Nt<TR>::ROWS_AT);
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1;
     const int l16 = lane & 15, lq = lane >> 4;
@@ -517,7 +527,7 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
     const int first = sgpr((int)(all * xcd / XCD) + (int)blockIdx.x / XCD);
     if (first >= w.end) return;
     w.ring = (unsigned)(uintptr_t)(lds_void_t*)ring;
-    w.rinfo = w.ring + 2 * Nt<TR>::STAGE;
+    w.rinfo = w.ring + Nt<TR>::ROWS_AT;
     w.div = 0xFFFFFFFFu / (unsigned)a.k;
     w.wave = wave;
     w.lane = lane;
@@ -543,14 +553,17 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
         wg_barrier();
     }
     nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
-    nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
-    if (KIND != DX && a.KT == 1) {                         // (the next item's rows are wanted now)
-        MOE_WAIT_VMCNT(0);
-        wg_barrier();
+#pragma unroll
+    for (int st = 0; st < Nt<TR>::RING; ++st) {
+        nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
+        if (st + 1 == Nt<TR>::RING) break;
+        if (KIND != DX && a.KT < Nt<TR>::RING) {           // (the next item's rows may be wanted now)
+            MOE_WAIT_VMCNT(0);
+            wg_barrier();
+        }
+        nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
     }
-    nt_advance<KIND, TR>(a, w, tiles, rinfo, L);
-    nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
-    MOE_WAIT_VMCNT(Nt<TR>::LPS);
+    MOE_WAIT_VMCNT((Nt<TR>::RING - 1) * Nt<TR>::LPS);
     wg_barrier();
     NtAcc<TR> acc;
     NtFrags<TR> fr[2];
@@ -567,7 +580,7 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
         ni_on = ni_on > Nt<TR>::NI ? Nt<TR>::NI : ni_on;
         if (ni_on == Nt<TR>::NI) nt_contract<KIND, TR, true>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
         else nt_contract<KIND, TR, false>(a, w, tiles, rinfo, L, ln, ring, buf, acc, fr, stores, ni_on);
-        nt_finish<KIND, TR>(a, it, rinfo + (seq & 3) * TR, acc, wm, wn, lane, ni_on);
+        nt_finish<KIND, TR>(a, it, rinfo + (seq & 7) * TR, acc, wm, wn, lane, ni_on);
         // store instructions just issued, at least: two for every 32 rows x 32 features (SwiGLU: gates and ups make one block of outputs)
         int cols = (a.N - it.n0 - wm * 128 + 31) / 32;
         cols = cols < 0 ? 0 : cols > 4 ? 4 : cols;
@@ -753,14 +766,6 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
     return __builtin_bit_cast(bf16x8, v);
 }
 
-// Memory operations of a step that may be under way at its end: those of two steps (eight loads and the fetch of source rows each), and an item's stores
-// issued between.
-__device__ __forceinline__ void tn_wait(int stores) {
-    if (stores >= 45) MOE_WAIT_VMCNT(63);
-    else if (stores >= 32) MOE_WAIT_VMCNT(50);
-    else if (stores >= 16) MOE_WAIT_VMCNT(34);
-    else MOE_WAIT_VMCNT(18);
-}
 // Step S multiplies the half in buffer 2 pair + S (its fragments are in registers), reads the next one's fragments and issues the loads of the fourth one
 // behind it into the same buffer, which everybody has read.  What moves the places on stands between the multiplications: a wavefront has
 // its SIMD for itself, an instruction that none of them covers costs its whole time.
@@ -797,9 +802,10 @@ __device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const 
     unsigned row;
     tn_groups<S, 0>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
     slot = (slot + 1) & 7;
-    // everybody has read the next half, and the one behind it is there
+    // everybody has read the next half, and the one behind it is there: what was issued before the last two steps (eight loads and a fetch of source
+    // rows each) and an item's stores
     MOE_WAIT_LGKMCNT(0);
-    tn_wait(stores);
+    wait_landed<18>(stores);
     wg_barrier();
     if (S == 1) {
         if (L.left <= 0) tn_next_item<ES>(a, w, th, L);
