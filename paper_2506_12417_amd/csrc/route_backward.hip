@@ -5,8 +5,10 @@
 //   over the k chosen (renorm): dl[t,i_j] = g_j (dgate_w[t,j] - D), 0 elsewhere
 //   dl += dlogits_add     dx = dx_add + dl W_g^T     dW_g = x^T dl     db = sum_t dl
 //
-// Both products are fp32 throughout (v_mfma_f32_16x16x4_f32): dl is never rounded.  dW_g and db are summed over ranges of tokens, whose
-// parts a second launch adds up in their order: no atomics.
+// Both products are made by the 16-bit matrix instruction of fp32 values taken apart: v = hi + mid + lo, each bf16 (24 bits in all), whose products are exact
+// and whose sums are fp32.  dl has three parts, x and W_g one where they are bf16 and three where they are fp32 (then without the products
+// below 2^-24).  dW_g and db are summed over ranges of tokens, whose parts a second launch adds up in their order: no atomics.
+//
 #include "common.h"
 #include "gemm_util.h"
 
@@ -83,87 +85,196 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
     }
 }
 
-// ---- dx: 64 tokens x 64 columns a work-group, a wavefront 16 tokens; terms (experts) 32 at a time through LDS
-constexpr int KC = 32, PAD = KC + 4;
-template <typename W>
-__global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* __restrict__ add, int T, int d, int E,
-                                                 float* __restrict__ dx) {
-    __shared__ __attribute__((aligned(16))) float sl[64 * PAD], sw[64 * PAD];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
-    const int t0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
-    f32x4 acc[4] = {};
-    for (int e0 = 0; e0 < E; e0 += KC) {
-        __syncthreads();
+// ---- fp32 values in parts
+template <int N> struct Parts { bf16x8 p[N]; };
+__device__ __forceinline__ Parts<3> take_apart(const float (&v)[8]) {
+    Parts<3> r;
 #pragma unroll
-        for (int i = 0; i < 64 * KC / NTH; ++i) {
-            const int r = (i * NTH + tid) / KC, c = tid % KC;
-            sl[r * PAD + c] = t0 + r < T && e0 + c < E ? dl[(size_t)(t0 + r) * E + e0 + c] : 0.f;
-            sw[r * PAD + c] = c0 + r < d && e0 + c < E ? load_as_f32(w + (size_t)(c0 + r) * E + e0 + c) : 0.f;
+    for (int i = 0; i < 8; ++i) {
+        const __bf16 hi = (__bf16)v[i];
+        const float rest = v[i] - (float)hi;
+        const __bf16 mid = (__bf16)rest;
+        // (an infinity or a NaN is in the first part: the others would make NaN of an infinity's products)
+        const bool plain = __builtin_fabsf(v[i]) < __builtin_inff() && __builtin_fabsf((float)hi) < __builtin_inff();
+        r.p[0][i] = hi;
+        r.p[1][i] = plain ? mid : (__bf16)0.f;
+        r.p[2][i] = plain ? (__bf16)(rest - (float)mid) : (__bf16)0.f;
+    }
+    return r;
+}
+// acc += a b: the products of the parts, the small ones first
+template <int NA, int NB> __device__ __forceinline__ void multiply(const Parts<NA>& a, const Parts<NB>& b, f32x4& acc) {
+#pragma unroll
+    for (int s = 2; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+            if (s - i >= 0 && s - i < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
+}
+// Eight neighbours of a row of n values from column c on, zeros behind it.  VEC: n is a multiple of 8 and the rows are aligned.
+template <bool VEC> __device__ __forceinline__ Parts<3> fetch8(const float* row, int n, int c, bool on) {
+    float v[8];
+    if (VEC) {
+        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
+        if (on && c < n) {
+            a = ((const f32x4*)(row + c))[0];
+            b = ((const f32x4*)(row + c))[1];
         }
-        __syncthreads();
 #pragma unroll
-        for (int s = 0; s < KC; s += 16) {
-            const f32x4 b = *(const f32x4*)(sl + (wave * 16 + l16) * PAD + s + lq * 4);
+        for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
+    } else {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const f32x4 a = *(const f32x4*)(sw + (n * 16 + l16) * PAD + s + lq * 4);
+        for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : 0.f;
+    }
+    return take_apart(v);
+}
+template <bool VEC> __device__ __forceinline__ Parts<1> fetch8(const uint16_t* row, int n, int c, bool on) {
+    typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
+    u16x8 v = {};
+    if (VEC) {
+        if (on && c < n) v = *(const u16x8*)(row + c);
+    } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i], b[i], acc[n], 0, 0, 0);
+        for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : (unsigned short)0;
+    }
+    return Parts<1>{__builtin_bit_cast(bf16x8, v)};
+}
+template <typename E> constexpr int PARTS = sizeof(E) == 4 ? 3 : 1;
+
+// ---- dx: a wavefront keeps dl of 16 NT tokens in registers (KS steps of 32 experts) and goes over columns, 32 at a time, whose rows of W_g come from the
+// caches.  Matrix row 16 h + j of 32 stands for column 8 (j / 4) + 4 h + j % 4, so that a lane has eight neighbours.
+template <typename W, int KS, int NT, bool VEC>
+__global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* __restrict__ add, int T, int d, int E, int columns,
+                                                 float* __restrict__ dx) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
+    const int t0 = ((int)blockIdx.x * (NTH / 64) + (int)(threadIdx.x >> 6)) * 16 * NT;
+    if (t0 >= T) return;
+    Parts<3> g[NT][KS];
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) g[n][s] = fetch8<VEC>(dl + (size_t)(t0 + n * 16 + l16) * E, E, s * 32 + lq * 8, t0 + n * 16 + l16 < T);
+    const int first = (int)blockIdx.y * columns, last = first + columns < d ? first + columns : d;
+    for (int c0 = first; c0 < last; c0 += 32) {
+        f32x4 acc[NT][2] = {};
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int c = c0 + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
+                const Parts<PARTS<W>> m = fetch8<VEC>(w + (size_t)c * E, E, s * 32 + lq * 8, c < d);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) multiply(m, g[n][s], acc[n][h]);
+            }
+        const int c = c0 + lq * 8;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int t = t0 + n * 16 + l16;
+            if (t >= T || c >= d) continue;                // (d is a multiple of 8)
+            const size_t at = (size_t)t * d + c;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4 v = acc[n][h];
+                if (add) v += *(const f32x4*)(add + at + 4 * h);
+                *(f32x4*)(dx + at + 4 * h) = v;
             }
         }
     }
-    const int t = t0 + wave * 16 + l16;
-    if (t >= T) return;
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
-        const int c = c0 + n * 16 + lq * 4;
-        if (c >= d) continue;                              // (d is a multiple of 8)
-        const size_t at = (size_t)t * d + c;
-        f32x4 v = acc[n];
-        if (add) v += *(const f32x4*)(add + at);
-        *(f32x4*)(dx + at) = v;
-    }
 }
 
-// ---- dW_g over a range of tokens: 64 rows (of x's columns) x 64 experts a work-group, a wavefront 16 rows; 32 tokens at a time through LDS
-constexpr int TC = 32, ROW = 64 + 16;
-template <typename X>
+// ---- dW_g over a range of tokens: 64 of x's columns x 128 experts a work-group, 32 tokens at a time through LDS (fetched while the 32 before are multiplied);
+// a wavefront has 64 columns x 32 experts.  The contraction lies outermost in both operands: the reads that transpose bring a column's terms together.
+// LDS: panels of 32 tokens x 64 columns, 128 bytes a row, whose 32-byte pieces are turned by the row, so that the reads touch all banks.
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+constexpr int TC = 32, PANEL = TC * 128;
+__device__ __forceinline__ int panel_at(int row, int c) { return row * 128 + (((c >> 4) ^ (row >> 1 & 3)) * 32) + (c & 15) * 2; }      // of column c < 64
+__device__ __forceinline__ bf16x8 read_transposed(const unsigned char* panel, int block, int l16, int lq) {
+    typedef __attribute__((ext_vector_type(8))) short s16x8;
+    s16x4 v[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) v[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(panel + panel_at(i * 16 + lq * 4 + (l16 >> 2), block * 16 + (l16 & 3) * 4)));
+    const s16x8 r = __builtin_shufflevector(v[0], v[1], 0, 1, 2, 3, 4, 5, 6, 7);
+    return __builtin_bit_cast(bf16x8, r);
+}
+template <int N> __device__ __forceinline__ void put8(unsigned char* at, int step, const Parts<N>& v) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) *(bf16x8*)(at + i * step) = v.p[i];
+}
+
+template <typename X, bool VEC>
 __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const float* __restrict__ dl, int T, int d, int E, int range, float* __restrict__ part) {
-    __shared__ __attribute__((aligned(16))) float sx[TC * ROW], sl[TC * ROW];
+    constexpr int NX = PARTS<X>, BUF = (NX + 6) * PANEL;   // x's parts, then dl's: [part][two panels]
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
-    const int c0 = blockIdx.x * 64, e0 = blockIdx.y * 64, first = blockIdx.z * range, last = first + range < T ? first + range : T;
-    f32x4 acc[4] = {};
-    float db = 0.f;
-    for (int t0 = first; t0 < last; t0 += TC) {
-        __syncthreads();
+    const int c0 = blockIdx.x * 64, e0 = blockIdx.y * 128, first = blockIdx.z * range, last = first + range < T ? first + range : T;
+    // a thread has eight columns of x and, twice, eight experts of dl
+    const int xr = tid >> 3, xc = (tid & 7) * 8, er = tid >> 4, ec = (tid & 15) * 8;
+    Parts<NX> gx;
+    Parts<3> ge[2];
+    float db[8] = {};
+    auto fetch = [&](int t0) {
+        gx = fetch8<true>(x + (size_t)(t0 + xr) * d, d, c0 + xc, x && t0 + xr < last);
 #pragma unroll
-        for (int i = 0; i < TC * 64 / NTH; ++i) {
-            const int r = i * (NTH / 64) + wave, t = t0 + r;
-            sx[r * ROW + lane] = x && t < last && c0 + lane < d ? load_as_f32(x + (size_t)t * d + c0 + lane) : 0.f;
-            sl[r * ROW + lane] = t < last && e0 + lane < E ? dl[(size_t)t * E + e0 + lane] : 0.f;
+        for (int i = 0; i < 2; ++i) ge[i] = fetch8<VEC>(dl + (size_t)(t0 + er + i * 16) * E, E, e0 + ec, t0 + er + i * 16 < last);
+    };
+    auto put = [&](int buf) {
+        unsigned char* to = lds + buf * BUF;
+        put8(to + panel_at(xr, xc), PANEL, gx);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            put8(to + NX * PANEL + (ec >> 6) * PANEL + panel_at(er + i * 16, ec & 63), 2 * PANEL, ge[i]);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) db[c] += ((float)ge[i].p[2][c] + (float)ge[i].p[1][c]) + (float)ge[i].p[0][c];
         }
-        __syncthreads();
+    };
+    f32x4 acc[4][2] = {};
+    fetch(first);
+    int buf = 0;
+    for (int t0 = first; t0 < last; t0 += TC, buf ^= 1) {
+        put(buf);
+        __syncthreads();                                   // (one is enough: whoever writes this buffer again has passed the next)
+        if (t0 + TC < last) fetch(t0 + TC);
+        const unsigned char* from = lds + buf * BUF;
+        Parts<3> e[2];
 #pragma unroll
-        for (int s = 0; s < TC; s += 4) {
-            const float b = sx[(s + lq) * ROW + wave * 16 + l16];
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-            for (int n = 0; n < 4; ++n)
-                acc[n] = __builtin_amdgcn_mfma_f32_16x16x4f32(sl[(s + lq) * ROW + n * 16 + l16], b, acc[n], 0, 0, 0);
+            for (int i = 0; i < 3; ++i) e[b].p[i] = read_transposed(from + (NX + 2 * i + (wave >> 1)) * PANEL, (wave & 1) * 2 + b, l16, lq);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            Parts<NX> v;
+#pragma unroll
+            for (int i = 0; i < NX; ++i) v.p[i] = read_transposed(from + i * PANEL, m, l16, lq);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) multiply(e[b], v, acc[m][b]);
         }
-        if (wave == 0 && blockIdx.x == 0)
-            for (int r = 0; r < TC; ++r) db += sl[r * ROW + lane];
     }
     // part: [range][d + 1][E], the last row for db
     float* to = part + (size_t)blockIdx.z * (d + 1) * E;
-    const int c = c0 + wave * 16 + l16;
-    if (c < d) {
 #pragma unroll
-        for (int n = 0; n < 4; ++n)
+    for (int m = 0; m < 4; ++m) {
+        const int c = c0 + m * 16 + l16;
+        if (c >= d || !x) continue;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (e0 + n * 16 + lq * 4 + i < E) to[(size_t)c * E + e0 + n * 16 + lq * 4 + i] = acc[n][i];
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int e = e0 + wave * 32 + b * 16 + lq * 4 + i;
+                if (e < E) to[(size_t)c * E + e] = acc[m][b][i];
+            }
     }
-    if (wave == 0 && blockIdx.x == 0 && e0 + lane < E) to[(size_t)d * E + e0 + lane] = db;
+    if (blockIdx.x == 0) {                                 // sixteen threads have each column
+        float* sums = (float*)lds;
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) sums[er * 128 + ec + c] = db[c];
+        __syncthreads();
+        if (tid < 128 && e0 + tid < E) {
+            float s = 0.f;
+            for (int r = 0; r < 16; ++r) s += sums[r * 128 + tid];
+            to[(size_t)d * E + e0 + tid] = s;
+        }
+    }
 }
 __global__ __launch_bounds__(NTH) void dw_sum_kernel(const float* __restrict__ part, int ranges, int d, int E, float* __restrict__ dw, float* __restrict__ db) {
     const size_t i = (size_t)blockIdx.x * NTH + threadIdx.x, n = (size_t)d * E, step = n + E;
@@ -179,13 +290,26 @@ __global__ __launch_bounds__(NTH) void dw_sum_kernel(const float* __restrict__ p
 
 // Ranges of tokens that dW_g is summed over: enough work-groups for the chip, 64 tokens at least.
 int ranges_of(int T, int d, int E) {
-    const int tiles = ((d + 63) / 64) * ((E + 63) / 64);
-    int n = (1024 + tiles - 1) / tiles;
+    const int tiles = ((d + 63) / 64) * ((E + 127) / 128);
+    int n = (512 + tiles - 1) / tiles;
     const int most = (T + 63) / 64;
     if (n > most) n = most;
     if (n < 1) n = 1;
     const int range = ((T + n - 1) / n + TC - 1) / TC * TC;
     return range > 0 ? (T + range - 1) / range : 1;
+}
+
+template <typename W> void launch_dx(const W* w, bool vec, const float* dl, const float* add, int T, int d, int E, float* dx, hipStream_t st) {
+    // columns a work-group: as many as leave four wavefronts a SIMD, 32 at least
+    const int nt = E <= 128 ? 2 : 1, groups = (T + 64 * nt - 1) / (64 * nt);
+    int splits = (1024 + groups - 1) / groups;
+    int columns = ((d + splits - 1) / splits + 31) / 32 * 32;
+    splits = (d + columns - 1) / columns;
+    auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, splits), dim3(NTH), 0, st, dl, w, add, T, d, E, columns, dx); };
+    if (E <= 32) vec ? go(dx_kernel<W, 1, 2, true>) : go(dx_kernel<W, 1, 2, false>);
+    else if (E <= 64) vec ? go(dx_kernel<W, 2, 2, true>) : go(dx_kernel<W, 2, 2, false>);
+    else if (E <= 128) vec ? go(dx_kernel<W, 4, 2, true>) : go(dx_kernel<W, 4, 2, false>);
+    else vec ? go(dx_kernel<W, 8, 1, true>) : go(dx_kernel<W, 8, 1, false>);
 }
 
 }  // namespace
@@ -208,24 +332,23 @@ extern "C" int moe_route_topk_backward(const float* dgate_w, const float* gate_w
     if (T > 0) {
         MOE_REQUIRE(dgate_w && gate_w && expert_idx && (logits || renorm) && dlogits && (w_gate || !dx) && (x || !dw_gate), MOE_ERR_ARG, "%s: null pointer", me);
         MOE_REQUIRE(!sums || (ws && ws_bytes >= need), MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", me, ws_bytes, need);
-        MOE_REQUIRE((((uintptr_t)dx | (uintptr_t)dx_add) & 15) == 0 && (((uintptr_t)ws | (uintptr_t)dlogits) & 3) == 0, MOE_ERR_UNSUPPORTED, "%s: dx and dx_add have to be aligned to 16 bytes", me);
+        MOE_REQUIRE((((uintptr_t)dx | (uintptr_t)dx_add | (uintptr_t)x) & 15) == 0 && (((uintptr_t)ws | (uintptr_t)dlogits) & 3) == 0, MOE_ERR_UNSUPPORTED,
+                    "%s: x, dx and dx_add have to be aligned to 16 bytes", me);
     }
     if (T == 0 && !sums) return MOE_OK;
     const hipStream_t st = (hipStream_t)stream;
     int ranges = 0;
     if (T > 0) {
         hipLaunchKernelGGL(dlogits_kernel, dim3((T + 3) / 4), dim3(NTH), 0, st, dgate_w, gate_w, expert_idx, logits, dlogits_add, T, E, k, renorm, dlogits);
-        if (dx) {
-            const dim3 grid((d + 63) / 64, (T + 63) / 64);
-            if (dt == MOE_F32) hipLaunchKernelGGL(dx_kernel<float>, grid, dim3(NTH), 0, st, dlogits, (const float*)w_gate, dx_add, T, d, E, dx);
-            else hipLaunchKernelGGL(dx_kernel<uint16_t>, grid, dim3(NTH), 0, st, dlogits, (const uint16_t*)w_gate, dx_add, T, d, E, dx);
-        }
+        const bool vec = E % 8 == 0 && (((uintptr_t)dlogits | (uintptr_t)w_gate) & 15) == 0;
+        if (dx) dt == MOE_F32 ? launch_dx((const float*)w_gate, vec, dlogits, dx_add, T, d, E, dx, st) : launch_dx((const uint16_t*)w_gate, vec, dlogits, dx_add, T, d, E, dx, st);
         if (sums) {
             ranges = ranges_of(T, d, E);
             const int range = ((T + ranges - 1) / ranges + TC - 1) / TC * TC;
-            const dim3 grid(dw_gate ? (d + 63) / 64 : 1, (E + 63) / 64, ranges);
-            if (dt == MOE_F32) hipLaunchKernelGGL(dw_kernel<float>, grid, dim3(NTH), 0, st, (const float*)(dw_gate ? x : nullptr), dlogits, T, d, E, range, (float*)ws);
-            else hipLaunchKernelGGL(dw_kernel<uint16_t>, grid, dim3(NTH), 0, st, (const uint16_t*)(dw_gate ? x : nullptr), dlogits, T, d, E, range, (float*)ws);
+            const dim3 grid(dw_gate ? (d + 63) / 64 : 1, (E + 127) / 128, ranges);
+            auto go = [&](auto kern, auto* from) { hipLaunchKernelGGL(kern, grid, dim3(NTH), 0, st, dw_gate ? from : nullptr, dlogits, T, d, E, range, (float*)ws); };
+            if (dt == MOE_F32) vec ? go(dw_kernel<float, true>, (const float*)x) : go(dw_kernel<float, false>, (const float*)x);
+            else vec ? go(dw_kernel<uint16_t, true>, (const uint16_t*)x) : go(dw_kernel<uint16_t, false>, (const uint16_t*)x);
         }
     }
     if (sums) {
