@@ -87,7 +87,7 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
 
 // ---- fp32 values in parts
 template <int N> struct Parts { bf16x8 p[N]; };
-__device__ __forceinline__ Parts<3> take_apart(const float (&v)[8]) {
+__device__ __forceinline__ Parts<3> take_apart(__attribute__((ext_vector_type(8))) float v) {
     Parts<3> r;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -111,24 +111,22 @@ template <int NA, int NB> __device__ __forceinline__ void multiply(const Parts<N
             if (s - i >= 0 && s - i < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
 }
 // Eight neighbours of a row of n values from column c on, zeros behind it.  VEC: n is a multiple of 8 and the rows are aligned.
-template <bool VEC> __device__ __forceinline__ Parts<3> fetch8(const float* row, int n, int c, bool on) {
-    float v[8];
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
+template <bool VEC> __device__ __forceinline__ f32x8 fetch8(const float* row, int n, int c, bool on) {
+    f32x8 v = {};
     if (VEC) {
-        f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = a;
         if (on && c < n) {
-            a = ((const f32x4*)(row + c))[0];
-            b = ((const f32x4*)(row + c))[1];
+            const f32x4 a = ((const f32x4*)(row + c))[0], b = ((const f32x4*)(row + c))[1];
+            v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < 4 ? a[i & 3] : b[i & 3];
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : 0.f;
     }
-    return take_apart(v);
+    return v;
 }
-template <bool VEC> __device__ __forceinline__ Parts<1> fetch8(const uint16_t* row, int n, int c, bool on) {
-    typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
+template <bool VEC> __device__ __forceinline__ u16x8 fetch8(const uint16_t* row, int n, int c, bool on) {
     u16x8 v = {};
     if (VEC) {
         if (on && c < n) v = *(const u16x8*)(row + c);
@@ -136,15 +134,16 @@ template <bool VEC> __device__ __forceinline__ Parts<1> fetch8(const uint16_t* r
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : (unsigned short)0;
     }
-    return Parts<1>{__builtin_bit_cast(bf16x8, v)};
+    return v;
 }
+__device__ __forceinline__ Parts<1> take_apart(u16x8 v) { return Parts<1>{__builtin_bit_cast(bf16x8, v)}; }
 template <typename E> constexpr int PARTS = sizeof(E) == 4 ? 3 : 1;
 
 // ---- dx: a wavefront keeps dl of 16 NT tokens in registers (KS steps of 32 experts) and goes over columns, 32 at a time, whose rows of W_g come from the
 // caches.  Matrix row 16 h + j of 32 stands for column 8 (j / 4) + 4 h + j % 4, so that a lane has eight neighbours.
 template <typename W, int KS, int NT, bool VEC>
-__global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* __restrict__ add, int T, int d, int E, int columns,
-                                                 float* __restrict__ dx) {
+__global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* add, int T, int d, int E, int columns,
+                                                 float* dx) {       // (dx may be add)
     const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
     const int t0 = ((int)blockIdx.x * (NTH / 64) + (int)(threadIdx.x >> 6)) * 16 * NT;
     if (t0 >= T) return;
@@ -152,31 +151,36 @@ __global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, c
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int s = 0; s < KS; ++s) g[n][s] = fetch8<VEC>(dl + (size_t)(t0 + n * 16 + l16) * E, E, s * 32 + lq * 8, t0 + n * 16 + l16 < T);
+        for (int s = 0; s < KS; ++s) g[n][s] = take_apart(fetch8<VEC>(dl + (size_t)(t0 + n * 16 + l16) * E, E, s * 32 + lq * 8, t0 + n * 16 + l16 < T));
     const int first = (int)blockIdx.y * columns, last = first + columns < d ? first + columns : d;
     for (int c0 = first; c0 < last; c0 += 32) {
-        f32x4 acc[NT][2] = {};
+        f32x4 acc[NT][2] = {}, old[NT][2] = {};
+        const int c = c0 + lq * 8;
+        if (add) {                                         // (on its way while the products are made)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+                if (t0 + n * 16 + l16 < T && c < d) {
+                    const f32x4* from = (const f32x4*)(add + (size_t)(t0 + n * 16 + l16) * d + c);
+                    old[n][0] = from[0];
+                    old[n][1] = from[1];
+                }
+        }
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int c = c0 + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
-                const Parts<PARTS<W>> m = fetch8<VEC>(w + (size_t)c * E, E, s * 32 + lq * 8, c < d);
+                const int col = c0 + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
+                const Parts<PARTS<W>> m = take_apart(fetch8<VEC>(w + (size_t)col * E, E, s * 32 + lq * 8, col < d));
 #pragma unroll
                 for (int n = 0; n < NT; ++n) multiply(m, g[n][s], acc[n][h]);
             }
-        const int c = c0 + lq * 8;
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             const int t = t0 + n * 16 + l16;
             if (t >= T || c >= d) continue;                // (d is a multiple of 8)
-            const size_t at = (size_t)t * d + c;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                f32x4 v = acc[n][h];
-                if (add) v += *(const f32x4*)(add + at + 4 * h);
-                *(f32x4*)(dx + at + 4 * h) = v;
-            }
+            f32x4* to = (f32x4*)(dx + (size_t)t * d + c);
+            to[0] = acc[n][0] + old[n][0];
+            to[1] = acc[n][1] + old[n][1];
         }
     }
 }
@@ -209,31 +213,27 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
     const int c0 = blockIdx.x * 64, e0 = blockIdx.y * 128, first = blockIdx.z * range, last = first + range < T ? first + range : T;
     // a thread has eight columns of x and, twice, eight experts of dl
     const int xr = tid >> 3, xc = (tid & 7) * 8, er = tid >> 4, ec = (tid & 15) * 8;
-    Parts<NX> gx;
-    Parts<3> ge[2];
+    // (two sets: what the step after the next needs is on its way)
+    decltype(fetch8<true>(x, 0, 0, false)) gx[2];
+    f32x8 ge[2][2];
     float db[8] = {};
-    auto fetch = [&](int t0) {
-        gx = fetch8<true>(x + (size_t)(t0 + xr) * d, d, c0 + xc, x && t0 + xr < last);
+    auto fetch = [&](int t0, int set) {
+        gx[set] = fetch8<true>(x + (size_t)(t0 + xr) * d, d, c0 + xc, x && t0 + xr < last);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ge[i] = fetch8<VEC>(dl + (size_t)(t0 + er + i * 16) * E, E, e0 + ec, t0 + er + i * 16 < last);
-    };
-    auto put = [&](int buf) {
-        unsigned char* to = lds + buf * BUF;
-        put8(to + panel_at(xr, xc), PANEL, gx);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            put8(to + NX * PANEL + (ec >> 6) * PANEL + panel_at(er + i * 16, ec & 63), 2 * PANEL, ge[i]);
-#pragma unroll
-            for (int c = 0; c < 8; ++c) db[c] += ((float)ge[i].p[2][c] + (float)ge[i].p[1][c]) + (float)ge[i].p[0][c];
-        }
+        for (int i = 0; i < 2; ++i) ge[set][i] = fetch8<VEC>(dl + (size_t)(t0 + er + i * 16) * E, E, e0 + ec, t0 + er + i * 16 < last);
     };
     f32x4 acc[4][2] = {};
-    fetch(first);
-    int buf = 0;
-    for (int t0 = first; t0 < last; t0 += TC, buf ^= 1) {
-        put(buf);
+    auto step = [&](int t0, int buf) {
+        unsigned char* to = lds + buf * BUF;
+        put8(to + panel_at(xr, xc), PANEL, take_apart(gx[buf]));
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            put8(to + NX * PANEL + (ec >> 6) * PANEL + panel_at(er + i * 16, ec & 63), 2 * PANEL, take_apart(ge[buf][i]));
+#pragma unroll
+            for (int c = 0; c < 8; ++c) db[c] += ge[buf][i][c];
+        }
+        fetch(t0 + 2 * TC, buf);                           // (behind the range: zeros)
         __syncthreads();                                   // (one is enough: whoever writes this buffer again has passed the next)
-        if (t0 + TC < last) fetch(t0 + TC);
         const unsigned char* from = lds + buf * BUF;
         Parts<3> e[2];
 #pragma unroll
@@ -248,6 +248,12 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
 #pragma unroll
             for (int b = 0; b < 2; ++b) multiply(e[b], v, acc[m][b]);
         }
+    };
+    fetch(first, 0);
+    fetch(first + TC, 1);
+    for (int t0 = first; t0 < last; t0 += 2 * TC) {
+        step(t0, 0);
+        if (t0 + TC < last) step(t0 + TC, 1);
     }
     // part: [range][d + 1][E], the last row for db
     float* to = part + (size_t)blockIdx.z * (d + 1) * E;
@@ -280,6 +286,7 @@ __global__ __launch_bounds__(NTH) void dw_sum_kernel(const float* __restrict__ p
     const size_t i = (size_t)blockIdx.x * NTH + threadIdx.x, n = (size_t)d * E, step = n + E;
     if (i >= step) return;
     float s = 0.f;
+#pragma unroll 8
     for (int r = 0; r < ranges; ++r) s += part[r * step + i];
     if (i < n) {
         if (dw) dw[i] = s;
@@ -301,14 +308,14 @@ int ranges_of(int T, int d, int E) {
 
 template <typename W> void launch_dx(const W* w, bool vec, const float* dl, const float* add, int T, int d, int E, float* dx, hipStream_t st) {
     // columns a work-group: as many as leave four wavefronts a SIMD, 32 at least
-    const int nt = E <= 128 ? 2 : 1, groups = (T + 64 * nt - 1) / (64 * nt);
+    const int nt = E <= 64 ? 2 : 1, groups = (T + 64 * nt - 1) / (64 * nt);
     int splits = (1024 + groups - 1) / groups;
     int columns = ((d + splits - 1) / splits + 31) / 32 * 32;
     splits = (d + columns - 1) / columns;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, splits), dim3(NTH), 0, st, dl, w, add, T, d, E, columns, dx); };
     if (E <= 32) vec ? go(dx_kernel<W, 1, 2, true>) : go(dx_kernel<W, 1, 2, false>);
     else if (E <= 64) vec ? go(dx_kernel<W, 2, 2, true>) : go(dx_kernel<W, 2, 2, false>);
-    else if (E <= 128) vec ? go(dx_kernel<W, 4, 2, true>) : go(dx_kernel<W, 4, 2, false>);
+    else if (E <= 128) vec ? go(dx_kernel<W, 4, 1, true>) : go(dx_kernel<W, 4, 1, false>);
     else vec ? go(dx_kernel<W, 8, 1, true>) : go(dx_kernel<W, 8, 1, false>);
 }
 
