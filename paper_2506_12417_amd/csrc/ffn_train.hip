@@ -62,6 +62,13 @@ __device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsign
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
 }
 
+// A store of 16 bytes.  Its data registers may not be written in the instruction behind it: with an offset in a scalar register the compiler takes
+// that for safe, and with two wavefronts a SIMD the last lanes' first values came out as what was written there next.
+__device__ __forceinline__ void store_b128(u32x4 v, __amdgpu_buffer_rsrc_t r, unsigned voff, unsigned soff) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, 0);
+    asm volatile("s_nop 1" : : "v"(v) : "memory");         // (they live until behind it)
+}
+
 // The lane's number, formed where it is used: held in a register over the loops it ends up in scratch memory, and the wait for its way back is one
 // for all loads under way.
 __device__ __forceinline__ int lane_now() {
@@ -359,8 +366,8 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
 #pragma unroll
                 for (int b = 0; b < 4; ++b)
                     if (f0 + b * 32 < a.N) {
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][0]), ro, at, (unsigned)(f0 + b * 32) * 4u, 0);
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][1]), ro, at + 16u, (unsigned)(f0 + b * 32) * 4u, 0);
+                        store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][0]), ro, at, (unsigned)(f0 + b * 32) * 4u);
+                        store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][1]), ro, at + 16u, (unsigned)(f0 + b * 32) * 4u);
                     }
             }
         }
@@ -411,7 +418,7 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                                 for (int c = 0; c < 8; ++c) v[i][c] *= g[c] * sigmoid(g[c]);
                             }
                             const u32x4 w = {half_bits(v[i][0], v[i][1]), half_bits(v[i][2], v[i][3]), half_bits(v[i][4], v[i][5]), half_bits(v[i][6], v[i][7])};
-                            __builtin_amdgcn_raw_buffer_store_b128(w, rh, row * F * 2u + (unsigned)lq * 16u, (unsigned)((SW ? f0 / 2 : zc) + i * 32) * 2u, 0);
+                            store_b128(w, rh, row * F * 2u + (unsigned)lq * 16u, (unsigned)((SW ? f0 / 2 : zc) + i * 32) * 2u);
                         }
                     }
                 }
@@ -497,9 +504,9 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                     wh[c] = gate[g] * h;
                 }
                 const unsigned col = (unsigned)(f0 + b * 32) * 2u;
-                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(wh), rw, wo, col, 0);
-                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz0), rz, zo, col, 0);
-                if (SW) __builtin_amdgcn_raw_buffer_store_b128(to_bf16(dz1), rz, zo, col + F * 2u, 0);
+                store_b128(to_bf16(wh), rw, wo, col);
+                store_b128(to_bf16(dz0), rz, zo, col);
+                if (SW) store_b128(to_bf16(dz1), rz, zo, col + F * 2u);
                 __builtin_amdgcn_sched_barrier(0);
             }
             dgate = quarter_sum(dgate);
@@ -602,9 +609,15 @@ struct TnArgs {
     void *dwa, *dwb, *dwo;
 };
 
-constexpr int TN_BUF = 32 * 512;   // LDS: an operand's 32 rows of 256 columns; the N operand's four buffers, then the M operand's
-constexpr int TN_IDS = 8 * TN_BUF; // behind them source rows: [8 halves][4 wavefronts][64 lanes]
-constexpr size_t TN_SMEM = TN_IDS + 8 * 4 * 256;
+// TS: the side of a tile of dW, 256 (a work-group a CU) or 128 (two).
+template <int TS> struct Tn {
+    static constexpr int PANELS = TS / 64, BLOCKS = TS / 32;          // of 64 columns; of 16 columns, a wavefront
+    static constexpr int BUF = 32 * TS * 2;                // LDS: an operand's 32 rows; the N operand's four buffers, then the M operand's
+    static constexpr int IDS = 8 * BUF;                    // behind them source rows: [8 halves][4 wavefronts][64 lanes]
+    static constexpr int LOADS = 2 * PANELS;               // of a thread, for a half
+    static constexpr int GROUPS = BLOCKS * BLOCKS / 4;     // of four matrix instructions a step
+    static constexpr size_t SMEM = IDS + 8 * 4 * 256;
+};
 
 struct TnItem {
     int e, row0, n, m0, n0, M, N;
@@ -615,7 +628,7 @@ struct TnItem {
 
 struct TnShape { int ta, tb, per_mat, per_expert; };       // tiles along d and F
 
-template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, const TnShape& sh, int item) {
+template <int TS, int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, const TnShape& sh, int item) {
     TnItem it;
     it.e = sgpr(item / sh.per_expert);
     const int local = item - it.e * sh.per_expert, mat = local / sh.per_mat, at = local - mat * sh.per_mat;
@@ -626,8 +639,8 @@ template <int ES> __device__ __forceinline__ TnItem tn_locate(const TnArgs& a, c
     const int grp = at / (GROUP_ROWS * tn), rem = at - grp * GROUP_ROWS * tn;
     const int gs = tm - grp * GROUP_ROWS < GROUP_ROWS ? tm - grp * GROUP_ROWS : GROUP_ROWS;
     const int cb = rem / gs;
-    it.n0 = sgpr(cb * 256);
-    it.m0 = sgpr((grp * GROUP_ROWS + rem - cb * gs) * 256);
+    it.n0 = sgpr(cb * TS);
+    it.m0 = sgpr((grp * GROUP_ROWS + rem - cb * gs) * TS);
     it.row0 = sgpr(a.offsets[it.e]);
     it.n = sgpr(a.offsets[it.e + 1]) - it.row0;
     it.zc = mat == 1 ? a.F : 0;
@@ -672,9 +685,9 @@ struct TnAhead {
 };
 __device__ __forceinline__ unsigned rows_of_stage(int left) { return (unsigned)(left < 0 ? 0 : left < 64 ? left : 64); }
 // Turns to the first item with rows from L.item on.
-template <int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
+template <int TS, int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
     for (; L.item < w.end; L.item += w.stride) {
-        const TnItem it = tn_locate<ES>(a, w.sh, L.item);
+        const TnItem it = tn_locate<TS, ES>(a, w.sh, L.item);
         if (it.n == 0) continue;
         const int ld = it.out ? a.F : a.Z;
         L.left = it.n;
@@ -685,8 +698,8 @@ template <int ES> __device__ __forceinline__ void tn_turn(const TnArgs& a, const
         L.cd = (unsigned)(it.out ? it.m0 : it.n0 + it.zc) * 2u;
         L.cg = (unsigned)(it.out ? it.n0 : it.m0) * 2u;
         const unsigned to = w.ring + (unsigned)(w.wave * 1024);
-        L.to_d = to + (it.out ? 4 * TN_BUF : 0);
-        L.to_g = to + (it.out ? 0 : 4 * TN_BUF);
+        L.to_d = to + (it.out ? 4 * Tn<TS>::BUF : 0);
+        L.to_g = to + (it.out ? 0 : 4 * Tn<TS>::BUF);
         return;
     }
     L.left = 0;                                            // past the last item: nothing is fetched, the schedule stays
@@ -701,9 +714,9 @@ __device__ __forceinline__ void tn_step_on(TnLoads& L) {
     L.rd[1] = (unsigned)(at >> 32);
     L.rd[2] = rows_of_stage(L.left) * L.ld_d;
 }
-template <int ES> __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
+template <int TS, int ES> __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L) {
     if (L.item < w.end) L.item += w.stride;
-    tn_turn<ES>(a, w, th, L);
+    tn_turn<TS, ES>(a, w, th, L);
 }
 __device__ __forceinline__ void tn_turn(const TnArgs& a, const TnWork& w, TnAhead& p) {
     for (; p.item < w.end; p.item += w.stride) {
@@ -727,8 +740,8 @@ __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, T
     tn_turn(a, w, p);
 }
 // Every lane's source row of half h of a stage, into one of eight tables of its wavefront's (behind the expert's last row: zeros).
-__device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const TnAhead& p, int h, int slot) {
-    load_to_lds4(p.src, w.ring + (unsigned)(TN_IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
+template <int TS> __device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const TnAhead& p, int h, int slot) {
+    load_to_lds4(p.src, w.ring + (unsigned)(Tn<TS>::IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
 }
 // Its offset.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
 __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
@@ -736,28 +749,29 @@ __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
     return __builtin_elementwise_add_sat(~*(lds_word*)(uintptr_t)(th.ids() + (unsigned)slot * 1024u), th.piece());
 }
 // load Q of half H: the direct operand's first
-template <int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, unsigned row) {
-    constexpr int p = Q & 3;
-    if constexpr (Q < 4) load_to_lds(L.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
+template <int TS, int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, unsigned row) {
+    constexpr int N = Tn<TS>::PANELS, p = Q % N;
+    if constexpr (Q < N) load_to_lds(L.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
     else load_to_lds(L.rg, L.to_g + buf_at, p * 4096, row, L.cg + (unsigned)p * 128u, 0u);
 }
-template <int H, int Q> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, unsigned row) {
-    if constexpr (Q < 8) {
-        tn_load<H, Q>(L, buf_at, row);
-        tn_loads<H, Q + 1>(L, buf_at, row);
+template <int TS, int H, int FROM, int TO> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, unsigned row) {
+    if constexpr (FROM < TO) {
+        tn_load<TS, H, FROM>(L, buf_at, row);
+        tn_loads<TS, H, FROM + 1, TO>(L, buf_at, row);
     }
 }
 
-typedef f32x4 TnAcc[8][8];         // [16 rows of dW][16 columns of dW]
-struct TnFrags { s16x4 n[8][2], m[8][2]; };
+template <int TS> using TnAcc = f32x4[Tn<TS>::BLOCKS][Tn<TS>::BLOCKS];         // [16 rows of dW][16 columns of dW]
+template <int TS> struct TnFrags { s16x4 n[Tn<TS>::BLOCKS][2], m[Tn<TS>::BLOCKS][2]; };
 
-// Read j (0..31) of the half in buffer `half` of two: four terms of a column of a 16-column block.  n[c]: this lane's place in block c of the N operand's
+// Read j of the half in buffer `half` of two: four terms of a column of a 16-column block.  n[c]: this lane's place in block c of the N operand's
 // first panel (pair of buffers included); the M operand's lie a wave-uniform distance behind.
 struct TnLane { unsigned n[4], to_m; };
-__device__ __forceinline__ void tn_read(TnFrags& fr, const TnLane& at, int half, int j) {
-    const int c = (j & 15) >> 1, i = j & 1, off = half * TN_BUF + (c >> 2) * 4096 + i * 2048;
+template <int TS> __device__ __forceinline__ void tn_read(TnFrags<TS>& fr, const TnLane& at, int half, int j) {
+    constexpr int B = Tn<TS>::BLOCKS;
+    const int c = j % (2 * B) >> 1, i = j & 1, off = half * Tn<TS>::BUF + (c >> 2) * 4096 + i * 2048;
     typedef __attribute__((address_space(3))) unsigned char lds_byte;
-    if (j < 16) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c & 3] + off));
+    if (j < 2 * B) fr.n[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)at.n[c & 3] + off));
     else fr.m[c][i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)((lds_byte*)(uintptr_t)(at.n[c & 3] + at.to_m) + off));
 }
 __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
@@ -769,75 +783,77 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
 // Step S multiplies the half in buffer 2 pair + S (its fragments are in registers), reads the next one's fragments and issues the loads of the fourth one
 // behind it into the same buffer, which everybody has read.  What moves the places on stands between the multiplications: a wavefront has
 // its SIMD for itself, an instruction that none of them covers costs its whole time.
-template <int S, int t>
-__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, const TnLane& ln, int pair, int slot, unsigned& row, TnAcc& acc,
-                                          TnFrags (&fr)[2]) {
-    if constexpr (t < 16) {
-        constexpr int m = t >> 1, n4 = (t & 1) * 4;
-        constexpr int Q = t < 12 && t % 3 != 2 ? t / 3 * 2 + t % 3 : -1;
-        if constexpr (t == 1) row = tn_row(th, (slot + 4) & 7);
-        if constexpr (t == 13) tn_fetch_ids(w, th, ahead, S, slot);
-        if constexpr (S == 1 && t == 14) tn_step_on(L);
-        if constexpr (S == 1 && t == 15) tn_step_on(ahead);
+template <int TS, int S, int t>
+__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, const TnLane& ln, int pair, int slot, unsigned& row, TnAcc<TS>& acc,
+                                          TnFrags<TS> (&fr)[2]) {
+    constexpr int B = Tn<TS>::BLOCKS, G = Tn<TS>::GROUPS, READS = 4 * B, SPREAD = 3 * G / 4, LOADS = Tn<TS>::LOADS;
+    if constexpr (t < G) {
+        constexpr int m = t / (B / 4), n4 = t % (B / 4) * 4;
+        if constexpr (t == 0) row = tn_row(th, (slot + 4) & 7);
+        if constexpr (t == G - 1) tn_fetch_ids<TS>(w, th, ahead, S, slot);
+        static_assert(SPREAD <= G - 1, "the places move on behind the loads");
+        if constexpr (S == 1 && t == (G > 4 ? G - 2 : G - 1)) tn_step_on(L);
+        if constexpr (S == 1 && t == G - 1) tn_step_on(ahead);
 #pragma unroll
         for (int n = n4; n < n4 + 4; ++n)
             acc[m][n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(tn_frag(fr[S].n[n]), tn_frag(fr[S].m[m]), acc[m][n], 0, 0, 0);
-        if (t < 12) {
+        if (t < SPREAD) {
 #pragma unroll
-            for (int j = t * 32 / 12; j < (t + 1) * 32 / 12; ++j) tn_read(fr[S ^ 1], ln, S ^ 1, j);
+            for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) tn_read<TS>(fr[S ^ 1], ln, S ^ 1, j);
         }
-        if constexpr (Q >= 0) tn_load<S, Q>(L, (unsigned)((pair * 2 + S) * TN_BUF), row);
+        if constexpr (t < SPREAD) tn_loads<TS, S, t * LOADS / SPREAD, (t + 1) * LOADS / SPREAD>(L, (unsigned)((pair * 2 + S) * Tn<TS>::BUF), row);
         __builtin_amdgcn_sched_barrier(0);
-        tn_groups<S, t + 1>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
+        tn_groups<TS, S, t + 1>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
     }
 }
-template <int ES, int S>
-__device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int& slot, TnAcc& acc, TnFrags (&fr)[2],
+template <int TS, int ES, int S>
+__device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int& slot, TnAcc<TS>& acc, TnFrags<TS> (&fr)[2],
                                         int stores) {
     const int pair = (slot >> 1) & 1;
     if (S == 1) {
 #pragma unroll
-        for (int c = 0; c < 4; ++c) ln.n[c] ^= 2 * TN_BUF;
+        for (int c = 0; c < 4; ++c) ln.n[c] ^= 2 * Tn<TS>::BUF;
     }
     unsigned row;
-    tn_groups<S, 0>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
+    tn_groups<TS, S, 0>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
     slot = (slot + 1) & 7;
-    // everybody has read the next half, and the one behind it is there: what was issued before the last two steps (eight loads and a fetch of source
+    // everybody has read the next half, and the one behind it is there: what was issued before the last two steps (their loads and a fetch of source
     // rows each) and an item's stores
     MOE_WAIT_LGKMCNT(0);
-    wait_landed<18>(stores);
+    wait_landed<2 * (Tn<TS>::LOADS + 1)>(stores);
     wg_barrier();
     if (S == 1) {
-        if (L.left <= 0) tn_next_item<ES>(a, w, th, L);
+        if (L.left <= 0) tn_next_item<TS, ES>(a, w, th, L);
         if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
 }
 
-template <int ES>
-__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int KT, int& slot, TnAcc& acc, TnFrags (&fr)[2],
-                                            int stores) {
-    tn_step<ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
-    tn_step<ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
+template <int TS, int ES>
+__device__ __forceinline__ void tn_contract(const TnArgs& a, const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, TnLane& ln, int KT, int& slot, TnAcc<TS>& acc,
+                                            TnFrags<TS> (&fr)[2], int stores) {
+    tn_step<TS, ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
+    tn_step<TS, ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, stores);
 #pragma clang loop unroll(disable)
     for (int kt = 1; kt < KT; ++kt) {
-        tn_step<ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
-        tn_step<ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
+        tn_step<TS, ES, 0>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
+        tn_step<TS, ES, 1>(a, w, th, L, ahead, ln, slot, acc, fr, 0);
     }
 }
 
-template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const TnItem& it, TnAcc& acc, int wm, int wn) {
+template <int TS, typename O, bool ADD> __device__ __forceinline__ void tn_finish(const TnItem& it, TnAcc<TS>& acc, int wm, int wn) {
     constexpr unsigned ES = sizeof(O);
     const int lane = lane_now(), l16 = lane & 15, lq = lane >> 4;
-    const int c0 = it.n0 + wm * 128;
+    constexpr int B = Tn<TS>::BLOCKS;
+    const int c0 = it.n0 + wm * (TS / 2);
     if (c0 >= it.N) return;
     const unsigned ld = (unsigned)it.N * ES;
-    const __amdgpu_buffer_rsrc_t ro = make_rsrc((unsigned char*)it.dw + (size_t)it.m0 * ld, (unsigned)(it.M - it.m0 < 256 ? it.M - it.m0 : 256) * ld);
+    const __amdgpu_buffer_rsrc_t ro = make_rsrc((unsigned char*)it.dw + (size_t)it.m0 * ld, (unsigned)(it.M - it.m0 < TS ? it.M - it.m0 : TS) * ld);
 #pragma unroll
-    for (int m = 0; m < 8; ++m) {
-        const unsigned row = (unsigned)(wn * 128 + m * 16 + l16) * ld;
+    for (int m = 0; m < B; ++m) {
+        const unsigned row = (unsigned)(wn * (TS / 2) + m * 16 + l16) * ld;
         __builtin_amdgcn_sched_barrier(0);                 // (16 rows at a time: there are no registers for more)
 #pragma unroll
-        for (int n = 0; n < 8; n += 2) {
+        for (int n = 0; n < B; n += 2) {
             if (c0 + n * 16 >= it.N) continue;
             const unsigned col = (unsigned)(c0 + n * 16) * ES;
             if constexpr (ES == 4) {
@@ -845,7 +861,7 @@ template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const 
                 for (int i = 0; i < 2; ++i) {
                     f32x4 v = acc[m][n + i];
                     if (ADD) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0));
-                    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0);
+                    store_b128(__builtin_bit_cast(u32x4, v), ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u);
                 }
             } else {
                 // a lane has columns 4 lq + r of two blocks of 16; lanes 16 apart exchange them, so that each has eight neighbours:
@@ -863,22 +879,22 @@ template <typename O, bool ADD> __device__ __forceinline__ void tn_finish(const 
 #pragma unroll
                     for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(i & 1 ? old[i >> 1] & 0xffff0000u : old[i >> 1] << 16);
                 }
-                __builtin_amdgcn_raw_buffer_store_b128(to_bf16(v), ro, at, col, 0);
+                store_b128(to_bf16(v), ro, at, col);
             }
         }
     }
 }
 
-template <typename O, bool ADD>
-__global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
+template <int TS, typename O, bool ADD>
+__global__ __launch_bounds__(NTH, TS == 256 ? 1 : 2) void gemm_tn_kernel(const TnArgs a) {
 #ifdef __HIP_DEVICE_COMPILE__
     extern __shared__ __attribute__((aligned(1024))) unsigned char ring[];
     constexpr int ES = sizeof(O);
     const int tid = threadIdx.x, lane = tid & 63, wave = sgpr(tid >> 6);
     const int wm = wave & 1, wn = wave >> 1, l16 = lane & 15, lq = lane >> 4;
     TnWork w;
-    w.sh.ta = (a.d + 255) / 256;
-    w.sh.tb = (a.F + 255) / 256;
+    w.sh.ta = (a.d + TS - 1) / TS;
+    w.sh.tb = (a.F + TS - 1) / TS;
     w.sh.per_mat = w.sh.ta * w.sh.tb;
     w.sh.per_expert = w.sh.per_mat * a.mats;
     // An item costs its stages and the store of its tile (about six stages' time).  The XCDs take neighbouring runs of equal cost.
@@ -900,63 +916,64 @@ __global__ __launch_bounds__(NTH) void gemm_tn_kernel(const TnArgs a) {
     TnLane ln;
     const int row = lq * 4 + (l16 >> 2);                   // lane (l16, lq) reads from rows 4 lq + l16 / 4 of sixteen
 #pragma unroll
-    for (int c = 0; c < 4; ++c) ln.n[c] = w.ring + (unsigned)(wm * 8192 + row * 128 + (l16 & 3) * 8) + (unsigned)((c ^ (row >> 1 & 3)) * 32);
-    ln.to_m = (unsigned)sgpr(4 * TN_BUF + (wn - wm) * 8192);
+    for (int c = 0; c < 4; ++c) ln.n[c] = w.ring + (unsigned)(wm * (TS * 32) + row * 128 + (l16 & 3) * 8) + (unsigned)((c ^ (row >> 1 & 3)) * 32);
+    ln.to_m = (unsigned)sgpr(4 * Tn<TS>::BUF + (wn - wm) * (TS * 32));
 
     TnThread th;
     th.wave = wave;
-    th.tables = w.ring + (unsigned)(TN_IDS + wave * 256);
+    th.tables = w.ring + (unsigned)(Tn<TS>::IDS + wave * 256);
 
     // two stages on their way, the source rows of the two behind them
     TnLoads L;
     L.item = first;
     L.vd = L.cd = L.cg = L.to_d = L.to_g = 0u;
-    tn_turn<ES>(a, w, th, L);
+    tn_turn<TS, ES>(a, w, th, L);
     TnAhead ahead;
     ahead.item = first;
     tn_turn(a, w, ahead);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        tn_fetch_ids(w, th, ahead, 0, 2 * st);
-        tn_fetch_ids(w, th, ahead, 1, 2 * st + 1);
+        tn_fetch_ids<TS>(w, th, ahead, 0, 2 * st);
+        tn_fetch_ids<TS>(w, th, ahead, 1, 2 * st + 1);
         tn_step_on(ahead);
         if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
     MOE_WAIT_VMCNT(0);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        tn_loads<0, 0>(L, (unsigned)(2 * st * TN_BUF), tn_row(th, 2 * st));
-        tn_fetch_ids(w, th, ahead, 0, 4 + 2 * st);
-        tn_loads<1, 0>(L, (unsigned)((2 * st + 1) * TN_BUF), tn_row(th, 2 * st + 1));
-        tn_fetch_ids(w, th, ahead, 1, 5 + 2 * st);
+        tn_loads<TS, 0, 0, Tn<TS>::LOADS>(L, (unsigned)(2 * st * Tn<TS>::BUF), tn_row(th, 2 * st));
+        tn_fetch_ids<TS>(w, th, ahead, 0, 4 + 2 * st);
+        tn_loads<TS, 1, 0, Tn<TS>::LOADS>(L, (unsigned)((2 * st + 1) * Tn<TS>::BUF), tn_row(th, 2 * st + 1));
+        tn_fetch_ids<TS>(w, th, ahead, 1, 5 + 2 * st);
         tn_step_on(L);
-        if (L.left <= 0) tn_next_item<ES>(a, w, th, L);
+        if (L.left <= 0) tn_next_item<TS, ES>(a, w, th, L);
         tn_step_on(ahead);
         if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
-    MOE_WAIT_VMCNT(18);
+    MOE_WAIT_VMCNT(2 * (Tn<TS>::LOADS + 1));
     wg_barrier();
-    TnAcc acc;
-    TnFrags fr[2];
+    TnAcc<TS> acc;
+    TnFrags<TS> fr[2];
 #pragma unroll
-    for (int j = 0; j < 32; ++j) tn_read(fr[0], ln, 0, j);
+    for (int j = 0; j < 4 * Tn<TS>::BLOCKS; ++j) tn_read<TS>(fr[0], ln, 0, j);
     int slot = 0, stores = 0;
     for (int item = first; item < w.end; item += w.stride) {
-        const TnItem it = tn_locate<ES>(a, w.sh, item);
+        const TnItem it = tn_locate<TS, ES>(a, w.sh, item);
         const int KT = (it.n + 63) / 64;
         if (ADD && KT == 0) continue;
-        int n_on = (it.N - it.n0 - wm * 128) / 16;         // 16-column blocks of this wavefront inside the matrix
-        n_on = n_on < 0 ? 0 : n_on > 8 ? 8 : n_on;
+        constexpr int B = Tn<TS>::BLOCKS;
+        int n_on = (it.N - it.n0 - wm * (TS / 2)) / 16;    // 16-column blocks of this wavefront inside the matrix
+        n_on = n_on < 0 ? 0 : n_on > B ? B : n_on;
 #pragma unroll
-        for (int m = 0; m < 8; ++m)
+        for (int m = 0; m < B; ++m)
 #pragma unroll
-            for (int n = 0; n < 8; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int n = 0; n < B; ++n) acc[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
         if (KT > 0) {
-            tn_contract<ES>(a, w, th, L, ahead, ln, KT, slot, acc, fr, stores);
+            tn_contract<TS, ES>(a, w, th, L, ahead, ln, KT, slot, acc, fr, stores);
             stores = 0;
         }
-        tn_finish<O, ADD>(it, acc, wm, wn);
-        stores += 4 * n_on * (ES / 2);                     // store instructions just issued
+        tn_finish<TS, O, ADD>(it, acc, wm, wn);
+        stores += B / 2 * n_on * (ES / 2);                 // store instructions just issued
     }
     MOE_WAIT_VMCNT(0);                                      // (the trailing empty loads still target this LDS)
 #endif
@@ -1000,20 +1017,30 @@ template <int KIND, int TR> int launch_nt(const NtArgs& a, hipStream_t st) {
     MOE_CHECK_LAUNCH("moe_grouped_ffn (training, over rows)");
     return MOE_OK;
 }
-// Rows per tile by the mean rows of an expert.
+// Rows per tile by the mean rows of an expert.  Measured, us by tiles of 64 / 128 / 256 rows: first products that are finished in place (KEEP, HID), mean 34 of
+// 2048 x 1408 152 / 166 / 219, mean 546 (32768 rows) 417 / 326 / 382, mean 2048 of 4096 x 14336 3225 / 2188 / 2256: three stages in LDS let an item's
+// stores go on longer.  Plain results (DX), mean 16 22 / 25 / 43, mean 34 169 / 156 / 187, mean 136 226 / 196 / 266, mean 546 625 / 470 / 460,
+// mean 2048 of 4096 x 14336 5675 / 3794 / 3640, of 512 x 512 (64 tiles of 256 rows x 256) 26 / 22 / 33.
 template <int KIND> int launch_nt_rows(const NtArgs& a, int A, hipStream_t st) {
     const long long mean = (A + a.E - 1) / a.E;
-    if (mean <= 64) return launch_nt<KIND, 64>(a, st);
-    if (mean < 512) return launch_nt<KIND, 128>(a, st);
-    return launch_nt<KIND, 256>(a, st);
+    if (mean <= (KIND == DX ? 32 : 64)) return launch_nt<KIND, 64>(a, st);
+    if constexpr (KIND == DX)
+        if (mean >= 512 && (long long)A / 256 * ((a.N + 255) / 256) >= 2 * MOE_GEMM_GRID) return launch_nt<KIND, 256>(a, st);
+    return launch_nt<KIND, 128>(a, st);
 }
-template <typename O, bool ADD> int launch_tn(const TnArgs& a, hipStream_t st) {
-    auto kern = gemm_tn_kernel<O, ADD>;
-    const int ok = set_smem(kern, TN_SMEM);
+template <int TS, typename O, bool ADD> int launch_tn(const TnArgs& a, hipStream_t st) {
+    auto kern = gemm_tn_kernel<TS, O, ADD>;
+    const int ok = set_smem(kern, Tn<TS>::SMEM);
     if (ok != MOE_OK) return ok;
-    hipLaunchKernelGGL(kern, dim3(MOE_GEMM_GRID), dim3(NTH), TN_SMEM, st, a);
+    hipLaunchKernelGGL(kern, dim3(MOE_GEMM_GRID * (TS == 256 ? 1 : 2)), dim3(NTH), Tn<TS>::SMEM, st, a);
     MOE_CHECK_LAUNCH("moe_grouped_ffn_backward (over the rows)");
     return MOE_OK;
+}
+// Tiles of 128 where those of 256 would leave CUs without one: four experts of 512 x 512 over 8192 rows 36 us instead of 67, one of 512 x 1024 88 instead of
+// 174.  Elsewhere they fetch twice the bytes for a product: 128 experts of 768 x 3072 over 16384 rows 662 instead of 564.
+template <typename O, bool ADD> int launch_tn_tile(const TnArgs& a, hipStream_t st) {
+    const long long tiles = (long long)a.E * a.mats * ((a.d + 255) / 256) * ((a.F + 255) / 256);
+    return tiles <= MOE_GEMM_GRID ? launch_tn<128, O, ADD>(a, st) : launch_tn<256, O, ADD>(a, st);
 }
 
 int check_shape(const char* what, int T, int d, int F, int E, int k, moe_act act, moe_dtype dt) {
@@ -1026,7 +1053,7 @@ int check_shape(const char* what, int T, int d, int F, int E, int k, moe_act act
     MOE_REQUIRE((long long)T * d * 2 < limit && 256ll * d * 4 < limit && 256ll * F * 4 < limit, MOE_ERR_UNSUPPORTED, "%s: T=%d rows of d=%d, F=%d pass 4 GiB", what, T, d, F);
     MOE_REQUIRE((long long)T * k < (1ll << 30), MOE_ERR_UNSUPPORTED, "%s: T=%d k=%d", what, T, k);
     MOE_REQUIRE(((long long)T * k / 64 + E) * ((F + 63) / 64) * 2 < (1ll << 30) && ((long long)T * k / 64 + E) * ((d + 63) / 64) < (1ll << 30) &&
-                    (long long)E * ((d + 255) / 256) * ((F + 255) / 256) * 3 < (1ll << 30),
+                    (long long)E * ((d + 127) / 128) * ((F + 127) / 128) * 3 < (1ll << 30),
                 MOE_ERR_UNSUPPORTED, "%s: T=%d k=%d E=%d d=%d F=%d make too many tiles", what, T, k, E, d, F);
     return MOE_OK;
 }
@@ -1164,8 +1191,8 @@ extern "C" int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const v
         t.dwa = dw_a;
         t.dwb = dw_b;
         t.dwo = dw_o;
-        if (dw_dt == MOE_F32) ok = accumulate ? launch_tn<float, true>(t, st) : launch_tn<float, false>(t, st);
-        else ok = accumulate ? launch_tn<uint16_t, true>(t, st) : launch_tn<uint16_t, false>(t, st);
+        if (dw_dt == MOE_F32) ok = accumulate ? launch_tn_tile<float, true>(t, st) : launch_tn_tile<float, false>(t, st);
+        else ok = accumulate ? launch_tn_tile<uint16_t, true>(t, st) : launch_tn_tile<uint16_t, false>(t, st);
         if (ok != MOE_OK) return ok;
     }
     return MOE_OK;
