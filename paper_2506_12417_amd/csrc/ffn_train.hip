@@ -859,7 +859,13 @@ template <int TS, typename O, bool ADD> __device__ __forceinline__ void tn_finis
             if constexpr (ES == 4) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    f32x4 v = acc[m][n + i];
+                    f32x4 v;                               // (a copy: the sums stay where the matrix instruction wants them)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float x = acc[m][n + i][r];
+                        asm volatile("" : "+v"(x));
+                        v[r] = x;
+                    }
                     if (ADD) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0));
                     store_b128(__builtin_bit_cast(u32x4, v), ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u);
                 }
