@@ -548,8 +548,8 @@ MOE_API int moe_permute_backward(const float* dx_perm, const int32_t* inv_perm, 
  *   dlogits [T,E] fp32 out      dx_add [T,d] fp32 or NULL      dx [T,d] fp32 out or NULL (may be dx_add)
  *   dw_gate [d,E] fp32 out or NULL      dbias [E] fp32 out or NULL
  *   ws: moe_workspace_bytes(MOE_OP_ROUTE_BACKWARD, T, d, 0, E, 0, dt) bytes; none and NULL without dw_gate and dbias
- * Both products are those of the fp32 values (summed in fp32).  A token with an expert_idx outside [0,E) has a row of NaN.
- * Requires what moe_route_topk requires, x, dx and dx_add aligned to 16 bytes, T <= 64 * 65535.  T = 0 sets dw_gate and dbias to zero.
+ * Both products are those of the fp32 values (summed in fp32; an infinity among these makes NaN of what it takes part in).  A token with an expert_idx outside [0,E) has a row of NaN.
+ * Requires what moe_route_topk requires, x, dx and dx_add aligned to 16 bytes, T <= 64 * 65535, d <= 2^20.  T = 0 sets dw_gate and dbias to zero.
  */
 MOE_API int moe_route_topk_backward(const float* dgate_w, const float* gate_w, const int32_t* expert_idx, const float* logits,
                                     const float* dlogits_add, const void* x, const void* w_gate, int T, int d, int E, int k,

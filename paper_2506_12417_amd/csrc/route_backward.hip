@@ -11,20 +11,27 @@
 //
 #include "common.h"
 #include "gemm_util.h"
+#include "lanes.h"
 
 namespace {
 
 constexpr int NTH = 256;
 
-__device__ __forceinline__ float shfl_sum(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
-    return v;
+// Sum and largest over the lanes: in rows of sixteen by exchanges, the rows' through scalar registers.
+__device__ __forceinline__ float lane_f32(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+__device__ __forceinline__ float wave_sum(float v) {
+    v += dpp_xchg<0>(v);
+    v += dpp_xchg<1>(v);
+    v += dpp_xchg<2>(v);
+    v += dpp_xchg<3>(v);
+    return (lane_f32(v, 0) + lane_f32(v, 16)) + (lane_f32(v, 32) + lane_f32(v, 48));
 }
-__device__ __forceinline__ float shfl_max(float v) {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) v = fmaxf(v, __shfl_xor(v, o));
-    return v;
+__device__ __forceinline__ float wave_max(float v) {
+    v = fmaxf(v, dpp_xchg<0>(v));
+    v = fmaxf(v, dpp_xchg<1>(v));
+    v = fmaxf(v, dpp_xchg<2>(v));
+    v = fmaxf(v, dpp_xchg<3>(v));
+    return fmaxf(fmaxf(lane_f32(v, 0), lane_f32(v, 16)), fmaxf(lane_f32(v, 32), lane_f32(v, 48)));
 }
 
 // ---- dl: a wavefront has a token, a lane up to four experts
@@ -41,7 +48,7 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
         e_of = idx[(size_t)t * k + lane];
     }
     const bool lost = __ballot(lane < k && (e_of < 0 || e_of >= E)) != 0;      // (a token whose logits are NaN)
-    const float D = shfl_sum(g * dg);
+    const float D = wave_sum(g * dg);
     float p[4], v[4];
     if (!renorm) {
         float most = -__builtin_inff(), sum = 0.f;
@@ -51,13 +58,13 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
             p[i] = e < E ? logits[(size_t)t * E + e] : -__builtin_inff();
             most = fmaxf(most, p[i]);
         }
-        most = shfl_max(most);
+        most = wave_max(most);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             p[i] = i * 64 + lane < E ? expf(p[i] - most) : 0.f;
             sum += p[i];
         }
-        sum = shfl_sum(sum);
+        sum = wave_sum(sum);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             p[i] /= sum;
@@ -68,8 +75,8 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
         for (int i = 0; i < 4; ++i) v[i] = p[i] = 0.f;
     }
     for (int j = 0; j < k; ++j) {
-        const int e = __shfl(e_of, j);
-        const float a = renorm ? __shfl(g, j) * (__shfl(dg, j) - D) : __shfl(dg, j);
+        const int e = __builtin_amdgcn_readlane(e_of, j);
+        const float a = renorm ? lane_f32(g, j) * (lane_f32(dg, j) - D) : lane_f32(dg, j);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (e == i * 64 + lane) v[i] += a;
@@ -94,11 +101,9 @@ __device__ __forceinline__ Parts<3> take_apart(__attribute__((ext_vector_type(8)
         const __bf16 hi = (__bf16)v[i];
         const float rest = v[i] - (float)hi;
         const __bf16 mid = (__bf16)rest;
-        // (an infinity or a NaN is in the first part: the others would make NaN of an infinity's products)
-        const bool plain = __builtin_fabsf(v[i]) < __builtin_inff() && __builtin_fabsf((float)hi) < __builtin_inff();
         r.p[0][i] = hi;
-        r.p[1][i] = plain ? mid : (__bf16)0.f;
-        r.p[2][i] = plain ? (__bf16)(rest - (float)mid) : (__bf16)0.f;
+        r.p[1][i] = mid;
+        r.p[2][i] = (__bf16)(rest - (float)mid);
     }
     return r;
 }
@@ -110,79 +115,115 @@ template <int NA, int NB> __device__ __forceinline__ void multiply(const Parts<N
         for (int i = 0; i < NA; ++i)
             if (s - i >= 0 && s - i < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
 }
-// Eight neighbours of a row of n values from column c on, zeros behind it.  VEC: n is a multiple of 8 and the rows are aligned.
+// Rows that a work-group reads, through a buffer descriptor: what is not `on`, or lies behind a row's n values, reads as zero without a branch (behind
+// branches with loads in them the compiler waits for all that is under way).  Eight neighbours of row r from column c on.  VEC: n is a multiple
+// of 8 and the rows are aligned.
 typedef __attribute__((ext_vector_type(8))) float f32x8;
 typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
-template <bool VEC> __device__ __forceinline__ f32x8 fetch8(const float* row, int n, int c, bool on) {
-    f32x8 v = {};
-    if (VEC) {
-        if (on && c < n) {
-            const f32x4 a = ((const f32x4*)(row + c))[0], b = ((const f32x4*)(row + c))[1];
-            v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
+typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
+constexpr unsigned NOWHERE = 0xFFFFFF00u;
+template <bool VEC> __device__ __forceinline__ f32x8 fetch8(const float*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
+    const unsigned at = (r * (unsigned)n + (unsigned)c) * 4u;
+    f32x8 v;
+    if constexpr (VEC) {
+        const unsigned o = on && c < n ? at : NOWHERE;
+        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, o, 0, 0)), b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, o + 16, 0, 0));
+        v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : 0.f;
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, on && c + i < n ? at + 4u * i : NOWHERE, 0, 0));
     }
     return v;
 }
-template <bool VEC> __device__ __forceinline__ u16x8 fetch8(const uint16_t* row, int n, int c, bool on) {
-    u16x8 v = {};
-    if (VEC) {
-        if (on && c < n) v = *(const u16x8*)(row + c);
+template <bool VEC> __device__ __forceinline__ u16x8 fetch8(const uint16_t*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
+    const unsigned at = (r * (unsigned)n + (unsigned)c) * 2u;
+    u16x8 v;
+    if constexpr (VEC) {
+        v = __builtin_bit_cast(u16x8, __builtin_amdgcn_raw_buffer_load_b128(rows, on && c < n ? at : NOWHERE, 0, 0));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = on && c + i < n ? row[c + i] : (unsigned short)0;
+        for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b16(rows, on && c + i < n ? at + 2u * i : NOWHERE, 0, 0);
     }
     return v;
 }
+template <typename E> struct Eight { typedef f32x8 type; };
+template <> struct Eight<uint16_t> { typedef u16x8 type; };
 __device__ __forceinline__ Parts<1> take_apart(u16x8 v) { return Parts<1>{__builtin_bit_cast(bf16x8, v)}; }
 template <typename E> constexpr int PARTS = sizeof(E) == 4 ? 3 : 1;
 
-// ---- dx: a wavefront keeps dl of 16 NT tokens in registers (KS steps of 32 experts) and goes over columns, 32 at a time, whose rows of W_g come from the
-// caches.  Matrix row 16 h + j of 32 stands for column 8 (j / 4) + 4 h + j % 4, so that a lane has eight neighbours.
-template <typename W, int KS, int NT, bool VEC>
+// ---- dx: a work-group has dl of TT tokens in LDS, in parts, and goes over columns: a wavefront 32 of every 128, whose rows of W_g and added values are fetched
+// while the 32 before are multiplied.  (With dl in registers and every wavefront fetching W_g for itself those fetches took 30 us: 16384 x 768, E = 128.)
+// LDS: [part][token][32 KS experts], 16-byte pieces turned by the token, so that the reads of sixteen tokens touch all banks.
+template <typename W, int KS, bool VEC>
 __global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* add, int T, int d, int E, int columns,
                                                  float* dx) {       // (dx may be add)
-    const int lane = threadIdx.x & 63, l16 = lane & 15, lq = lane >> 4;
-    const int t0 = ((int)blockIdx.x * (NTH / 64) + (int)(threadIdx.x >> 6)) * 16 * NT;
-    if (t0 >= T) return;
-    Parts<3> g[NT][KS];
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) g[n][s] = take_apart(fetch8<VEC>(dl + (size_t)(t0 + n * 16 + l16) * E, E, s * 32 + lq * 8, t0 + n * 16 + l16 < T));
+#ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass has no buffer descriptors)
+    constexpr int TT = KS <= 4 ? 64 : 32, N = TT / 16, P = KS * 4, ROW = P * 16, TURN = P < 16 ? 16 / P : 1;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[3 * TT * ROW];
+    auto place = [](int t, int piece) { return t * ROW + ((piece ^ (t / TURN & (P < 16 ? P - 1 : 15))) << 4); };
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
+    const int t0 = (int)blockIdx.x * TT;
+    const unsigned rows = (unsigned)(T - t0 < TT ? T - t0 : TT);
+    const __amdgpu_buffer_rsrc_t rl = make_rsrc(dl + (size_t)t0 * E, rows * (unsigned)E * 4u), rm = make_rsrc(w, (unsigned)d * (unsigned)E * (unsigned)sizeof(W));
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(add + (size_t)t0 * d, add ? rows * (unsigned)d * 4u : 0u), ro = make_rsrc(dx + (size_t)t0 * d, rows * (unsigned)d * 4u);
     const int first = (int)blockIdx.y * columns, last = first + columns < d ? first + columns : d;
-    for (int c0 = first; c0 < last; c0 += 32) {
-        f32x4 acc[NT][2] = {}, old[NT][2] = {};
-        const int c = c0 + lq * 8;
-        if (add) {                                         // (on its way while the products are made)
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                if (t0 + n * 16 + l16 < T && c < d) {
-                    const f32x4* from = (const f32x4*)(add + (size_t)(t0 + n * 16 + l16) * d + c);
-                    old[n][0] = from[0];
-                    old[n][1] = from[1];
-                }
-        }
+    typename Eight<W>::type next[KS][2];
+    f32x4 old[2][N][2];
+    auto fetch = [&](int c0, f32x4 (&o)[N][2]) {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int col = c0 + 8 * (l16 >> 2) + 4 * h + (l16 & 3);
-                const Parts<PARTS<W>> m = take_apart(fetch8<VEC>(w + (size_t)col * E, E, s * 32 + lq * 8, col < d));
+            for (int h = 0; h < 2; ++h) next[s][h] = fetch8<VEC>(w, rm, E, (unsigned)(c0 + 16 * h + l16), s * 32 + lq * 8, c0 + 16 * h + l16 < last);
+        const int c = c0 + lq * 4;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) multiply(m, g[n][s], acc[n][h]);
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                o[n][h] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                        ra, c + 16 * h < last ? ((unsigned)(n * 16 + l16) * (unsigned)d + (unsigned)(c + 16 * h)) * 4u : NOWHERE, 0, 0));
+    };
+    f32x8 raw[TT * P / NTH];
+#pragma unroll
+    for (int i = 0; i < TT * P / NTH; ++i) raw[i] = fetch8<VEC>(dl, rl, E, (unsigned)((i * NTH + tid) / P), (i * NTH + tid) % P * 8, true);
+    fetch(first + wave * 32, old[0]);
+#pragma unroll
+    for (int i = 0; i < TT * P / NTH; ++i) {
+        const Parts<3> v = take_apart(raw[i]);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) *(bf16x8*)(lds + q * TT * ROW + place((i * NTH + tid) / P, (i * NTH + tid) % P)) = v.p[q];
+    }
+    __syncthreads();
+    auto step = [&](int c0, f32x4 (&here)[N][2], f32x4 (&later)[N][2]) {
+        Parts<PARTS<W>> m[KS][2];
+#pragma unroll
+        for (int s = 0; s < KS; ++s)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) m[s][h] = take_apart(next[s][h]);
+        fetch(c0 + 128, later);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            f32x4 acc[2] = {};
+#pragma unroll
+            for (int s = 0; s < KS; ++s) {
+                Parts<3> g;
+#pragma unroll
+                for (int q = 0; q < 3; ++q) g.p[q] = *(const bf16x8*)(lds + q * TT * ROW + place(n * 16 + l16, s * 4 + lq));
+#pragma unroll
+                for (int h = 0; h < 2; ++h) multiply(m[s][h], g, acc[h]);
             }
 #pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const int t = t0 + n * 16 + l16;
-            if (t >= T || c >= d) continue;                // (d is a multiple of 8)
-            f32x4* to = (f32x4*)(dx + (size_t)t * d + c);
-            to[0] = acc[n][0] + old[n][0];
-            to[1] = acc[n][1] + old[n][1];
+            for (int h = 0; h < 2; ++h) {                  // (d is a multiple of 8)
+                const int c = c0 + lq * 4 + 16 * h;
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[h] + here[n][h]), ro,
+                                                       c < last ? ((unsigned)(n * 16 + l16) * (unsigned)d + (unsigned)c) * 4u : NOWHERE, 0, 0);
+            }
         }
+    };
+    for (int c0 = first + wave * 32; c0 < last; c0 += 256) {
+        step(c0, old[0], old[1]);
+        if (c0 + 128 < last) step(c0 + 128, old[1], old[0]);
     }
+#endif
 }
 
 // ---- dW_g over a range of tokens: 64 of x's columns x 128 experts a work-group, 32 tokens at a time through LDS (fetched while the 32 before are multiplied);
@@ -190,7 +231,8 @@ __global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, c
 // LDS: panels of 32 tokens x 64 columns, 128 bytes a row, whose 32-byte pieces are turned by the row, so that the reads touch all banks.
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-constexpr int TC = 32, PANEL = TC * 128;
+constexpr int TC = 32;
+[[maybe_unused]] constexpr int PANEL = TC * 128;
 __device__ __forceinline__ int panel_at(int row, int c) { return row * 128 + (((c >> 4) ^ (row >> 1 & 3)) * 32) + (c & 15) * 2; }      // of column c < 64
 __device__ __forceinline__ bf16x8 read_transposed(const unsigned char* panel, int block, int l16, int lq) {
     typedef __attribute__((ext_vector_type(8))) short s16x8;
@@ -207,6 +249,7 @@ template <int N> __device__ __forceinline__ void put8(unsigned char* at, int ste
 
 template <typename X, bool VEC>
 __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const float* __restrict__ dl, int T, int d, int E, int range, float* __restrict__ part) {
+#ifdef __HIP_DEVICE_COMPILE__
     constexpr int NX = PARTS<X>, BUF = (NX + 6) * PANEL;   // x's parts, then dl's: [part][two panels]
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2 * BUF];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, lq = lane >> 4;
@@ -214,13 +257,15 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
     // a thread has eight columns of x and, twice, eight experts of dl
     const int xr = tid >> 3, xc = (tid & 7) * 8, er = tid >> 4, ec = (tid & 15) * 8;
     // (two sets: what the step after the next needs is on its way)
-    decltype(fetch8<true>(x, 0, 0, false)) gx[2];
+    typename Eight<X>::type gx[2];
     f32x8 ge[2][2];
     float db[8] = {};
     auto fetch = [&](int t0, int set) {
-        gx[set] = fetch8<true>(x + (size_t)(t0 + xr) * d, d, c0 + xc, x && t0 + xr < last);
+        const unsigned rows = (unsigned)(last - t0 < 0 ? 0 : last - t0 < TC ? last - t0 : TC);
+        const __amdgpu_buffer_rsrc_t rx = make_rsrc(x + (size_t)t0 * d, x ? rows * (unsigned)d * (unsigned)sizeof(X) : 0u), rl = make_rsrc(dl + (size_t)t0 * E, rows * (unsigned)E * 4u);
+        gx[set] = fetch8<true>(x, rx, d, (unsigned)xr, c0 + xc, true);
 #pragma unroll
-        for (int i = 0; i < 2; ++i) ge[set][i] = fetch8<VEC>(dl + (size_t)(t0 + er + i * 16) * E, E, e0 + ec, t0 + er + i * 16 < last);
+        for (int i = 0; i < 2; ++i) ge[set][i] = fetch8<VEC>(dl, rl, E, (unsigned)(er + i * 16), e0 + ec, true);
     };
     f32x4 acc[4][2] = {};
     auto step = [&](int t0, int buf) {
@@ -281,6 +326,7 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
             to[(size_t)d * E + e0 + tid] = s;
         }
     }
+#endif
 }
 __global__ __launch_bounds__(NTH) void dw_sum_kernel(const float* __restrict__ part, int ranges, int d, int E, float* __restrict__ dw, float* __restrict__ db) {
     const size_t i = (size_t)blockIdx.x * NTH + threadIdx.x, n = (size_t)d * E, step = n + E;
@@ -298,7 +344,7 @@ __global__ __launch_bounds__(NTH) void dw_sum_kernel(const float* __restrict__ p
 // Ranges of tokens that dW_g is summed over: enough work-groups for the chip, 64 tokens at least.
 int ranges_of(int T, int d, int E) {
     const int tiles = ((d + 63) / 64) * ((E + 127) / 128);
-    int n = (512 + tiles - 1) / tiles;
+    int n = 512 / tiles;                                   // (two work-groups a CU, and not one more than that)
     const int most = (T + 63) / 64;
     if (n > most) n = most;
     if (n < 1) n = 1;
@@ -307,16 +353,16 @@ int ranges_of(int T, int d, int E) {
 }
 
 template <typename W> void launch_dx(const W* w, bool vec, const float* dl, const float* add, int T, int d, int E, float* dx, hipStream_t st) {
-    // columns a work-group: as many as leave four wavefronts a SIMD, 32 at least
-    const int nt = E <= 64 ? 2 : 1, groups = (T + 64 * nt - 1) / (64 * nt);
-    int splits = (1024 + groups - 1) / groups;
-    int columns = ((d + splits - 1) / splits + 31) / 32 * 32;
+    // columns a work-group: as many as leave three of them a CU, 128 at least
+    const int tt = E <= 128 ? 64 : 32, groups = (T + tt - 1) / tt;
+    int splits = (768 + groups - 1) / groups;
+    const int columns = ((d + splits - 1) / splits + 127) / 128 * 128;
     splits = (d + columns - 1) / columns;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, splits), dim3(NTH), 0, st, dl, w, add, T, d, E, columns, dx); };
-    if (E <= 32) vec ? go(dx_kernel<W, 1, 2, true>) : go(dx_kernel<W, 1, 2, false>);
-    else if (E <= 64) vec ? go(dx_kernel<W, 2, 2, true>) : go(dx_kernel<W, 2, 2, false>);
-    else if (E <= 128) vec ? go(dx_kernel<W, 4, 1, true>) : go(dx_kernel<W, 4, 1, false>);
-    else vec ? go(dx_kernel<W, 8, 1, true>) : go(dx_kernel<W, 8, 1, false>);
+    if (E <= 32) vec ? go(dx_kernel<W, 1, true>) : go(dx_kernel<W, 1, false>);
+    else if (E <= 64) vec ? go(dx_kernel<W, 2, true>) : go(dx_kernel<W, 2, false>);
+    else if (E <= 128) vec ? go(dx_kernel<W, 4, true>) : go(dx_kernel<W, 4, false>);
+    else vec ? go(dx_kernel<W, 8, true>) : go(dx_kernel<W, 8, false>);
 }
 
 }  // namespace
@@ -333,7 +379,7 @@ extern "C" int moe_route_topk_backward(const float* dgate_w, const float* gate_w
     MOE_REQUIRE(T >= 0 && d >= 1 && E >= 1 && k >= 1 && k <= E, MOE_ERR_ARG, "%s: T=%d d=%d E=%d k=%d", me, T, d, E, k);
     MOE_REQUIRE(moe_dtype_ok(dt), MOE_ERR_UNSUPPORTED, "%s: dtype %d", me, (int)dt);
     MOE_REQUIRE(E <= MOE_MAX_EXPERTS && k <= MOE_MAX_TOPK && d % 8 == 0, MOE_ERR_UNSUPPORTED, "%s: d=%d E=%d k=%d", me, d, E, k);
-    MOE_REQUIRE(T <= 64 * 65535, MOE_ERR_UNSUPPORTED, "%s: T=%d", me, T);
+    MOE_REQUIRE(T <= 64 * 65535 && d <= (1 << 20), MOE_ERR_UNSUPPORTED, "%s: T=%d d=%d", me, T, d);
     const bool sums = dw_gate || dbias;
     const size_t need = sums ? moe_route_back_bytes(T, d, E) : 0;
     if (T > 0) {

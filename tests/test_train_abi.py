@@ -104,6 +104,7 @@ def test_route_arguments():
         assert route(**{a: None}) == B.MOE_ERR_ARG
     assert route(k=9, E=16) == B.MOE_ERR_UNSUPPORTED and route(k=9) == B.MOE_ERR_ARG and route(d=60) == B.MOE_ERR_UNSUPPORTED
     assert route(E=B.MOE_MAX_EXPERTS + 1) == B.MOE_ERR_UNSUPPORTED and route(dx=FAKE + 4) == B.MOE_ERR_UNSUPPORTED
+    assert route(T=64 * 65535 + 1) == B.MOE_ERR_UNSUPPORTED and route(d=2 ** 20 + 8) == B.MOE_ERR_UNSUPPORTED and route(x=FAKE + 8) == B.MOE_ERR_UNSUPPORTED
     assert route(ws=None) == B.MOE_ERR_WORKSPACE
     assert route(ws_bytes=B.moe_workspace_bytes(B.MOE_OP_ROUTE_BACKWARD, 4, 64, 0, 8, 0, BF16) - 1) == B.MOE_ERR_WORKSPACE
 
