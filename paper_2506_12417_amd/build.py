@@ -216,6 +216,40 @@ def check_no_flat_access(asm_text: str):
     return bad
 
 
+def check_training_kernels(asm_text: str):
+    """The kernels of ffn_train.hip load global -> LDS with hand-written instructions, in front of which M0 is set to their
+    target, and keep the data registers of a 16-byte store unchanged for the instruction behind it.  Sound only if the compiler
+    uses M0 for nothing else there, puts nothing between, and writes no such register.  Returns (kernel, instruction)
+    violations: a mention of M0 or such a load outside of the two sequences, a write to a store's data right behind it."""
+    loads = (("s_add_u32 m0, ", "v_add_u32_e64 ", "buffer_load_dwordx4 "), ("s_mov_b32 m0, ", "s_nop 0", "buffer_load_dword "))
+
+    def regs(operand):
+        m = re.match(r"v(\d+)$|v\[(\d+):(\d+)\]$", operand.strip())
+        if not m:
+            return set()
+        return {int(m.group(1))} if m.group(1) else set(range(int(m.group(2)), int(m.group(3)) + 1))
+
+    def operands(c):
+        return c.split(None, 1)[1].split(",") if " " in c or "\t" in c else [""]
+
+    bad, found = [], 0
+    for m in re.finditer(r"^(_Z\w*gemm_[nt][nt]_kernel\w*):[^\n]*\n(.*?)\.Lfunc_end", asm_text, flags=re.S | re.M):
+        found += 1
+        code = [c for c in (raw.split(";")[0].strip() for raw in m.group(2).split("\n")) if c and not c.startswith(".")]
+        at = 0
+        while at < len(code):
+            c, behind = code[at], code[at + 1] if at + 1 < len(code) else ""
+            if any(all(x.startswith(p) for x, p in zip(code[at:at + 3], q)) for q in loads) and code[at + 2:at + 3] and code[at + 2].endswith(" lds"):
+                at += 3
+                continue
+            if re.search(r"\bm0\b|\blds$", c):
+                bad.append((m.group(1), c))
+            if c.startswith("buffer_store_dwordx4 ") and behind.startswith(("v_", "ds_read", "buffer_load")) and regs(operands(c)[0]) & regs(operands(behind)[0]):
+                bad.append((m.group(1), c + "; " + behind))
+            at += 1
+    return bad if found else [("(none)", "no gemm_nt_kernel or gemm_tn_kernel found in the assembly")]
+
+
 def build(verbose: bool = True, jobs: int = 8) -> str:
     """Compiles every source (always; no staleness check) and links libmoe.so."""
     obj_dir = os.path.join(HERE, "_build")
@@ -264,6 +298,9 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     if bad:
         raise RuntimeError("ffn_stream.hip: registers of the weight loads are touched by other code:\n%s"
                            % "\n".join("  %s: %s" % b for b in bad[:20]))
+    bad = check_training_kernels(open(asm_paths[-1]).read())
+    if bad:
+        raise RuntimeError("ffn_train.hip: loads to LDS or stores that the compiler has taken apart:\n%s" % "\n".join("  %s: %s" % b for b in bad[:20]))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:

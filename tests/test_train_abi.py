@@ -129,3 +129,25 @@ def test_layers_that_do_not_train():
     from paper_2506_12417_amd.layer import MoELayer
     with pytest.raises(AssertionError):
         MoELayer(4, 64, 64, 2, 1, "relu", "f32", 0, device="cpu", train=True)
+
+
+def test_build_checks_the_hand_written_loads_and_stores():
+    """build.check_training_kernels: M0 belongs to the loads to LDS, whose three instructions stay together, and a store's registers live on."""
+    import os
+    from paper_2506_12417_amd import build as b
+    load = "\ts_add_u32 m0, s4, 0x1000\n\tv_add_u32_e64 v1, v2, s5 clamp\n\tbuffer_load_dwordx4 v1, s[0:3], s6 offen lds\n"
+    small = "\ts_mov_b32 m0, s7\n\ts_nop 0\n\tbuffer_load_dword v3, s[8:11], 0 offen lds\n"
+    store = "\tbuffer_store_dwordx4 v[4:7], v8, s[0:3], s9 offen\n\ts_nop 1\n"
+    text = lambda body: "_ZN1x14gemm_tn_kernelILi0EEEvv: ; @k\n" + body + "\ts_endpgm\n.Lfunc_end0:\n"      # noqa: E731
+    assert b.check_training_kernels(text(load + small + ".LBB0_1:\n" + store + load)) == []
+    for line in ("s_mov_b32 m0, s1", "v_readlane_b32 s2, v1, m0", "buffer_load_dwordx4 v1, s[0:3], s6 offen lds"):
+        assert [c for _, c in b.check_training_kernels(text(load + "\t" + line + "\n" + store))] == [line], line
+    for line, n in (("v_mov_b32_e32 v4, 0", 1), ("v_pk_add_f16 v7, v1, v2", 1), ("v_mov_b32_e32 v3, v4", 0), ("v_accvgpr_write_b32 a4, v4", 0), ("v_mov_b64_e32 v[6:7], v[0:1]", 1)):
+        assert len(b.check_training_kernels(text(store.replace("\ts_nop 1\n", "\t" + line + "\n\ts_nop 1\n")))) == n, line
+    torn = load.replace("\tbuffer", "\tv_mov_b32_e32 v9, 0\n\tbuffer")
+    assert len(b.check_training_kernels(text(torn))) == 2
+    assert b.check_training_kernels("_Z1av:\n\ts_endpgm\n.Lfunc_end0:\n")          # no such kernel at all: reported
+    asm = os.path.join(os.path.dirname(b.LIB), "_build", "ffn_train.s")
+    if os.path.exists(asm):          # the assembly of the library that is loaded here
+        whole = open(asm).read()
+        assert whole.count(" offen lds") > 500 and b.check_training_kernels(whole) == [] and b.check_no_flat_access(whole) == []
