@@ -104,7 +104,7 @@ class MoEBlock:
         self.u_in = u
         if prefers_few(L) and not L.train:
             L.forward_few(u, self.v, stream)
-        elif self.train or L.fold_combine:
+        elif self.train or L.train or L.fold_combine:
             L.forward(u, stream, y=self.v)
         else:
             # the layer's combine in the same pass as what follows it: v is never stored

@@ -73,7 +73,7 @@ class MoELayer:
                  fuse_gather: Optional[bool] = None, train: bool = False):
         self.T, self.d, self.F, self.E, self.k, self.renorm = T, d, F, E, k, renorm
         assert not train or dtype == "bf16", "the experts' gradients are there for bf16 layers"
-        self.train = train
+        self.train, self.kept_of = train, None
         self.A = T * k
         self.act = B.MOE_SWIGLU if act == "swiglu" else B.MOE_RELU
         self.dt = B.MOE_BF16 if dtype == "bf16" else B.MOE_F32
@@ -294,6 +294,7 @@ class MoELayer:
         y = self.own_y if y is None else y
         B.check_rows("x", x, self.T, self.d, (self.tdt,), self.own_y.device)
         B.check_rows("y", y, self.T, self.d, (torch.float32, torch.bfloat16), self.own_y.device)
+        self.kept_of = None                  # (nothing is kept for backward() here)
         if y.dtype == torch.float32:
             self.y = y
         g, s = self.experts, self.shared if self.shared_F else None
@@ -379,7 +380,7 @@ class MoELayer:
     def _forward_train(self, x: torch.Tensor, routed: bool, stream) -> torch.Tensor:
         g, shape, kinds = self.experts, (self.T, self.d, self.F, self.E), (self.act, self.dt)
         B.check_rows("x", x, self.T, self.d, (self.tdt,), self.own_y.device)
-        self.was_routed = routed             # by the caller: the gate values are not the router's, which gets no gradient
+        self.kept_of = "routed" if routed else "whole"      # routed by the caller: the gate values are not the router's, which gets no gradient
         if not routed:
             self.route(x, self.logits, stream)
         self.permute_plan(stream)
@@ -403,7 +404,8 @@ class MoELayer:
         those of the matrices and the router go to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).
         dy: [T,d] fp32 or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the experts'
         gradients are added to what `grad` holds (the router's are not: they are set)."""
-        assert self.train, "MoELayer(train=True) keeps what the gradients are made of"
+        assert self.train and self.kept_of, "the forward() of a MoELayer(train=True) keeps what the gradients are made of"
+        assert dlogits_add is None or self.kept_of == "whole", "forward() was given the choice: the router has no gradient"
         T, d, E, k, dev = self.T, self.d, self.E, self.k, self.own_y.device
         B.check_rows("dy", dy, T, d, (torch.float32, self.tdt), dev)
         B.check_rows("x", x, T, d, (self.tdt,), dev)
@@ -418,7 +420,7 @@ class MoELayer:
             add = self.dx_sum
         B.moe_grouped_ffn_backward(dy, dy_dt, x, T, d, self.F, E, k, self.act, self.dt, w["a"], w["b"], w["o"], self.offsets, self.perm, self.inv_perm,
                                    self.gate_w, *self.kept[""], self.dx_perm, self.dgate_w, g["a"], g["b"], g["o"], self.dt, acc, self.back_ws, n, stream)
-        if not self.was_routed:
+        if self.kept_of == "whole":
             B.moe_route_topk_backward(self.dgate_w, self.gate_w, self.expert_idx, self.logits, dlogits_add, x, self.W_g, T, d, E, k, self.renorm, self.dt,
                                       self.dlogits, add, self.dx_sum, g["W_g"], g["bias"], self.back_ws, n, stream)
             add = self.dx_sum

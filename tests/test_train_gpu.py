@@ -537,6 +537,27 @@ def test_refused_calls_of_a_layer():
         plain.backward(dy, x)
     with pytest.raises(AssertionError):
         L.forward(x, rows=True)
+    L.forward_few(x)                                       # (a decode step keeps nothing)
+    with pytest.raises(AssertionError):
+        L.backward(dy, x)
+    L.expert_idx.fill_(0)
+    L.forward(x, routed=True)
+    with pytest.raises(AssertionError):
+        L.backward(dy, x, torch.zeros((9, 3), device=dev))
+
+
+@pytest.mark.parametrize("T,k,act,shared_F", [(48, 1, "relu", 0), (120, 2, "swiglu", 64)])
+def test_block_for_inference_with_a_layer_that_trains(T, k, act, shared_F):
+    torch, B, dev = _gpu()
+    from paper_2506_12417_amd.block import MoEBlock
+    L, _ = trained_layer(T, 256, 512, 4, k, act, 1 if k > 1 else 0, shared_F)
+    h = torch.randn((T, 256), device=dev).bfloat16()
+    out = []
+    for train in (True, False):
+        b = MoEBlock(L, pre="rms", next="rms", train=train)
+        y, u = b.forward(h)
+        out.append((y.clone(), u.clone()))
+    assert torch.equal(out[0][0], out[1][0]) and torch.equal(out[0][1], out[1][1])
 
 
 @pytest.mark.parametrize("T,k,act,shared_F", [(48, 1, "relu", 0), (120, 2, "swiglu", 64)])
