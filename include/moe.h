@@ -475,7 +475,7 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
  *
  * so that a value is off by at most m / 254.  Where one of the 64 is NaN or infinite all of them read back as NaN; where m is below 2^-100
  * as 0.
- *   x [rows,n] dt, any n and any alignment      q [rows,n] int8      scale [rows, ceil(n / 64)] fp32
+ *   x [rows,n] dt, any n and any alignment      q [rows,n] int8      scale [rows, ceil(n / 64)] fp32, less than 2^29 of them
  * rows = 0 is a no-op.  No output may overlap an input.
  */
 MOE_API int moe_keep_rows(const void* x, moe_dtype dt, long long rows, int n, int8_t* q, float* scale, void* stream);
@@ -527,7 +527,8 @@ MOE_API int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const void
  *
  *   dy [T,d] dy_dt      y_perm [A,d] fp32 (NULL without dgate_w)      gate_w [T,k] fp32 or NULL (all ones)
  *   dy_perm [A,d] perm_dt out or NULL      dgate_w [T,k] fp32 out or NULL      dx_add [T,d] fp32 or NULL      dx [T,d] dx_dt out
- * A negative inv_perm entry has no row: dgate_w is 0 there, and it adds nothing to dx.  Any d, any alignment.  dx may be dx_add (both fp32); no
+ * A negative inv_perm entry has no row: dgate_w is 0 there, and it adds nothing to dx.  Any d, any alignment, T ceil(d / 512) < 2^26 (T < 2^26 for
+ * moe_unpermute_combine_backward), T k < 2^31.  dx may be dx_add (both fp32); no
  * other output may overlap an input.  T = 0 is a no-op.
  */
 MOE_API int moe_unpermute_combine_backward(const void* dy, moe_dtype dy_dt, const float* y_perm, const int32_t* inv_perm,

@@ -105,8 +105,8 @@ __global__ __launch_bounds__(NTH) void keep_restore_kernel(const int8_t* __restr
 
 int keep_grid(const char* what, long long rows, int n, size_t* blocks, unsigned* grid) {
     *blocks = (size_t)rows * (size_t)((n + KEEP_BLOCK - 1) / KEEP_BLOCK);
-    const size_t g = (*blocks * 8 + NTH - 1) / NTH;
-    MOE_REQUIRE(g < (1ull << 31), MOE_ERR_UNSUPPORTED, "%s: %lld rows of %d values", what, rows, n);
+    const size_t g = (*blocks * 8 + NTH - 1) / NTH;        // (a launch has less than 2^32 threads)
+    MOE_REQUIRE(g < (1ull << 24), MOE_ERR_UNSUPPORTED, "%s: %lld rows of %d values", what, rows, n);
     *grid = (unsigned)g;
     return MOE_OK;
 }
