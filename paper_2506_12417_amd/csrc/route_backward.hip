@@ -9,6 +9,7 @@
 // and whose sums are fp32.  dl has three parts, x and W_g one where they are bf16 and three where they are fp32 (then without the products
 // below 2^-24).  dW_g and db are summed over ranges of tokens, whose parts a second launch adds up in their order: no atomics.
 //
+#include <type_traits>
 #include "common.h"
 #include "gemm_util.h"
 #include "lanes.h"
@@ -34,7 +35,8 @@ __device__ __forceinline__ float wave_max(float v) {
     return fmaxf(fmaxf(lane_f32(v, 0), lane_f32(v, 16)), fmaxf(lane_f32(v, 32), lane_f32(v, 48)));
 }
 
-// ---- dl: a wavefront has a token, a lane up to four experts
+// ---- dl: a wavefront has a token, a lane N experts
+template <int N>
 __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ dgate_w, const float* __restrict__ gate_w, const int32_t* __restrict__ idx,
                                                       const float* __restrict__ logits, const float* __restrict__ add, int T, int E, int k, int renorm,
                                                       float* __restrict__ dl) {
@@ -49,40 +51,40 @@ __global__ __launch_bounds__(NTH) void dlogits_kernel(const float* __restrict__ 
     }
     const bool lost = __ballot(lane < k && (e_of < 0 || e_of >= E)) != 0;      // (a token whose logits are NaN)
     const float D = wave_sum(g * dg);
-    float p[4], v[4];
+    float p[N], v[N];
     if (!renorm) {
         float most = -__builtin_inff(), sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             const int e = i * 64 + lane;
             p[i] = e < E ? logits[(size_t)t * E + e] : -__builtin_inff();
             most = fmaxf(most, p[i]);
         }
         most = wave_max(most);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             p[i] = i * 64 + lane < E ? expf(p[i] - most) : 0.f;
             sum += p[i];
         }
         sum = wave_sum(sum);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < N; ++i) {
             p[i] /= sum;
             v[i] = -D;
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = p[i] = 0.f;
+        for (int i = 0; i < N; ++i) v[i] = p[i] = 0.f;
     }
     for (int j = 0; j < k; ++j) {
         const int e = __builtin_amdgcn_readlane(e_of, j);
         const float a = renorm ? lane_f32(g, j) * (lane_f32(dg, j) - D) : lane_f32(dg, j);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int i = 0; i < N; ++i)
             if (e == i * 64 + lane) v[i] += a;
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N; ++i) {
         const int e = i * 64 + lane;
         if (e >= E) continue;
         const size_t at = (size_t)t * E + e;
@@ -116,18 +118,19 @@ template <int NA, int NB> __device__ __forceinline__ void multiply(const Parts<N
             if (s - i >= 0 && s - i < NB) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.p[i], b.p[s - i], acc, 0, 0, 0);
 }
 // Rows that a work-group reads, through a buffer descriptor: what is not `on`, or lies behind a row's n values, reads as zero without a branch (behind
-// branches with loads in them the compiler waits for all that is under way).  Eight neighbours of row r from column c on.  VEC: n is a multiple
-// of 8 and the rows are aligned.
+// branches with loads in them the compiler waits for all that is under way).  Eight neighbours of row r from column c on.  VEC: n is a multiple of
+// this (8, 4 or 1) and the rows are aligned to as many values.
 typedef __attribute__((ext_vector_type(8))) float f32x8;
+typedef __attribute__((ext_vector_type(4))) unsigned short u16x4;
 typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 constexpr unsigned NOWHERE = 0xFFFFFF00u;
-template <bool VEC> __device__ __forceinline__ f32x8 fetch8(const float*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
+template <int VEC> __device__ __forceinline__ f32x8 fetch8(const float*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
     const unsigned at = (r * (unsigned)n + (unsigned)c) * 4u;
     f32x8 v;
-    if constexpr (VEC) {
-        const unsigned o = on && c < n ? at : NOWHERE;
-        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, o, 0, 0)), b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, o + 16, 0, 0));
+    if constexpr (VEC >= 4) {
+        const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, on && c < n ? at : NOWHERE, 0, 0));
+        const f32x4 b = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(rows, on && c + 4 < n ? at + 16u : NOWHERE, 0, 0));
         v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
 #pragma unroll
@@ -135,11 +138,15 @@ template <bool VEC> __device__ __forceinline__ f32x8 fetch8(const float*, __amdg
     }
     return v;
 }
-template <bool VEC> __device__ __forceinline__ u16x8 fetch8(const uint16_t*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
+template <int VEC> __device__ __forceinline__ u16x8 fetch8(const uint16_t*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
     const unsigned at = (r * (unsigned)n + (unsigned)c) * 2u;
     u16x8 v;
-    if constexpr (VEC) {
+    if constexpr (VEC == 8) {
         v = __builtin_bit_cast(u16x8, __builtin_amdgcn_raw_buffer_load_b128(rows, on && c < n ? at : NOWHERE, 0, 0));
+    } else if constexpr (VEC == 4) {
+        const u16x4 a = __builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(rows, on && c < n ? at : NOWHERE, 0, 0));
+        const u16x4 b = __builtin_bit_cast(u16x4, __builtin_amdgcn_raw_buffer_load_b64(rows, on && c + 4 < n ? at + 8u : NOWHERE, 0, 0));
+        v = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = __builtin_amdgcn_raw_buffer_load_b16(rows, on && c + i < n ? at + 2u * i : NOWHERE, 0, 0);
@@ -154,7 +161,7 @@ template <typename E> constexpr int PARTS = sizeof(E) == 4 ? 3 : 1;
 // ---- dx: a work-group has dl of TT tokens in LDS, in parts, and goes over columns: a wavefront 32 of every 128, whose rows of W_g and added values are fetched
 // while the 32 before are multiplied.  (With dl in registers and every wavefront fetching W_g for itself those fetches took 30 us: 16384 x 768, E = 128.)
 // LDS: [part][token][32 KS experts], 16-byte pieces turned by the token, so that the reads of sixteen tokens touch all banks.
-template <typename W, int KS, bool VEC>
+template <typename W, int KS, int VEC>
 __global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, const W* __restrict__ w, const float* add, int T, int d, int E, int columns,
                                                  float* dx) {       // (dx may be add)
 #ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass has no buffer descriptors)
@@ -247,7 +254,7 @@ template <int N> __device__ __forceinline__ void put8(unsigned char* at, int ste
     for (int i = 0; i < N; ++i) *(bf16x8*)(at + i * step) = v.p[i];
 }
 
-template <typename X, bool VEC>
+template <typename X, int VEC>
 __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const float* __restrict__ dl, int T, int d, int E, int range, float* __restrict__ part) {
 #ifdef __HIP_DEVICE_COMPILE__
     constexpr int NX = PARTS<X>, BUF = (NX + 6) * PANEL;   // x's parts, then dl's: [part][two panels]
@@ -263,7 +270,7 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
     auto fetch = [&](int t0, int set) {
         const unsigned rows = (unsigned)(last - t0 < 0 ? 0 : last - t0 < TC ? last - t0 : TC);
         const __amdgpu_buffer_rsrc_t rx = make_rsrc(x + (size_t)t0 * d, x ? rows * (unsigned)d * (unsigned)sizeof(X) : 0u), rl = make_rsrc(dl + (size_t)t0 * E, rows * (unsigned)E * 4u);
-        gx[set] = fetch8<true>(x, rx, d, (unsigned)xr, c0 + xc, true);
+        gx[set] = fetch8<8>(x, rx, d, (unsigned)xr, c0 + xc, true);
 #pragma unroll
         for (int i = 0; i < 2; ++i) ge[set][i] = fetch8<VEC>(dl, rl, E, (unsigned)(er + i * 16), e0 + ec, true);
     };
@@ -307,12 +314,16 @@ __global__ __launch_bounds__(NTH) void dw_kernel(const X* __restrict__ x, const 
         const int c = c0 + m * 16 + l16;
         if (c >= d || !x) continue;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2; ++b) {
+            const int e = e0 + wave * 32 + b * 16 + lq * 4;
+            if constexpr (VEC >= 4) {
+                if (e < E) *(f32x4*)(to + (size_t)c * E + e) = acc[m][b];
+            } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int e = e0 + wave * 32 + b * 16 + lq * 4 + i;
-                if (e < E) to[(size_t)c * E + e] = acc[m][b][i];
+                for (int i = 0; i < 4; ++i)
+                    if (e + i < E) to[(size_t)c * E + e + i] = acc[m][b][i];
             }
+        }
     }
     if (blockIdx.x == 0) {                                 // sixteen threads have each column
         float* sums = (float*)lds;
@@ -352,17 +363,26 @@ int ranges_of(int T, int d, int E) {
     return range > 0 ? (T + range - 1) / range : 1;
 }
 
-template <typename W> void launch_dx(const W* w, bool vec, const float* dl, const float* add, int T, int d, int E, float* dx, hipStream_t st) {
+template <typename F> void by_vec(int vec, F&& f) {
+    if (vec == 8) f(std::integral_constant<int, 8>{});
+    else if (vec == 4) f(std::integral_constant<int, 4>{});
+    else f(std::integral_constant<int, 1>{});
+}
+template <typename W> void launch_dx(const W* w, int vec, const float* dl, const float* add, int T, int d, int E, float* dx, hipStream_t st) {
     // columns a work-group: as many as leave three of them a CU, 128 at least
     const int tt = E <= 128 ? 64 : 32, groups = (T + tt - 1) / tt;
     int splits = (768 + groups - 1) / groups;
     const int columns = ((d + splits - 1) / splits + 127) / 128 * 128;
     splits = (d + columns - 1) / columns;
     auto go = [&](auto kern) { hipLaunchKernelGGL(kern, dim3(groups, splits), dim3(NTH), 0, st, dl, w, add, T, d, E, columns, dx); };
-    if (E <= 32) vec ? go(dx_kernel<W, 1, true>) : go(dx_kernel<W, 1, false>);
-    else if (E <= 64) vec ? go(dx_kernel<W, 2, true>) : go(dx_kernel<W, 2, false>);
-    else if (E <= 128) vec ? go(dx_kernel<W, 4, true>) : go(dx_kernel<W, 4, false>);
-    else vec ? go(dx_kernel<W, 8, true>) : go(dx_kernel<W, 8, false>);
+    auto by_size = [&](auto v) {
+        constexpr int V = decltype(v)::value;
+        if (E <= 32) go(dx_kernel<W, 1, V>);
+        else if (E <= 64) go(dx_kernel<W, 2, V>);
+        else if (E <= 128) go(dx_kernel<W, 4, V>);
+        else go(dx_kernel<W, 8, V>);
+    };
+    by_vec(vec, by_size);
 }
 
 }  // namespace
@@ -392,16 +412,19 @@ extern "C" int moe_route_topk_backward(const float* dgate_w, const float* gate_w
     const hipStream_t st = (hipStream_t)stream;
     int ranges = 0;
     if (T > 0) {
-        hipLaunchKernelGGL(dlogits_kernel, dim3((T + 3) / 4), dim3(NTH), 0, st, dgate_w, gate_w, expert_idx, logits, dlogits_add, T, E, k, renorm, dlogits);
-        const bool vec = E % 8 == 0 && (((uintptr_t)dlogits | (uintptr_t)w_gate) & 15) == 0;
+        auto first = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((T + 3) / 4), dim3(NTH), 0, st, dgate_w, gate_w, expert_idx, logits, dlogits_add, T, E, k, renorm, dlogits); };
+        E <= 64 ? first(dlogits_kernel<1>) : E <= 128 ? first(dlogits_kernel<2>) : first(dlogits_kernel<4>);
+        const int vec = (((uintptr_t)dlogits | (uintptr_t)w_gate | (uintptr_t)ws) & 15) != 0 ? 1 : E % 8 == 0 ? 8 : E % 4 == 0 ? 4 : 1;
         if (dx) dt == MOE_F32 ? launch_dx((const float*)w_gate, vec, dlogits, dx_add, T, d, E, dx, st) : launch_dx((const uint16_t*)w_gate, vec, dlogits, dx_add, T, d, E, dx, st);
         if (sums) {
             ranges = ranges_of(T, d, E);
             const int range = ((T + ranges - 1) / ranges + TC - 1) / TC * TC;
             const dim3 grid(dw_gate ? (d + 63) / 64 : 1, (E + 127) / 128, ranges);
             auto go = [&](auto kern, auto* from) { hipLaunchKernelGGL(kern, grid, dim3(NTH), 0, st, dw_gate ? from : nullptr, dlogits, T, d, E, range, (float*)ws); };
-            if (dt == MOE_F32) vec ? go(dw_kernel<float, true>, (const float*)x) : go(dw_kernel<float, false>, (const float*)x);
-            else vec ? go(dw_kernel<uint16_t, true>, (const uint16_t*)x) : go(dw_kernel<uint16_t, false>, (const uint16_t*)x);
+            by_vec(vec < 4 ? 1 : 4, [&](auto v) {          // (dl and the sums are fp32)
+                constexpr int V = decltype(v)::value == 8 ? 4 : decltype(v)::value;
+                dt == MOE_F32 ? go(dw_kernel<float, V>, (const float*)x) : go(dw_kernel<uint16_t, V>, (const uint16_t*)x);
+            });
         }
     }
     if (sums) {
