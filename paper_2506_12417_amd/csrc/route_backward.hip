@@ -125,6 +125,7 @@ typedef __attribute__((ext_vector_type(4))) unsigned short u16x4;
 typedef __attribute__((ext_vector_type(8))) unsigned short u16x8;
 typedef __attribute__((ext_vector_type(4))) unsigned int u32x4;
 constexpr unsigned NOWHERE = 0xFFFFFF00u;
+[[maybe_unused]] constexpr int NONTEMPORAL = 2;
 template <int VEC> __device__ __forceinline__ f32x8 fetch8(const float*, __amdgpu_buffer_rsrc_t rows, int n, unsigned r, int c, bool on) {
     const unsigned at = (r * (unsigned)n + (unsigned)c) * 4u;
     f32x8 v;
@@ -222,7 +223,7 @@ __global__ __launch_bounds__(NTH) void dx_kernel(const float* __restrict__ dl, c
             for (int h = 0; h < 2; ++h) {                  // (d is a multiple of 8)
                 const int c = c0 + lq * 4 + 16 * h;
                 __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[h] + here[n][h]), ro,
-                                                       c < last ? ((unsigned)(n * 16 + l16) * (unsigned)d + (unsigned)c) * 4u : NOWHERE, 0, 0);
+                                                       c < last ? ((unsigned)(n * 16 + l16) * (unsigned)d + (unsigned)c) * 4u : NOWHERE, 0, NONTEMPORAL);
             }
         }
     };
