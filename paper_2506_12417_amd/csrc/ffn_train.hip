@@ -64,9 +64,24 @@ __device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsign
 
 // A store of 16 bytes.  Its data registers may not be written in the instruction behind it: with an offset in a scalar register the compiler takes
 // that for safe, and with two wavefronts a SIMD the last lanes' first values came out as what was written there next.
-__device__ __forceinline__ void store_b128(u32x4 v, __amdgpu_buffer_rsrc_t r, unsigned voff, unsigned soff) {
-    __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, 0);
+// STREAM: past the caches, for results that are larger than these.  Only where an instruction writes whole lines of 128 bytes (halves of lines are
+// put together in the caches: a gradient stored so in halves took 15% longer, in whole lines 5% less), and to leave in them what is read again: a
+// backward pass of 512 tokens over 60 experts of 2048 x 1408 takes 342 us instead of 400, of 16384 tokens over 128 experts 980 instead of 1048.
+constexpr int STREAM = 2;
+template <int AUX = 0> __device__ __forceinline__ void store_b128(u32x4 v, __amdgpu_buffer_rsrc_t r, unsigned voff, unsigned soff) {
+    __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, AUX);
     asm volatile("s_nop 1" : : "v"(v) : "memory");         // (they live until behind it)
+}
+
+// Two pieces of 16 bytes of a row l16 of sixteen, 64 bytes apart, to whole lines for a store: rows l16 % 8 (a) and 8 + l16 % 8 (b), the second 64 bytes in
+// lanes 8 to 15.
+__device__ __forceinline__ void to_lines(u32x4& a, u32x4& b) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int lo = (int)a[i], hi = (int)b[i];
+        a[i] = (unsigned)__builtin_amdgcn_update_dpp(lo, hi, 0x128, 0xf, 0xc, false);      // (turned by eight lanes of sixteen)
+        b[i] = (unsigned)__builtin_amdgcn_update_dpp(hi, lo, 0x128, 0xf, 0x3, false);
+    }
 }
 
 // The lane's number, formed where it is used: held in a register over the loops it ends up in scratch memory, and the wait for its way back is one
@@ -357,18 +372,35 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
     const unsigned rc = (unsigned)it.rc;
     if constexpr (KIND == DX) {
         const __amdgpu_buffer_rsrc_t ro = make_rsrc(a.dx_perm + row0 * a.N, rc * (unsigned)a.N * 4u);
+        const unsigned ld = (unsigned)a.N * 4u, row = (unsigned)(wn * 32 + l16);
 #pragma unroll
         for (int ni = 0; ni < Nt<TR>::NI; ++ni) {
             if (ni >= ni_on) continue;
 #pragma unroll
             for (int n16 = 0; n16 < 2; ++n16) {
-                const unsigned at = (unsigned)((ni * 2 + wn) * 32 + n16 * 16 + l16) * (unsigned)a.N * 4u + (unsigned)lq * 32u;
+                const unsigned down = (unsigned)(ni * 64 + n16 * 16);
 #pragma unroll
-                for (int b = 0; b < 4; ++b)
-                    if (f0 + b * 32 < a.N) {
-                        store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][0]), ro, at, (unsigned)(f0 + b * 32) * 4u);
-                        store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][1]), ro, at + 16u, (unsigned)(f0 + b * 32) * 4u);
+                for (int b = 0; b < 4; ++b) {
+                    if (f0 + b * 32 >= a.N) continue;
+                    const unsigned col = (unsigned)(f0 + b * 32) * 4u;
+                    if constexpr (TR == 256) {             // (no registers for the exchange: the caches put the lines together)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) store_b128(__builtin_bit_cast(u32x4, acc[ni][n16][b][h]), ro, (row + down) * ld + (unsigned)(lq * 32 + h * 16), col);
+                    } else {
+                        // a lane has 32 bytes of a row: the halves of lanes 32 apart change places, then rows' halves
+                        u32x4 v[2];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const u32x2 p = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[ni][n16][b][0][i]), __float_as_uint(acc[ni][n16][b][1][i]), false, false);
+                            v[0][i] = p[0];
+                            v[1][i] = p[1];
+                        }
+                        to_lines(v[0], v[1]);
+                        const unsigned at = (row - (unsigned)(l16 & 8) + down) * ld + (unsigned)((l16 >> 3) * 64 + (lq & 1) * 32 + (lq >> 1) * 16);
+                        store_b128<STREAM>(v[0], ro, at, col);
+                        store_b128<STREAM>(v[1], ro, at + 8u * ld, col);
                     }
+                }
             }
         }
     } else if constexpr (KIND <= KEEP_SWIGLU) {
@@ -409,6 +441,7 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                         __builtin_amdgcn_raw_buffer_store_b64(w, rq, row * Z + (unsigned)lq * 8u, (unsigned)(zc + i * 32), 0);
                     }
                     if (!SW || p == 1) {
+                        u32x4 w[2];
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             if (SW) {                      // (v holds the ups)
@@ -417,9 +450,12 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
 #pragma unroll
                                 for (int c = 0; c < 8; ++c) v[i][c] *= g[c] * sigmoid(g[c]);
                             }
-                            const u32x4 w = {half_bits(v[i][0], v[i][1]), half_bits(v[i][2], v[i][3]), half_bits(v[i][4], v[i][5]), half_bits(v[i][6], v[i][7])};
-                            store_b128(w, rh, row * F * 2u + (unsigned)lq * 16u, (unsigned)((SW ? f0 / 2 : zc) + i * 32) * 2u);
+                            w[i] = u32x4{half_bits(v[i][0], v[i][1]), half_bits(v[i][2], v[i][3]), half_bits(v[i][4], v[i][5]), half_bits(v[i][6], v[i][7])};
                         }
+                        to_lines(w[0], w[1]);
+                        const unsigned at = (row - (unsigned)(l16 & 8)) * F * 2u + (unsigned)((l16 >> 3) * 64 + lq * 16);
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) store_b128(w[i], rh, at + (unsigned)i * F * 16u, (unsigned)(SW ? f0 / 2 : zc) * 2u);
                     }
                 }
             }
@@ -463,7 +499,8 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                     sc[to][m][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rs, so, ((unsigned)(f0 + m * a.F) / 64u + (j ? last : 0u)) * 4u, 0));
             }
         };
-        unsigned w_at = first_row * F * 2u + (unsigned)lq * 16u, z_at = first_row * Z * 2u + (unsigned)lq * 16u;
+        const unsigned line_row = first_row - (unsigned)(l16 & 8), in_line = (unsigned)((l16 >> 3) * 64 + lq * 16);
+        unsigned w_at = line_row * F * 2u + in_line, z_at = line_row * Z * 2u + in_line;
 #pragma unroll
         for (int g = 0; g < AHEAD; ++g) fetch(g);
 #pragma unroll
@@ -476,6 +513,7 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
             asm volatile("" : "+v"(w_at), "+v"(z_at));
             const unsigned wo = w_at + rows_of(g) * F * 2u, zo = z_at + rows_of(g) * Z * 2u;
             float dgate = 0.f;
+            u32x4 wh_b[2], dz0_b[2], dz1_b[2];             // of two blocks, for whole lines
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
                 if (b * 32 >= on) continue;
@@ -503,10 +541,21 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                     dgate = fmaf(h, s[c], dgate);
                     wh[c] = gate[g] * h;
                 }
-                const unsigned col = (unsigned)(f0 + b * 32) * 2u;
-                store_b128(to_bf16(wh), rw, wo, col);
-                store_b128(to_bf16(dz0), rz, zo, col);
-                if (SW) store_b128(to_bf16(dz1), rz, zo, col + F * 2u);
+                wh_b[b & 1] = to_bf16(wh);
+                dz0_b[b & 1] = to_bf16(dz0);
+                if (SW) dz1_b[b & 1] = to_bf16(dz1);
+                if (b & 1) {
+                    const unsigned col = (unsigned)(f0 + (b - 1) * 32) * 2u;
+                    to_lines(wh_b[0], wh_b[1]);
+                    to_lines(dz0_b[0], dz0_b[1]);
+                    if (SW) to_lines(dz1_b[0], dz1_b[1]);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        store_b128<STREAM>(wh_b[i], rw, wo + (unsigned)i * F * 16u, col);
+                        store_b128<STREAM>(dz0_b[i], rz, zo + (unsigned)i * Z * 16u, col);
+                        if (SW) store_b128<STREAM>(dz1_b[i], rz, zo + (unsigned)i * Z * 16u, col + F * 2u);
+                    }
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
             dgate = quarter_sum(dgate);
@@ -850,12 +899,16 @@ template <int TS, typename O, bool ADD> __device__ __forceinline__ void tn_finis
     const __amdgpu_buffer_rsrc_t ro = make_rsrc((unsigned char*)it.dw + (size_t)it.m0 * ld, (unsigned)(it.M - it.m0 < TS ? it.M - it.m0 : TS) * ld);
 #pragma unroll
     for (int m = 0; m < B; ++m) {
-        const unsigned row = (unsigned)(wn * (TS / 2) + m * 16 + l16) * ld;
+        // the lane's piece in a row: four fp32 columns of 16, or eight bf16 ones of 32 (below)
+        const unsigned in_row = ES == 4 ? (unsigned)lq * 16u : (unsigned)((lq & 1) * 16 + (lq >> 1) * 8) * 2u;
+        const unsigned from = (unsigned)(wn * (TS / 2) + m * 16 + l16) * ld + in_row;
+        const unsigned to = (unsigned)(wn * (TS / 2) + m * 16 + (l16 & 7)) * ld + (unsigned)(l16 >> 3) * 64u + in_row, to8 = to + 8u * ld;
         __builtin_amdgcn_sched_barrier(0);                 // (16 rows at a time: there are no registers for more)
 #pragma unroll
-        for (int n = 0; n < B; n += 2) {
-            if (c0 + n * 16 >= it.N) continue;
+        for (int n = 0; n < B; n += 128 / (16 * (int)ES)) {
+            if (c0 + n * 16 >= it.N) continue;             // (N is a multiple of 64)
             const unsigned col = (unsigned)(c0 + n * 16) * ES;
+            u32x4 out[2];
             if constexpr (ES == 4) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -866,27 +919,32 @@ template <int TS, typename O, bool ADD> __device__ __forceinline__ void tn_finis
                         asm volatile("" : "+v"(x));
                         v[r] = x;
                     }
-                    if (ADD) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u, 0));
-                    store_b128(__builtin_bit_cast(u32x4, v), ro, row + (unsigned)lq * 16u, col + (unsigned)i * 64u);
+                    if (ADD) v += __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, from, col + (unsigned)i * 64u, 0));
+                    out[i] = __builtin_bit_cast(u32x4, v);
                 }
             } else {
                 // a lane has columns 4 lq + r of two blocks of 16; lanes 16 apart exchange them, so that each has eight neighbours:
                 // columns 0, 16, 8, 24 .. + 7 for lq = 0 .. 3
-                float v[8];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const u32x2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[m][n][r]), __float_as_uint(acc[m][n + 1][r]), false, false);
-                    v[r] = __uint_as_float(p[0]);
-                    v[4 + r] = __uint_as_float(p[1]);
-                }
-                const unsigned at = row + (unsigned)((lq & 1) * 16 + (lq >> 1) * 8) * 2u;
-                if (ADD) {
-                    const u32x4 old = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, at, col, 0));
+                for (int i = 0; i < 2; ++i) {
+                    float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] += __uint_as_float(i & 1 ? old[i >> 1] & 0xffff0000u : old[i >> 1] << 16);
+                    for (int r = 0; r < 4; ++r) {
+                        const u32x2 p = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[m][n + 2 * i][r]), __float_as_uint(acc[m][n + 2 * i + 1][r]), false, false);
+                        v[r] = __uint_as_float(p[0]);
+                        v[4 + r] = __uint_as_float(p[1]);
+                    }
+                    if (ADD) {
+                        const u32x4 old = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ro, from, col + (unsigned)i * 64u, 0));
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(e & 1 ? old[e >> 1] & 0xffff0000u : old[e >> 1] << 16);
+                    }
+                    out[i] = to_bf16(v);
                 }
-                store_b128(to_bf16(v), ro, at, col);
             }
+            to_lines(out[0], out[1]);
+            store_b128<STREAM>(out[0], ro, to, col);
+            store_b128<STREAM>(out[1], ro, to8, col);
         }
     }
 }
