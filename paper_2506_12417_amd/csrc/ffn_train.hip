@@ -15,9 +15,9 @@
 // that these start without a pause.  The fragments of the next 32 terms are read while those before are multiplied.
 //
 // Measured (us: the first product in 8 bits, its counterpart in the backward pass, dx, dW; parts of the whole calls):
-//   8192 tokens, top-4 of 60 experts of 2048 x 1408, SwiGLU        450   310   475   965     0.84, 0.61, 0.80, 0.59 PFLOP/s
-//   16384 tokens, top-1 of 128 experts of 768 x 4 768, ReLU              226   177   540
-//   8192 tokens, top-2 of 8 experts of 4096 x 14336, SwiGLU             2120  3690  5420     0.91, 1.04, 1.06 PFLOP/s
+//   8192 tokens, top-4 of 60 experts of 2048 x 1408, SwiGLU     450   304   444   893     0.84, 0.62, 0.85, 0.63 PFLOP/s
+//   16384 tokens, top-1 of 128 experts of d = 768, F = 4 d             225   193   506
+//   8192 tokens, top-2 of 8 experts of 4096 x 14336, SwiGLU           2116  3650  5303     0.91, 1.05, 1.09 PFLOP/s
 // What bounds them now.  The loops: the way from the L2s to LDS and the matrix instructions together (dW: 64 KB a stage of 64 rows, 1.4 us for the
 // fetch alone, 2.0 with its multiplications; the L2s deliver 8.5 TB/s, the matrix units are busy 60% of the time).  An item's end: nothing covers the
 // epilogue (13 us of the backward pass's first product, mostly vector instructions), and loads behind an item's stores are counted behind
@@ -75,7 +75,7 @@ __device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsign
 // that for safe, and with two wavefronts a SIMD the last lanes' first values came out as what was written there next.
 // STREAM: past the caches, for results that are larger than these.  Only where an instruction writes whole lines of 128 bytes (halves of lines are
 // put together in the caches: a gradient stored so in halves took 15% longer, in whole lines 5% less), and to leave in them what is read again: a
-// backward pass of 100 tokens over 128 experts of 768 x 4 768 takes 342 us instead of 400, of 16384 tokens 980 instead of 1048.
+// backward pass of 100 tokens over 128 experts of d = 768, F = 4 d, takes 342 us instead of 400, of 16384 tokens 980 instead of 1048.
 constexpr int STREAM = 2;
 template <int AUX = 0> __device__ __forceinline__ void store_b128(u32x4 v, __amdgpu_buffer_rsrc_t r, unsigned voff, unsigned soff) {
     __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, AUX);
@@ -1110,7 +1110,7 @@ template <int TS, typename O, bool ADD> int launch_tn(const TnArgs& a, hipStream
     return MOE_OK;
 }
 // Tiles of 128 where those of 256 would leave CUs without one: four experts of 512 x 512 over 8192 rows 36 us instead of 67, one of 512 x 1024 88 instead of
-// 174.  Elsewhere they fetch twice the bytes for a product: 128 experts of 768 x 4 768 over 16384 rows 649 instead of 545.
+// 174.  Elsewhere they fetch twice the bytes for a product: 128 experts of d = 768, F = 4 d, over 16384 rows 649 instead of 545.
 template <typename O, bool ADD> int launch_tn_tile(const TnArgs& a, hipStream_t st) {
     const long long tiles = (long long)a.E * a.mats * ((a.d + 255) / 256) * ((a.F + 255) / 256);
     return tiles <= MOE_GEMM_GRID ? launch_tn<128, O, ADD>(a, st) : launch_tn<256, O, ADD>(a, st);

@@ -4,8 +4,8 @@
 //   moe_permute_backward             dx[t] = dx_add[t] + sum_j dx_perm[inv_perm[t k + j]]
 //
 // HBM bound: every row is read once and written once, past the caches, whole lines an instruction.  An assignment without a row (inv_perm negative)
-// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048: 62 us for 436 MB and 60 us for 370 MB; with eight neighbouring columns a lane, so that
-// fp32 rows were moved in halves of 32 bytes, 74 and 65.
+// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 97 us for 436 MB and 65 us for 370 MB (one after the
+// other 157; with eight neighbouring columns a lane, so that fp32 rows were moved in halves of 32 bytes, 165).
 #include "common.h"
 #include "gemm_util.h"
 #include "lanes.h"
