@@ -4,7 +4,8 @@
 //   moe_permute_backward             dx[t] = dx_add[t] + sum_j dx_perm[inv_perm[t k + j]]
 //
 // HBM bound: every row is read once and written once, past the caches, whole lines an instruction.  An assignment without a row (inv_perm negative)
-// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 97 us for 436 MB and 65 us for 370 MB (one after the
+// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 90 us for 436 MB and 65 us for 370 MB (before the
+// combine loaded a piece ahead 94; both one after the
 // other 157; with eight neighbouring columns a lane, so that fp32 rows were moved in halves of 32 bytes, 165).
 #include "common.h"
 #include "gemm_util.h"
@@ -87,46 +88,88 @@ __device__ __forceinline__ float wave_sum(float v) {
            (__int_as_float(__builtin_amdgcn_readlane(b, 32)) + __int_as_float(__builtin_amdgcn_readlane(b, 48)));
 }
 
-// A wavefront has a token; its rows go GROUP at a time, so that dy is fetched once for up to four of them.
+// The same through a buffer descriptor of the row, without branches (behind these the compiler waits for all loads that are under way): what lies behind the
+// row's end, or in a row that is none, reads as zero.
+[[maybe_unused]] constexpr int NONTEMPORAL = 2;
+template <bool VEC> __device__ __forceinline__ void fetch(const float*, __amdgpu_buffer_rsrc_t row, int piece, int lane, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += VEC ? 4 : 1) {
+        const unsigned at = (unsigned)col_of<VEC>(piece, lane, i) * 4u;
+        if constexpr (VEC) {
+            const f32x4 a = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(row, at, 0, NONTEMPORAL));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = a[j];
+        } else {
+            v[i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(row, at, 0, NONTEMPORAL));
+        }
+    }
+}
+template <bool VEC> __device__ __forceinline__ void fetch(const uint16_t*, __amdgpu_buffer_rsrc_t row, int piece, int lane, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i += VEC ? 4 : 1) {
+        const unsigned at = (unsigned)col_of<VEC>(piece, lane, i) * 2u;
+        if constexpr (VEC) {
+            const u32x2 a = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(row, at, 0, NONTEMPORAL));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = __uint_as_float(j & 1 ? a[j >> 1] & 0xffff0000u : a[j >> 1] << 16);
+        } else {
+            v[i] = bf16_to_f32((uint16_t)__builtin_amdgcn_raw_buffer_load_b16(row, at, 0, NONTEMPORAL));
+        }
+    }
+}
+
+// A wavefront has a token; its rows go GROUP at a time, so that dy is fetched once for up to four of them.  A piece's loads are issued before the stores of
+// the piece before it: loads and stores are counted together, a load behind stores waits for their way to memory.
 template <typename D, typename P, bool VEC>
 __global__ __launch_bounds__(NTH) void combine_backward_kernel(const D* __restrict__ dy, const float* __restrict__ y_perm, const int32_t* __restrict__ inv_perm,
                                                                const float* __restrict__ gate_w, int T, int d, int k, P* __restrict__ dy_perm,
                                                                float* __restrict__ dgate_w) {
+#ifdef __HIP_DEVICE_COMPILE__                              // (the host's pass has no buffer descriptors)
     const int t = sgpr((int)(blockIdx.x * (NTH / 64) + (threadIdx.x >> 6))), lane = threadIdx.x & 63;
     if (t >= T) return;
-    const D* from = dy + (size_t)t * d;
+    const __amdgpu_buffer_rsrc_t from = make_rsrc(dy + (size_t)t * d, (unsigned)d * (unsigned)sizeof(D));
+    const int pieces = (d + 511) / 512;
     for (int j0 = 0; j0 < k; j0 += GROUP) {
         int row[GROUP];
         float w[GROUP], sum[GROUP];
+        __amdgpu_buffer_rsrc_t ys[GROUP];
 #pragma unroll
         for (int j = 0; j < GROUP; ++j) {
             const size_t a = (size_t)t * k + j0 + j;
             const bool on = j0 + j < k;
-            row[j] = on ? inv_perm[a] : -1;
+            row[j] = sgpr(on ? inv_perm[a] : -1);
             w[j] = on && gate_w ? gate_w[a] : 1.f;
             sum[j] = 0.f;
+            ys[j] = make_rsrc(y_perm + (size_t)(row[j] < 0 ? 0 : row[j]) * d, dgate_w && row[j] >= 0 ? (unsigned)d * 4u : 0u);
         }
-        for (int piece = 0; piece * 512 < d; ++piece) {
-            float g[8], y[GROUP][8];
-            fetch<VEC>(from, d, piece, lane, true, g);
-            if (dgate_w) {
+        struct Piece { float g[8], y[GROUP][8]; };
+        auto load = [&](int piece, Piece& p) {
+            fetch<VEC>(dy, from, piece, lane, p.g);
 #pragma unroll
-                for (int j = 0; j < GROUP; ++j) fetch<VEC>(y_perm + (size_t)(row[j] < 0 ? 0 : row[j]) * d, d, piece, lane, row[j] >= 0, y[j]);
+            for (int j = 0; j < GROUP; ++j) fetch<VEC>(y_perm, ys[j], piece, lane, p.y[j]);
+        };
+        auto step = [&](int piece, const Piece& here, Piece& next) {
+            load(piece + 1, next);                         // (behind the last: zeros)
 #pragma unroll
-                for (int j = 0; j < GROUP; ++j)
+            for (int j = 0; j < GROUP; ++j)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sum[j] = fmaf(g[i], y[j][i], sum[j]);
-            }
+                for (int i = 0; i < 8; ++i) sum[j] = fmaf(here.g[i], here.y[j][i], sum[j]);
             if (dy_perm) {
 #pragma unroll
                 for (int j = 0; j < GROUP; ++j) {
                     if (row[j] < 0) continue;
                     float v[8];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) v[i] = w[j] * g[i];
+                    for (int i = 0; i < 8; ++i) v[i] = w[j] * here.g[i];
                     put<VEC>(dy_perm + (size_t)row[j] * d, d, piece, lane, v);
                 }
             }
+        };
+        Piece a, b;
+        load(0, a);
+        for (int piece = 0; piece < pieces; piece += 2) {
+            step(piece, a, b);
+            if (piece + 1 < pieces) step(piece + 1, b, a);
         }
         if (dgate_w) {
 #pragma unroll
@@ -136,6 +179,7 @@ __global__ __launch_bounds__(NTH) void combine_backward_kernel(const D* __restri
             }
         }
     }
+#endif
 }
 
 template <typename P, bool VEC>
@@ -174,7 +218,7 @@ extern "C" int moe_unpermute_combine_backward(const void* dy, moe_dtype dy_dt, c
                                               int k, void* dy_perm, moe_dtype perm_dt, float* dgate_w, void* stream) {
     MOE_REQUIRE(T >= 0 && d >= 1 && k >= 1, MOE_ERR_ARG, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
     MOE_REQUIRE(moe_dtype_ok(dy_dt) && moe_dtype_ok(perm_dt), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: dtypes %d, %d", (int)dy_dt, (int)perm_dt);
-    MOE_REQUIRE((long long)T * k < (1ll << 31) && T < (1 << 26), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: T=%d k=%d", T, k);
+    MOE_REQUIRE((long long)T * k < (1ll << 31) && T < (1 << 26) && d < (1 << 29), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(dy && inv_perm && (dy_perm || dgate_w) && (y_perm || !dgate_w), MOE_ERR_ARG, "moe_unpermute_combine_backward: null pointer");
     const bool vec = whole_pieces(d, {dy, y_perm, dy_perm});

@@ -98,6 +98,7 @@ def test_combine_and_permute_arguments():
         assert permute(**{a: None}) == B.MOE_ERR_ARG
     # more threads than a launch has
     assert combine(T=2 ** 26, k=1) == B.MOE_ERR_UNSUPPORTED and permute(T=2 ** 26, k=1) == B.MOE_ERR_UNSUPPORTED and permute(T=2 ** 20, d=2 ** 16) == B.MOE_ERR_UNSUPPORTED
+    assert combine(T=1, d=2 ** 29) == B.MOE_ERR_UNSUPPORTED
     assert rows(rows=2 ** 29, n=64) == B.MOE_ERR_UNSUPPORTED and restore(rows=2 ** 23, n=4096) == B.MOE_ERR_UNSUPPORTED
 
 
