@@ -4,9 +4,8 @@
 //   moe_permute_backward             dx[t] = dx_add[t] + sum_j dx_perm[inv_perm[t k + j]]
 //
 // HBM bound: every row is read once and written once, past the caches, whole lines an instruction.  An assignment without a row (inv_perm negative)
-// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 90 us for 436 MB and 65 us for 370 MB (before the
-// combine loaded a piece ahead 94; both one after the
-// other 157; with eight neighbouring columns a lane, so that fp32 rows were moved in halves of 32 bytes, 165).
+// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 90 us for 436 MB and 65 us for 370 MB.
+// (With eight neighbouring columns a lane, so that fp32 rows were moved in halves of 32 bytes, a pass of both took 8 us more.)
 #include "common.h"
 #include "gemm_util.h"
 #include "lanes.h"
