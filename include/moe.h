@@ -471,7 +471,7 @@ MOE_API int moe_unpermute_combine(const float* y_perm, const int32_t* inv_perm, 
  *
  * Kept in 8 bits: 64 neighbouring columns of a row (fewer at its end) share a scale,
  *
- *   m = the largest |v| of the 64      scale = m / 127      q = 127 v / m to the nearest integer      read back: q * scale
+ *   m = the largest |v| of the 64      scale = m / 127      q = 127 v / m to the nearest integer, ties to even      read back: q * scale
  *
  * so that a value is off by at most m / 254.  Where one of the 64 is NaN or infinite all of them read back as NaN; where m is below 2^-100
  * as 0.
@@ -484,7 +484,7 @@ MOE_API int moe_keep_restore(const int8_t* q, const float* scale, long long rows
 /* The first product of moe_grouped_ffn, which keeps its result z for the backward pass.  With r, e, t as there and Z = F (MOE_RELU) or 2F (MOE_SWIGLU):
  *
  *   z[r] = x[perm[r] / k] W_in_e  (MOE_SWIGLU: F gates, then F ups)      h_scratch[r] = relu(z), or silu(gate) * up, as moe_grouped_ffn has it
- *   z_q, z_scale = z in 8 bits as above; with MOE_RELU relu(z), where a value above zero is kept as at least one step of its scale, so that the
+ *   z_q, z_scale = z in 8 bits as above (within 2^-15 of a tie either way); with MOE_RELU relu(z), where a value above zero is kept as at least one step of its scale, so that the
  *   activation's slope is not lost (in a block whose largest value is at least 2^-100)
  *
  *   x [T,d] dt      w_in: as moe_grouped_ffn      offsets [E+1], perm [A]: from the sort      h_scratch [A,F] 2 bytes a value, out: what

@@ -2,6 +2,7 @@
 //
 //   m = max |v| of the block     scale = m / 127     q = v 127 / m to the nearest integer, ties to even     read back: q scale
 //
+// (ffn_train.hip multiplies by a reciprocal, which is off by 2^-15 of a step at most: ties go either way.)
 // The error is at most half a scale, m / 254.  POSITIVE (ReLU): negative values are kept as 0 and what is above zero as at least 1, so that the
 // activation's slope is not lost.  A block that holds an infinity or a NaN has a scale of NaN; one whose m is below
 // MOE_KEEP_LEAST is kept as zeros (127 / m would leave fp32's range).
@@ -34,6 +35,15 @@ template <bool POSITIVE> __device__ __forceinline__ unsigned keep_value(float v,
     float q = v * to_q;
     if (POSITIVE) q = v > 0.f && to_q > 0.f ? __builtin_fmaxf(q, 1.f) : 0.f;
     return __float_as_uint(q + 12582912.f);
+}
+// The same to the nearest for certain: 127 v - q m tells on which side of the tie the quotient lies (m and v are brought down, exactly, so
+// that it has room).  m: the block's largest magnitude.
+__device__ __forceinline__ unsigned keep_nearest(float v, float m, float to_q) {
+    const float q = __builtin_rintf(v * to_q), down = to_q > 0.f ? m * 0x1p-16f : __builtin_inff();
+    const float p = q * down, rest = fmaf(q, down, -p), twice = 2.f * (fmaf(v * 0x1p-16f, 127.f, -p) - rest);
+    const bool odd = ((int)q & 1) != 0;
+    const float up = twice > down || (twice == down && odd) ? 1.f : 0.f, less = twice < -down || (twice == -down && odd) ? 1.f : 0.f;
+    return __float_as_uint(q + (up - less) + 12582912.f);
 }
 // the low bytes of four words
 __device__ __forceinline__ unsigned pack_bytes(unsigned a, unsigned b, unsigned c, unsigned d) {

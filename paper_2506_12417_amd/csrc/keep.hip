@@ -55,17 +55,18 @@ __global__ __launch_bounds__(NTH) void keep_rows_kernel(const E* __restrict__ x,
     most = max_u32(most, (unsigned)dpp_xchg<2>((int)most));
     if (!on) return;
     const KeepScale k = keep_scale(most);
+    auto nearest = [&](float a) { return keep_nearest(a, __uint_as_float(most), k.to_q); };
     if (l8 == 0) scale[at] = k.scale;
     int8_t* to = q + row * n;
     if constexpr (VEC) {
         const int c = col_of<true>(block, l8, 0);
-        const u32x2 w = {keep_four<false>(v[0], v[1], v[2], v[3], k.to_q), keep_four<false>(v[4], v[5], v[6], v[7], k.to_q)};
+        const u32x2 w = {pack_bytes(nearest(v[0]), nearest(v[1]), nearest(v[2]), nearest(v[3])), pack_bytes(nearest(v[4]), nearest(v[5]), nearest(v[6]), nearest(v[7]))};
         if (c < n) *(u32x2*)(to + c) = w;
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int c = col_of<false>(block, l8, i);
-            if (c < n) to[c] = (int8_t)keep_value<false>(v[i], k.to_q);
+            if (c < n) to[c] = (int8_t)nearest(v[i]);
         }
     }
 }

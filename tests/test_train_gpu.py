@@ -75,6 +75,24 @@ def test_keep_rows_special_values():
         assert ((out[i, :64] / x[i, :64] - 1).abs() < 1e-6).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("odd", [0, 1])
+def test_keep_rows_ties(dtype, odd):
+    """127 v / m = n + 1/2 exactly, of values that both types hold: to the even neighbour."""
+    torch, B, dev = _gpu()
+    n = torch.arange(126, dtype=torch.float64, device=dev).reshape(2, 63)
+    v = torch.cat([torch.full((2, 1), 127 / 128, dtype=torch.float64, device=dev), (2 * n + 1) / 256], 1)
+    want = torch.cat([torch.full((2, 1), 127.0, dtype=torch.float64, device=dev), torch.round((n + 0.5))], 1)
+    assert (want[:, 1:] % 2 == 0).all()
+    x = torch.cat([torch.cat([v, -v]) * 2.0 ** e for e in (-99, -3, 0, 1, 128)]).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    assert (x.double()[8:12] == torch.cat([v, -v])).all()
+    hold = torch.empty(x.numel() + 1, dtype=x.dtype, device=dev)
+    hold[odd:odd + x.numel()] = x.reshape(-1)
+    q, scale = torch.empty(x.shape, dtype=torch.int8, device=dev), torch.empty((x.shape[0], 1), device=dev)
+    B.moe_keep_rows(hold[odd:], B.dtype_code(x), x.shape[0], 64, q, scale)
+    assert (q.double() == torch.cat([want, -want] * 5)).all()
+
+
 # ------------------------------------------------------------------------------------------------ the experts
 SHAPES = [  # T, d, F, E, k, act, kind of routing
     (1, 64, 64, 1, 1, "relu", {}),
