@@ -1,6 +1,6 @@
 // moe_keep_rows and moe_keep_restore: rows of activations kept in 8 bits with a scale for every 64 columns (keep.h), and read back.
 // Eight lanes hold a block, eight values each, so that its largest value takes three exchanges inside a row of lanes.  HBM bound: 8192 x 2048
-// in fp32 there and back in 26.5 us (136 MB, 5.1 TB/s), rows of 777 values, one by one, 1501 of them in 9.7 us, of which most is the two launches.
+// in fp32 there and back in 27 us (136 MB, 5.0 TB/s), rows of 777 values, one by one, 1501 of them in 9.5 us, of which most is the two launches.
 #include "common.h"
 #include "keep.h"
 #include "lanes.h"

@@ -4,7 +4,7 @@
 //   moe_permute_backward             dx[t] = dx_add[t] + sum_j dx_perm[inv_perm[t k + j]]
 //
 // HBM bound: every row is read once and written once, past the caches, whole lines an instruction.  An assignment without a row (inv_perm negative)
-// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 90 us for 436 MB and 65 us for 370 MB.
+// has dgate_w 0 and adds nothing.  8192 tokens, k = 4, d = 2048, rows in fp32, the rest in bf16: 92 us for 436 MB and 65 us for 370 MB.
 // (With eight neighbouring columns a lane, so that fp32 rows were moved in halves of 32 bytes, a pass of both took 8 us more.)
 #include "common.h"
 #include "gemm_util.h"
