@@ -95,6 +95,48 @@ def _reads_writes(code: str):
     return read, written
 
 
+def _control_flow(body: str):
+    """A kernel's basic blocks (a label starts one, a branch ends one) and each block's successors."""
+    blocks, cur, label_of = [], {"label": None, "code": []}, {}
+    for raw in body.split("\n"):
+        line = raw.split(";")[0].strip().replace("\t", " ")
+        if not line:
+            continue
+        lm = re.fullmatch(r"(\.LBB\w+):", line)
+        if lm:
+            if cur["code"] or cur["label"]:
+                blocks.append(cur)
+            cur = {"label": lm.group(1), "code": []}
+            continue
+        if line.startswith("."):
+            continue
+        cur["code"].append(line)
+        if line.startswith("s_branch") or line.startswith("s_cbranch") or line.startswith("s_endpgm") or line.startswith("s_setpc"):
+            blocks.append(cur)
+            cur = {"label": None, "code": []}
+    if cur["code"] or cur["label"]:
+        blocks.append(cur)
+    for i, b in enumerate(blocks):
+        if b["label"]:
+            label_of[b["label"]] = i
+    succ = []
+    for i, b in enumerate(blocks):
+        s_ = []
+        last = b["code"][-1] if b["code"] else ""
+        if last.startswith("s_branch"):
+            s_.append(label_of[last.split()[1]])
+        elif last.startswith("s_cbranch"):
+            s_.append(label_of[last.split()[1]])
+            if i + 1 < len(blocks):
+                s_.append(i + 1)
+        elif last.startswith("s_endpgm") or last.startswith("s_setpc"):
+            pass
+        elif i + 1 < len(blocks):
+            s_.append(i + 1)
+        succ.append(s_)
+    return blocks, succ
+
+
 def check_stream_registers(asm_text: str):
     """The kernels of ffn_stream.hip load their weights with buffer_load_dwordx4 written as
     assembly: the compiler neither tracks nor waits for these loads (the kernel waits itself), it
@@ -112,44 +154,7 @@ def check_stream_registers(asm_text: str):
         return [("(none)", "no gemm_stream_kernel found in the assembly")]
     for m in kernels:
         kernel, body = m.group(1), m.group(2)
-        # basic blocks: a label starts one, a branch ends one
-        blocks, cur, label_of = [], {"label": None, "code": []}, {}
-        for raw in body.split("\n"):
-            line = raw.split(";")[0].strip()
-            if not line:
-                continue
-            lm = re.fullmatch(r"(\.LBB\w+):", line)
-            if lm:
-                if cur["code"] or cur["label"]:
-                    blocks.append(cur)
-                cur = {"label": lm.group(1), "code": []}
-                continue
-            if line.startswith("."):
-                continue
-            cur["code"].append(line)
-            if line.startswith("s_branch") or line.startswith("s_cbranch") or line.startswith("s_endpgm") or line.startswith("s_setpc"):
-                blocks.append(cur)
-                cur = {"label": None, "code": []}
-        if cur["code"] or cur["label"]:
-            blocks.append(cur)
-        for i, b in enumerate(blocks):
-            if b["label"]:
-                label_of[b["label"]] = i
-        succ = []
-        for i, b in enumerate(blocks):
-            s_ = []
-            last = b["code"][-1] if b["code"] else ""
-            if last.startswith("s_branch"):
-                s_.append(label_of[last.split()[1]])
-            elif last.startswith("s_cbranch"):
-                s_.append(label_of[last.split()[1]])
-                if i + 1 < len(blocks):
-                    s_.append(i + 1)
-            elif last.startswith("s_endpgm") or last.startswith("s_setpc"):
-                pass
-            elif i + 1 < len(blocks):
-                s_.append(i + 1)
-            succ.append(s_)
+        blocks, succ = _control_flow(body)
         n_loads = sum(1 for b in blocks for c in b["code"] if _STREAM_LOAD.fullmatch(c))
         if n_loads == 0:
             bad.append((kernel, "no weight load found"))
@@ -213,6 +218,88 @@ def check_no_flat_access(asm_text: str):
         code = line.split(";")[0].strip()
         if kernel and "gemm_" in kernel and re.match(r"flat_(load|store|atomic)", code):
             bad.append((kernel, code))
+    return bad
+
+
+_SREG = re.compile(r"(?<!\w)(?:s\[(\d+):(\d+)\]|s(\d+)(?!\w)|(vcc_lo|vcc_hi|vcc)(?!\w))")
+_VCC = {"vcc": {106, 107}, "vcc_lo": {106}, "vcc_hi": {107}}
+_MEMORY = ("buffer_", "global_", "flat_", "scratch_")
+# (their second operand, a carry, is written too)
+_CARRY_OUT = ("v_add_co", "v_sub_co", "v_subrev_co", "v_addc_co", "v_subb_co", "v_subbrev_co", "v_div_scale", "v_mad_u64", "v_mad_i64")
+
+
+def _sgprs(text: str):
+    out = set()
+    for m in _SREG.finditer(text):
+        if m.group(4):
+            out |= _VCC[m.group(4)]
+        elif m.group(3):
+            out.add(int(m.group(3)))
+        else:
+            out |= set(range(int(m.group(1)), int(m.group(2)) + 1))
+    return out
+
+
+def check_scalar_wait_states(asm_text: str):
+    """The hardware does not check that a scalar register which a vector instruction writes (v_readfirstlane, v_readlane, a
+    comparison, a carry) has arrived where it is read: a vector memory instruction needs five wait states between, a lane
+    read's index four, any other vector instruction two.  The compiler sees to that between its own instructions and knows
+    nothing of those in inline assembly.  Walks every kernel's control flow with the wait states since each such write (an
+    instruction is one, s_nop N is N + 1) and returns (kernel, instruction) violations."""
+    bad = []
+    for m in re.finditer(r"^(_Z\w+):[^\n]*\n(.*?)\.Lfunc_end", asm_text, flags=re.S | re.M):
+        blocks, succ = _control_flow(m.group(2))
+        code = []                      # of each block: (instruction, read, needed, written by a vector instruction, by a scalar one, states)
+        for b in blocks:
+            rows = []
+            for c in b["code"]:
+                op, _, rest = c.partition(" ")
+                ops = rest.split(",")
+                read, late, early, need, states = set(), set(), set(), 0, 1
+                if op.startswith(_MEMORY):
+                    read, need = _sgprs(rest), 5
+                elif op.startswith(("v_cmp", "v_readfirstlane", "v_readlane")):
+                    late = _VCC["vcc"] if op.startswith("v_cmp") and op.endswith("_e32") else _sgprs(ops[0])
+                    read, need = _sgprs(",".join(ops[1:])), 4 if op.startswith("v_readlane") else 2
+                elif op.startswith(_CARRY_OUT) and len(ops) > 2:
+                    late, read, need = _sgprs(ops[1]), _sgprs(",".join(ops[2:])), 2
+                elif op.startswith("v_"):
+                    read, need = _sgprs(",".join(ops[1:])), 2
+                elif op == "s_nop":
+                    states = int(rest, 0) + 1
+                elif op.startswith("s_") and not op.startswith(("s_cmp", "s_bitcmp", "s_waitcnt", "s_barrier", "s_branch", "s_cbranch")):
+                    early = _sgprs(ops[0])
+                if need == 2:
+                    read = read - _VCC["vcc"]           # (carries and selects, which have their own path)
+                rows.append((c, read, need, late, early, states))
+            code.append(rows)
+
+        def walk(i, since, report=None):
+            since = dict(since)
+            for c, read, need, late, early, states in code[i]:
+                if report is not None and any(since.get(r, 9) < need for r in read):
+                    report.append((m.group(1), c))
+                since = {r: n + states for r, n in since.items() if n + states < 5 and r not in early}
+                for r in late:
+                    since[r] = 0
+            return since
+
+        entry, work = [None] * len(blocks), [0] if blocks else []
+        if blocks:
+            entry[0] = {}
+        while work:
+            i = work.pop()
+            out = walk(i, entry[i])
+            for j in succ[i]:
+                if entry[j] is None:
+                    entry[j] = dict(out)
+                    work.append(j)
+                elif any(entry[j].get(r, 9) > n for r, n in out.items()):
+                    entry[j].update({r: n for r, n in out.items() if entry[j].get(r, 9) > n})
+                    work.append(j)
+        for i in range(len(blocks)):
+            if entry[i] is not None:
+                walk(i, entry[i], bad)
     return bad
 
 
@@ -301,6 +388,9 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     bad = check_training_kernels(open(asm_paths[-1]).read())
     if bad:
         raise RuntimeError("ffn_train.hip: loads to LDS or stores that the compiler has taken apart:\n%s" % "\n".join("  %s: %s" % b for b in bad[:20]))
+    bad = check_scalar_wait_states(open(asm_paths[-1]).read())
+    if bad:
+        raise RuntimeError("ffn_train.hip: scalar registers read too soon after a vector instruction's write:\n%s" % "\n".join("  %s: %s" % b for b in bad[:20]))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:

@@ -57,18 +57,27 @@ __device__ __forceinline__ u32x4 descriptor(const void* p, unsigned bytes) {
     const uint64_t u = (uint64_t)p;
     return u32x4{(unsigned)sgpr((int)(unsigned)u), (unsigned)sgpr((int)(unsigned)(u >> 32)) & 0xffffu, (unsigned)sgpr((int)bytes), 0x00020000u};
 }
+// What a load below may read: the words in scalar registers, which a vector instruction (the lane read that brings them there, where the compiler holds
+// them in vector registers over a loop) has not written for five wait states.  The hardware does not check this, and the compiler sees to it for
+// its own loads only; the build counts the states in the assembly.  Once for a half's loads: a lane read of each word in front of each load leaves two.
+__device__ __forceinline__ u32x4 scalars(const u32x4& r) {
+    return u32x4{(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
+}
+__device__ __forceinline__ u32x4 settled(const u32x4& r) {
+    u32x4 d = scalars(r);
+    asm volatile("s_nop 4" : "+s"(d));
+    return d;
+}
 // 16 bytes a lane to LDS at base + at (bytes, wave-uniform) + 16 lane, from voff + add (the sum saturates: an offset beyond everything stays that);
 // only this one is range-checked, soff is not.  (M0 may not be used in the instruction behind the one that sets it: the sum stands between.)
 __device__ __forceinline__ void load_to_lds(const u32x4& r, unsigned base, unsigned at, unsigned voff, unsigned add, unsigned soff) {
-    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
     unsigned sum;
     asm volatile("s_add_u32 m0, %1, %2\n\tv_add_u32_e64 %0, %3, %4 clamp\n\tbuffer_load_dwordx4 %0, %5, %6 offen lds"
-                 : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "s"(add), "s"(d), "s"(soff) : "memory", "scc");
+                 : "=&v"(sum) : "s"(base), "i"(at), "v"(voff), "s"(add), "s"(r), "s"(soff) : "memory", "scc");
 }
 // 4 bytes a lane
 __device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsigned voff) {
-    const u32x4 d = {(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(d) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(to), "v"(voff), "s"(r) : "memory");
 }
 
 // A store of 16 bytes.  Its data registers may not be written in the instruction behind it: with an offset in a scalar register the compiler takes
@@ -235,7 +244,7 @@ struct NtWork {
 // (gather) the assignments of an item's rows: eight items' tables in turn
 template <int TR> __device__ __forceinline__ void nt_fetch_rows(const NtArgs& a, const NtWork& w, const NtItem& it, int seq) {
     if (w.wave * 64 < TR)
-        load_to_lds4(descriptor(a.perm + it.row0, (unsigned)it.rc * 4u), w.rinfo + (unsigned)((seq & 7) * TR + w.wave * 64) * 4u, (unsigned)(w.wave * 64 + w.lane) * 4u);
+        load_to_lds4(settled(descriptor(a.perm + it.row0, (unsigned)it.rc * 4u)), w.rinfo + (unsigned)((seq & 7) * TR + w.wave * 64) * 4u, (unsigned)(w.wave * 64 + w.lane) * 4u);
 }
 
 template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs& a, const NtWork& w, const Sums& tiles, const int* rinfo, NtLoader<TR>& L) {
@@ -270,17 +279,22 @@ template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs
 }
 
 // load Q of the loader's stage (the features first)
-template <int KIND, int TR, int Q> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L) {
+struct NtFrom { u32x4 rr, rf; };
+// (but for DX the compiler keeps both in scalar registers: copies of them would only take more)
+template <int KIND, int TR> __device__ __forceinline__ NtFrom nt_from(const NtLoader<TR>& L) {
+    return KIND == DX ? NtFrom{settled(L.rr), settled(L.rf)} : NtFrom{scalars(L.rr), scalars(L.rf)};
+}
+template <int KIND, int TR, int Q> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const NtFrom& from) {
     const unsigned to = w.ring + (unsigned)(L.buf * Nt<TR>::STAGE + w.wave * 1024);
     if constexpr (Q < Nt<TR>::NFL)
-        load_to_lds(L.rf, to, Q * 4096, L.vf, (unsigned)(Q * 32) * (unsigned)a.ld_w * 2u, (unsigned)(KIND == DX && L.kt >= a.KT0 ? L.kt - a.KT0 : L.kt) * 128u);
+        load_to_lds(from.rf, to, Q * 4096, L.vf, (unsigned)(Q * 32) * (unsigned)a.ld_w * 2u, (unsigned)(KIND == DX && L.kt >= a.KT0 ? L.kt - a.KT0 : L.kt) * 128u);
     else
-        load_to_lds(L.rr, to, Nt<TR>::F_BYTES + (Q - Nt<TR>::NFL) * 4096, L.vr[Q - Nt<TR>::NFL], 0u, (unsigned)L.kt * 128u);
+        load_to_lds(from.rr, to, Nt<TR>::F_BYTES + (Q - Nt<TR>::NFL) * 4096, L.vr[Q - Nt<TR>::NFL], 0u, (unsigned)L.kt * 128u);
 }
-template <int KIND, int TR, int FROM, int TO> __device__ __forceinline__ void nt_loads(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L) {
+template <int KIND, int TR, int FROM, int TO> __device__ __forceinline__ void nt_loads(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const NtFrom& from) {
     if constexpr (FROM < TO) {
-        nt_load<KIND, TR, FROM>(a, w, L);
-        nt_loads<KIND, TR, FROM + 1, TO>(a, w, L);
+        nt_load<KIND, TR, FROM>(a, w, L, from);
+        nt_loads<KIND, TR, FROM + 1, TO>(a, w, L, from);
     }
 }
 // after the last load of a stage
@@ -308,8 +322,8 @@ template <int TR> __device__ __forceinline__ void nt_read(NtFrags<TR>& fr, const
 // this one has left.  FIRST: of an item's first RING - 1 stages,
 // behind whose loads the stores of the item before (at least `stores`) may be under way.
 template <int KIND, int TR, int S, bool FULL, int t>
-__device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const unsigned char* ring, int at_f, int at_r, NtAcc<TR>& acc,
-                                          NtFrags<TR> (&fr)[2], int ni_on) {
+__device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const NtFrom& from, const unsigned char* ring, int at_f, int at_r,
+                                          NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int ni_on) {
     constexpr int G = Nt<TR>::NI * 4, READS = 8 + 2 * Nt<TR>::NI, SPREAD = G >= 16 ? 12 : G, LPS = Nt<TR>::LPS;
     if constexpr (t < G) {
         constexpr int ni = t >> 2, n16 = (t >> 1) & 1, b0 = (t & 1) * 2;
@@ -324,9 +338,9 @@ __device__ __forceinline__ void nt_groups(const NtArgs& a, const NtWork& w, cons
 #pragma unroll
             for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) nt_read<TR>(fr[S ^ 1], ring, j, at_f, at_r);
         }
-        if constexpr (S == 1) nt_loads<KIND, TR, t * LPS / G, (t + 1) * LPS / G>(a, w, L);
+        if constexpr (S == 1) nt_loads<KIND, TR, t * LPS / G, (t + 1) * LPS / G>(a, w, L, from);
         __builtin_amdgcn_sched_barrier(0);
-        nt_groups<KIND, TR, S, FULL, t + 1>(a, w, L, ring, at_f, at_r, acc, fr, ni_on);
+        nt_groups<KIND, TR, S, FULL, t + 1>(a, w, L, from, ring, at_f, at_r, acc, fr, ni_on);
     }
 }
 template <int KIND, int TR, int S, bool FIRST, bool FULL>
@@ -334,7 +348,9 @@ __device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const 
                                         NtAcc<TR>& acc, NtFrags<TR> (&fr)[2], int stores, int ni_on) {
     if (S == 1) buf = buf + 1 == Nt<TR>::RING ? 0 : buf + 1;
     const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
-    nt_groups<KIND, TR, S, FULL, 0>(a, w, L, ring, at_f, at_r, acc, fr, ni_on);
+    NtFrom from = {};
+    if (S == 1) from = nt_from<KIND, TR>(L);
+    nt_groups<KIND, TR, S, FULL, 0>(a, w, L, from, ring, at_f, at_r, acc, fr, ni_on);
     if (S == 0) {
         // everybody has read all of this stage, and the next one is there
         MOE_WAIT_LGKMCNT(0);
@@ -620,7 +636,7 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
     nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
 #pragma unroll
     for (int st = 0; st < Nt<TR>::RING; ++st) {
-        nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L);
+        nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L, nt_from<KIND, TR>(L));
         if (st + 1 == Nt<TR>::RING) break;
         if (KIND != DX && a.KT < Nt<TR>::RING) {           // (the next item's rows may be wanted now)
             MOE_WAIT_VMCNT(0);
@@ -799,7 +815,7 @@ __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, T
 }
 // Every lane's source row of half h of a stage, into one of eight tables of its wavefront's (behind the expert's last row: zeros).
 template <int TS> __device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const TnAhead& p, int h, int slot) {
-    load_to_lds4(p.src, w.ring + (unsigned)(Tn<TS>::IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
+    load_to_lds4(settled(p.src), w.ring + (unsigned)(Tn<TS>::IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
 }
 // Its offset.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
 __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
@@ -807,15 +823,17 @@ __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
     return __builtin_elementwise_add_sat(~*(lds_word*)(uintptr_t)(th.ids() + (unsigned)slot * 1024u), th.piece());
 }
 // load Q of half H: the direct operand's first
-template <int TS, int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, unsigned buf_at, unsigned row) {
+struct TnFrom { u32x4 rd, rg; };
+__device__ __forceinline__ TnFrom tn_from(const TnLoads& L) { return TnFrom{settled(L.rd), settled(L.rg)}; }
+template <int TS, int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, const TnFrom& from, unsigned buf_at, unsigned row) {
     constexpr int N = Tn<TS>::PANELS, p = Q % N;
-    if constexpr (Q < N) load_to_lds(L.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
-    else load_to_lds(L.rg, L.to_g + buf_at, p * 4096, row, L.cg + (unsigned)p * 128u, 0u);
+    if constexpr (Q < N) load_to_lds(from.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
+    else load_to_lds(from.rg, L.to_g + buf_at, p * 4096, row, L.cg + (unsigned)p * 128u, 0u);
 }
-template <int TS, int H, int FROM, int TO> __device__ __forceinline__ void tn_loads(const TnLoads& L, unsigned buf_at, unsigned row) {
+template <int TS, int H, int FROM, int TO> __device__ __forceinline__ void tn_loads(const TnLoads& L, const TnFrom& from, unsigned buf_at, unsigned row) {
     if constexpr (FROM < TO) {
-        tn_load<TS, H, FROM>(L, buf_at, row);
-        tn_loads<TS, H, FROM + 1, TO>(L, buf_at, row);
+        tn_load<TS, H, FROM>(L, from, buf_at, row);
+        tn_loads<TS, H, FROM + 1, TO>(L, from, buf_at, row);
     }
 }
 
@@ -842,8 +860,8 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
 // behind it into the same buffer, which everybody has read.  What moves the places on stands between the multiplications: a wavefront has
 // its SIMD for itself, an instruction that none of them covers costs its whole time.
 template <int TS, int S, int t>
-__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, TnAhead& ahead, const TnLane& ln, int pair, int slot, unsigned& row, TnAcc<TS>& acc,
-                                          TnFrags<TS> (&fr)[2]) {
+__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, const TnFrom& from, TnAhead& ahead, const TnLane& ln, int pair, int slot,
+                                          unsigned& row, TnAcc<TS>& acc, TnFrags<TS> (&fr)[2]) {
     constexpr int B = Tn<TS>::BLOCKS, G = Tn<TS>::GROUPS, READS = 4 * B, SPREAD = 3 * G / 4, LOADS = Tn<TS>::LOADS;
     if constexpr (t < G) {
         constexpr int m = t / (B / 4), n4 = t % (B / 4) * 4;
@@ -859,9 +877,9 @@ __device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, T
 #pragma unroll
             for (int j = t * READS / SPREAD; j < (t + 1) * READS / SPREAD; ++j) tn_read<TS>(fr[S ^ 1], ln, S ^ 1, j);
         }
-        if constexpr (t < SPREAD) tn_loads<TS, S, t * LOADS / SPREAD, (t + 1) * LOADS / SPREAD>(L, (unsigned)((pair * 2 + S) * Tn<TS>::BUF), row);
+        if constexpr (t < SPREAD) tn_loads<TS, S, t * LOADS / SPREAD, (t + 1) * LOADS / SPREAD>(L, from, (unsigned)((pair * 2 + S) * Tn<TS>::BUF), row);
         __builtin_amdgcn_sched_barrier(0);
-        tn_groups<TS, S, t + 1>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
+        tn_groups<TS, S, t + 1>(w, th, L, from, ahead, ln, pair, slot, row, acc, fr);
     }
 }
 template <int TS, int ES, int S>
@@ -873,7 +891,7 @@ __device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const 
         for (int c = 0; c < 4; ++c) ln.n[c] ^= 2 * Tn<TS>::BUF;
     }
     unsigned row;
-    tn_groups<TS, S, 0>(w, th, L, ahead, ln, pair, slot, row, acc, fr);
+    tn_groups<TS, S, 0>(w, th, L, tn_from(L), ahead, ln, pair, slot, row, acc, fr);
     slot = (slot + 1) & 7;
     // everybody has read the next half, and the one behind it is there: what was issued before the last two steps (their loads and a fetch of source
     // rows each) and an item's stores
@@ -1014,9 +1032,9 @@ __global__ __launch_bounds__(NTH, TS == 256 ? 1 : 2) void gemm_tn_kernel(const T
     MOE_WAIT_VMCNT(0);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        tn_loads<TS, 0, 0, Tn<TS>::LOADS>(L, (unsigned)(2 * st * Tn<TS>::BUF), tn_row(th, 2 * st));
+        tn_loads<TS, 0, 0, Tn<TS>::LOADS>(L, tn_from(L), (unsigned)(2 * st * Tn<TS>::BUF), tn_row(th, 2 * st));
         tn_fetch_ids<TS>(w, th, ahead, 0, 4 + 2 * st);
-        tn_loads<TS, 1, 0, Tn<TS>::LOADS>(L, (unsigned)((2 * st + 1) * Tn<TS>::BUF), tn_row(th, 2 * st + 1));
+        tn_loads<TS, 1, 0, Tn<TS>::LOADS>(L, tn_from(L), (unsigned)((2 * st + 1) * Tn<TS>::BUF), tn_row(th, 2 * st + 1));
         tn_fetch_ids<TS>(w, th, ahead, 1, 5 + 2 * st);
         tn_step_on(L);
         if (L.left <= 0) tn_next_item<TS, ES>(a, w, th, L);
