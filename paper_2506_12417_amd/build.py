@@ -381,6 +381,10 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
         if bad:
             raise RuntimeError("%s: kernel state behind generic pointers (flat accesses):\n%s"
                                % (os.path.basename(asm_path), "\n".join("  %s: %s" % b for b in bad[:20])))
+        bad = check_scalar_wait_states(open(asm_path).read())
+        if bad:
+            raise RuntimeError("%s: scalar registers read too soon after a vector instruction's write:\n%s"
+                               % (os.path.basename(asm_path), "\n".join("  %s: %s" % b for b in bad[:20])))
     bad = check_stream_registers(open(asm_paths[1]).read())
     if bad:
         raise RuntimeError("ffn_stream.hip: registers of the weight loads are touched by other code:\n%s"
@@ -388,9 +392,6 @@ def build(verbose: bool = True, jobs: int = 8) -> str:
     bad = check_training_kernels(open(asm_paths[-1]).read())
     if bad:
         raise RuntimeError("ffn_train.hip: loads to LDS or stores that the compiler has taken apart:\n%s" % "\n".join("  %s: %s" % b for b in bad[:20]))
-    bad = check_scalar_wait_states(open(asm_paths[-1]).read())
-    if bad:
-        raise RuntimeError("ffn_train.hip: scalar registers read too soon after a vector instruction's write:\n%s" % "\n".join("  %s: %s" % b for b in bad[:20]))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB]
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
     if r.returncode != 0:

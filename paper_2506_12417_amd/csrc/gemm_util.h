@@ -90,6 +90,7 @@ __device__ __forceinline__ void take_ticket(int32_t* ctr) {
     asm volatile(
         "s_mov_b64 %0, exec\n\t"
         "s_mov_b64 exec, 1\n\t"
+        "s_nop 2\n\t"                                    // (ctr may come from a lane read: five wait states in all)
         "global_atomic_add " MOE_TICKET_REG ", %1, %2, %3 sc0\n\t"
         "s_mov_b64 exec, %0"
         : "=&s"(saved)

@@ -42,10 +42,10 @@ def test_paths():
     assert found(around) and not found(around.replace(".LBB0_2:\n", ".LBB0_2:\n\ts_nop 3\n"))
 
 
-@pytest.mark.parametrize("name", ["ffn_train.s"])
+@pytest.mark.parametrize("name", ["ffn_train.s", "ffn_bf16.s", "ffn_stream.s", "ffn_wide.s", "ffn_rows.s", "ffn_f32.s"])
 def test_the_built_kernels(name):
     asm = os.path.join(os.path.dirname(b.LIB), "_build", name)
     if not os.path.exists(asm):
         pytest.skip("no assembly of the library that is loaded here")
     text = open(asm).read()
-    assert text.count("v_readfirstlane_b32") > 50 and b.check_scalar_wait_states(text) == []
+    assert "v_readfirstlane_b32" in text and b.check_scalar_wait_states(text) == []
