@@ -59,9 +59,17 @@ __device__ __forceinline__ u32x4 descriptor(const void* p, unsigned bytes) {
 }
 // What a load below may read: the words in scalar registers, which a vector instruction (the lane read that brings them there, where the compiler holds
 // them in vector registers over a loop) has not written for five wait states.  The hardware does not check this, and the compiler sees to it for
-// its own loads only; the build counts the states in the assembly.  Once for a half's loads: a lane read of each word in front of each load leaves two.
+// its own loads only; the build counts the states in the assembly.  settled: with the wait.  pinned: at this place, for a load with matrix instructions
+// before it, once for a half's loads (in front of each load they would be two states ahead of it; with the wait a backward pass over 8192 tokens, 8 experts of
+// 4096 x 14336, takes 11.5 ms instead of 11.2).
 __device__ __forceinline__ u32x4 scalars(const u32x4& r) {
     return u32x4{(unsigned)sgpr((int)r[0]), (unsigned)sgpr((int)r[1]), (unsigned)sgpr((int)r[2]), (unsigned)sgpr((int)r[3])};
+}
+__device__ __forceinline__ u32x4 pinned(const u32x4& r) {
+    u32x4 d = scalars(r);
+    asm volatile("" : "+s"(d));
+    __builtin_amdgcn_sched_barrier(0);
+    return d;
 }
 __device__ __forceinline__ u32x4 settled(const u32x4& r) {
     u32x4 d = scalars(r);
@@ -280,10 +288,6 @@ template <int KIND, int TR> __device__ __forceinline__ void nt_turn(const NtArgs
 
 // load Q of the loader's stage (the features first)
 struct NtFrom { u32x4 rr, rf; };
-// (but for DX the compiler keeps both in scalar registers: copies of them would only take more)
-template <int KIND, int TR> __device__ __forceinline__ NtFrom nt_from(const NtLoader<TR>& L) {
-    return KIND == DX ? NtFrom{settled(L.rr), settled(L.rf)} : NtFrom{scalars(L.rr), scalars(L.rf)};
-}
 template <int KIND, int TR, int Q> __device__ __forceinline__ void nt_load(const NtArgs& a, const NtWork& w, const NtLoader<TR>& L, const NtFrom& from) {
     const unsigned to = w.ring + (unsigned)(L.buf * Nt<TR>::STAGE + w.wave * 1024);
     if constexpr (Q < Nt<TR>::NFL)
@@ -349,7 +353,7 @@ __device__ __forceinline__ void nt_half(const NtArgs& a, const NtWork& w, const 
     if (S == 1) buf = buf + 1 == Nt<TR>::RING ? 0 : buf + 1;
     const int at_f = buf * Nt<TR>::STAGE + (ln.f_rd ^ (S == 0 ? 64 : 0)), at_r = buf * Nt<TR>::STAGE + (ln.r_rd ^ (S == 0 ? 64 : 0));
     NtFrom from = {};
-    if (S == 1) from = nt_from<KIND, TR>(L);
+    if (S == 1) from = NtFrom{KIND == DX ? pinned(L.rr) : scalars(L.rr), scalars(L.rf)};      // (the others the compiler holds in scalar registers)
     nt_groups<KIND, TR, S, FULL, 0>(a, w, L, from, ring, at_f, at_r, acc, fr, ni_on);
     if (S == 0) {
         // everybody has read all of this stage, and the next one is there
@@ -636,7 +640,7 @@ __global__ __launch_bounds__(NTH) void gemm_nt_kernel(const NtArgs a) {
     nt_turn<KIND, TR>(a, w, tiles, rinfo, L);
 #pragma unroll
     for (int st = 0; st < Nt<TR>::RING; ++st) {
-        nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L, nt_from<KIND, TR>(L));
+        nt_loads<KIND, TR, 0, Nt<TR>::LPS>(a, w, L, NtFrom{settled(L.rr), settled(L.rf)});
         if (st + 1 == Nt<TR>::RING) break;
         if (KIND != DX && a.KT < Nt<TR>::RING) {           // (the next item's rows may be wanted now)
             MOE_WAIT_VMCNT(0);
@@ -814,8 +818,8 @@ __device__ __forceinline__ void tn_next_item(const TnArgs& a, const TnWork& w, T
     tn_turn(a, w, p);
 }
 // Every lane's source row of half h of a stage, into one of eight tables of its wavefront's (behind the expert's last row: zeros).
-template <int TS> __device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const TnAhead& p, int h, int slot) {
-    load_to_lds4(settled(p.src), w.ring + (unsigned)(Tn<TS>::IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
+template <int TS> __device__ __forceinline__ void tn_fetch_ids(const TnWork& w, const TnThread& th, const u32x4& src, int h, int slot) {
+    load_to_lds4(src, w.ring + (unsigned)(Tn<TS>::IDS + slot * 1024 + w.wave * 256), th.row4() + (unsigned)h * 128u);
 }
 // Its offset.  (One that is not there has the largest offset, and keeps it: the range check reads zeros.)
 __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
@@ -823,8 +827,7 @@ __device__ __forceinline__ unsigned tn_row(const TnThread& th, int slot) {
     return __builtin_elementwise_add_sat(~*(lds_word*)(uintptr_t)(th.ids() + (unsigned)slot * 1024u), th.piece());
 }
 // load Q of half H: the direct operand's first
-struct TnFrom { u32x4 rd, rg; };
-__device__ __forceinline__ TnFrom tn_from(const TnLoads& L) { return TnFrom{settled(L.rd), settled(L.rg)}; }
+struct TnFrom { u32x4 rd, rg, src; };
 template <int TS, int H, int Q> __device__ __forceinline__ void tn_load(const TnLoads& L, const TnFrom& from, unsigned buf_at, unsigned row) {
     constexpr int N = Tn<TS>::PANELS, p = Q % N;
     if constexpr (Q < N) load_to_lds(from.rd, L.to_d + buf_at, p * 4096, L.vd, L.cd + (unsigned)(H * 32) * L.ld_d + (unsigned)p * 128u, 0u);
@@ -860,13 +863,14 @@ __device__ __forceinline__ bf16x8 tn_frag(const s16x4 (&f)[2]) {
 // behind it into the same buffer, which everybody has read.  What moves the places on stands between the multiplications: a wavefront has
 // its SIMD for itself, an instruction that none of them covers costs its whole time.
 template <int TS, int S, int t>
-__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, const TnFrom& from, TnAhead& ahead, const TnLane& ln, int pair, int slot,
+__device__ __forceinline__ void tn_groups(const TnWork& w, const TnThread& th, TnLoads& L, TnFrom& from, TnAhead& ahead, const TnLane& ln, int pair, int slot,
                                           unsigned& row, TnAcc<TS>& acc, TnFrags<TS> (&fr)[2]) {
     constexpr int B = Tn<TS>::BLOCKS, G = Tn<TS>::GROUPS, READS = 4 * B, SPREAD = 3 * G / 4, LOADS = Tn<TS>::LOADS;
     if constexpr (t < G) {
         constexpr int m = t / (B / 4), n4 = t % (B / 4) * 4;
         if constexpr (t == 0) row = tn_row(th, (slot + 4) & 7);
-        if constexpr (t == G - 1) tn_fetch_ids<TS>(w, th, ahead, S, slot);
+        if constexpr (t == G - 2) from.src = pinned(ahead.src);
+        if constexpr (t == G - 1) tn_fetch_ids<TS>(w, th, from.src, S, slot);
         static_assert(SPREAD <= G - 1, "the places move on behind the loads");
         if constexpr (S == 1 && t == (G > 4 ? G - 2 : G - 1)) tn_step_on(L);
         if constexpr (S == 1 && t == G - 1) tn_step_on(ahead);
@@ -891,7 +895,8 @@ __device__ __forceinline__ void tn_step(const TnArgs& a, const TnWork& w, const 
         for (int c = 0; c < 4; ++c) ln.n[c] ^= 2 * Tn<TS>::BUF;
     }
     unsigned row;
-    tn_groups<TS, S, 0>(w, th, L, tn_from(L), ahead, ln, pair, slot, row, acc, fr);
+    TnFrom from = {pinned(L.rd), scalars(L.rg)};
+    tn_groups<TS, S, 0>(w, th, L, from, ahead, ln, pair, slot, row, acc, fr);
     slot = (slot + 1) & 7;
     // everybody has read the next half, and the one behind it is there: what was issued before the last two steps (their loads and a fetch of source
     // rows each) and an item's stores
@@ -1024,18 +1029,18 @@ __global__ __launch_bounds__(NTH, TS == 256 ? 1 : 2) void gemm_tn_kernel(const T
     tn_turn(a, w, ahead);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        tn_fetch_ids<TS>(w, th, ahead, 0, 2 * st);
-        tn_fetch_ids<TS>(w, th, ahead, 1, 2 * st + 1);
+        tn_fetch_ids<TS>(w, th, settled(ahead.src), 0, 2 * st);
+        tn_fetch_ids<TS>(w, th, settled(ahead.src), 1, 2 * st + 1);
         tn_step_on(ahead);
         if (ahead.left <= 0) tn_next_item(a, w, ahead);
     }
     MOE_WAIT_VMCNT(0);
 #pragma unroll
     for (int st = 0; st < 2; ++st) {
-        tn_loads<TS, 0, 0, Tn<TS>::LOADS>(L, tn_from(L), (unsigned)(2 * st * Tn<TS>::BUF), tn_row(th, 2 * st));
-        tn_fetch_ids<TS>(w, th, ahead, 0, 4 + 2 * st);
-        tn_loads<TS, 1, 0, Tn<TS>::LOADS>(L, tn_from(L), (unsigned)((2 * st + 1) * Tn<TS>::BUF), tn_row(th, 2 * st + 1));
-        tn_fetch_ids<TS>(w, th, ahead, 1, 5 + 2 * st);
+        tn_loads<TS, 0, 0, Tn<TS>::LOADS>(L, TnFrom{settled(L.rd), settled(L.rg)}, (unsigned)(2 * st * Tn<TS>::BUF), tn_row(th, 2 * st));
+        tn_fetch_ids<TS>(w, th, settled(ahead.src), 0, 4 + 2 * st);
+        tn_loads<TS, 1, 0, Tn<TS>::LOADS>(L, TnFrom{settled(L.rd), settled(L.rg)}, (unsigned)((2 * st + 1) * Tn<TS>::BUF), tn_row(th, 2 * st + 1));
+        tn_fetch_ids<TS>(w, th, settled(ahead.src), 1, 5 + 2 * st);
         tn_step_on(L);
         if (L.left <= 0) tn_next_item<TS, ES>(a, w, th, L);
         tn_step_on(ahead);
