@@ -527,7 +527,7 @@ MOE_API int moe_grouped_ffn_backward(const void* dy, moe_dtype dy_dt, const void
  *
  *   dy [T,d] dy_dt      y_perm [A,d] fp32 (NULL without dgate_w)      gate_w [T,k] fp32 or NULL (all ones)
  *   dy_perm [A,d] perm_dt out or NULL      dgate_w [T,k] fp32 out or NULL      dx_add [T,d] fp32 or NULL      dx [T,d] dx_dt out
- * A negative inv_perm entry has no row: dgate_w is 0 there, and it adds nothing to dx.  Any d, any alignment, T ceil(d / 512) < 2^26 (T < 2^26, d < 2^29 for
+ * A negative inv_perm entry has no row: dgate_w is 0 there, and it adds nothing to dx.  Any d, any alignment, T ceil(d / 512) <= 2^26 - 4 (T <= 2^26 - 4, d < 2^29 for
  * moe_unpermute_combine_backward), T k < 2^31.  dx may be dx_add (both fp32); no
  * other output may overlap an input.  T = 0 is a no-op.
  */

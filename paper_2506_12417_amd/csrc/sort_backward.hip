@@ -211,13 +211,16 @@ bool whole_pieces(int d, std::initializer_list<const void*> ps) {
     return d % 8 == 0 && (all & 15) == 0;
 }
 
+// A launch has less than 2^32 threads: work-groups of NTH, the last one whole.
+bool wavefronts_fit(long long n) { return (n + NTH / 64 - 1) / (NTH / 64) < (1ll << 32) / NTH; }
+
 }  // namespace
 
 extern "C" int moe_unpermute_combine_backward(const void* dy, moe_dtype dy_dt, const float* y_perm, const int32_t* inv_perm, const float* gate_w, int T, int d,
                                               int k, void* dy_perm, moe_dtype perm_dt, float* dgate_w, void* stream) {
     MOE_REQUIRE(T >= 0 && d >= 1 && k >= 1, MOE_ERR_ARG, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
     MOE_REQUIRE(moe_dtype_ok(dy_dt) && moe_dtype_ok(perm_dt), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: dtypes %d, %d", (int)dy_dt, (int)perm_dt);
-    MOE_REQUIRE((long long)T * k < (1ll << 31) && T < (1 << 26) && d < (1 << 29), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
+    MOE_REQUIRE((long long)T * k < (1ll << 31) && wavefronts_fit(T) && d < (1 << 29), MOE_ERR_UNSUPPORTED, "moe_unpermute_combine_backward: T=%d d=%d k=%d", T, d, k);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(dy && inv_perm && (dy_perm || dgate_w) && (y_perm || !dgate_w), MOE_ERR_ARG, "moe_unpermute_combine_backward: null pointer");
     const bool vec = whole_pieces(d, {dy, y_perm, dy_perm});
@@ -239,8 +242,8 @@ extern "C" int moe_permute_backward(const float* dx_perm, const int32_t* inv_per
                                     void* stream) {
     MOE_REQUIRE(T >= 0 && d >= 1 && k >= 1, MOE_ERR_ARG, "moe_permute_backward: T=%d d=%d k=%d", T, d, k);
     MOE_REQUIRE(moe_dtype_ok(dx_dt), MOE_ERR_UNSUPPORTED, "moe_permute_backward: dtype %d", (int)dx_dt);
-    const int pieces = (int)(((long long)d + 511) / 512);  // (of a wavefront each; a launch has less than 2^32 threads)
-    MOE_REQUIRE((long long)T * k < (1ll << 31) && (long long)T * pieces < (1 << 26), MOE_ERR_UNSUPPORTED, "moe_permute_backward: T=%d d=%d k=%d", T, d, k);
+    const int pieces = (int)(((long long)d + 511) / 512);  // (of a wavefront each)
+    MOE_REQUIRE((long long)T * k < (1ll << 31) && wavefronts_fit((long long)T * pieces), MOE_ERR_UNSUPPORTED, "moe_permute_backward: T=%d d=%d k=%d", T, d, k);
     if (T == 0) return MOE_OK;
     MOE_REQUIRE(dx_perm && inv_perm && dx, MOE_ERR_ARG, "moe_permute_backward: null pointer");
     const bool vec = whole_pieces(d, {dx_perm, dx_add, dx});
