@@ -57,7 +57,8 @@ class MoEBlock:
         self.u = torch.empty((T, d), dtype=layer.tdt, device=dev)
         self.y = torch.empty((T, d), dtype=self.h_tdt, device=dev)
         self.u_next = torch.empty((T, d), dtype=layer.tdt, device=dev) if self.next else None
-        # (trained, the block keeps v itself: the layer may run again, for another block or alone, before the backward calls)
+        # (trained, the block keeps v itself: the layer may run again, for another block or alone, before end_backward and pre_backward.  Not before
+        # backward(): what the layer's own gradients are made of is kept once, by the layer, for its last pass)
         self.v = torch.empty((T, d), dtype=f32, device=dev) if train else None
         if train:
             self.pre_stats = torch.empty((T, 2), dtype=f32, device=dev)
@@ -68,6 +69,7 @@ class MoEBlock:
             self.dv = torch.empty((T, d), dtype=f32, device=dev)
             self.dh = torch.empty((T, d), dtype=self.h_tdt, device=dev)
             self.pre_own = True              # whether the last forward() has run the pre norm
+            self.layer_pass = 0              # the layer's pass that the last forward() was
 
     def load(self, **arrays: np.ndarray):
         """Parameters by name (NAMES), fp32: [d], and the gate [d] or [T,d].  What is not loaded counts as ones (weights) or zeros."""
@@ -106,6 +108,7 @@ class MoEBlock:
             L.forward_few(u, self.v, stream)
         elif self.train or L.train or L.fold_combine:
             L.forward(u, stream, y=self.v)
+            self.layer_pass = L.kept_pass
         else:
             # the layer's combine in the same pass as what follows it: v is never stored
             L.forward(u, stream=stream, rows=True)
@@ -145,7 +148,13 @@ class MoEBlock:
                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """The whole block's gradients, with a layer that trains (MoELayer(train=True)): from those of y and u' to h's (a buffer of the block's) and
         None; or, where forward() was given u, to what the residual connection passes on to h and the gradient of u (du_next of the block that
-        has made it).  Parameters' gradients go to `grad` and the layer's `grad`.  It belongs to the layer's last forward()."""
+        has made it).  Parameters' gradients go to `grad` and the layer's `grad`.  It belongs to the layer's last forward(): refused where that
+        was not this block's last one."""
+        L = self.layer
+        if not (self.train and L.train):
+            raise B.MoeError(B.MOE_ERR_ARG, "all gradients need MoEBlock(train=True) with a MoELayer(train=True)")
+        if L.kept_of is None or L.kept_pass != self.layer_pass:
+            raise B.MoeError(B.MOE_ERR_ARG, "the layer has run since this block's forward(): what it kept is gone")
         dv, dh = self.end_backward(h, dy, du_next, stream)
-        du = self.layer.backward(dv, self.u_in, None, accumulate, stream)
+        du = L.backward(dv, self.u_in, None, accumulate, stream)
         return (self.pre_backward(h, du, stream), None) if self.pre_own else (dh, du)

@@ -73,7 +73,8 @@ class MoELayer:
                  fuse_gather: Optional[bool] = None, train: bool = False):
         self.T, self.d, self.F, self.E, self.k, self.renorm = T, d, F, E, k, renorm
         assert not train or dtype == "bf16", "the experts' gradients are there for bf16 layers"
-        self.train, self.kept_of = train, None
+        # what backward() would be for: nothing (what a pass has kept is gone once another call has routed or sorted), or the pass of this number
+        self.train, self.kept_of, self.kept_pass = train, None, 0
         self.A = T * k
         self.act = B.MOE_SWIGLU if act == "swiglu" else B.MOE_RELU
         self.dt = B.MOE_BF16 if dtype == "bf16" else B.MOE_F32
@@ -215,6 +216,7 @@ class MoELayer:
 
     # ------------------------------------------------------------------ the path, step by step
     def route(self, x, logits_out=None, stream=None):
+        self.kept_of = None
         if self.packed_router:
             B.moe_route_topk_packed(x, self.W_gt, self.w_norm2, self.bias, self.T, self.d, self.E, self.k,
                                     self.renorm, self.dt, self.expert_idx, self.gate_w, logits_out, stream)
@@ -224,11 +226,13 @@ class MoELayer:
 
     def permute(self, x, stream=None):
         """x = None: only the sort (counts, offsets, perm, inv_perm); x_perm is left alone."""
+        self.kept_of = None
         B.moe_permute(x, self.expert_idx, self.T, self.d, self.E, self.k, self.dt, self.counts, self.offsets,
                       self.perm, self.inv_perm, None if x is None else self.x_perm, self.ws, self.ws_bytes, stream)
 
     def permute_plan(self, stream=None):
         """The sort (no row gather) and the plan: one launch where the library offers it."""
+        self.kept_of = None
         if 1 <= self.A <= B.MOE_PERMUTE_PLAN_MAX:
             B.moe_permute_plan(self.expert_idx, self.T, self.E, self.k, self.counts, self.offsets, self.perm, self.inv_perm,
                                self.tile_m, self.n_bins, self.q_tokens, self.policy, self.tiles, self.tile_capacity,
@@ -380,7 +384,7 @@ class MoELayer:
     def _forward_train(self, x: torch.Tensor, routed: bool, stream) -> torch.Tensor:
         g, shape, kinds = self.experts, (self.T, self.d, self.F, self.E), (self.act, self.dt)
         B.check_rows("x", x, self.T, self.d, (self.tdt,), self.own_y.device)
-        self.kept_of = "routed" if routed else "whole"      # routed by the caller: the gate values are not the router's, which gets no gradient
+        self.kept_of = None
         if not routed:
             self.route(x, self.logits, stream)
         self.permute_plan(stream)
@@ -388,7 +392,7 @@ class MoELayer:
         table = (g.in_ptrs, g.out_ptrs, self.tiles, self.plan_hdr, self.ffn_tile_m, self.h)
         if self.fold_combine:
             B.moe_grouped_ffn_top1_phase(2, None, *shape, *kinds, *table, self.perm, self.gate_w, self.y, stream)
-            return self.y
+            return self._kept(routed)
         B.moe_grouped_ffn_phase(2, None, self.A, *shape[1:], *kinds, *table, self.y_perm, stream)
         if self.shared_F:
             s, one = self.shared, (self.T, self.d, self.shared_F, 1)
@@ -396,11 +400,17 @@ class MoELayer:
             B.moe_grouped_ffn_phase(2, None, *one, B.MOE_SWIGLU, self.dt, s.in_ptrs, s.out_ptrs, self.s_tiles, self.s_hdr, self.s_ffn_tile_m, self.s_h,
                                     self.s_y, stream)
         self.combine(True, stream)
+        return self._kept(routed)
+
+    def _kept(self, routed: bool) -> torch.Tensor:
+        self.kept_of = "routed" if routed else "whole"      # routed by the caller: the gate values are not the router's, which gets no gradient
+        self.kept_pass += 1
         return self.y
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, dlogits_add: Optional[torch.Tensor] = None, accumulate: bool = False,
                  stream=None) -> torch.Tensor:
-        """The gradients of the last forward() of a training layer (train=True), whose x this is: returns that of x ([T,d], the layer's type);
+        """The gradients of the last forward() of a training layer (train=True), whose x this is (refused where the layer has routed or sorted
+        since): returns that of x ([T,d], the layer's type);
         those of the matrices and the router go to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).
         dy: [T,d] fp32 or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the experts'
         gradients are added to what `grad` holds (the router's are not: they are set)."""
