@@ -183,7 +183,7 @@ __global__ __launch_bounds__(NTH) void combine_backward_kernel(const D* __restri
 
 template <typename P, bool VEC>
 __global__ __launch_bounds__(NTH) void permute_backward_kernel(const float* __restrict__ dx_perm, const int32_t* __restrict__ inv_perm, int T, int d, int k,
-                                                               const float* __restrict__ dx_add, P* __restrict__ dx, int pieces) {
+                                                               const float* dx_add, P* dx, int pieces) {      // (dx may be dx_add)
     const size_t id = (size_t)blockIdx.x * (NTH / 64) + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     const int t = sgpr((int)(id / (unsigned)pieces)), piece = sgpr((int)(id % (unsigned)pieces));

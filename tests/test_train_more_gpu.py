@@ -79,3 +79,17 @@ def test_block_that_is_not_trained_has_no_backward():
         plain.backward(h, dy, du)
     with pytest.raises(B.MoeError):
         a.backward(h, dy, du)                              # (its own forward() has not run)
+
+
+# ------------------------------------------------------------------------------------------------ in place
+@pytest.mark.parametrize("T,d,k", [(1, 5000, 1), (1, 4096, 1), (77, 777, 3), (130, 2048, 4), (3, 8, 9), (2000, 513, 2)])
+def test_permute_backward_adds_in_place(T, d, k):
+    torch, B, dev = _gpu()
+    rows, add, inv = torch.randn((T * k, d), device=dev), torch.randn((T, d), device=dev), torch.randperm(T * k, device=dev).int()
+    dx = torch.empty((T, d), device=dev)
+    B.moe_permute_backward(rows, inv, T, d, k, add, dx, B.MOE_F32)
+    want = add.double() + rows.double()[inv.long()].reshape(T, k, d).sum(1)
+    mag = add.double().abs() + rows.double().abs()[inv.long()].reshape(T, k, d).sum(1)
+    assert ((dx.double() - want).abs() <= (k + 1) * R.U32 * mag).all()
+    B.moe_permute_backward(rows, inv, T, d, k, add, add, B.MOE_F32)
+    assert torch.equal(dx, add)
