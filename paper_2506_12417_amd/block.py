@@ -11,7 +11,7 @@ import numpy as np
 import torch
 
 from . import binding as B
-from .layer import MoELayer, to_device
+from .layer import MoELayer, add_up, to_device
 
 KINDS = {"none": B.MOE_NORM_NONE, "rms": B.MOE_NORM_RMS, "layer": B.MOE_NORM_LAYER}
 NAMES = ("pre_w", "pre_b", "post_w", "post_b", "gate", "next_w", "next_b")
@@ -64,6 +64,7 @@ class MoEBlock:
             self.pre_stats = torch.empty((T, 2), dtype=f32, device=dev)
             self.end_stats = torch.empty((T, 4), dtype=f32, device=dev)
             self.grad: Dict[str, torch.Tensor] = {}
+            self.part: Dict[str, torch.Tensor] = {}      # (a pass's own gradients, where backward() adds them up)
             n = max(B.moe_workspace_bytes(op, T, d, 0, 0, 0, layer.dt) for op in (B.MOE_OP_NORM_BACKWARD, B.MOE_OP_BLOCK_END_BACKWARD))
             self.ws = torch.empty(max(n, 16), dtype=torch.uint8, device=dev)
             self.dv = torch.empty((T, d), dtype=f32, device=dev)
@@ -78,7 +79,7 @@ class MoEBlock:
             assert name in NAMES and rows and np.shape(a) in (((self.d,), (1, self.d)) if rows == 1 else ((rows, self.d),)), name
             self.param[name] = to_device(np.asarray(a, dtype=np.float32).reshape(-1, self.d), self.layer.device)
             if self.train:
-                self.grad["d" + name] = torch.empty_like(self.param[name])
+                self.grad["d" + name], self.part["d" + name] = torch.empty_like(self.param[name]), torch.empty_like(self.param[name])
 
     def _check(self, dtype: torch.dtype, **tensors: Optional[torch.Tensor]):
         for name, t in tensors.items():
@@ -148,13 +149,23 @@ class MoEBlock:
                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
         """The whole block's gradients, with a layer that trains (MoELayer(train=True)): from those of y and u' to h's (a buffer of the block's) and
         None; or, where forward() was given u, to what the residual connection passes on to h and the gradient of u (du_next of the block that
-        has made it).  Parameters' gradients go to `grad` and the layer's `grad`.  It belongs to the layer's last forward(): refused where that
+        has made it).  Parameters' gradients go to `grad` and the layer's `grad`; accumulate: all of them are added to what is
+        there (that of the micro-batches before).  It belongs to the layer's last forward(): refused where that
         was not this block's last one."""
         L = self.layer
         if not (self.train and L.train):
             raise B.MoeError(B.MOE_ERR_ARG, "all gradients need MoEBlock(train=True) with a MoELayer(train=True)")
         if L.kept_of is None or L.kept_pass != self.layer_pass:
             raise B.MoeError(B.MOE_ERR_ARG, "the layer has run since this block's forward(): what it kept is gone")
-        dv, dh = self.end_backward(h, dy, du_next, stream)
-        du = L.backward(dv, self.u_in, None, accumulate, stream)
-        return (self.pre_backward(h, du, stream), None) if self.pre_own else (dh, du)
+        total = self.grad
+        try:
+            self.grad = self.part if accumulate else total
+            dv, dh = self.end_backward(h, dy, du_next, stream)
+            du = L.backward(dv, self.u_in, None, accumulate, stream, accumulate_router=accumulate)
+            if self.pre_own:
+                dh = self.pre_backward(h, du, stream)
+        finally:
+            self.grad = total
+        if accumulate:
+            add_up(total, {n: t for n, t in self.part.items() if self.pre_own or not n.startswith("dpre")}, L.zero, stream)
+        return (dh, None) if self.pre_own else (dh, du)

@@ -35,6 +35,14 @@ def default_q_tokens(dt: int) -> int:
     return B.moe_token_threshold(100e12 / XCDS, 4, 6.0e12 / XCDS)
 
 
+def add_up(total: Dict[str, Optional[torch.Tensor]], part: Dict[str, Optional[torch.Tensor]], zero: torch.Tensor, stream=None):
+    """Adds fp32 gradients of one pass to those of the passes before, by name: a tensor is one token's row here, whose gradient the row at place
+    `zero` (an int32 0 on the device) is added to in place."""
+    for name, p in part.items():
+        if p is not None:
+            B.moe_permute_backward(p, zero, 1, p.numel(), 1, total[name], total[name], B.MOE_F32, stream)
+
+
 class ExpertGroup:
     """Packed weights of a set of experts on the device, plus the pointer tables the FFN reads."""
 
@@ -161,6 +169,8 @@ class MoELayer:
             need = max(need, B.moe_workspace_bytes(B.MOE_OP_FFN_BACKWARD, T, d, F, n, rows // max(T, 1), self.dt))
         self.grad = {n: None if w is None else torch.empty_like(w) for n, w in self.weight.items()}
         self.grad["W_g"], self.grad["bias"] = new((d, E), f32), new((E,), f32)
+        self.router_part = {n: torch.empty_like(self.grad[n]) for n in ("W_g", "bias")}      # (a pass's own, where they are added up)
+        self.zero = torch.zeros(1, dtype=torch.int32, device=dev)
         self.logits, self.dlogits, self.dgate_w = new((T, E), f32), new((T, E), f32), new((T, k), f32)
         self.dx_perm, self.dx_sum, self.dx = new((A, d), f32), new((T, d), f32), new((T, d), self.tdt)
         self.back_ws = new((max(need, 16),), torch.uint8)
@@ -408,12 +418,12 @@ class MoELayer:
         return self.y
 
     def backward(self, dy: torch.Tensor, x: torch.Tensor, dlogits_add: Optional[torch.Tensor] = None, accumulate: bool = False,
-                 stream=None) -> torch.Tensor:
+                 stream=None, accumulate_router: bool = False) -> torch.Tensor:
         """The gradients of the last forward() of a training layer (train=True), whose x this is (refused where the layer has routed or sorted
         since): returns that of x ([T,d], the layer's type);
         those of the matrices and the router go to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).
         dy: [T,d] fp32 or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the experts'
-        gradients are added to what `grad` holds (the router's are not: they are set)."""
+        gradients are added to what `grad` holds; accumulate_router: the router's are, too (without it they are set)."""
         assert self.train and self.kept_of, "the forward() of a MoELayer(train=True) keeps what the gradients are made of"
         assert dlogits_add is None or self.kept_of == "whole", "forward() was given the choice: the router has no gradient"
         T, d, E, k, dev = self.T, self.d, self.E, self.k, self.own_y.device
@@ -431,8 +441,11 @@ class MoELayer:
         B.moe_grouped_ffn_backward(dy, dy_dt, x, T, d, self.F, E, k, self.act, self.dt, w["a"], w["b"], w["o"], self.offsets, self.perm, self.inv_perm,
                                    self.gate_w, *self.kept[""], self.dx_perm, self.dgate_w, g["a"], g["b"], g["o"], self.dt, acc, self.back_ws, n, stream)
         if self.kept_of == "whole":
+            router = self.router_part if accumulate_router else g
             B.moe_route_topk_backward(self.dgate_w, self.gate_w, self.expert_idx, self.logits, dlogits_add, x, self.W_g, T, d, E, k, self.renorm, self.dt,
-                                      self.dlogits, add, self.dx_sum, g["W_g"], g["bias"], self.back_ws, n, stream)
+                                      self.dlogits, add, self.dx_sum, router["W_g"], router["bias"], self.back_ws, n, stream)
+            if accumulate_router:
+                add_up(g, router, self.zero, stream)
             add = self.dx_sum
         B.moe_permute_backward(self.dx_perm, self.inv_perm, T, d, k, add, self.dx, self.dt, stream)
         return self.dx

@@ -93,3 +93,110 @@ def test_permute_backward_adds_in_place(T, d, k):
     assert ((dx.double() - want).abs() <= (k + 1) * R.U32 * mag).all()
     B.moe_permute_backward(rows, inv, T, d, k, add, add, B.MOE_F32)
     assert torch.equal(dx, add)
+
+
+# ------------------------------------------------------------------------------------------------ micro-batches
+def check_sums(torch, names, got, one, two):
+    """fp32 gradients are added with one rounding, bf16 ones are rounded once a call."""
+    assert names
+    for n in names:
+        a, b, s = one[n].double(), two[n].double(), got[n].double()
+        if got[n].dtype == torch.float32:
+            assert torch.equal(got[n], one[n] + two[n]), n
+        else:
+            assert ((s - a - b).abs() <= R.U16 * 1.01 * (b.abs() + s.abs())).all(), n
+
+
+@pytest.mark.parametrize("gate,post,next_,pre,du_next,shared_F", [("none", "rms", "rms", "rms", True, 64), ("shared", "layer", "layer", "layer", True, 0),
+                                                                  ("token", "none", "rms", "layer", False, 0)])
+def test_block_adds_up_all_gradients(gate, post, next_, pre, du_next, shared_F):
+    torch, B, dev = _gpu()
+    from paper_2506_12417_amd.block import MoEBlock
+    T, d = 70, 128
+    r = np.random.default_rng(5)
+    par = {n: r.standard_normal(d).astype(np.float32) for n in ("pre_w", "post_w", "next_w")}
+    par.update({n: r.standard_normal(d).astype(np.float32) for n, kind in (("pre_b", pre), ("post_b", post), ("next_b", next_)) if kind == "layer"})
+    if post == "none":
+        del par["post_w"]
+    if gate != "none":
+        par["gate"] = r.standard_normal((1 if gate == "shared" else T, d)).astype(np.float32)
+
+    def made():
+        L, _ = trained_layer(T, d, 192, 4, 2, "swiglu", 1, shared_F)
+        b = MoEBlock(L, pre=pre, post=post, next=next_, gate=gate, alpha=0.5, train=True)
+        b.load(**par)
+        return b
+
+    def grads(b):
+        return {n: t.clone() for n, t in list(b.grad.items()) + [("layer " + n, t) for n, t in b.layer.grad.items() if t is not None]}
+
+    batches = [[torch.randn((T, d), device=dev).bfloat16() for _ in range(3)] for _ in range(2)]
+    alone = []
+    for h, dy, du in batches:
+        b = made()
+        b.forward(h)
+        dh = b.backward(h, dy, du if du_next else None)[0]
+        alone.append((grads(b), dh.clone()))
+    b = made()
+    for i, (h, dy, du) in enumerate(batches):
+        b.forward(h)
+        dh = b.backward(h, dy, du if du_next else None, accumulate=i > 0)[0]
+        assert torch.equal(dh, alone[i][1])
+    assert set(b.grad) == {"d" + n for n in par}
+    check_sums(torch, list(alone[0][0]), grads(b), alone[0][0], alone[1][0])
+    # without it everything is set again
+    b.forward(batches[0][0])
+    b.backward(*batches[0][:2], batches[0][2] if du_next else None)
+    assert all(torch.equal(alone[0][0][n], t) for n, t in grads(b).items())
+
+
+def test_block_adds_up_where_u_is_given_and_in_a_graph():
+    torch, B, dev = _gpu()
+    from paper_2506_12417_amd.block import MoEBlock
+    T, d = 48, 256
+    L, _ = trained_layer(T, d, 512, 4, 1, "relu", 0)
+    b = MoEBlock(L, pre="rms", next="rms", train=True)
+    b.load(pre_w=np.full(d, 1.1, np.float32), next_w=np.full(d, 0.9, np.float32))
+    h, u, dy, du = (torch.randn((T, d), device=dev).bfloat16() for _ in range(4))
+    b.forward(h, u)
+    b.backward(h, dy, du)
+    one, pre = {n: t.clone() for n, t in L.grad.items() if t is not None}, b.grad["dpre_w"].fill_(3.0).clone()
+    b.forward(h, u)
+    b.backward(h, dy, du, accumulate=True)
+    assert torch.equal(b.grad["dpre_w"], pre)              # (the pre norm has not run: its gradients are another block's)
+    assert torch.equal(L.grad["W_g"], 2 * one["W_g"]) and torch.equal(L.grad["bias"], 2 * one["bias"])
+    b.forward(h)
+    b.backward(h, dy, du)
+    first = {n: t.clone() for n, t in list(b.grad.items()) + [("layer " + n, t) for n, t in L.grad.items() if t is not None]}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.forward(h)
+        b.backward(h, dy, du, accumulate=True)
+    for i in range(3):
+        for n, t in list(b.grad.items()) + [("layer " + n, t) for n, t in L.grad.items() if t is not None]:
+            t.copy_(first[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        for n in ("dpre_w", "dnext_w", "layer W_g", "layer bias"):
+            assert torch.equal((L.grad[n[6:]] if n.startswith("layer") else b.grad[n]), 2 * first[n]), (i, n)
+
+
+def test_layer_adds_up_the_routers_gradients_too():
+    torch, B, dev = _gpu()
+    L, _ = trained_layer(70, 128, 192, 4, 2, "swiglu", 1)
+    M, _ = trained_layer(70, 128, 192, 4, 2, "swiglu", 1)
+    xs, dys, extra = [torch.randn((70, 128), device=dev).bfloat16() for _ in range(2)], [torch.randn((70, 128), device=dev) for _ in range(2)], torch.randn((70, 4), device=dev)
+    alone = []
+    for x, dy in zip(xs, dys):
+        M.forward(x)
+        M.backward(dy, x, extra)
+        alone.append({n: t.clone() for n, t in M.grad.items() if t is not None})
+    for i in range(2):
+        L.forward(xs[i])
+        L.backward(dys[i], xs[i], extra, accumulate=i > 0, accumulate_router=i > 0)
+    check_sums(torch, list(alone[0]), L.grad, *alone)
+    # the choice was the caller's: the router's gradients are left alone
+    held = {n: L.grad[n].clone() for n in ("W_g", "bias")}
+    L.forward(xs[0], routed=True)
+    L.backward(dys[0], xs[0], accumulate=True, accumulate_router=True)
+    assert all(torch.equal(L.grad[n], t) for n, t in held.items())
