@@ -548,17 +548,15 @@ __device__ __forceinline__ void nt_finish(const NtArgs& a, const NtItem& it, con
                 if (b * 32 >= on) continue;
                 float s[8], wh[8], dz0[8], dz1[8];
                 lane_values<false>(acc[ni][n16][b], s);
-                // a byte with its top bit turned is the value + 128
-                const unsigned zw[2] = {q[at][0][b][0] ^ 0x80808080u, q[at][0][b][1] ^ 0x80808080u};
-                const unsigned uw[2] = {q[at][MATS - 1][b][0] ^ 0x80808080u, q[at][MATS - 1][b][1] ^ 0x80808080u};
-                const float zs = sc[at][0][b >> 1], us = sc[at][MATS - 1][b >> 1], z0 = -128.f * zs, u0 = -128.f * us;
+                const unsigned zw[2] = {q[at][0][b][0], q[at][0][b][1]}, uw[2] = {q[at][MATS - 1][b][0], q[at][MATS - 1][b][1]};
+                const float zs = sc[at][0][b >> 1], us = sc[at][MATS - 1][b >> 1];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
-                    const float z = fmaf((float)(zw[c >> 2] >> (8 * (c & 3)) & 255u), zs, z0);
+                    const float z = (float)(int8_t)(zw[c >> 2] >> (8 * (c & 3))) * zs;
                     const float dh = gate[g] * s[c];
                     float h;
                     if (SW) {
-                        const float u = fmaf((float)(uw[c >> 2] >> (8 * (c & 3)) & 255u), us, u0);
+                        const float u = (float)(int8_t)(uw[c >> 2] >> (8 * (c & 3))) * us;
                         const float sig = sigmoid(z), silu = z * sig;
                         h = silu * u;
                         dz0[c] = dh * u * fmaf(silu, 1.f - sig, sig);

@@ -200,3 +200,33 @@ def test_layer_adds_up_the_routers_gradients_too():
     L.forward(xs[0], routed=True)
     L.backward(dys[0], xs[0], accumulate=True, accumulate_router=True)
     assert all(torch.equal(L.grad[n], t) for n, t in held.items())
+
+
+# ------------------------------------------------------------------------------------------------ extremes
+@pytest.mark.parametrize("act", ["relu", "swiglu"])
+def test_scales_at_the_end_of_fp32(act):
+    """q scale is a number where 128 scale is not."""
+    torch, B, dev = _gpu()
+    from test_train_gpu import make_case
+    T, d, F, E, k = 75, 128, 192, 3, 2
+    (x, x64), (dy, dy64), w, gate, rt = make_case(torch, T, d, F, E, k, act, {}, 6)
+    r = np.random.default_rng(7)
+    A, big = T * k, np.float32(2.67e36)
+    assert 128 * float(big) > np.finfo(np.float32).max > 127 * float(big)
+    q = r.integers(0, 128, (A, F))
+    q[r.random((A, F)) < 0.2] = 0
+    scale = np.full((A, F // 64), big)
+    if act == "swiglu":                                    # (gates at or below zero: silu is 0 there; ups of any size)
+        q = np.concatenate([-q, r.integers(-127, 128, (A, F))], 1)
+        scale = np.concatenate([scale, (r.random((A, F // 64)) * 0.04).astype(np.float32)], 1)
+    q = q.astype(np.int8)
+    w32, w64 = {n: v[0] for n, v in w.items()}, {n: v[1] for n, v in w.items()}
+    dx, dgate, dw = run_back(torch, B, x, dy, w32, torch.from_numpy(gate).to(dev), rt, torch.from_numpy(q).to(dev), torch.from_numpy(scale).to(dev), T, d, F, E, k, act,
+                             dw={n: None for n in "abo"} if act == "relu" else None, dw_t=torch.float32, dgate=act == "swiglu")
+    with np.errstate(over="ignore"):
+        (dxp, dxe), (dg, dge), ref = R.ffn_backward(x64, dy64, w64, rt, k, gate.astype(np.float64), R.restore(q, scale), act)
+    within("dx_perm", dx[:A], dxp, dxe)
+    if act == "swiglu":
+        within("dgate_w", dgate, dg.reshape(T, k), dge.reshape(T, k))
+        for n in ref:
+            within("dw " + n, dw[n], ref[n][0], ref[n][1] + np.abs(ref[n][0]) * R.U32)
