@@ -212,7 +212,7 @@ def test_scales_at_the_end_of_fp32(act):
     (x, x64), (dy, dy64), w, gate, rt = make_case(torch, T, d, F, E, k, act, {}, 6)
     r = np.random.default_rng(7)
     A, big = T * k, np.float32(2.67e36)
-    assert 128 * float(big) > np.finfo(np.float32).max > 127 * float(big)
+    assert 128 * float(big) > float(np.finfo(np.float32).max) > 127 * float(big)
     q = r.integers(0, 128, (A, F))
     q[r.random((A, F)) < 0.2] = 0
     scale = np.full((A, F // 64), big)
@@ -230,3 +230,114 @@ def test_scales_at_the_end_of_fp32(act):
         within("dgate_w", dgate, dg.reshape(T, k), dge.reshape(T, k))
         for n in ref:
             within("dw " + n, dw[n], ref[n][0], ref[n][1] + np.abs(ref[n][0]) * R.U32)
+
+
+# ------------------------------------------------------------------------------------------------ sums that are exact
+# Whole numbers (times powers of two) of few bits: every product and sum below is a number that its type holds, so that the gradients have to be equal to
+# the definition's to the last bit, and a row that is missing, doubled or of another place shows.  dy, x and the matrices hold -1, 0 and 1, gates and hidden
+# values powers of two; SwiGLU's gates are 32, 64 and 128, whose sigmoid is 1 in fp32.  s is a sum of d such terms: below 256 it has bf16's 8 bits.
+BIG = [  # T, d, F, E, k, act, rows of the experts by weight (0: none)
+    (33000, 1088, 64, 4, 1, "relu", (3, 0, 5, 1)),         # (256 rows a tile for dx)
+    (33000, 1088, 64, 4, 1, "swiglu", (3, 0, 5, 1)),       # (and the second matrix behind the first)
+    (16500, 2112, 1088, 4, 2, "swiglu", (4, 3, 2, 1)),     # (and tiles of 256 x 256 for dW)
+    (2400, 576, 832, 24, 2, "relu", None),
+    (2400, 576, 832, 24, 2, "swiglu", None),               # (tiles of 256 x 256, some hundred ragged rows an expert, two panels' remainders)
+    (1300, 320, 2112, 40, 1, "relu", None),
+    (700, 192, 448, 5, 3, "swiglu", None),                 # (tiles of 128 x 128)
+    (98304, 64, 14336, 2, 1, "swiglu", (1, 900)),          # (offsets beyond 2^32 bytes)
+]
+
+
+def whole_case(torch, T, d, F, E, k, act, weights, seed):
+    dev, gen = "cuda:0", torch.Generator(device="cuda:0").manual_seed(seed)
+    three = lambda *shape: torch.randint(-1, 2, shape, device=dev, generator=gen).bfloat16()      # noqa: E731
+    p = torch.tensor(weights if weights else [1.0 + e % 4 for e in range(E)], device=dev, dtype=torch.float32)
+    idx = torch.multinomial(p.expand(T, E), k, generator=gen)
+    flat = idx.reshape(-1)
+    perm = torch.sort(flat, stable=True)[1]
+    inv = torch.empty_like(perm)
+    inv[perm] = torch.arange(T * k, device=dev)
+    counts = torch.bincount(flat, minlength=E).tolist()
+    rt = dict(offsets=np.concatenate([[0], np.cumsum(counts)]), perm=perm.cpu().numpy(), inv=inv.cpu().numpy(), counts=counts)
+    w = {n: three(E, d, F) for n in ("ab" if act == "swiglu" else "a")}
+    w["o"] = three(E, F, d)
+    gate = 2.0 ** torch.randint(-1, 2, (T, k), device=dev, generator=gen).float()
+    A, nb = T * k, F // 64
+    if act == "relu":
+        q = torch.randint(-3, 3, (A, F), device=dev, generator=gen, dtype=torch.int8)
+        q = torch.where(q < 0, 0, 2 ** q.clamp_min(0)).to(torch.int8)
+        scale = 2.0 ** torch.randint(-1, 2, (A, nb), device=dev, generator=gen).float()
+    else:
+        q = torch.empty((A, 2 * F), dtype=torch.int8, device=dev)
+        q[:, :F] = 32 * 2 ** torch.randint(0, 2, (A, F), device=dev, generator=gen, dtype=torch.int8)
+        q[:, F:] = torch.randint(-2, 3, (A, F), device=dev, generator=gen, dtype=torch.int8)
+        scale = 2.0 ** torch.randint(0, 2, (A, 2 * nb), device=dev, generator=gen).float()
+    return three(T, d), three(T, d), w, gate, rt, q, scale
+
+
+def check_whole(torch, got, x, dy, w, gate, rt, q, scale, T, d, F, E, k, act, before=None):
+    dx_perm, dgate_w, dw = got
+    dgate = torch.zeros(T * k, dtype=torch.float64, device="cuda:0")
+    for e in range(E):
+        sl = slice(int(rt["offsets"][e]), int(rt["offsets"][e + 1]))
+        a = torch.from_numpy(rt["perm"][sl]).to("cuda:0")
+        X, DY, g = x[a // k].double(), dy[a // k].double(), gate.reshape(-1)[a].double()[:, None]
+        dx = torch.zeros((len(a), d), dtype=torch.float64, device="cuda:0")
+        for f in range(0, F, 1088):
+            cols = slice(f, min(f + 1088, F))
+            kept = [q[sl, m * F + f:m * F + cols.stop].double() * scale[sl].double().repeat_interleave(64, 1)[:, m * F + f:m * F + cols.stop] for m in range(len(w) - 1)]
+            s = DY @ w["o"][e][cols].double().t()
+            assert float(s.abs().max() if len(a) else 0) < 256
+            if act == "relu":
+                h, dz = kept[0], [g * s * (kept[0] > 0)]
+            else:
+                h, dz = kept[0] * kept[1], [g * s * kept[1], g * s * kept[0]]
+            dgate[a] += (h * s).sum(1)
+            want = {"o": (g * h).t() @ DY}
+            for n, v in zip("ab", dz):
+                want[n] = X.t() @ v
+                dx += v @ w[n][e][:, cols].double().t()
+            for n, v in want.items():
+                out = dw[n][e][cols] if n == "o" else dw[n][e][:, cols]
+                if before is not None:
+                    v = v + (before[n][e][cols] if n == "o" else before[n][e][:, cols]).double()
+                assert float(v.abs().max()) < 2 ** 24 and torch.equal(out, v.to(out.dtype)), (e, n, f)
+        if dx_perm is not None:
+            assert torch.equal(dx_perm[sl], dx.float()), e
+    if dgate_w is not None:
+        assert torch.equal(dgate_w.reshape(-1), dgate.float())
+
+
+@pytest.mark.parametrize("T,d,F,E,k,act,weights", BIG)
+def test_gradients_of_whole_numbers(T, d, F, E, k, act, weights):
+    torch, B, dev = _gpu()
+    print("[case] whole numbers", T, d, F, E, k, act, flush=True)
+    x, dy, w, gate, rt, q, scale = case = whole_case(torch, T, d, F, E, k, act, weights, T + d)
+    args = (torch, B, x, dy, w, gate, rt, q, scale, T, d, F, E, k, act)
+    for t in (torch.bfloat16, torch.float32):
+        got = run_back(*args, dw_t=t)
+        check_whole(torch, got, *case, T, d, F, E, k, act)
+        if T > 50000:
+            return
+        before = {n: v.clone() for n, v in got[2].items() if v is not None}
+        _, _, dw = run_back(*args, dw=got[2], accumulate=1, dgate=False, dxp=False)
+        check_whole(torch, (None, None, dw), *case, T, d, F, E, k, act, before=before)
+
+
+def test_whole_numbers_show_a_lost_row():
+    """The check itself, with an oracle that lacks a row's share, and one that has another row's."""
+    torch, B, dev = _gpu()
+    T, d, F, E, k, act, weights = BIG[6]
+    x, dy, w, gate, rt, q, scale = whole_case(torch, T, d, F, E, k, act, weights, 1)
+    got = run_back(torch, B, x, dy, w, gate, rt, q, scale, T, d, F, E, k, act, dw_t=torch.float32)
+    check_whole(torch, got, x, dy, w, gate, rt, q, scale, T, d, F, E, k, act)
+    for other in (torch.cat([x[:-1], torch.zeros_like(x[:1])]), x.flip(0)):
+        with pytest.raises(AssertionError):
+            check_whole(torch, got, other, dy, w, gate, rt, q, scale, T, d, F, E, k, act)
+
+
+@pytest.mark.parametrize("T,d,F,E,k,act,renorm,shared_F", [(2600, 256, 512, 4, 1, "relu", 0, 0), (1900, 320, 192, 3, 2, "swiglu", 1, 128)])
+def test_layer_of_many_rows_an_expert(T, d, F, E, k, act, renorm, shared_F):
+    """The second product on tall tiles, of what the first one has left."""
+    import test_train_gpu
+    test_train_gpu.test_layer(T, d, F, E, k, act, renorm, shared_F)
