@@ -36,22 +36,6 @@ template <bool VEC> __device__ __forceinline__ void fetch(const float* row, int 
         }
     }
 }
-template <bool VEC> __device__ __forceinline__ void fetch(const uint16_t* row, int d, int piece, int lane, bool on, float (&v)[8]) {
-    if constexpr (VEC) {
-        const int c = col_of<true>(piece, lane, 0);
-        u32x2 a[2] = {};
-        if (on && c < d) a[0] = __builtin_nontemporal_load((const u32x2*)(row + c));
-        if (on && c + 256 < d) a[1] = __builtin_nontemporal_load((const u32x2*)(row + c + 256));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i & 1 ? a[i >> 2][i >> 1 & 1] & 0xffff0000u : a[i >> 2][i >> 1 & 1] << 16);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = col_of<false>(piece, lane, i);
-            v[i] = on && c < d ? bf16_to_f32(row[c]) : 0.f;
-        }
-    }
-}
 template <bool VEC> __device__ __forceinline__ void put(float* row, int d, int piece, int lane, const float (&v)[8]) {
     if constexpr (VEC) {
         const int c = col_of<true>(piece, lane, 0);
