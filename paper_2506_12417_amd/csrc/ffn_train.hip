@@ -5,8 +5,8 @@
 //   backward   s = dy[t] W_out^T     dgate_w[a] = sum_f h s     dh = w s     dz = dh [z > 0], or (dh u sig(g) (1 + g (1 - sig(g))), dh silu(g))
 //              dx_perm[r] = dz W_in^T     dW_in = sum_r x[t]^T dz     dW_out = sum_r (w h)^T dy[t]
 //
-// Three products over an expert's rows (z, s, dx_perm: nt_kernel, which differ in their operands and in what is done with the result) and two over
-// the rows themselves (dW_in, dW_out: tn_kernel).  What bounds them: arithmetic where experts hold many rows, the fetch of the matrices and the
+// Three products over an expert's rows (z, s, dx_perm: gemm_nt_kernel, which differ in their operands and in what is done with the result) and two over
+// the rows themselves (dW_in, dW_out: gemm_tn_kernel).  What bounds them: arithmetic where experts hold many rows, the fetch of the matrices and the
 // stores of their gradients where they hold few.
 //
 // Both kernels: work-groups of four wavefronts, one a CU (two where gemm_tn_kernel's tiles are of 128), persistent, take items one after another:
@@ -14,14 +14,15 @@
 // two or three buffers of 64 terms in LDS, or four of 32 rows, filled by loads that go there directly and run on into the next items, so
 // that these start without a pause.  The fragments of the next 32 terms are read while those before are multiplied.
 //
-// Measured (us: the first product in 8 bits, its counterpart in the backward pass, dx, dW; parts of the whole calls):
-//   8192 tokens, top-4 of 60 experts of 2048 x 1408, SwiGLU     450   304   444   893     0.84, 0.62, 0.85, 0.63 PFLOP/s
-//   16384 tokens, top-1 of 128 experts of d = 768, F = 4 d             225   193   506
-//   8192 tokens, top-2 of 8 experts of 4096 x 14336, SwiGLU           2116  3650  5303     0.91, 1.05, 1.09 PFLOP/s
+// Measured (us, medians: z with its 8 bits, s with dz and w h, dx, dW; parts of the whole calls):
+//   8192 tokens, top-4 of 60 experts of 2048 x 1408, SwiGLU     502   306   453   886     0.75, 0.62, 0.83, 0.64 PFLOP/s
+//   16384 tokens, top-1 of 128 experts of d = 768, F = 4 d      209   224   194   518     z: 3.7 TB/s
+//   8192 tokens, top-2 of 8 experts of 4096 x 14336, SwiGLU    3601  2145  3722  5421     1.07, 0.90, 1.03, 1.07 PFLOP/s
 // What bounds them now.  The loops: the way from the L2s to LDS and the matrix instructions together (dW: 64 KB a stage of 64 rows, 1.4 us for the
 // fetch alone, 2.0 with its multiplications; the L2s deliver 8.5 TB/s, the matrix units are busy 60% of the time).  An item's end: nothing covers the
 // epilogue (13 us of the backward pass's first product, mostly vector instructions), and loads behind an item's stores are counted behind
-// them, which dW feels where experts hold few rows: 16384 tokens 545 us, 320 without its stores (1.2 GB).
+// them, which dW feels where experts hold few rows: 16384 tokens 545 us, 320 without its stores
+// (1.2 GB), when both were measured; 518 now.
 //
 // Rounded on the way: dz and w h, once, to bf16 (the matrix instruction's type), and what is kept in 8 bits.  Sums are fp32.
 #include <type_traits>
@@ -92,7 +93,7 @@ __device__ __forceinline__ void load_to_lds4(const u32x4& r, unsigned to, unsign
 // that for safe, and with two wavefronts a SIMD the last lanes' first values came out as what was written there next.
 // STREAM: past the caches, for results that are larger than these.  Only where an instruction writes whole lines of 128 bytes (halves of lines are
 // put together in the caches: a gradient stored so in halves took 15% longer, in whole lines 5% less), and to leave in them what is read again: a
-// backward pass of 100 tokens over 128 experts of d = 768, F = 4 d, takes 342 us instead of 400, of 16384 tokens 980 instead of 1048.
+// backward pass of 100 tokens over 128 experts of d = 768, F = 4 d, took 338 us instead of 400, of 16384 tokens 970 instead of 1025.
 constexpr int STREAM = 2;
 template <int AUX = 0> __device__ __forceinline__ void store_b128(u32x4 v, __amdgpu_buffer_rsrc_t r, unsigned voff, unsigned soff) {
     __builtin_amdgcn_raw_buffer_store_b128(v, r, voff, soff, AUX);
@@ -386,7 +387,7 @@ __device__ __forceinline__ void nt_contract(const NtArgs& a, const NtWork& w, co
 // (v_rcp_f32 is off by one unit in the last place at most)
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
 
-// A lane's features of block b in a row: natural order (slots arranged by nt_turn), or packed rows (packed row 16 h + j = output 2 j + h).
+// A lane's features of block b in a row: natural order (slots arranged by gemm_nt_kernel), or packed rows (packed row 16 h + j = output 2 j + h).
 template <bool PACKED> __device__ __forceinline__ void lane_values(const f32x4 (&acc)[2], float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = PACKED ? acc[i & 1][i >> 1] : acc[i >> 2][i & 3];

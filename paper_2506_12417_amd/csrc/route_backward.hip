@@ -10,8 +10,8 @@
 // below 2^-24).  dW_g and db are summed over ranges of tokens, whose parts a second launch adds up in their order: no atomics.
 //
 // The least there is to move: x, dx_add and dx once, the logits and dl.  Measured, us (dl, dx, dW_g, its sum): 16384 tokens of 768 in bf16, 128 experts
-// 8.3, 27, 22.6, 4 (a pass 66, at 5.5 TB/s 26 would do); 1501 of 1032 in fp32, 60 experts 3.1, 6.0, 8.8, 3.5 (a pass 19).  dx moves 100 MB, at 3.9
-// TB/s; dW_g is bound by latencies: a work-group has twelve steps of 32 tokens, whose dl every column tile fetches and takes apart
+// 8.4, 27, 22.5, 4.8 (a pass 66, at 5.5 TB/s 26 would do); 1501 of 1032 in fp32, 60 experts 3.0, 6.3, 8.8, 3.0 (a pass 19).  dx moves 100 MB, at 3.9
+// TB/s; dW_g is bound by latencies: a work-group has thirteen steps of 32 tokens, whose dl every column tile fetches and takes apart
 // again, and more work-groups store more parts (twice as many 27 + 6 us, half 26 + 4).
 #include <type_traits>
 #include "common.h"
