@@ -151,7 +151,7 @@ class MoEBlock:
         None; or, where forward() was given u, to what the residual connection passes on to h and the gradient of u (du_next of the block that
         has made it).  Parameters' gradients go to `grad` and the layer's `grad`; accumulate: all of them are added to what is
         there (that of the micro-batches before).  It belongs to the layer's last forward(): refused where that
-        was not this block's last one."""
+        was not this block's last one; h, and u where it was given, have to be as they were.  The layer's products read dv rounded to bf16."""
         L = self.layer
         if not (self.train and L.train):
             raise B.MoeError(B.MOE_ERR_ARG, "all gradients need MoEBlock(train=True) with a MoELayer(train=True)")

@@ -420,10 +420,10 @@ class MoELayer:
     def backward(self, dy: torch.Tensor, x: torch.Tensor, dlogits_add: Optional[torch.Tensor] = None, accumulate: bool = False,
                  stream=None, accumulate_router: bool = False) -> torch.Tensor:
         """The gradients of the last forward() of a training layer (train=True), whose x this is (refused where the layer has routed or sorted
-        since): returns that of x ([T,d], the layer's type);
-        those of the matrices and the router go to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).
-        dy: [T,d] fp32 or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the experts'
-        gradients are added to what `grad` holds; accumulate_router: the router's are, too (without it they are set)."""
+        since; x, gate_w and `weight` have to be as they were): returns that of x ([T,d], the layer's type); those of the matrices and the router go
+        to `grad`: a, b (SwiGLU's up matrices), o, the shared expert's sa, sb, so, and W_g and bias (fp32).  dy: [T,d] fp32 (rounded once to bf16,
+        the products' type) or the layer's type.  dlogits_add: [T,E] fp32, the gradient of a loss on the logits themselves.  accumulate: the
+        experts' gradients are added to what `grad` holds; accumulate_router: the router's are, too (without it they are set)."""
         assert self.train and self.kept_of, "the forward() of a MoELayer(train=True) keeps what the gradients are made of"
         assert dlogits_add is None or self.kept_of == "whole", "forward() was given the choice: the router has no gradient"
         T, d, E, k, dev = self.T, self.d, self.E, self.k, self.own_y.device
